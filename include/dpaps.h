@@ -310,6 +310,44 @@ int kge_sgd_epoch(ps_handle ps, int64_t num_entities, int32_t dim, int64_t num_t
                   const int64_t *part_ptr_host, int32_t num_parts, int64_t batch, int32_t lookahead, float lr, float eps,
                   double *loss_host_out, void *stream);
 
+/* ---- token models: embeddings and weight matrices that lie in the server ------------------------------------------ */
+/* Token t of a vocabulary of num_tokens tokens is key first_key + t; its embedding is the first `dim` values of the key
+ * (dim <= value_len), so that several tables, and matrices, can share a server.  Tokens are int32 or int64 (PS_I32, PS_I64);
+ * a token equal to pad_token (which may lie outside the vocabulary; PS_NO_PAD: none) is padding: no key is accessed for it.
+ * Any other token outside [0, num_tokens) is an error found on the device (PS_EKEY, deferred, see the top): nothing is
+ * changed then.  n = 0 is allowed everywhere; n < 2^31 (PS_ELIMIT).
+ * Tensors other than the server's values are 32-bit floats or 16-bit ones (PS_F32, PS_BF16, PS_F16), in rows whose
+ * elements are contiguous; strides count elements.  All sums are in 32 bits; a result is rounded to its type once.
+ * The tensors of a call must not overlap the ones it writes.  None of these calls waits for the stream, except where
+ * scratch of the library has to grow (as for ps_push: emb_grad and emb_adagrad_step, muon_orthogonalize and muon_step).
+ * worker: as for ps_pull / ps_push (locality statistics, of every token that is not padding); with location caches the
+ * replies set the requester's entries, too. */
+enum { PS_F32 = 0, PS_BF16 = 1, PS_F16 = 2 };    /* types of values */
+enum { PS_I32 = 0, PS_I64 = 1 };                 /* types of tokens */
+#define PS_NO_PAD INT64_MIN
+#define PS_EMB_MAX_DIM 65536
+
+/* out[p * out_stride + c] = scale * (value c of token p), rounded to out_type; zero where token p is padding.  An
+ * access like ps_pull of the tokens' keys.  out_stride >= dim. */
+int emb_lookup(ps_handle ps, int32_t worker, int64_t first_key, int64_t num_tokens, int32_t dim, const void *tokens, int32_t token_type, int64_t n,
+               int64_t pad_token, float scale, void *out, int32_t out_type, int64_t out_stride, void *stream);
+
+/* The gradient of a lookup with respect to its table: grad[v * dim + c] = scale * sum over the p whose token is v of
+ * dout[p * dout_stride + c], a contiguous fp32 matrix of num_tokens x dim (dim <= PS_EMB_MAX_DIM; the server's values have no part
+ * in it, the handle lends its scratch).  accumulate != 0: added to what grad holds; rows of tokens that are not mentioned
+ * are then left alone, otherwise they become zero.  Padding contributes nothing, whatever dout holds there.  dout_stride may be 0
+ * (one row for all).  The order of the additions depends on the arguments only: the terms of a token, in increasing p,
+ * in ranges of the sorted tokens, and the ranges' sums one after the other. */
+int emb_grad(ps_handle ps, int64_t num_tokens, int32_t dim, const void *tokens, int32_t token_type, int64_t n, int64_t pad_token, float scale,
+             const void *dout, int32_t dout_type, int64_t dout_stride, float *grad, int32_t accumulate, void *stream);
+
+/* One step of AdaGrad with that gradient, on the rows of the tokens mentioned; the accumulators lie next to the values, as in the
+ * knowledge-graph calls: a key holds [0, dim) the embedding, [dim, 2 dim) the accumulators (2 dim <= value_len).  With
+ * g = the token's row of the gradient: accumulator += g^2, then value -= lr g / sqrt(accumulator + eps) - one step per token
+ * and call, on the sum of its terms.  eps > 0.  Counted as a pull and a push of the tokens' keys. */
+int emb_adagrad_step(ps_handle ps, int32_t worker, int64_t first_key, int64_t num_tokens, int32_t dim, const void *tokens, int32_t token_type, int64_t n,
+                     int64_t pad_token, float scale, const void *dout, int32_t dout_type, int64_t dout_stride, float lr, float eps, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

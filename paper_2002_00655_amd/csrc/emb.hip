@@ -1,0 +1,425 @@
+// Tokens: the lookup of their embeddings in the server, the gradient of that lookup, and a step of AdaGrad with it.
+//
+// Token t is key first_key + t, its embedding the first `dim` values of the key.
+//   lookup     out_p = s E[t_p]                                     (zero where t_p is padding)
+//   gradient   g_v = s sum over the p with t_p = v of dout_p
+//   AdaGrad    G_v += g_v^2,  E_v -= lr g_v / sqrt(G_v + eps)       (G_v: the key's next `dim` values)
+// The sums go over sorted tokens: the pairs (token, position) are brought into that order (key_sort.hip) and cut into
+// ranges, and the terms of a token inside one range are added one after the other in increasing position, in 32 bits,
+// from zero; the sums of a token's ranges are then added in range order.  No floating-point atomics: the result
+// depends on the arguments only.
+#include "elements.h"
+#include "token_ids.h"
+
+#include <type_traits>
+
+namespace {
+
+inline unsigned grid_for(int64_t n, int block) { return (unsigned)((n + block - 1) / block); }
+inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+__device__ __forceinline__ uint64_t readlane_u64(uint64_t x, int l) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), l);
+    return ((uint64_t)hi << 32) | lo;
+}
+
+__global__ __launch_bounds__(256) void k_emb_check(TokenIds t, int32_t *err) {
+    const int64_t p = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (p < t.n && t.bad(t.at(p))) atomicExch(err, PS_EKEY);
+}
+
+__global__ __launch_bounds__(256) void k_route_tokens(RouteArgs a, TokenIds t, const int32_t *err) {
+    __shared__ RouteLds l;
+    route_tokens_block(a, t, l, blockIdx.x, flag_ahead(err));
+}
+
+// the replies of an access have set the requester's location cache (k_cache_replies, for tokens)
+__global__ __launch_bounds__(256) void k_token_replies(TokenIds t, int32_t worker, const int32_t *owner, int16_t *loc_row, const int32_t *err) {
+    if (*(volatile const int32_t *)err) return;
+    const int64_t p = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (p >= t.n) return;
+    const int64_t id = t.at(p);
+    if (id == t.pad) return;
+    const int32_t o = owner[t.first + id];
+    if (o != worker) loc_row[t.first + id] = (int16_t)o;
+}
+
+// ---- lookup ---------------------------------------------------------------------------------------------------------
+// The result in pieces of W values, P a row, a workgroup 256 * AHEAD consecutive pieces, a thread every 256th: its tokens,
+// then its pieces of the rows, are asked for together.  The first route.blocks workgroups count the statistics.
+template <class Out, int W, int AHEAD, bool STREAM>
+__global__ __launch_bounds__(256) void k_emb_lookup(RouteArgs route, TokenIds t, uint32_t P, double inv_P, int64_t L, float scale, const float *val, Out *out,
+                                                    int64_t stride, int32_t *err) {
+    const bool few = t.n <= FEW_KEYS;
+    const int32_t stop = few ? 0 : flag_ahead(err);
+    __shared__ RouteLds l;
+    if ((int)blockIdx.x < route.blocks) {
+        if (few && few_tokens_off(t, err)) return;
+        route_tokens_block(route, t, l, blockIdx.x, stop);
+        return;
+    }
+    const int64_t block = blockIdx.x - route.blocks;
+    // (the quotients of numbers up to 1023 + 2048: see k_pull)
+    const int64_t first = block * (256 * AHEAD), total = t.n * P;
+    const int64_t p0 = quotient(first, P, inv_P);
+    const uint32_t c0 = (uint32_t)(first - p0 * P);
+    const float inv_Pf = (float)inv_P;
+    int64_t id[AHEAD];
+    uint32_t c[AHEAD], row[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+        const uint32_t at = c0 + u * 256u + threadIdx.x;
+        row[u] = (uint32_t)(((float)at + 0.5f) * inv_Pf);
+        c[u] = at - row[u] * P;
+        id[u] = first + u * 256 + threadIdx.x < total ? t.at(p0 + row[u]) : t.pad;
+    }
+    if (few ? few_tokens_off(t, err) : stop != 0) return;
+    Vec<float, W> x[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+        x[u] = Vec<float, W>{};
+        if (first + u * 256 + threadIdx.x < total && id[u] != t.pad) x[u] = load_vec<float, W>(val + (t.first + id[u]) * L + (int64_t)c[u] * W) * scale;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (first + u * 256 + threadIdx.x < total) store_vec<Out, W, STREAM>(out + (p0 + row[u]) * stride + (int64_t)c[u] * W, x[u]);
+}
+
+// ---- sums over sorted tokens ----------------------------------------------------------------------------------------
+// The keys that are sorted: the tokens; padding behind all of them.
+__global__ __launch_bounds__(256) void k_emb_keys(TokenIds t, int64_t *keys, int32_t *err) {
+    const int64_t p = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (p >= t.n) return;
+    const int64_t id = t.at(p);
+    if (t.bad(id)) atomicExch(err, PS_EKEY);
+    keys[p] = id == t.pad ? t.count : id;
+}
+
+struct EmbSums {
+    const uint64_t *skeys; const uint32_t *spos; int64_t n;      // the sorted pairs
+    int64_t count, first;                                        // tokens, the key of token 0
+    int32_t range;                                               // sorted positions of a range, at most 64
+    int32_t D;
+    const void *dout; int64_t stride;
+    float scale;
+    float *part;                                                 // two rows of D per range
+    float *to; int64_t L;                                        // where a token's row is: the gradient (L = D) or the store
+    float lr, eps;
+    int64_t clear_blocks;                                        // workgroups that clear the rows of tokens not mentioned
+};
+
+// What becomes of a token's sum: a row of the gradient, added to what is there, or a step of AdaGrad.
+enum EmbMode { EMB_GRAD, EMB_GRAD_ADD, EMB_ADAGRAD };
+template <int MODE, int W> struct Old { Vec<float, W> v[MODE == EMB_GRAD ? 1 : MODE]; };
+template <int MODE, int W>
+__device__ __forceinline__ void emb_read(Old<MODE, W> &o, const EmbSums &a, int64_t token, int c) {
+    const float *p = a.to + (a.first + token) * a.L + (int64_t)c * W;
+    if constexpr (MODE >= EMB_GRAD_ADD) o.v[0] = load_vec<float, W>(p);
+    if constexpr (MODE == EMB_ADAGRAD) o.v[1] = load_vec<float, W>(p + a.D);
+}
+template <int MODE, int W>
+__device__ __forceinline__ void emb_finish(const Old<MODE, W> &o, const EmbSums &a, int64_t token, int c, Vec<float, W> sum) {
+    float *p = a.to + (a.first + token) * a.L + (int64_t)c * W;
+    const Vec<float, W> g = sum * a.scale;
+    if constexpr (MODE == EMB_GRAD) store_vec<float, W>(p, g);
+    if constexpr (MODE == EMB_GRAD_ADD) store_vec<float, W>(p, o.v[0] + g);
+    if constexpr (MODE == EMB_ADAGRAD) {
+        const Vec<float, W> G = o.v[1] + g * g;
+        Vec<float, W> e = o.v[0];
+        if constexpr (W == 1) e = e - a.lr * g / sqrtf(G + a.eps);
+        else
+            for (int i = 0; i < W; ++i) e[i] = e[i] - a.lr * g[i] / sqrtf(G[i] + a.eps);
+        store_vec<float, W>(p, e);
+        store_vec<float, W>(p + a.D, G);
+    }
+}
+
+// whether a row is mentioned: the place of token v among the sorted ones
+__device__ __forceinline__ bool emb_mentioned(const EmbSums &a, int64_t v) {
+    int64_t lo = 0, hi = a.n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if ((int64_t)a.skeys[mid] < v) lo = mid + 1; else hi = mid;
+    }
+    return lo < a.n && (int64_t)a.skeys[lo] == v;
+}
+
+constexpr int CLEAR_ROWS = 16;                         // of a wavefront
+constexpr uint64_t NOKEY = ~0ull;
+
+// A wavefront per range and 64 pieces of W values; UN rows are on their way together.  The first workgroups clear the rows of tokens
+// that are not mentioned (EMB_GRAD), the next ones count the statistics.
+template <class T, int W, int MODE>
+__global__ __launch_bounds__(256) void k_emb_sums(RouteArgs route, TokenIds t, EmbSums a, const int32_t *err) {
+    constexpr int UN = MODE == EMB_ADAGRAD ? 8 : W >= 4 ? 8 : 16;
+    const int32_t stop = flag_ahead(err);
+    const int lane = threadIdx.x & 63;
+    int64_t block = blockIdx.x;
+    if constexpr (MODE == EMB_GRAD) {
+        if (block < a.clear_blocks) {
+            if (blockIdx.y != 0 || stop) return;
+            const int64_t v0 = (block * 4 + (threadIdx.x >> 6)) * CLEAR_ROWS;
+            const bool clear = lane < CLEAR_ROWS && v0 + lane < a.count && !emb_mentioned(a, v0 + lane);
+            for (u64 left = __ballot(clear); left != 0; left &= left - 1ull) {
+                float *p = a.to + (v0 + __ffsll((long long)left) - 1) * a.L;
+                for (int c = lane * W; c < a.D; c += 64 * W) store_vec<float, W>(p + c, Vec<float, W>{});
+            }
+            return;
+        }
+        block -= a.clear_blocks;
+    }
+    if constexpr (MODE == EMB_ADAGRAD) {
+        __shared__ RouteLds l;
+        if (block < route.blocks) {
+            if (blockIdx.y == 0) route_tokens_block(route, t, l, (int)block, stop);
+            return;
+        }
+        block -= route.blocks;
+    }
+    const int64_t r = block * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), q0 = r * a.range;
+    if (q0 >= a.n) return;
+    const int here = (int)(a.n - q0 < a.range ? a.n - q0 : a.range);
+    const uint64_t mk = lane < here ? a.skeys[q0 + lane] : NOKEY;       // lane i: sorted position q0 + i
+    const uint64_t before = lane < here && q0 + lane > 0 ? a.skeys[q0 + lane - 1] : NOKEY;
+    const uint64_t next = q0 + here < a.n ? a.skeys[q0 + here] : NOKEY;
+    const int mp = lane < here ? (int)a.spos[q0 + lane] : 0;
+    if (stop) return;
+    const int cnt = __popcll(__ballot(lane < here && (int64_t)mk < a.count));          // padding comes last
+    if (cnt == 0) return;
+    u64 heads = __ballot(lane < cnt && before != mk);                   // positions where a token's terms start
+    const bool first_open = (heads & 1) == 0;                           // the first token's terms continue from the range before,
+    const bool last_open = next == readlane_u64(mk, cnt - 1);           // the last one's go on in the range behind
+    const u64 ends = (heads >> 1) | (1ull << (cnt - 1));                // positions where they end
+    const int c = blockIdx.y * 64 + lane;
+    const bool in = c * W < a.D;
+    const T *dout = reinterpret_cast<const T *>(a.dout) + (int64_t)c * W;
+    Vec<float, W> v = {};
+    Old<MODE, W> kept;                                                  // of the token whose terms are being added
+    bool from_zero = first_open;                                        // its terms started in a range before
+    for (int i0 = 0; i0 < cnt; i0 += UN) {
+        Vec<float, W> d[UN];
+        Old<MODE, W> old[UN];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            d[i] = Vec<float, W>{};
+            if (in && i0 + i < cnt) {
+                d[i] = load_vec<T, W>(dout + (int64_t)(uint32_t)__builtin_amdgcn_readlane(mp, i0 + i) * a.stride);
+                if constexpr (MODE != EMB_GRAD)
+                    if ((heads >> (i0 + i)) & 1) emb_read<MODE, W>(old[i], a, (int64_t)readlane_u64(mk, i0 + i), c);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int u = i0 + i;
+            if (u < cnt) {
+                if ((heads >> u) & 1) {
+                    v = Vec<float, W>{};
+                    from_zero = false;
+                    if constexpr (MODE != EMB_GRAD) kept = old[i];
+                }
+                v = v + d[i];
+                if ((ends >> u) & 1) {
+                    const bool open = u == cnt - 1 && last_open;
+                    if (in) {
+                        if (from_zero || open) store_vec<float, W>(a.part + (2 * r + (from_zero ? 0 : 1)) * (int64_t)a.D + (int64_t)c * W, v);
+                        else emb_finish<MODE, W>(kept, a, (int64_t)readlane_u64(mk, u), c, v);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// Tokens whose terms fill more than one range: the wavefront of the range in which they start adds the sums of the ranges behind
+// it, in order.  blockIdx.y: which 64 pieces.
+constexpr int JOIN_AHEAD = 32;
+template <int W, int MODE>
+__global__ __launch_bounds__(256) void k_emb_join(EmbSums a, const int32_t *err) {
+    const int32_t stop = flag_ahead(err);
+    const int lane = threadIdx.x & 63;
+    const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), R = a.range;
+    const int64_t q1 = (r + 1) * R;
+    if (q1 >= a.n) return;
+    const uint64_t key = a.skeys[q1 - 1], next = a.skeys[q1];
+    if (stop != 0 || next != key || (int64_t)key >= a.count) return;
+    if (r > 0 && a.skeys[q1 - R] == key && a.skeys[q1 - R - 1] == key) return;         // they started earlier
+    // the ranges behind that begin with the token follow one another: 64 are looked at, spread over what is left
+    const int64_t nranges = (a.n + R - 1) / R;
+    int64_t lo = r + 1, hi = nranges, by = 1;
+    while (lo < hi) {
+        const int64_t at = lo + lane * by;
+        const u64 b = __ballot(at < hi && a.skeys[(at < hi ? at : lo) * R] == key);
+        const int run = b == ~0ull ? 64 : __ffsll((long long)~b) - 1;
+        if (run < 64 && lo + run * by < hi) hi = lo + run * by;
+        if (run > 0) lo += (run - 1) * by + 1;
+        by = (hi - lo + 63) / 64;
+    }
+    const int64_t m = lo - (r + 1);
+    const int c = blockIdx.y * 64 + lane;
+    if (c * W >= a.D) return;
+    const float *part = a.part + (int64_t)c * W;
+    Old<MODE, W> old;
+    emb_read<MODE, W>(old, a, (int64_t)key, c);
+    Vec<float, W> v = load_vec<float, W>(part + (2 * r + 1) * (int64_t)a.D);
+    for (int64_t j = 1; j <= m; j += JOIN_AHEAD) {
+        Vec<float, W> d[JOIN_AHEAD];
+#pragma unroll
+        for (int i = 0; i < JOIN_AHEAD; ++i) d[i] = j + i <= m ? load_vec<float, W>(part + 2 * (r + j + i) * (int64_t)a.D) : Vec<float, W>{};
+#pragma unroll
+        for (int i = 0; i < JOIN_AHEAD; ++i)
+            if (j + i <= m) v = v + d[i];
+    }
+    emb_finish<MODE, W>(old, a, (int64_t)key, c, v);
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------
+// What all calls check of their tokens.
+int token_ids(dpaps_ps *ps, int64_t first_key, int64_t num_tokens, bool in_store, const void *tokens, int32_t token_type, int64_t n, int64_t pad, TokenIds *t) {
+    if (n < 0 || (n > 0 && !tokens) || num_tokens <= 0 || first_key < 0 || (token_type != PS_I32 && token_type != PS_I64)) return PS_EINVAL;
+    if (in_store && (num_tokens > ps->K || first_key > ps->K - num_tokens)) return PS_EINVAL;
+    if (n >= ((int64_t)1 << 31)) return PS_ELIMIT;
+    t->ids = tokens; t->wide = token_type == PS_I64; t->n = n; t->first = first_key; t->count = num_tokens; t->pad = pad;
+    return PS_OK;
+}
+
+template <class Out>
+int lookup(dpaps_ps *ps, const RouteArgs &a, const TokenIds &t, int32_t dim, float scale, Out *out, int32_t type, int64_t stride, hipStream_t st) {
+    const auto fits = [&](int w) { return rows_allow(ps->val, PS_F32, dim, ps->L, w) && rows_allow(out, type, dim, stride, w); };
+#define LOOKUP(W, AHEAD)                                                                                                                          \
+    do {                                                                                                                                          \
+        const uint32_t P = (uint32_t)(dim / W);                                                                                                   \
+        const unsigned grid = (unsigned)a.blocks + grid_for(t.n * P, 256 * AHEAD);                                                                \
+        k_emb_lookup<Out, W, AHEAD, false><<<grid, 256, 0, st>>>(a, t, P, 1.0 / P, ps->L, scale, ps->val, out, stride, ps->err);                  \
+    } while (0)
+    if (sizeof(Out) == 2 && fits(8)) LOOKUP(8, 2);
+    else if (fits(4)) LOOKUP(4, 4);
+    else if (fits(2)) LOOKUP(2, 4);
+    else LOOKUP(1, 8);
+#undef LOOKUP
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+
+// The sorted pairs and what the sums need, in the handle's scratch.
+int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, int32_t dout_type, int mode, hipStream_t st) {
+    const int bits = dpaps_key_bits(t.count + 1);
+    // values of a lane, and so the wavefronts that a row takes
+    const auto fits = [&](int w) { return rows_allow(a.dout, dout_type, a.D, a.stride, w) && rows_allow(a.to, PS_F32, a.D, a.L, w); };
+    const int W = dout_type != PS_F32 && mode != EMB_ADAGRAD && a.D > 256 && fits(8) ? 8 : a.D > 64 && fits(4) ? 4 : 1;
+    const int64_t slices = (a.D / W + 63) / 64;
+    // ranges of 64 positions, shorter ones where those would be fewer wavefronts than the compute units hold
+    a.range = 64;
+    while (a.range > 8 && ceil_div64(t.n, a.range) * slices < 8 * (int64_t)ps->num_cu) a.range /= 2;
+    const int64_t nranges = ceil_div64(t.n, a.range);
+    const size_t off_skeys = up256((size_t)t.n * 8), off_spos = 2 * off_skeys, off_part = off_spos + up256((size_t)t.n * 4),
+                 off_sort = off_part + up256((size_t)nranges * 2 * (size_t)a.D * sizeof(float));
+    int rc = dpaps_ws_reserve(ps, off_sort + dpaps_sort_scratch_bytes(t.n, bits));
+    if (rc) return rc;
+    char *ws = (char *)ps->ws;
+    if (t.n > 0) {
+        k_emb_keys<<<grid_for(t.n, 256), 256, 0, st>>>(t, (int64_t *)ws, ps->err);
+        PS_HIP(ps, hipGetLastError());
+        rc = dpaps_sort_pairs(ps, (int64_t *)ws, t.n, bits, false, (uint64_t *)(ws + off_skeys), (uint32_t *)(ws + off_spos), ws + off_sort, st);
+        if (rc) return rc;
+    }
+    a.skeys = (const uint64_t *)(ws + off_skeys); a.spos = (const uint32_t *)(ws + off_spos); a.n = t.n; a.count = t.count; a.first = t.first;
+    a.part = (float *)(ws + off_part);
+    a.clear_blocks = mode == EMB_GRAD ? ceil_div64(t.count, 4 * CLEAR_ROWS) : 0;
+    const dim3 grid((unsigned)(a.clear_blocks + route.blocks + ceil_div64(nranges, 4)), (unsigned)slices), join((unsigned)ceil_div64(nranges, 4), (unsigned)slices);
+    if (grid.x == 0) return PS_OK;
+#define SUMS(T, WW, MODE)                                                                     \
+    do {                                                                                      \
+        k_emb_sums<T, WW, MODE><<<grid, 256, 0, st>>>(route, t, a, ps->err);                  \
+        PS_HIP(ps, hipGetLastError());                                                        \
+        if (nranges > 1) k_emb_join<WW, MODE><<<join, 256, 0, st>>>(a, ps->err);              \
+    } while (0)
+#define MODES(T, WW)                                                                          \
+    do {                                                                                      \
+        if (mode == EMB_GRAD) SUMS(T, WW, EMB_GRAD);                                          \
+        else if (mode == EMB_GRAD_ADD) SUMS(T, WW, EMB_GRAD_ADD);                             \
+        else if constexpr (WW < 8) SUMS(T, WW, EMB_ADAGRAD);                                  \
+    } while (0)
+#define WIDTHS(T)                                                                             \
+    do {                                                                                      \
+        if (W == 1) MODES(T, 1);                                                              \
+        else if (W == 4) MODES(T, 4);                                                         \
+        else if constexpr (sizeof(T) == 2) MODES(T, 8);                                       \
+    } while (0)
+    if (dout_type == PS_F32) WIDTHS(float);
+    else if (dout_type == PS_BF16) WIDTHS(bf16_t);
+    else WIDTHS(f16_t);
+#undef WIDTHS
+#undef MODES
+#undef SUMS
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+
+}  // namespace
+
+int dpaps_route_tokens(dpaps_ps *ps, int32_t worker, const TokenIds &t, bool pull, bool push, hipStream_t st) {
+    if (worker < 0 || t.n == 0) return PS_OK;
+    if (ps->loc && pull && push) {       // with location caches the second access is routed after the first one's replies
+        const int rc = dpaps_route_tokens(ps, worker, t, true, false, st);
+        return rc ? rc : dpaps_route_tokens(ps, worker, t, false, true, st);
+    }
+    const RouteArgs a = dpaps_route_args(ps, worker, t.n, pull ? PS_STAT_PULL_LOCAL : PS_STAT_PUSH_LOCAL, pull ? PS_STAT_PULL_REMOTE : PS_STAT_PUSH_REMOTE,
+                                         pull && push ? PS_STAT_PUSH_LOCAL : -1, pull && push ? PS_STAT_PUSH_REMOTE : -1, st);
+    k_route_tokens<<<a.blocks, 256, 0, st>>>(a, t, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    if (ps->loc) {
+        k_token_replies<<<grid_for(t.n, 256), 256, 0, st>>>(t, worker, ps->owner, ps->loc + (int64_t)worker * ps->K, ps->err);
+        PS_HIP(ps, hipGetLastError());
+    }
+    return PS_OK;
+}
+
+extern "C" int emb_lookup(ps_handle ps, int32_t worker, int64_t first_key, int64_t num_tokens, int32_t dim, const void *tokens, int32_t token_type, int64_t n,
+                          int64_t pad_token, float scale, void *out, int32_t out_type, int64_t out_stride, void *stream) {
+    if (!ps || !is_element_type(out_type) || dim <= 0 || dim > ps->L || (n > 0 && (!out || out_stride < dim))) return PS_EINVAL;
+    if (worker < -1 || worker >= ps->W) return PS_EWORKER;
+    TokenIds t;
+    int rc = token_ids(ps, first_key, num_tokens, true, tokens, token_type, n, pad_token, &t);
+    if (rc || n == 0) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    if (n > FEW_KEYS) {
+        k_emb_check<<<grid_for(n, 256), 256, 0, st>>>(t, ps->err);
+        PS_HIP(ps, hipGetLastError());
+    }
+    RouteArgs a{};
+    if (!ps->loc) a = dpaps_route_args(ps, worker, n, PS_STAT_PULL_LOCAL, PS_STAT_PULL_REMOTE, -1, -1, st);
+    if (out_type == PS_F32) rc = lookup(ps, a, t, dim, scale, (float *)out, out_type, out_stride, st);
+    else if (out_type == PS_BF16) rc = lookup(ps, a, t, dim, scale, (bf16_t *)out, out_type, out_stride, st);
+    else rc = lookup(ps, a, t, dim, scale, (f16_t *)out, out_type, out_stride, st);
+    if (rc || !ps->loc) return rc;
+    return dpaps_route_tokens(ps, worker, t, true, false, st);         // (behind the check, which few tokens have in the lookup)
+}
+
+extern "C" int emb_grad(ps_handle ps, int64_t num_tokens, int32_t dim, const void *tokens, int32_t token_type, int64_t n, int64_t pad_token, float scale,
+                        const void *dout, int32_t dout_type, int64_t dout_stride, float *grad, int32_t accumulate, void *stream) {
+    if (!ps || !is_element_type(dout_type) || dim <= 0 || dim > PS_EMB_MAX_DIM || !grad || (n > 0 && (!dout || dout_stride < 0))) return PS_EINVAL;
+    TokenIds t;
+    const int rc = token_ids(ps, 0, num_tokens, false, tokens, token_type, n, pad_token, &t);
+    if (rc) return rc;
+    EmbSums a{};
+    a.D = dim; a.dout = dout; a.stride = dout_stride; a.scale = scale; a.to = grad; a.L = dim;
+    return sums_of(ps, RouteArgs{}, t, a, dout_type, accumulate ? EMB_GRAD_ADD : EMB_GRAD, (hipStream_t)stream);
+}
+
+extern "C" int emb_adagrad_step(ps_handle ps, int32_t worker, int64_t first_key, int64_t num_tokens, int32_t dim, const void *tokens, int32_t token_type,
+                                int64_t n, int64_t pad_token, float scale, const void *dout, int32_t dout_type, int64_t dout_stride, float lr, float eps,
+                                void *stream) {
+    if (!ps || !is_element_type(dout_type) || dim <= 0 || dim > ps->L / 2 || !(eps > 0.0f) || (n > 0 && (!dout || dout_stride < 0))) return PS_EINVAL;
+    if (worker < -1 || worker >= ps->W) return PS_EWORKER;
+    TokenIds t;
+    int rc = token_ids(ps, first_key, num_tokens, true, tokens, token_type, n, pad_token, &t);
+    if (rc || n == 0) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    EmbSums a{};
+    a.D = dim; a.dout = dout; a.stride = dout_stride; a.scale = scale; a.to = ps->val; a.L = ps->L; a.lr = lr; a.eps = eps;
+    RouteArgs route{};
+    if (!ps->loc) route = dpaps_route_args(ps, worker, n, PS_STAT_PULL_LOCAL, PS_STAT_PULL_REMOTE, PS_STAT_PUSH_LOCAL, PS_STAT_PUSH_REMOTE, st);
+    rc = sums_of(ps, route, t, a, dout_type, EMB_ADAGRAD, st);
+    return rc || !ps->loc ? rc : dpaps_route_tokens(ps, worker, t, true, true, st);
+}

@@ -666,6 +666,9 @@ static RouteArgs route_args(dpaps_ps *ps, int32_t worker, const int64_t *keys, i
     a.blocks = route_grid(n);
     return a;
 }
+RouteArgs dpaps_route_args(dpaps_ps *ps, int32_t worker, int64_t n, int st_local, int st_remote, int st_local2, int st_remote2, hipStream_t st) {
+    return route_args(ps, worker, nullptr, n, st_local, st_remote, st_local2, st_remote2, st);
+}
 static int cache_replies(dpaps_ps *ps, int32_t worker, const int64_t *keys, int64_t n, hipStream_t st) {
     if (worker < 0 || n == 0 || !ps->loc) return PS_OK;
     k_cache_replies<<<grid_for(n, 256), 256, 0, st>>>(keys, n, worker, ps->owner, ps->loc + (int64_t)worker * ps->K, ps->err);

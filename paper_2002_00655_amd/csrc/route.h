@@ -179,7 +179,9 @@ struct RouteArgs {
 constexpr int ROUTE_AHEAD = 4;
 
 // stop: the handle's error flag, the same in all threads; looked at when the first keys are on their way.
-__device__ __forceinline__ void route_access_block(const RouteArgs &a, RouteLds &l, int block, int32_t stop = 0) {
+// key_of(p, k): puts the access's p-th key in k; false: there is none (a token that is padding).
+template <class KeyOf>
+__device__ __forceinline__ void route_access_block(const RouteArgs &a, RouteLds &l, int block, int32_t stop, KeyOf key_of) {
     route_lds_init(l, a.W);
     const double inv_per_home = 1.0 / (double)a.per_home;
     const int64_t step = (int64_t)a.blocks * blockDim.x;
@@ -191,8 +193,8 @@ __device__ __forceinline__ void route_access_block(const RouteArgs &a, RouteLds 
 #pragma unroll
         for (int u = 0; u < ROUTE_AHEAD; ++u) {
             const int64_t p = base + u * step + threadIdx.x;
-            active[u] = p < a.n;
-            k[u] = active[u] ? a.keys[p] : 0;
+            k[u] = 0;
+            active[u] = p < a.n && key_of(p, k[u]);
         }
         if (stop) return;
 #pragma unroll
@@ -216,6 +218,11 @@ __device__ __forceinline__ void route_access_block(const RouteArgs &a, RouteLds 
     // (only without location caches: with them the first access's replies change how the second is routed)
     if (a.stat_local2 >= 0) route_lds_flush(l, a.stats, a.stat_local2, a.stat_remote2, PS_STAT_MSG_ACC_REQ, PS_STAT_MSG_ACC_FWD, PS_STAT_MSG_ACC_REPLY);
 }
+__device__ __forceinline__ void route_access_block(const RouteArgs &a, RouteLds &l, int block, int32_t stop = 0) {
+    route_access_block(a, l, block, stop, [&](int64_t p, int64_t &k) { k = a.keys[p]; return true; });
+}
 
+// ps_store.hip: the statistics of one access of n keys that the kernel names itself (route_access_block's key_of)
+RouteArgs dpaps_route_args(dpaps_ps *ps, int32_t worker, int64_t n, int st_local, int st_remote, int st_local2, int st_remote2, hipStream_t st);
 // ps_store.hip: the statistics of a step that pulls and pushes the same n keys, counted by one workgroup (which puts the keys in)
 RouteArgs dpaps_step_route(dpaps_ps *ps, int32_t worker, int64_t n, hipStream_t st);

@@ -25,7 +25,11 @@ OPT_MF_EXACT, OPT_MF_CACHE_ROWS, OPT_MF_WAVES, OPT_MF_PROFILE, OPT_MF_GROUPED, O
 
 EXPORTS = ["ps_create", "ps_destroy", "ps_pull", "ps_push", "ps_push_noalloc", "ps_localize", "ps_owner", "ps_stats", "ps_status",
            "ps_set_option", "ps_last_error", "mf_block_ratings", "mf_load_ratings", "mf_sgd_epoch", "mf_sgd_epoch_handoff", "mf_train_sse",
-           "mf_profile_read", "kge_sgd_step", "kge_sgd_epoch"]
+           "mf_profile_read", "kge_sgd_step", "kge_sgd_epoch", "emb_lookup", "emb_grad", "emb_adagrad_step"]
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}         # PS_F32, PS_BF16, PS_F16
+_TOKENS = {torch.int32: 0, torch.int64: 1}                              # PS_I32, PS_I64
+_NO_PAD = -(1 << 63)                                                     # PS_NO_PAD
 
 
 class PSError(RuntimeError):
@@ -60,6 +64,9 @@ def load_library() -> C.CDLL:
     lib.mf_profile_read.argtypes = [vp, vp, vp, vp]
     lib.kge_sgd_step.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, i32, vp, i32, vp, f32, f32, vp, vp]
     lib.kge_sgd_epoch.argtypes = [vp, i64, i32, i64, vp, vp, vp, i32, vp, i32, vp, vp, i32, i64, i32, f32, f32, vp, vp]
+    lib.emb_lookup.argtypes = [vp, i32, i64, i64, i32, vp, i32, i64, i64, f32, vp, i32, i64, vp]
+    lib.emb_grad.argtypes = [vp, i64, i32, vp, i32, i64, i64, f32, vp, i32, i64, vp, i32, vp]
+    lib.emb_adagrad_step.argtypes = [vp, i32, i64, i64, i32, vp, i32, i64, i64, f32, vp, i32, i64, f32, f32, vp]
     for name in EXPORTS:
         if name != "ps_last_error":
             getattr(lib, name).restype = C.c_int
@@ -86,6 +93,31 @@ def _per_row(t: torch.Tensor, rows: int) -> tuple[int, int]:
         return 0, 0
     _dev(t, torch.int32)
     return (t.shape[1] if t.dim() == 2 and t.shape[0] == rows else t.reshape(rows, -1).shape[1]), t.data_ptr()
+
+
+def _tokens(t: torch.Tensor) -> tuple[int, int, int]:
+    """Where the tokens are, their type, how many."""
+    kind = _TOKENS.get(t.dtype)
+    if kind is None or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"expected contiguous CUDA tokens of int32 or int64, got {t.dtype} on {t.device}")
+    return t.data_ptr(), kind, t.numel()
+
+
+def _rows(t: torch.Tensor, n: int, copy: bool = True) -> tuple[torch.Tensor, int, int, int]:
+    """A tensor of n rows (its last dimension a row, the others counted together): what has to stay alive until the call is made, where
+    it is, its type, the rows' distance in elements.  Rows that do not lie at one distance are copied, or refused."""
+    kind = _TYPES.get(t.dtype)
+    if kind is None or not t.is_cuda or t.dim() == 0:
+        raise TypeError(f"expected a CUDA tensor of float32, bfloat16 or float16, got {t.dtype} on {t.device}")
+    if t.dim() != 2:
+        r = t.reshape(n, t.shape[-1])
+        if not copy and r.data_ptr() != t.data_ptr():
+            raise ValueError(f"the rows of a result have to lie at one distance, got shape {tuple(t.shape)}, strides {t.stride()}")
+        t = r
+    rows, cols = t.shape
+    if rows != n or (n > 0 and cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"expected {n} rows whose elements are contiguous, got shape {tuple(t.shape)}, strides {t.stride()}")
+    return t, t.data_ptr(), kind, (t.stride(0) if n > 1 else cols)
 
 
 def _host(a, dtype) -> np.ndarray:
@@ -237,6 +269,46 @@ class ParameterServer:
                                        int(lookahead), float(lr), float(eps), C.addressof(loss) if want_loss else None, _stream()),
                     "kge_sgd_epoch")
         return float(loss.value) if want_loss else None
+
+    # -- token models -------------------------------------------------------------
+    def emb_lookup(self, tokens, first_key: int = 0, num_tokens: int | None = None, dim: int | None = None, scale: float = 1.0,
+                   pad_token: int | None = None, worker: int = -1, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None):
+        """The scaled embeddings of `tokens` (any shape), in `dtype`, shape [*tokens.shape, dim] (see include/dpaps.h)."""
+        at, kind, n = _tokens(tokens)
+        dim = self.L if dim is None else dim
+        if out is None:
+            out = torch.empty((*tokens.shape, dim), dtype=dtype, device=tokens.device)
+        elif out.shape != (*tokens.shape, dim):
+            raise ValueError(f"out must have the shape {(*tokens.shape, dim)}")
+        _, to, out_kind, stride = _rows(out, n, copy=False)
+        self._check(_lib.emb_lookup(self._h, worker, first_key, self.K - first_key if num_tokens is None else num_tokens, dim, at, kind, n,
+                                    _NO_PAD if pad_token is None else pad_token, scale, to, out_kind, stride, _stream()), "emb_lookup")
+        return out
+
+    def emb_grad(self, tokens, dout, num_tokens: int, scale: float = 1.0, pad_token: int | None = None, grad: torch.Tensor | None = None,
+                 accumulate: bool = False):
+        """The gradient of a lookup with respect to its table, [num_tokens, dim] in fp32, from that of its output (see include/dpaps.h)."""
+        (at, kind, n), dim = _tokens(tokens), dout.shape[-1]
+        kept, frm, dout_kind, stride = _rows(dout, n)
+        if grad is None:
+            if accumulate:
+                raise ValueError("accumulate needs the gradient to add to")
+            grad = torch.empty((num_tokens, dim), dtype=torch.float32, device=tokens.device)
+        _dev(grad, torch.float32)
+        if grad.shape != (num_tokens, dim):
+            raise ValueError(f"grad must have the shape {(num_tokens, dim)}")
+        self._check(_lib.emb_grad(self._h, num_tokens, dim, at, kind, n, _NO_PAD if pad_token is None else pad_token, scale, frm, dout_kind, stride,
+                                  grad.data_ptr(), int(accumulate), _stream()), "emb_grad")
+        return grad
+
+    def emb_adagrad_step(self, tokens, dout, lr: float, eps: float, first_key: int = 0, num_tokens: int | None = None, scale: float = 1.0,
+                         pad_token: int | None = None, worker: int = -1) -> None:
+        """One step of AdaGrad on the rows that `tokens` mention, from the gradient of their lookup's output (see include/dpaps.h)."""
+        (at, kind, n), dim = _tokens(tokens), dout.shape[-1]
+        kept, frm, dout_kind, stride = _rows(dout, n)
+        self._check(_lib.emb_adagrad_step(self._h, worker, first_key, self.K - first_key if num_tokens is None else num_tokens, dim, at, kind, n,
+                                          _NO_PAD if pad_token is None else pad_token, scale, frm, dout_kind, stride, lr, eps, _stream()),
+                    "emb_adagrad_step")
 
 
 def mf_block_ratings(m, n, rows, cols, vals, row_bounds, col_bounds):

@@ -1,0 +1,351 @@
+"""Tokens (emb_lookup, emb_grad, emb_adagrad_step) against the formulas in 64 bits: types, row lengths, strides and alignments,
+one token to many, padding, tokens of all rows and of one, rows of a table in a larger server; refusals and bad tokens.
+
+Tolerances, relative to the sum of the absolute values that go into a result: a sum of m terms in 32 bits, in ranges of up to 64 and over
+the ranges, has at most (64 + m / 8) roundings behind each other, of 2^-24 each; in practice the root of that."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ["float32", "bfloat16", "float16"]
+ROUND = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}      # half a unit of 24, 8 and 11 bits, relative
+
+
+def _server(K, L, W=1, seed=0):
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng = np.random.default_rng(seed)
+    values = rng.standard_normal((K, L)).astype(np.float32)
+    values[:, L // 2:] = np.abs(values[:, L // 2:])
+    srv = P.ParameterServer(K, L, W)
+    srv.push(torch.arange(K, device="cuda"), torch.from_numpy(values).cuda())
+    return srv, values
+
+
+def _all(srv):
+    import torch
+    return srv.pull(torch.arange(srv.K, device="cuda")).cpu().numpy()
+
+
+def _close(got, want, scale, rel):
+    """|got - want| <= rel * scale, element by element (and a little for numbers that the type cannot hold exactly near zero)"""
+    err = np.abs(got.astype(np.float64) - want)
+    bad = err > rel * scale + 6.0e-8 * (rel > 2.0 ** -12)
+    assert not bad.any(), (int(bad.sum()), float((err / np.maximum(scale, 1e-300)).max()), rel)
+
+
+def _sums(tokens, dout, V, pad):
+    keep = tokens != pad if pad is not None else np.ones(tokens.size, bool)
+    want, mag = np.zeros((V, dout.shape[1])), np.zeros((V, dout.shape[1]))
+    np.add.at(want, tokens[keep], dout[keep])
+    np.add.at(mag, tokens[keep], np.abs(dout[keep]))
+    return want, mag, np.bincount(tokens[keep], minlength=V)
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 2048, 2049, 5000])
+@pytest.mark.parametrize("K,L,dim,first", [(700, 128, 128, 0), (300, 100, 50, 20), (97, 51, 51, 7), (64, 1024, 512, 0), (50, 1, 1, 3), (40, 1022, 1022, 0)])
+def test_lookup(n, K, L, dim, first):
+    import torch
+    print(f"case n={n} K={K} L={L} dim={dim}", flush=True)
+    rng = np.random.default_rng(n + L)
+    srv, values = _server(K, L)
+    V = K - first - 2
+    for kind in TYPES:
+        for wide in (False, True):
+            for pad in (None, 0, -100):
+                tokens = rng.integers(0, V, size=n)
+                if pad is not None:
+                    tokens[rng.random(n) < 0.4] = pad
+                t = torch.from_numpy(tokens.astype(np.int64 if wide else np.int32)).cuda()
+                got = srv.emb_lookup(t, first_key=first, num_tokens=V, dim=dim, scale=3.7, pad_token=pad, dtype=getattr(torch, kind))
+                want = values.astype(np.float64)[np.maximum(tokens, 0) + first, :dim] * np.float64(np.float32(3.7))
+                if pad is not None:
+                    want[tokens == pad] = 0.0
+                _close(got.float().cpu().numpy(), want, np.abs(want), 2.0 ** -24 + ROUND[kind] * (kind != "float32"))
+    srv.status()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("offset,gap", [(0, 0), (1, 0), (0, 3), (2, 6), (4, 4), (8, 8)])
+def test_lookup_into_strided_rows(kind, offset, gap):
+    """Rows at any distance and alignment; what lies between them stays."""
+    import torch
+    rng = np.random.default_rng(offset + gap)
+    srv, values = _server(90, 64)
+    tokens = torch.from_numpy(rng.integers(0, 90, size=(5, 7))).cuda()
+    base = torch.full((35 * (64 + gap) + offset + 64,), 7.0, device="cuda", dtype=getattr(torch, kind))
+    out = base[offset:].as_strided((5, 7, 64), (7 * (64 + gap), 64 + gap, 1))
+    assert srv.emb_lookup(tokens, out=out) is out
+    assert torch.equal(out, torch.from_numpy(values).cuda()[tokens].to(out.dtype))
+    left = base.clone()
+    left[offset:].as_strided((5, 7, 64), (7 * (64 + gap), 64 + gap, 1)).fill_(7.0)
+    assert (left == 7.0).all()
+
+
+def test_lookup_passes_infinities_and_nan_and_no_padding_row():
+    import torch
+    srv, _ = _server(10, 8)
+    srv.push(torch.tensor([3, 4], device="cuda"), torch.tensor([[float("inf")] * 8, [float("nan")] * 8], device="cuda"))
+    out = srv.emb_lookup(torch.tensor([3, 4, 5], device="cuda"), pad_token=4, dtype=torch.bfloat16)
+    assert torch.isinf(out[0]).all() and (out[1] == 0).all() and torch.isfinite(out[2].float()).all()
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 7, 64, 65, 130, 2048, 2049, 9000, 70_000])
+@pytest.mark.parametrize("V,D", [(1, 4), (37, 64), (900, 100), (5000, 51), (300, 512), (2000, 260), (40, 1030), (70_001, 8)])
+def test_gradient(n, V, D):
+    import torch
+    from paper_2002_00655_amd import ps as P
+    if n * D > 20_000_000:
+        n = 20_000_000 // D
+    print(f"case n={n} V={V} D={D}", flush=True)
+    rng = np.random.default_rng(n + V + D)
+    srv = P.ParameterServer(1, 1, 1)
+    for i, kind in enumerate(TYPES):
+        pad = (None, V // 2, -1)[i]
+        tokens = np.minimum((V * rng.random(n) ** 3).astype(np.int64), V - 1)           # the first ones often
+        if pad is not None:
+            tokens[rng.random(n) < 0.2] = pad
+        dout = torch.from_numpy(rng.standard_normal((n, D)).astype(np.float32)).cuda().to(getattr(torch, kind))
+        t = torch.from_numpy(tokens.astype(np.int32 if i % 2 else np.int64)).cuda()
+        want, mag, count = _sums(tokens, dout.double().cpu().numpy(), V, pad)
+        tol = (64 + count / 8 + 3)[:, None] * 2.0 ** -24
+        scale = np.float64(np.float32(0.3))
+        got = srv.emb_grad(t, dout, V, scale=0.3, pad_token=pad, grad=torch.full((V, D), 9.0, device="cuda"))
+        _close(got.cpu().numpy(), want * scale, mag * scale, tol)
+        assert (got.cpu().numpy()[count == 0] == 0.0).all()
+        had = torch.from_numpy(rng.standard_normal((V, D)).astype(np.float32)).cuda()
+        more = srv.emb_grad(t, dout, V, scale=0.3, pad_token=pad, grad=had.clone(), accumulate=True)
+        assert torch.equal(more, torch.where(torch.from_numpy(count == 0).cuda()[:, None], had, had + got))
+        again = srv.emb_grad(t, dout, V, scale=0.3, pad_token=pad)
+        assert torch.equal(again, got)
+    srv.status()
+
+
+@pytest.mark.parametrize("what", ["one token", "all padding", "every token once", "two tokens in turn"])
+@pytest.mark.parametrize("n,D", [(65, 16), (4096, 128), (30_000, 72)])
+def test_gradient_of_extreme_batches(what, n, D):
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng = np.random.default_rng(n)
+    V = n + 3
+    tokens = {"one token": np.full(n, 5), "all padding": np.full(n, 1), "every token once": rng.permutation(n), "two tokens in turn": np.arange(n) % 2 * 7}[what]
+    pad = 1 if what == "all padding" else None
+    dout = rng.standard_normal((n, D)).astype(np.float32)
+    got = P.ParameterServer(1, 1, 1).emb_grad(torch.from_numpy(tokens).cuda(), torch.from_numpy(dout).cuda(), V, pad_token=pad).cpu().numpy()
+    want, mag, count = _sums(tokens, dout.astype(np.float64), V, pad)
+    _close(got, want, mag, (64 + count / 8 + 3)[:, None] * 2.0 ** -24)
+    if what == "every token once":
+        assert np.array_equal(got[tokens], dout)
+
+
+def test_gradient_of_padding_is_ignored_whatever_it_holds():
+    import torch
+    from paper_2002_00655_amd import ps as P
+    tokens = torch.tensor([2, 0, 2, 0, 1], device="cuda", dtype=torch.int32)
+    dout = torch.ones(5, 12, device="cuda")
+    dout[1], dout[3] = float("nan"), float("inf")
+    got = P.ParameterServer(1, 1, 1).emb_grad(tokens, dout, 3, pad_token=0)
+    assert torch.equal(got, torch.tensor([0.0, 1.0, 2.0], device="cuda")[:, None].expand(3, 12))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_gradient_of_broadcast_strided_and_misaligned_rows(kind):
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng, srv = np.random.default_rng(5), P.ParameterServer(1, 1, 1)
+    dt = getattr(torch, kind)
+    for D in (64, 96, 512):
+        tokens = torch.from_numpy(rng.integers(0, 50, size=(30, 11))).cuda()
+        one = torch.from_numpy(rng.integers(-8, 9, size=D).astype(np.float32)).cuda().to(dt)
+        count = torch.bincount(tokens.flatten(), minlength=50).float()
+        assert torch.equal(srv.emb_grad(tokens, one.expand(30, 11, D), 50), count[:, None] * one.float())
+        for offset, gap in ((0, 8), (1, 0), (3, 5)):
+            base = torch.from_numpy(rng.integers(-8, 9, size=330 * (D + gap) + offset + D).astype(np.float32)).cuda().to(dt)
+            rows = base[offset:].as_strided((30, 11, D), (11 * (D + gap), D + gap, 1))
+            want = torch.zeros(50, D, device="cuda", dtype=torch.float64).index_add_(0, tokens.flatten(), rows.reshape(330, D).double())
+            assert torch.equal(srv.emb_grad(tokens, rows, 50).double(), want)           # (integers: exact in any order)
+        # rows that lie at no one distance
+        rows = torch.from_numpy(rng.integers(-8, 9, size=(11, 30, D)).astype(np.float32)).cuda().to(dt).transpose(0, 1)
+        want = torch.zeros(50, D, device="cuda", dtype=torch.float64).index_add_(0, tokens.flatten(), rows.reshape(330, D).double())
+        assert torch.equal(srv.emb_grad(tokens, rows, 50).double(), want)
+
+
+def test_gradient_against_differences():
+    """<dout, lookup(E + h X) - lookup(E - h X)> / 2h = <grad, X>: the lookup is linear, so no more than roundings."""
+    import torch
+    rng = np.random.default_rng(0)
+    V, D, n, h = 60, 24, 500, 0.5
+    a, va = _server(V, D, seed=1)
+    x = rng.standard_normal((V, D)).astype(np.float32)
+    tokens = torch.from_numpy(rng.integers(0, V, size=n)).cuda()
+    dout = torch.from_numpy(rng.standard_normal((n, D)).astype(np.float32)).cuda()
+    keys, dx = torch.arange(V, device="cuda"), torch.from_numpy(x).cuda()
+    a.push(keys, h * dx)
+    up = a.emb_lookup(tokens, scale=1.5, pad_token=4).double()
+    a.push(keys, -2 * h * dx)
+    down = a.emb_lookup(tokens, scale=1.5, pad_token=4).double()
+    grad = a.emb_grad(tokens, dout, V, scale=1.5, pad_token=4).double()
+    left, right = float((dout.double() * (up - down)).sum() / (2 * h)), float((grad * dx.double()).sum())
+    size = float((dout.double() * up).abs().sum())
+    assert abs(left - right) <= size * 2.0 ** -22, (left, right)
+
+
+@pytest.mark.parametrize("n", [0, 1, 3, 64, 65, 2048, 2049, 20_000])
+@pytest.mark.parametrize("V,D,L,first", [(50, 64, 128, 0), (333, 25, 51, 11), (4000, 128, 300, 5), (700, 512, 1024, 0), (9, 1, 2, 0)])
+def test_adagrad_step(n, V, D, L, first):
+    import torch
+    print(f"case n={n} V={V} D={D} L={L}", flush=True)
+    rng = np.random.default_rng(n + V)
+    K = first + V + 4
+    srv, values = _server(K, L, seed=n)
+    values[:, D:2 * D] = np.abs(values[:, D:2 * D])
+    srv2, _ = _server(1, 1)
+    import paper_2002_00655_amd.ps as P
+    srv = P.ParameterServer(K, L, 1)
+    srv.push(torch.arange(K, device="cuda"), torch.from_numpy(values).cuda())
+    want = values.astype(np.float64)
+    err = np.zeros_like(want)
+    lr, eps = 0.1, 1e-6
+    for kind, pad in (("float32", None), ("bfloat16", 0), ("float16", None)):
+        tokens = np.minimum((V * rng.random(n) ** 2).astype(np.int64), V - 1)
+        dout = torch.from_numpy(rng.standard_normal((n, D)).astype(np.float32)).cuda().to(getattr(torch, kind))
+        srv.emb_adagrad_step(torch.from_numpy(tokens).cuda(), dout, lr, eps, first_key=first, num_tokens=V, scale=0.7, pad_token=pad)
+        g, mag, count = _sums(tokens, dout.double().cpu().numpy(), V, pad)
+        s = np.float64(np.float32(0.7))
+        g, mag = g * s, mag * s
+        rows = slice(first, first + V)
+        dg = mag * (64 + count / 8 + 3)[:, None] * 2.0 ** -24                      # what the sum may be off by
+        hit = count > 0
+        G = want[rows, D:2 * D] + g * g
+        root = np.sqrt(G + np.float32(eps))
+        err[rows, D:2 * D] += np.where(hit[:, None], 2 * np.abs(g) * dg + dg ** 2 + 4 * G * 2.0 ** -24, 0)
+        # of lr g / root, |d/dg| <= lr / root, and of G through the root lr |g| / (2 root^3)
+        err[rows, :D] += np.where(hit[:, None], np.float32(lr) * (dg / root + np.abs(g) * err[rows, D:2 * D] / (2 * root ** 3) + 8 * 2.0 ** -24 * (np.abs(g) / root))
+                                  + 2.0 ** -23 * (np.abs(want[rows, :D]) + lr), 0)
+        want[rows, :D] -= np.float32(lr) * g / root
+        want[rows, D:2 * D] = G
+    got = _all(srv)
+    off = np.abs(got - want)
+    assert (off <= err + 1e-12).all(), float((off - err).max())
+    srv.status()
+    srv2.status()
+
+
+@pytest.mark.parametrize("n", [1, 300, 3000])
+@pytest.mark.parametrize("caches", [0, 1])
+def test_statistics_are_those_of_pull_and_push(n, caches):
+    """A lookup is counted as a pull of the tokens' keys without the padding, a step as a pull and a push."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng = np.random.default_rng(n)
+    K, L, W, first, V = 900, 16, 5, 100, 640
+    a, b = P.ParameterServer(K, L, W), P.ParameterServer(K, L, W)
+    for s in (a, b):
+        s.set_option(P.OPT_LOCATION_CACHES, caches)
+        s.localize(torch.arange(0, K, 3, device="cuda"), 2)
+    for i in range(4):
+        tokens = rng.integers(0, V, size=n)
+        tokens[rng.random(n) < 0.2] = 17
+        worker = int(rng.integers(-1, W))
+        t, keys = torch.from_numpy(tokens.astype(np.int32 if i % 2 else np.int64)).cuda(), torch.from_numpy(tokens[tokens != 17] + first).cuda()
+        a.emb_lookup(t, first_key=first, num_tokens=V, pad_token=17, worker=worker)
+        b.pull(keys, worker)
+        assert a.stats() == b.stats()
+        a.emb_adagrad_step(t, torch.ones(n, 8, device="cuda"), 0.1, 1e-8, first_key=first, num_tokens=V, pad_token=17, worker=worker)
+        b.pull(keys, worker)
+        b.push(keys, torch.zeros(keys.numel(), L, device="cuda"), worker)
+        assert a.stats() == b.stats()
+        for s in (a, b):
+            s.localize(torch.from_numpy(rng.integers(0, K, size=50)).cuda(), int(rng.integers(0, W))) if i < 0 else None
+    assert torch.equal(a.owner(), b.owner())
+
+
+@pytest.mark.parametrize("n", [1, 64, 2048, 2049, 140_000])
+@pytest.mark.parametrize("bad", [-1, 640, 1 << 40])
+def test_a_bad_token_changes_nothing(n, bad):
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng = np.random.default_rng(n)
+    print(f"case n={n} bad={bad}", flush=True)
+    srv, values = _server(900, 16, W=3)
+    tokens = rng.integers(0, 640, size=n)
+    tokens[int(rng.integers(0, n))] = bad
+    t = torch.from_numpy(tokens).cuda()
+    out, grad, dout = torch.full((n, 16), 7.0, device="cuda"), torch.full((640, 8), 7.0, device="cuda"), torch.ones(n, 8, device="cuda")
+    stats = srv.stats()
+    for call in (lambda: srv.emb_lookup(t, num_tokens=640, out=out, worker=1), lambda: srv.emb_grad(t, dout, 640, grad=grad),
+                 lambda: srv.emb_grad(t, dout, 640, grad=grad, accumulate=True),
+                 lambda: srv.emb_adagrad_step(t, dout, 0.1, 1e-8, num_tokens=640, worker=1)):
+        call()
+        call()                                                    # (nor does a later call before the status is asked for)
+        with pytest.raises(P.PSError) as e:
+            srv.status()
+        assert e.value.code == P.PS_EKEY
+    assert (out == 7.0).all() and (grad == 7.0).all() and np.array_equal(_all(srv), values) and srv.stats() == stats
+    # a pad token outside the vocabulary is no error
+    srv.emb_lookup(t, num_tokens=640, pad_token=bad)
+    srv.status()
+
+
+def test_refusals():
+    import torch
+    from paper_2002_00655_amd import ps as P
+    srv, values = _server(100, 16, W=2)
+    t, dout = torch.zeros(5, dtype=torch.int64, device="cuda"), torch.zeros(5, 8, device="cuda")
+    bad = [(P.PS_EINVAL, lambda: srv.emb_lookup(t, dim=17)), (P.PS_EINVAL, lambda: srv.emb_lookup(t, first_key=50, num_tokens=51)),
+           (P.PS_EINVAL, lambda: srv.emb_lookup(t, first_key=-1, num_tokens=5)), (P.PS_EINVAL, lambda: srv.emb_lookup(t, num_tokens=0)),
+           (P.PS_EWORKER, lambda: srv.emb_lookup(t, worker=2)), (P.PS_EWORKER, lambda: srv.emb_lookup(t, worker=-2)),
+           (P.PS_EINVAL, lambda: srv.emb_adagrad_step(t, torch.zeros(5, 9, device="cuda"), 0.1, 1e-8)),
+           (P.PS_EINVAL, lambda: srv.emb_adagrad_step(t, dout, 0.1, 0.0)), (P.PS_EINVAL, lambda: srv.emb_adagrad_step(t, dout, 0.1, float("nan"))),
+           (P.PS_EWORKER, lambda: srv.emb_adagrad_step(t, dout, 0.1, 1e-8, worker=2)), (P.PS_EINVAL, lambda: srv.emb_adagrad_step(t, dout, 0.1, 1e-8, first_key=100)),
+           (P.PS_EINVAL, lambda: srv.emb_grad(t, dout, 0))]
+    for code, call in bad:
+        with pytest.raises(P.PSError) as e:
+            call()
+        assert e.value.code == code
+    for call in (lambda: srv.emb_lookup(t.float()), lambda: srv.emb_lookup(t.cpu()), lambda: srv.emb_lookup(t, dtype=torch.float64), lambda: srv.emb_grad(t, dout.double(), 5),
+                 lambda: srv.emb_grad(t, dout, 5, grad=torch.zeros(5, 8, device="cuda", dtype=torch.float16))):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: srv.emb_grad(t, dout[:4], 5), lambda: srv.emb_grad(t, dout, 5, accumulate=True), lambda: srv.emb_lookup(t, out=torch.zeros(5, 15, device="cuda")),
+                 lambda: srv.emb_grad(t, dout, 5, grad=torch.zeros(6, 8, device="cuda")), lambda: srv.emb_grad(t, torch.zeros(8, 5, device="cuda").t(), 5),
+                 lambda: srv.emb_lookup(t.view(5, 1), out=torch.zeros(1, 5, 16, device="cuda").transpose(0, 1)[:, :, ::1][:, :, :15])):
+        with pytest.raises(ValueError):
+            call()
+    srv.status()
+    assert np.array_equal(_all(srv), values)
+
+
+def test_calls_on_another_stream_and_in_a_graph():
+    """The calls go to the current stream; once scratch has its size they can be captured, and replays see new inputs."""
+    import torch
+    rng = np.random.default_rng(3)
+    V, D, n = 500, 64, 3000
+    srv, _ = _server(V, 2 * D)
+    ref, _ = _server(V, 2 * D)
+    t = torch.from_numpy(rng.integers(0, V, size=n)).cuda()
+    dout, out, grad = torch.zeros(n, D, device="cuda"), torch.zeros(n, D, device="cuda", dtype=torch.bfloat16), torch.zeros(V, D, device="cuda")
+
+    def step(s):
+        s.emb_lookup(t, dim=D, scale=2.0, out=out)
+        s.emb_grad(t, dout, V, grad=grad)
+        s.emb_adagrad_step(t, dout, 0.1, 1e-8)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(srv)
+    torch.cuda.current_stream().wait_stream(side)
+    step(ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(srv)
+    for i in range(3):
+        t.copy_(torch.from_numpy(rng.integers(0, V, size=n)))
+        dout.copy_(torch.from_numpy(rng.standard_normal((n, D)).astype(np.float32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        a = out.clone(), grad.clone()
+        step(ref)
+        assert torch.equal(a[0], out) and torch.equal(a[1], grad) and np.array_equal(_all(srv), _all(ref)), i
