@@ -348,6 +348,28 @@ int emb_grad(ps_handle ps, int64_t num_tokens, int32_t dim, const void *tokens, 
 int emb_adagrad_step(ps_handle ps, int32_t worker, int64_t first_key, int64_t num_tokens, int32_t dim, const void *tokens, int32_t token_type, int64_t n,
                      int64_t pad_token, float scale, const void *dout, int32_t dout_type, int64_t dout_stride, float lr, float eps, void *stream);
 
+/* Orthogonalise `batch` matrices of rows x cols, each X_0 = D / (|D|_F + eps) and then `steps` times
+ *   A = X X',  X <- a X + (b A + c A^2) X,   (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * (X' X and from the right where rows > cols, which is the same matrix).  Matrix i starts at row i * rows of `in` and `out`, whose rows
+ * are in_ld and out_ld >= cols elements apart.  A zero matrix stays zero; one that holds an infinity or no number becomes NaN, the others do not.
+ * The products are carried out with numbers of 24 bits where the result has type PS_F32 or PS_F16, of 11 bits where it is rounded to
+ * PS_BF16 (8 bits); sums are in 32 bits.  1 <= steps <= 100, eps >= 0; the server's values have no part in it.  `out` must not
+ * overlap `in`.  Limits (PS_ELIMIT): sides of PS_MUON_MAX_SIDE, PS_MUON_MAX_BATCH matrices.  Scratch: 20 bytes per element of
+ * the matrices, more for small ones (sides count as multiples of 64 or 128), grown as needed. */
+#define PS_MUON_MAX_SIDE 32768
+#define PS_MUON_MAX_BATCH 65535
+int muon_orthogonalize(ps_handle ps, int32_t batch, int32_t rows, int32_t cols, const void *in, int32_t in_type, int64_t in_ld, void *out, int32_t out_type,
+                       int64_t out_ld, int32_t steps, float eps, void *stream);
+
+/* One step of weight matrices that lie in the server, by their orthogonalised momentum: row r of matrix i is key
+ * first_key + i * rows + r, [0, dim) the weights W, [dim, 2 dim) the momentum M (2 dim <= value_len), grad holds the gradients as `in` above.
+ *   M <- momentum M + grad;   D = grad + momentum M if nesterov, else M;   O = D orthogonalised (24 bits);
+ *   W <- (1 - lr weight_decay) W - lr sqrt(max(1, rows / dim)) O
+ * (Momentum kept as a running mean, M <- momentum M + (1 - momentum) grad, gives the same O up to eps.)  Counted as a
+ * pull and a push of the matrices' keys. */
+int muon_step(ps_handle ps, int32_t worker, int64_t first_key, int32_t batch, int32_t rows, int32_t dim, const void *grad, int32_t grad_type, int64_t grad_ld,
+              float lr, float momentum, int32_t nesterov, float weight_decay, int32_t steps, float eps, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,7 +25,8 @@ OPT_MF_EXACT, OPT_MF_CACHE_ROWS, OPT_MF_WAVES, OPT_MF_PROFILE, OPT_MF_GROUPED, O
 
 EXPORTS = ["ps_create", "ps_destroy", "ps_pull", "ps_push", "ps_push_noalloc", "ps_localize", "ps_owner", "ps_stats", "ps_status",
            "ps_set_option", "ps_last_error", "mf_block_ratings", "mf_load_ratings", "mf_sgd_epoch", "mf_sgd_epoch_handoff", "mf_train_sse",
-           "mf_profile_read", "kge_sgd_step", "kge_sgd_epoch", "emb_lookup", "emb_grad", "emb_adagrad_step"]
+           "mf_profile_read", "kge_sgd_step", "kge_sgd_epoch", "emb_lookup", "emb_grad", "emb_adagrad_step",
+           "muon_orthogonalize", "muon_step"]
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}         # PS_F32, PS_BF16, PS_F16
 _TOKENS = {torch.int32: 0, torch.int64: 1}                              # PS_I32, PS_I64
@@ -67,6 +68,8 @@ def load_library() -> C.CDLL:
     lib.emb_lookup.argtypes = [vp, i32, i64, i64, i32, vp, i32, i64, i64, f32, vp, i32, i64, vp]
     lib.emb_grad.argtypes = [vp, i64, i32, vp, i32, i64, i64, f32, vp, i32, i64, vp, i32, vp]
     lib.emb_adagrad_step.argtypes = [vp, i32, i64, i64, i32, vp, i32, i64, i64, f32, vp, i32, i64, f32, f32, vp]
+    lib.muon_orthogonalize.argtypes = [vp, i32, i32, i32, vp, i32, i64, vp, i32, i64, i32, f32, vp]
+    lib.muon_step.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32, i64, f32, f32, i32, f32, i32, f32, vp]
     for name in EXPORTS:
         if name != "ps_last_error":
             getattr(lib, name).restype = C.c_int
@@ -118,6 +121,15 @@ def _rows(t: torch.Tensor, n: int, copy: bool = True) -> tuple[torch.Tensor, int
     if rows != n or (n > 0 and cols > 1 and t.stride(1) != 1):
         raise ValueError(f"expected {n} rows whose elements are contiguous, got shape {tuple(t.shape)}, strides {t.stride()}")
     return t, t.data_ptr(), kind, (t.stride(0) if n > 1 else cols)
+
+
+def _matrices(t: torch.Tensor) -> tuple[int, int, int]:
+    if t.dim() < 2:
+        raise ValueError(f"expected matrices, got shape {tuple(t.shape)}")
+    batch = 1
+    for d in t.shape[:-2]:
+        batch *= d
+    return batch, t.shape[-2], t.shape[-1]
 
 
 def _host(a, dtype) -> np.ndarray:
@@ -309,6 +321,26 @@ class ParameterServer:
         self._check(_lib.emb_adagrad_step(self._h, worker, first_key, self.K - first_key if num_tokens is None else num_tokens, dim, at, kind, n,
                                           _NO_PAD if pad_token is None else pad_token, scale, frm, dout_kind, stride, lr, eps, _stream()),
                     "emb_adagrad_step")
+
+    def muon_orthogonalize(self, x: torch.Tensor, steps: int = 5, eps: float = 1e-7, dtype: torch.dtype | None = None, out: torch.Tensor | None = None):
+        """Matrices [..., rows, cols] orthogonalised by Newton-Schulz products, in x's type or `dtype` (see include/dpaps.h)."""
+        batch, rows, cols = _matrices(x)
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
+        elif out.shape != x.shape:
+            raise ValueError(f"out must have the shape {tuple(x.shape)}")
+        kept, frm, in_kind, in_ld = _rows(x, batch * rows)
+        _, to, out_kind, out_ld = _rows(out, batch * rows, copy=False)
+        self._check(_lib.muon_orthogonalize(self._h, batch, rows, cols, frm, in_kind, in_ld, to, out_kind, out_ld, steps, eps, _stream()), "muon_orthogonalize")
+        return out
+
+    def muon_step(self, first_key: int, grad: torch.Tensor, lr: float, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                  steps: int = 5, eps: float = 1e-7, worker: int = -1) -> None:
+        """One step of weight matrices in the server, from their gradients [..., rows, dim] (see include/dpaps.h)."""
+        batch, rows, dim = _matrices(grad)
+        kept, frm, kind, ld = _rows(grad, batch * rows)
+        self._check(_lib.muon_step(self._h, worker, first_key, batch, rows, dim, frm, kind, ld, lr, momentum, int(nesterov), weight_decay, steps, eps,
+                                   _stream()), "muon_step")
 
 
 def mf_block_ratings(m, n, rows, cols, vals, row_bounds, col_bounds):
