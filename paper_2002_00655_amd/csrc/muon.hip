@@ -26,19 +26,21 @@ constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float X_SCALE = 16384.0f, G_SCALE = 16384.0f, P_SCALE = 8192.0f;
 
 typedef f16_t half8 __attribute__((ext_vector_type(8)));
-typedef f16_t half4 __attribute__((ext_vector_type(4)));
-typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-// A matrix in scratch: element (r, k) of a row of ld elements.  SPLIT: 8 high parts, then their 8 low parts, and so on.
-template <bool SPLIT> __device__ __forceinline__ int64_t place(int64_t r, int k, int ld) {
-    return SPLIT ? r * (2 * (int64_t)ld) + (k >> 3) * 16 + (k & 7) : r * (int64_t)ld + k;
+// A matrix in scratch lies as the matrix instruction takes it: 32 rows and 16 numbers of each are a block, in which lane l of a wavefront
+// finds its eight numbers, of row l % 32 from number 8 (l / 32) on, at 16 l bytes (SPLIT: the 64 lanes' high parts, then their
+// low parts); the blocks of the same rows follow one another.  So operands come into registers in whole lines, and never see LDS.
+// The eight numbers of row r from k on (k a multiple of 8), K numbers a row:
+template <bool SPLIT> __device__ __forceinline__ int64_t place8(int r, int k, int K) {
+    return ((int64_t)(r >> 5) * (K >> 4) + (k >> 4)) * (SPLIT ? 1024 : 512) + ((k & 8) * 4 + (r & 31)) * 8;
 }
 
 // ---- the norm, and the momentum -------------------------------------------------------------------------------------
-constexpr int NORM_BLOCKS = 128;             // workgroups per matrix at most
+constexpr int NORM_BLOCKS = 256;             // workgroups per matrix at most
 
 struct MuonIn {
     const void *in; int64_t ld; int32_t type;    // batch * rows rows
@@ -66,23 +68,40 @@ __device__ __forceinline__ double sum_of_256(double x) {
 }
 
 // Of matrix blockIdx.y: sums of squares in 64 bits (no number of 32 bits overflows there); of a step, first M <- mu M + G, and
-// what is orthogonalised, D = G + mu M (Nesterov) or M.
-__global__ __launch_bounds__(256) void k_muon_norm(MuonIn a, const int32_t *err) {
-    if (a.val && *(volatile const int32_t *)err) return;
-    const int64_t row0 = (int64_t)blockIdx.y * a.rows;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// what is orthogonalised, D = G + mu M (Nesterov) or M.  V numbers of a row at a time, P = cols / V such pieces a row; a thread
+// goes through every (256 blocks)th piece of the matrix, AHEAD of them together.
+template <class T, int V, bool STEP>
+__global__ __launch_bounds__(256) void k_muon_norm(MuonIn a, uint32_t P, double inv_P, const int32_t *err) {
+    constexpr int AHEAD = STEP ? 2 : 4;
+    if (STEP && *(volatile const int32_t *)err) return;
+    const int64_t row0 = (int64_t)blockIdx.y * a.rows, pieces = (int64_t)a.rows * P, step = (int64_t)a.blocks * 256;
+    const T *in = reinterpret_cast<const T *>(a.in);
     double s = 0.0;
-    for (int r = blockIdx.x * 4 + wave; r < a.rows; r += a.blocks * 4) {
-        for (int c = lane; c < a.cols; c += 64) {
-            float x = element(a, row0 + r, c);
-            if (a.val) {
-                float *m = a.val + (a.first + row0 + r) * a.L + a.cols + c;
-                const float moment = a.mu * *m + x;
-                *m = moment;
-                x = a.nesterov ? x + a.mu * moment : moment;
-                a.d[(row0 + r) * a.cols + c] = x;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < pieces; at += step * AHEAD) {
+        Vec<float, V> x[AHEAD], m[AHEAD];
+        int64_t row[AHEAD];
+        int c[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t q = at + u * step < pieces ? at + u * step : 0, r = quotient(q, P, inv_P);
+            row[u] = row0 + r;
+            c[u] = (int)(q - r * P) * V;
+            x[u] = load_vec<T, V>(in + row[u] * a.ld + c[u]);
+            if constexpr (STEP) m[u] = load_vec<float, V>(a.val + (a.first + row[u]) * a.L + a.cols + c[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (at + u * step >= pieces) break;
+            if constexpr (STEP) {
+                const Vec<float, V> moment = a.mu * m[u] + x[u];
+                store_vec<float, V>(a.val + (a.first + row[u]) * a.L + a.cols + c[u], moment);
+                x[u] = a.nesterov ? x[u] + a.mu * moment : moment;
+                store_vec<float, V>(a.d + row[u] * a.cols + c[u], x[u]);
             }
-            s += (double)x * (double)x;
+            if constexpr (V == 1) s += (double)x[u] * (double)x[u];
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e) s += (double)x[u][e] * (double)x[u][e];
         }
     }
     s = sum_of_256(s);
@@ -91,16 +110,16 @@ __global__ __launch_bounds__(256) void k_muon_norm(MuonIn a, const int32_t *err)
 
 // X_0 both ways, zero where the padded matrices go on.  A norm that is no number, or infinite, makes all of the matrix NaN, as the division would.
 template <bool SPLIT>
-__device__ __forceinline__ void put8(f16_t *to, int64_t r, int k, int ld, const float (&v)[8]) {
+__device__ __forceinline__ void put8(f16_t *to, int r, int k, int K, const float (&v)[8]) {
     half8 hi, lo;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         hi[i] = (f16_t)v[i];
         lo[i] = (f16_t)(v[i] - (float)hi[i]);
     }
-    f16_t *p = to + place<SPLIT>(r, k, ld);
+    f16_t *p = to + place8<SPLIT>(r, k, K);
     *reinterpret_cast<half8 *>(p) = hi;
-    if constexpr (SPLIT) *reinterpret_cast<half8 *>(p + 8) = lo;
+    if constexpr (SPLIT) *reinterpret_cast<half8 *>(p + 512) = lo;
 }
 template <bool SPLIT>
 __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np, int mp, f16_t *x, f16_t *xt) {
@@ -112,16 +131,18 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;                     // of X
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;                       // of the matrix itself
-    for (int r = wave; r < 64; r += 4) {
-        const int rr = r0 + r, cc = c0 + lane;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+        const int r = wave + 4 * u, rr = r0 + r, cc = c0 + lane;
         const float v = rr < a.rows && cc < a.cols ? f * element(a, b * a.rows + rr, cc) : 0.0f;
         if (tall) tile[lane][r] = v; else tile[r][lane] = v;
     }
     __syncthreads();
     x += b * (int64_t)np * mp * (SPLIT ? 2 : 1);
     xt += b * (int64_t)np * mp * (SPLIT ? 2 : 1);
-    for (int q = threadIdx.x; q < 512; q += 256) {
-        const int r = q >> 3, k = (q & 7) * 8;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int r = u * 32 + (lane & 31), k = wave * 16 + (lane >> 5) * 8;
         float v[8], w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) { v[i] = tile[r][k + i]; w[i] = tile[k + i][r]; }
@@ -131,203 +152,384 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
 }
 
 // ---- the products ---------------------------------------------------------------------------------------------------
-constexpr int CHAIN = 8;                         // stages whose products one chain of matrix instructions adds (numbers of 24 bits)
+constexpr uint32_t DIES = 8;                     // compute dies, each with a cache of its own
+constexpr int CHAIN = 12;                        // blocks of k whose products one chain of matrix instructions adds (a multiple of DEPTH and KB)
 enum MuonProduct { MUON_GRAM, MUON_POLY, MUON_APPLY, MUON_LAST };
 struct MuonArgs {
     const f16_t *lhs, *rhs;                      // rows of K numbers
     int64_t lhs_size, rhs_size, out_size;        // of one matrix, in elements as they are stored
-    int32_t K, tiles_i, tiles_j;
+    int32_t K, tiles_i, tiles_j, tiles;          // tiles: of one matrix
+    int32_t shares; float *part;                 // workgroups that share a tile's sum over k, and where they put their sums
     f16_t *out; int32_t out_ld;                  // GRAM: A, POLY: P, APPLY: X
     f16_t *out_t; int32_t out_t_ld;              // APPLY: X transposed
     // LAST: the result
-    void *to; int64_t to_ld; int32_t to_type, tall, n, m;
+    void *to; int64_t to_ld; int32_t to_type, to_vec, tall, n, m;   // to_vec: eight numbers of a row can be written together
     float *val; int64_t L, first; float keep, step;    // of a step: W <- keep W - step X
 };
 
-// C[i][j] = sum_k L[i][k] R[j][k], a tile of TILE x TILE per workgroup of four wavefronts, each a quarter of it in 32 x 32 pieces
-// (v_mfma_f32_32x32x16_f16).  128 bytes of each row go through LDS at a time, straight from memory, two stages: the next
-// one is on its way while this one is multiplied.  A row's eight pieces of 16 bytes are exchanged by the row's number, so that
-// the 8 lanes that LDS serves together read different banks.
-template <int TILE, bool SPLIT, int MODE>
-__global__ __launch_bounds__(256) void k_muon_product(MuonArgs a, const int32_t *err) {
-    constexpr int W = TILE / 2, F = W / 32, STAGE = TILE * 128, LOADS = TILE * 8 / 256, BK = SPLIT ? 32 : 64, S = SPLIT ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][STAGE];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t b = blockIdx.y;
-    int ti, tj;
+template <bool SPLIT> __device__ __forceinline__ void get8(const f16_t *m, int r, int k, int K, float (&v)[8]) {
+    const f16_t *p = m + place8<SPLIT>(r, k, K);
+    const half8 hi = *reinterpret_cast<const half8 *>(p);
+    half8 lo = {};
+    if constexpr (SPLIT) lo = *reinterpret_cast<const half8 *>(p + 512);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = SPLIT ? (float)hi[e] + (float)lo[e] : (float)hi[e];
+}
+// eight neighbouring numbers of a row of the result, of which `left` are its
+__device__ __forceinline__ void put_result(const MuonArgs &a, int64_t row, int col, const float (&v)[8], int left) {
+    if (a.val) {
+        float *w = a.val + (a.first + row) * a.L + col;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) w[e] = a.keep * w[e] - a.step * v[e];
+        return;
+    }
+    const int64_t at = row * a.to_ld + col;
+    if (a.to_vec && left >= 8) {
+        Vec<float, 8> x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = v[e];
+        if (a.to_type == PS_F32) store_vec<float, 8>(reinterpret_cast<float *>(a.to) + at, x);
+        else if (a.to_type == PS_BF16) store_vec<bf16_t, 8>(reinterpret_cast<bf16_t *>(a.to) + at, x);
+        else store_vec<f16_t, 8>(reinterpret_cast<f16_t *>(a.to) + at, x);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (e >= left) break;
+        if (a.to_type == PS_F32) reinterpret_cast<float *>(a.to)[at + e] = v[e];
+        else if (a.to_type == PS_BF16) reinterpret_cast<bf16_t *>(a.to)[at + e] = (bf16_t)v[e];
+        else reinterpret_cast<f16_t *>(a.to)[at + e] = (f16_t)v[e];
+    }
+}
+// Which tile a workgroup has, and which share of the sum over k.  Workgroups go to the compute dies in turn: each die gets
+// neighbouring tiles, whose rows its cache then holds.
+struct Place { int64_t b; int ti, tj, share, tile; };
+template <int MODE>
+__device__ __forceinline__ Place place_of(const MuonArgs &a, uint32_t block, uint32_t all) {
+    const uint32_t die = block % DIES, at = die * (all / DIES) + (die < all % DIES ? die : all % DIES) + block / DIES;
+    Place p;
+    p.share = (int)(at % (uint32_t)a.shares);
+    p.tile = (int)(at / (uint32_t)a.shares);
+    p.b = p.tile / a.tiles;
+    const int tile = p.tile % a.tiles;
     if constexpr (MODE == MUON_GRAM || MODE == MUON_POLY) {                   // on and below the diagonal, row by row
-        ti = (int)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
-        while ((ti + 1) * (ti + 2) / 2 <= (int)blockIdx.x) ++ti;
-        while (ti * (ti + 1) / 2 > (int)blockIdx.x) --ti;
-        tj = (int)blockIdx.x - ti * (ti + 1) / 2;
+        p.ti = (int)((sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
+        while ((p.ti + 1) * (p.ti + 2) / 2 <= tile) ++p.ti;
+        while (p.ti * (p.ti + 1) / 2 > tile) --p.ti;
+        p.tj = tile - p.ti * (p.ti + 1) / 2;
     } else {
-        ti = (int)blockIdx.x % a.tiles_i;
-        tj = (int)blockIdx.x / a.tiles_i;
+        p.ti = tile % a.tiles_i;
+        p.tj = tile / a.tiles_i;
     }
-    const int64_t row_bytes = (int64_t)a.K * S * 2;
-    const char *lhs = reinterpret_cast<const char *>(a.lhs + b * a.lhs_size) + (int64_t)ti * TILE * row_bytes;
-    const char *rhs = reinterpret_cast<const char *>(a.rhs + b * a.rhs_size) + (int64_t)tj * TILE * row_bytes;
-    // piece q of a stage: row q / 8, its place q % 8 in LDS holds the row's piece (q % 8) ^ (row % 8)
-    int64_t from[LOADS];
+    return p;
+}
+
+// The sums leave by way of LDS, 64 x 64 at a time, so that rows of the result and rows of its mirror image are both written in whole
+// lines; the sums of KS wavefronts are added there.  x: 32 x 32 pieces, of which a lane has column lane % 32, rows
+// 8 g + 4 (lane / 32) + 0..3 for g = 0..3; from row i0, column j0 of matrix p.b.  mine: where this wavefront puts them, sums: the first one's place.
+constexpr int SUMS_LD = 68;                      // a row of 64 sums in LDS: 32 rows' pieces of 16 bytes lie in all banks
+template <int FI, int FJ, int KS, bool SPLIT, int MODE>
+__device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, const floatx16 (&x)[FI][FJ], int i0, int j0, float *mine, const float *sums, int group) {
+    constexpr float FACTOR = MODE == MUON_GRAM ? G_SCALE / (X_SCALE * X_SCALE) : MODE == MUON_APPLY ? 1.0f / P_SCALE : MODE == MUON_LAST ? 1.0f / (P_SCALE * X_SCALE) : 1.0f;
+    const bool rows = !(MODE == MUON_LAST && a.tall);
+    const bool columns = MODE == MUON_APPLY || (MODE == MUON_LAST && a.tall) || ((MODE == MUON_GRAM || MODE == MUON_POLY) && p.ti != p.tj);
+    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        const int q = (i * 4 + wave) * 64 + lane, row = q >> 3;
-        from[i] = row * row_bytes + (((q & 7) ^ (row & 7)) << 4);
-    }
-    const auto load = [&](int stage, int kt) {
+    for (int si = 0; si < FI / 2; ++si)
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int at = (i * 4 + wave) * 1024;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(lhs + from[i] + (int64_t)kt * 128),
-                                             (__attribute__((address_space(3))) void *)(&lds[stage][0][at]), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(rhs + from[i] + (int64_t)kt * 128),
-                                             (__attribute__((address_space(3))) void *)(&lds[stage][1][at]), 16, 0, 0);
-        }
-    };
-    const int wi = (wave >> 1) * W, wj = (wave & 1) * W, l32 = lane & 31, h = lane >> 5;
-    const auto piece = [&](int stage, int side, int row, int c) {
-        return *reinterpret_cast<const half8 *>(&lds[stage][side][row * 128 + ((c ^ (row & 7)) << 4)]);
-    };
-    floatx16 acc[F][F];
+        for (int sj = 0; sj < FJ / 2; ++sj) {
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+            for (int fi = 0; fi < 2; ++fi)
 #pragma unroll
-        for (int j = 0; j < F; ++j) acc[i][j] = floatx16{};
-    // The matrix instruction does not round its sums to the nearest: a chain of them loses up to a unit in the last place at each link, always the
-    // same way.  (One row of 5,000 in a chain of 313: an error of 72 units of 2^-24.)  So with numbers of 24 bits the chains are cut
-    // and their sums added by ordinary additions.
-    floatx16 total[SPLIT ? F : 1][SPLIT ? F : 1];
-    if constexpr (SPLIT) {
+                for (int fj = 0; fj < 2; ++fj)
 #pragma unroll
-        for (int i = 0; i < F; ++i)
+                    for (int e = 0; e < 16; ++e) mine[(fi * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) * SUMS_LD + fj * 32 + l32] = x[2 * si + fi][2 * sj + fj][e];
+            if constexpr (KS > 1) __syncthreads();
+            else asm volatile("" ::: "memory");                                // (a wavefront's accesses to LDS stay in order)
+            const int gi = i0 + si * 64, gj = j0 + sj * 64;
+            for (int way = rows ? 0 : 1; way < (columns ? 2 : 1); ++way) {
+#pragma unroll 2
+                for (int q = group; q < 8; q += KS) {
+                    const int r = (q & 1) * 32 + l32, c = (q >> 1) * 16 + h * 8;   // row r of what is written, numbers c .. c + 7
+                    float v[8];
 #pragma unroll
-            for (int j = 0; j < F; ++j) total[i][j] = floatx16{};
-    }
-    const int kts = a.K / BK;
-    load(0, 0);
-    for (int kt = 0; kt < kts; ++kt) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);                                    // vmcnt(0): this wavefront's part of the stage is there
-        __syncthreads();                                                       // and so are the others'; the other stage has been read
-        if (kt + 1 < kts) load((kt + 1) & 1, kt + 1);
-        const int st = kt & 1;
+                    for (int e = 0; e < 8; ++e) {
+                        const int w = way ? (c + e) * SUMS_LD + r : r * SUMS_LD + c + e;
+                        v[e] = sums[w];
 #pragma unroll
-        for (int s = 0; s < BK / 16; ++s) {
-            half8 l[F][S], r[F][S];
-#pragma unroll
-            for (int f = 0; f < F; ++f)
-#pragma unroll
-                for (int e = 0; e < S; ++e) {
-                    const int c = SPLIT ? 4 * s + 2 * h + e : 2 * s + h;
-                    l[f][e] = piece(st, 0, wi + f * 32 + l32, c);
-                    r[f][e] = piece(st, 1, wj + f * 32 + l32, c);
-                }
-#pragma unroll
-            for (int i = 0; i < F; ++i)
-#pragma unroll
-                for (int j = 0; j < F; ++j) {
-                    if constexpr (SPLIT) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][1], r[j][0], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][0], r[j][1], acc[i][j], 0, 0, 0);
+                        for (int k = 1; k < KS; ++k) v[e] += sums[k * (64 * SUMS_LD) + w];
+                        v[e] *= FACTOR;
                     }
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][0], r[j][0], acc[i][j], 0, 0, 0);
-                }
-        }
-        if constexpr (SPLIT) {
-            if ((kt & (CHAIN - 1)) == CHAIN - 1) {
+                    const int R = (way ? gj : gi) + r, C = (way ? gi : gj) + c;
+                    if constexpr (MODE == MUON_LAST) {
+                        const int height = way ? a.m : a.n, width = way ? a.n : a.m;
+                        if (R < height && C < width) put_result(a, p.b * height + R, C, v, width - C);
+                    } else {
+                        if constexpr (MODE == MUON_POLY) {                    // (A is symmetric: it is read as the result is written)
+                            float g[8];
+                            get8<SPLIT>(a.lhs + p.b * a.lhs_size, R, C, a.K, g);
 #pragma unroll
-                for (int i = 0; i < F; ++i)
-#pragma unroll
-                    for (int j = 0; j < F; ++j) { total[i][j] = total[i][j] + acc[i][j]; acc[i][j] = floatx16{}; }
-            }
-        }
-    }
-    if constexpr (SPLIT) {
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j) acc[i][j] = total[i][j] + acc[i][j];
-    }
-    // the result: of a 32 x 32 piece a lane has column lane % 32, rows 8 g + 4 (lane / 32) + 0..3 for g = 0..3
-    if (MODE == MUON_LAST && a.val && *(volatile const int32_t *)err) return;
-#pragma unroll
-    for (int fi = 0; fi < F; ++fi)
-#pragma unroll
-        for (int fj = 0; fj < F; ++fj)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int i = ti * TILE + wi + fi * 32 + 8 * g + 4 * h, j = tj * TILE + wj + fj * 32 + l32;
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[fi][fj][g * 4 + e];
-                if constexpr (MODE == MUON_LAST) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (i + e >= a.n || j >= a.m) continue;
-                        const float x = v[e] * (1.0f / (P_SCALE * X_SCALE));
-                        const int64_t row = b * (a.tall ? a.m : a.n) + (a.tall ? j : i + e), col = a.tall ? i + e : j;
-                        if (a.val) {
-                            float *w = a.val + (a.first + row) * a.L + col;
-                            *w = a.keep * *w - a.step * x;
-                        } else if (a.to_type == PS_F32) reinterpret_cast<float *>(a.to)[row * a.to_ld + col] = x;
-                        else if (a.to_type == PS_BF16) reinterpret_cast<bf16_t *>(a.to)[row * a.to_ld + col] = (bf16_t)x;
-                        else reinterpret_cast<f16_t *>(a.to)[row * a.to_ld + col] = (f16_t)x;
-                    }
-                } else {
-                    f16_t *out = a.out + b * a.out_size;
-                    if constexpr (MODE == MUON_GRAM) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] *= G_SCALE / (X_SCALE * X_SCALE);
-                    }
-                    if constexpr (MODE == MUON_APPLY) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] *= 1.0f / P_SCALE;
-                    }
-                    if constexpr (MODE == MUON_POLY) {
-                        // A at these places (it is symmetric: four in a row)
-                        const f16_t *p = a.lhs + b * a.lhs_size + place<SPLIT>(j, i, a.K);
-                        const half4 hi = *reinterpret_cast<const half4 *>(p);
-                        half4 lo = {};
-                        if constexpr (SPLIT) lo = *reinterpret_cast<const half4 *>(p + 8);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float g1 = SPLIT ? (float)hi[e] + (float)lo[e] : (float)hi[e];
-                            v[e] = v[e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g1 * (NS_B * P_SCALE / G_SCALE) + (i + e == j ? NS_A * P_SCALE : 0.0f);
+                            for (int e = 0; e < 8; ++e)
+                                v[e] = v[e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g[e] * (NS_B * P_SCALE / G_SCALE) + (R == C + e ? NS_A * P_SCALE : 0.0f);
                         }
-                    }
-                    half4 hi, lo;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        hi[e] = (f16_t)v[e];
-                        lo[e] = (f16_t)(v[e] - (float)hi[e]);
-                        f16_t *p = out + place<SPLIT>(i + e, j, a.out_ld);
-                        p[0] = hi[e];
-                        if constexpr (SPLIT) p[8] = lo[e];
-                    }
-                    f16_t *t = nullptr;                                       // the mirror place, or X transposed
-                    if constexpr (MODE == MUON_APPLY) t = a.out_t + b * a.out_size + place<SPLIT>(j, i, a.out_t_ld);
-                    else if (ti != tj) t = out + place<SPLIT>(j, i, a.out_ld);
-                    if (t) {
-                        *reinterpret_cast<half4 *>(t) = hi;
-                        if constexpr (SPLIT) *reinterpret_cast<half4 *>(t + 8) = lo;
+                        if (MODE == MUON_APPLY && way) put8<SPLIT>(a.out_t + p.b * a.out_size, R, C, a.out_t_ld, v);
+                        else put8<SPLIT>(a.out + p.b * a.out_size, R, C, a.out_ld, v);
                     }
                 }
             }
+            asm volatile("" ::: "memory");
+        }
+}
+
+// The sums of a wavefront: C[i][j] += sum_k L[i][k] R[j][k], 32 x 32 pieces (v_mfma_f32_32x32x16_f16).
+// The matrix instruction does not round its sums to the nearest: a chain of them loses up to a unit in the last place at each link, always the
+// same way.  (One row of 5,000 in a chain of 313: an error of 72 units of 2^-24.)  So with numbers of 24 bits the chains are cut, and their sums
+// added by ordinary additions.
+template <int FI, int FJ, bool SPLIT> struct Sums {
+    floatx16 acc[FI][FJ], total[SPLIT ? FI : 1][SPLIT ? FJ : 1];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) {
+                acc[i][j] = floatx16{};
+                if constexpr (SPLIT) total[i][j] = floatx16{};
+            }
+    }
+    template <int S> __device__ __forceinline__ void add(const half8 (&l)[FI][S], const half8 (&r)[FJ][S]) {
+#pragma unroll
+        for (int e = SPLIT ? 2 : 0; e >= 0; --e)                              // low high, high low, high high
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][e == 2 ? S - 1 : 0], r[j][e == 1 ? S - 1 : 0], acc[i][j], 0, 0, 0);
+    }
+    __device__ __forceinline__ void cut() {
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) { total[i][j] = total[i][j] + acc[i][j]; acc[i][j] = floatx16{}; }
+        }
+    }
+    __device__ __forceinline__ const floatx16 (&all() const)[FI][FJ] {
+        if constexpr (SPLIT) return total;
+        else return acc;
+    }
+};
+
+// Few or small tiles: 64 x 64 per workgroup, and its four wavefronts share the sum over k, a block in turn.  Operands come straight
+// from memory, DEPTH blocks ahead; nobody waits for anybody before the end.
+template <bool SPLIT, int MODE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_muon_small(MuonArgs a, const int32_t *err) {
+    constexpr int KS = 4, S = SPLIT ? 2 : 1, DEPTH = SPLIT ? 3 : 4;
+    __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];
+    const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const Place p = place_of<MODE>(a, blockIdx.x, gridDim.x);
+    const int i0 = p.ti * 64, j0 = p.tj * 64, blocks = a.K >> 4, cnt = blocks / KS;               // (sides are multiples of 64)
+    const f16_t *l = a.lhs + p.b * a.lhs_size + ((int64_t)(i0 >> 5) * blocks + group) * (512 * S), *r = a.rhs + p.b * a.rhs_size + ((int64_t)(j0 >> 5) * blocks + group) * (512 * S);
+    const int64_t next_rows = (int64_t)blocks * (512 * S);
+    half8 lf[DEPTH][2][S], rf[DEPTH][2][S];
+    const auto load = [&](half8 (&x)[2][S], half8 (&y)[2][S], int t) {
+        const int64_t off = (int64_t)t * (KS * 512 * S);
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int e = 0; e < S; ++e) {
+                x[f][e] = *reinterpret_cast<const half8 *>(l + off + f * next_rows + e * 512 + lane * 8);
+                y[f][e] = *reinterpret_cast<const half8 *>(r + off + f * next_rows + e * 512 + lane * 8);
+            }
+    };
+    Sums<2, 2, SPLIT> s;
+    s.clear();
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (d < cnt) load(lf[d], rf[d], d);
+    for (int c0 = 0; c0 < cnt; c0 += CHAIN) {
+        const int c1 = c0 + CHAIN < cnt ? c0 + CHAIN : cnt;
+        for (int t0 = c0; t0 < c1; t0 += DEPTH) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                const int t = t0 + d;
+                if (t < c1) {
+                    s.add(lf[d], rf[d]);
+                    if (t + DEPTH < cnt) load(lf[d], rf[d], t + DEPTH);
+                }
+            }
+        }
+        s.cut();
+    }
+    if (MODE == MUON_LAST && a.val && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
+    put_tile<2, 2, KS, SPLIT, MODE>(a, p, s.all(), i0, j0, lds[group], lds[0], group);
+}
+
+// until at most N of this wavefront's loads are on their way and all it has asked of LDS is there, then until all wavefronts are so far
+template <int N> __device__ __forceinline__ void wait_and_meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The order of a turn's instructions: after a product a read of LDS, as long as there are any, and the loads spread over the products - a
+// wavefront that has a vector unit to itself keeps its matrix pipe fed.
+template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinline__ void interleave() {
+    constexpr int R = (I + 1) * READS / PRODUCTS - I * READS / PRODUCTS, L = (I + 1) * LOADS / PRODUCTS - I * LOADS / PRODUCTS;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (R > 0) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+    if constexpr (L > 0) __builtin_amdgcn_sched_group_barrier(0x020, L, 0);
+    if constexpr (I + 1 < PRODUCTS) interleave<PRODUCTS, READS, LOADS, I + 1>();
+}
+
+// Larger ones: 64 FI x 64 FJ per workgroup, a quarter per wavefront, operands by way of LDS, so that a line is read from the die's cache by
+// one wavefront and used by two.  A stage has KB blocks of k; STAGES of them are in LDS or on their way there, straight from memory.  A wavefront
+// asks for the next block's operands before it multiplies the ones it has, also across the meeting of the wavefronts at which a
+// stage is given up and the next one is known to be there.
+template <int FI, int FJ, int KB, int STAGES, bool SPLIT, int MODE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu((FI + FJ) * KB * (SPLIT ? 2 : 1) <= 8 ? 2 : 1))) void k_muon_large(MuonArgs a, const int32_t *err) {
+    constexpr int S = SPLIT ? 2 : 1, TI = 64 * FI, TJ = 64 * FJ, U = KB == 1 ? 2 : KB, PER = KB * S, PIECES = (2 * FI + 2 * FJ) * PER, MINE = PIECES / 4, STAGE = PIECES * 1024;
+    static_assert(STAGES >= 3 && U % 2 == 0 && PIECES % 4 == 0 && MINE % KB == 0 && (2 * FI * PER) % MINE == 0 && MINE % PER == 0, "a wavefront's pieces are whole rows of one operand");
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const Place p = place_of<MODE>(a, blockIdx.x, gridDim.x);
+    const int blocks = a.K >> 4, turns = blocks / U, first = (int)((int64_t)turns * p.share / a.shares), cnt = (int)((int64_t)turns * (p.share + 1) / a.shares) - first;
+    // what this wavefront fetches of a stage: pieces of 1,024 bytes, PER of a block of rows
+    const char *from[MINE / PER];
+#pragma unroll
+    for (int i = 0; i < MINE / PER; ++i) {
+        const int rows = wave * (MINE / PER) + i;                             // block of 32 rows: first the left operand's 2 FI, then the right one's
+        const f16_t *m = rows < 2 * FI ? a.lhs + p.b * a.lhs_size + (int64_t)(p.ti * (2 * FI) + rows) * blocks * (512 * S)
+                                       : a.rhs + p.b * a.rhs_size + (int64_t)(p.tj * (2 * FJ) + rows - 2 * FI) * blocks * (512 * S);
+        from[i] = reinterpret_cast<const char *>(m) + (int64_t)first * (U * S * 1024);
+    }
+    const uint32_t lane16 = lane * 16;
+    const int last = cnt * (U / KB) - 1;
+    // a KB-th of stage t, into its slot; behind the last stage that one once more, into a slot that nobody reads, so that all turns are alike
+    const auto fetch = [&](int slot, int t, int kb) {
+        const int64_t off = (int64_t)(t < last ? t : last) * (PER * 1024);
+#pragma unroll
+        for (int i = kb * MINE / KB; i < (kb + 1) * MINE / KB; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from[i / PER] + off + (i % PER) * 1024 + lane16),
+                                             (__attribute__((address_space(3))) void *)(lds + slot * STAGE + (wave * MINE + i) * 1024), 16, 0, 0);
+    };
+    const int wi = wave >> 1, wj = wave & 1;
+    half8 lf[2][FI][S], rf[2][FJ][S];
+    const auto read = [&](half8 (&x)[FI][S], half8 (&y)[FJ][S], int slot, int kb) {
+        const unsigned char *at = lds + slot * STAGE + lane * 16;
+#pragma unroll
+        for (int f = 0; f < FI; ++f)
+#pragma unroll
+            for (int e = 0; e < S; ++e) x[f][e] = *reinterpret_cast<const half8 *>(at + ((wi * FI + f) * PER + kb * S + e) * 1024);
+#pragma unroll
+        for (int f = 0; f < FJ; ++f)
+#pragma unroll
+            for (int e = 0; e < S; ++e) y[f][e] = *reinterpret_cast<const half8 *>(at + ((2 * FI + wj * FJ + f) * PER + kb * S + e) * 1024);
+    };
+    Sums<FI, FJ, SPLIT> s;
+    s.clear();
+#pragma unroll
+    for (int t = 0; t < STAGES - 1; ++t)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) fetch(t, t, kb);
+    wait_and_meet<(STAGES - 2) * MINE>();
+    read(lf[0], rf[0], 0, 0);
+    int slot = 0, into = STAGES - 1, stage = 0;                               // where this stage is, and stage + STAGES - 1 goes
+    for (int c0 = 0; c0 < cnt; c0 += CHAIN / U) {
+        const int c1 = c0 + CHAIN / U < cnt ? c0 + CHAIN / U : cnt;
+        for (int t = c0; t < c1; ++t) {
+#pragma unroll
+            for (int kb = 0; kb < U; ++kb) {
+                const bool end = (kb + 1) % KB == 0;                          // of the stage: it has been read, and the next one is there
+                if (end) wait_and_meet<(STAGES - 3) * MINE + (KB - 1) * MINE / KB>();
+                const int next = !end ? slot : slot + 1 == STAGES ? 0 : slot + 1;
+                read(lf[(kb + 1) & 1], rf[(kb + 1) & 1], next, (kb + 1) % KB);
+                fetch(into, stage + STAGES - 1, kb % KB);
+                s.add(lf[kb & 1], rf[kb & 1]);
+                interleave<FI * FJ * (SPLIT ? 3 : 1), (FI + FJ) * S, MINE / KB>();
+                if (end) { into = slot; slot = next; ++stage; }
+            }
+        }
+        s.cut();
+    }
+    wait_and_meet<0>();                                                       // (nothing is on its way to LDS, and all stages have been read)
+    if (MODE == MUON_LAST && a.val && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
+    if (a.shares > 1) {
+        // a share of the sums: 16 bytes per lane at a time, as they are
+        floatx4 *to = reinterpret_cast<floatx4 *>(a.part) + ((int64_t)(p.tile * a.shares + p.share) * 4 + wave) * (FI * FJ * 4 * 64) + lane;
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const floatx16 v = s.all()[i][j];
+                    to[((i * FJ + j) * 4 + g) * 64] = floatx4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+                }
+        return;
+    }
+    float *const mine = reinterpret_cast<float *>(lds) + wave * (64 * SUMS_LD);
+    put_tile<FI, FJ, 1, SPLIT, MODE>(a, p, s.all(), p.ti * TI + wi * FI * 32, p.tj * TJ + wj * FJ * 32, mine, mine, 0);
+}
+
+// The shares of the sums added, in order; a wavefront has what one had in the kernel before.
+template <int FI, int FJ, bool SPLIT, int MODE>
+__global__ __launch_bounds__(64) void k_muon_join(MuonArgs a, int32_t shares) {
+    __shared__ __attribute__((aligned(16))) float lds[64 * SUMS_LD];
+    const Place p = place_of<MODE>(a, blockIdx.x >> 2, gridDim.x >> 2);       // (a.shares is 1 here)
+    const int wave = blockIdx.x & 3, lane = threadIdx.x;
+    floatx16 x[FI][FJ];
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) x[i][j] = floatx16{};
+    const floatx4 *from = reinterpret_cast<const floatx4 *>(a.part) + ((int64_t)p.tile * shares * 4 + wave) * (FI * FJ * 4 * 64) + lane;
+    for (int k = 0; k < shares; ++k) {
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const floatx4 v = from[(int64_t)k * (4 * FI * FJ * 4 * 64) + ((i * FJ + j) * 4 + g) * 64];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][j][4 * g + e] += v[e];
+                }
+    }
+    put_tile<FI, FJ, 1, SPLIT, MODE>(a, p, x, p.ti * 64 * FI + (wave >> 1) * FI * 32, p.tj * 64 * FJ + (wave & 1) * FJ * 32, lds, lds, 0);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
+// Sides count as multiples of the tile's.  256: large matrices of 16 bits; 128: where a quarter as many tiles of 128 as there
+// are numbers of them ... ; 64: the rest.
+#ifndef MIDN
+#define MIDN 256
+#endif
 struct MuonPlan {
     int32_t batch, n, m, tile, np, mp, blocks;
     bool tall, split;
-    size_t off_d, off_x, off_xt[2], off_g, off_p, bytes;
+    size_t off_d, off_x, off_xt[2], off_g, off_p, off_part, bytes;
 };
-MuonPlan muon_plan(int32_t batch, int32_t rows, int32_t cols, bool split, bool step) {
+inline int64_t half_of(int64_t t) { return t * (t + 1) / 2; }
+constexpr int MOST_SHARES = 8, STAGES_AT_LEAST = 2;
+// Workgroups that share a tile's sum over k: where there are fewer tiles than compute units.
+int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t stages) {
+    int64_t s = ps->num_cu / tiles;
+    if (s > MOST_SHARES) s = MOST_SHARES;
+    if (s > stages / STAGES_AT_LEAST) s = stages / STAGES_AT_LEAST;
+    return s < 2 ? 1 : (int)s;
+}
+MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols, bool split, bool step) {
     MuonPlan p{};
     p.batch = batch; p.tall = rows > cols; p.split = split;
     p.n = p.tall ? cols : rows; p.m = p.tall ? rows : cols;
     p.tile = 64;
-    if (ceil_div64(p.n, 128) * ceil_div64(p.n, 128) * batch >= 128) p.tile = 128;
+    if (p.n > MIDN) p.tile = 128;
+    if (!split && half_of(ceil_div64(p.n, 256)) * batch >= ps->num_cu) p.tile = 256;
     p.np = (int32_t)(ceil_div64(p.n, p.tile) * p.tile); p.mp = (int32_t)(ceil_div64(p.m, p.tile) * p.tile);
-    p.blocks = (int32_t)(ceil_div64(rows, 4) < NORM_BLOCKS ? ceil_div64(rows, 4) : NORM_BLOCKS);
+    const int64_t blocks = ceil_div64((int64_t)rows * cols, 4096);
+    p.blocks = (int32_t)(blocks < NORM_BLOCKS ? blocks : NORM_BLOCKS);
     const size_t size = split ? 4 : 2, nm = (size_t)batch * p.np * p.mp * size, nn = (size_t)batch * p.np * p.np * size;
     p.off_d = up256((size_t)batch * NORM_BLOCKS * sizeof(double));
     p.off_x = p.off_d + (step ? up256((size_t)batch * rows * cols * sizeof(float)) : 0);
@@ -335,14 +537,43 @@ MuonPlan muon_plan(int32_t batch, int32_t rows, int32_t cols, bool split, bool s
     p.off_xt[1] = p.off_xt[0] + up256(nm);
     p.off_g = p.off_xt[1] + up256(nm);
     p.off_p = p.off_g + up256(nn);
-    p.bytes = p.off_p + up256(nn);
+    p.off_part = p.off_p + up256(nn);
+    // (shares times tiles are at most as many as the compute units)
+    p.bytes = p.off_part + (p.tile == 128 ? (size_t)ps->num_cu * 128 * 128 * sizeof(float) : 0);
     return p;
 }
 
+template <int FI, int FJ, int KB, int STAGES, bool SPLIT, int MODE>
+int large(dpaps_ps *ps, const MuonArgs &a, int64_t tiles, hipStream_t st) {
+    static LdsAllowed allowed;
+    constexpr int STAGED = STAGES * 2 * (FI + FJ) * KB * (SPLIT ? 2 : 1) * 1024, SUMMED = 4 * 64 * SUMS_LD * 4, LDS = STAGED > SUMMED ? STAGED : SUMMED;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_large<FI, FJ, KB, STAGES, SPLIT, MODE>), LDS);
+    if (rc) return rc;
+    k_muon_large<FI, FJ, KB, STAGES, SPLIT, MODE><<<(unsigned)(tiles * a.shares), 256, LDS, st>>>(a, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
 template <int TILE, bool SPLIT, int MODE>
-int product(dpaps_ps *ps, const MuonArgs &a, int32_t batch, hipStream_t st) {
-    const int64_t tiles = MODE == MUON_GRAM || MODE == MUON_POLY ? (int64_t)a.tiles_i * (a.tiles_i + 1) / 2 : (int64_t)a.tiles_i * a.tiles_j;
-    k_muon_product<TILE, SPLIT, MODE><<<dim3((unsigned)tiles, (unsigned)batch), 256, 0, st>>>(a, ps->err);
+int product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
+    constexpr bool HALF = MODE == MUON_GRAM || MODE == MUON_POLY;
+    a.tiles = (int32_t)(HALF ? half_of(a.tiles_i) : (int64_t)a.tiles_i * a.tiles_j);
+    a.shares = 1;
+    const int64_t tiles = (int64_t)a.tiles * batch;
+    if constexpr (TILE == 64) {
+        k_muon_small<SPLIT, MODE><<<(unsigned)tiles, 256, 0, st>>>(a, ps->err);
+    } else if constexpr (TILE == 256) {
+        return large<4, 4, 2, 4, SPLIT, MODE>(ps, a, tiles, st);
+    } else {
+        constexpr int KB = SPLIT ? 2 : 4;                                     // so 128 KB of LDS; half of that where two workgroups share a compute unit
+        if constexpr (HALF) a.shares = shares_of(ps, tiles, a.K / 64);
+        const int rc = tiles > ps->num_cu ? large<2, 2, KB / 2, 4, SPLIT, MODE>(ps, a, tiles, st) : large<2, 2, KB, 4, SPLIT, MODE>(ps, a, tiles, st);
+        if (rc || a.shares == 1) return rc;
+        if constexpr (HALF) {
+            const int32_t shares = a.shares;
+            a.shares = 1;
+            k_muon_join<2, 2, SPLIT, MODE><<<(unsigned)(4 * tiles), 64, 0, st>>>(a, shares);
+        }
+    }
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
@@ -357,6 +588,7 @@ int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t s
     for (int s = 0; s < steps; ++s) {
         MuonArgs a{};
         a.tiles_i = p.np / TILE; a.tiles_j = p.mp / TILE;
+        a.part = (float *)(ws + p.off_part);
         a.lhs = a.rhs = x; a.lhs_size = a.rhs_size = nm; a.K = p.mp; a.out = g; a.out_ld = p.np; a.out_size = nn;
         int rc = product<TILE, SPLIT, MUON_GRAM>(ps, a, p.batch, st);
         if (rc) return rc;
@@ -378,16 +610,37 @@ int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t s
     return PS_OK;
 }
 
+template <class T>
+int norm_of(dpaps_ps *ps, const MuonPlan &p, const MuonIn &in, hipStream_t st) {
+    const dim3 grid((unsigned)p.blocks, (unsigned)p.batch);
+    const bool four = rows_allow(in.in, in.type, in.cols, in.ld, 4) &&
+                      (!in.val || (rows_allow(in.val + in.first * in.L + in.cols, PS_F32, in.cols, in.L, 4) && rows_allow(in.d, PS_F32, in.cols, in.cols, 4)));
+    const uint32_t P = (uint32_t)(four ? in.cols / 4 : in.cols);
+    if (in.val) {
+        if (four) k_muon_norm<T, 4, true><<<grid, 256, 0, st>>>(in, P, 1.0 / P, ps->err);
+        else k_muon_norm<T, 1, true><<<grid, 256, 0, st>>>(in, P, 1.0 / P, ps->err);
+    } else {
+        if (four) k_muon_norm<T, 4, false><<<grid, 256, 0, st>>>(in, P, 1.0 / P, ps->err);
+        else k_muon_norm<T, 1, false><<<grid, 256, 0, st>>>(in, P, 1.0 / P, ps->err);
+    }
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+
 int orthogonalize(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t steps, hipStream_t st) {
     char *ws = (char *)ps->ws;
     in.squares = (double *)ws;
     in.blocks = p.blocks;
     if (in.val) in.d = (float *)(ws + p.off_d);
-    k_muon_norm<<<dim3((unsigned)p.blocks, (unsigned)p.batch), 256, 0, st>>>(in, ps->err);
-    PS_HIP(ps, hipGetLastError());
+    int rc;
+    if (in.type == PS_F32) rc = norm_of<float>(ps, p, in, st);
+    else if (in.type == PS_BF16) rc = norm_of<bf16_t>(ps, p, in, st);
+    else rc = norm_of<f16_t>(ps, p, in, st);
+    if (rc) return rc;
     if (in.val) { in.in = in.d; in.ld = in.cols; in.type = PS_F32; }
     last.n = p.n; last.m = p.m; last.tall = p.tall;
     if (p.split) return p.tile == 128 ? iterate<128, true>(ps, p, in, last, steps, st) : iterate<64, true>(ps, p, in, last, steps, st);
+    if (p.tile == 256) return iterate<256, false>(ps, p, in, last, steps, st);
     return p.tile == 128 ? iterate<128, false>(ps, p, in, last, steps, st) : iterate<64, false>(ps, p, in, last, steps, st);
 }
 
@@ -401,13 +654,13 @@ extern "C" int muon_orthogonalize(ps_handle ps, int32_t batch, int32_t rows, int
     if (batch == 0 || rows == 0 || cols == 0) return PS_OK;
     if (!in || !out || in_ld < cols || out_ld < cols) return PS_EINVAL;
     if (!sizes_allowed(batch, rows, cols)) return PS_ELIMIT;
-    const MuonPlan p = muon_plan(batch, rows, cols, out_type != PS_BF16, false);
+    const MuonPlan p = muon_plan(ps, batch, rows, cols, out_type != PS_BF16, false);
     const int rc = dpaps_ws_reserve(ps, p.bytes);
     if (rc) return rc;
     MuonIn a{};
     a.in = in; a.ld = in_ld; a.type = in_type; a.rows = rows; a.cols = cols; a.eps = eps;
     MuonArgs last{};
-    last.to = out; last.to_ld = out_ld; last.to_type = out_type;
+    last.to = out; last.to_ld = out_ld; last.to_type = out_type; last.to_vec = rows_allow(out, out_type, 8, out_ld, 8);
     return orthogonalize(ps, p, a, last, steps, (hipStream_t)stream);
 }
 
@@ -421,7 +674,7 @@ extern "C" int muon_step(ps_handle ps, int32_t worker, int64_t first_key, int32_
     if (!grad || grad_ld < dim) return PS_EINVAL;
     if (!sizes_allowed(batch, rows, dim)) return PS_ELIMIT;
     // (of numbers of 32 bits the products are, too, whatever the gradient's type)
-    const MuonPlan p = muon_plan(batch, rows, dim, true, true);
+    const MuonPlan p = muon_plan(ps, batch, rows, dim, true, true);
     int rc = dpaps_ws_reserve(ps, p.bytes);
     if (rc) return rc;
     hipStream_t st = (hipStream_t)stream;
