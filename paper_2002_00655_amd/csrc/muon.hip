@@ -19,6 +19,7 @@
 #include "token_ids.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace {
 
@@ -26,6 +27,7 @@ constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float X_SCALE = 16384.0f, G_SCALE = 16384.0f, P_SCALE = 8192.0f;
 
 typedef f16_t half8 __attribute__((ext_vector_type(8)));
+typedef f16_t half4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -152,13 +154,16 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
 }
 
 // ---- the products ---------------------------------------------------------------------------------------------------
+#ifndef GJ
+#define GJ 4
+#endif
 constexpr uint32_t DIES = 8;                     // compute dies, each with a cache of its own
 constexpr int CHAIN = 12;                        // blocks of k whose products one chain of matrix instructions adds (a multiple of DEPTH and KB)
-enum MuonProduct { MUON_GRAM, MUON_POLY, MUON_APPLY, MUON_LAST };
+enum MuonProduct { MUON_GRAM, MUON_POLY, MUON_APPLY, MUON_LAST, MUON_STEP };       // LAST, STEP: APPLY with the result put where it belongs
 struct MuonArgs {
     const f16_t *lhs, *rhs;                      // rows of K numbers
     int64_t lhs_size, rhs_size, out_size;        // of one matrix, in elements as they are stored
-    int32_t K, tiles_i, tiles_j, tiles;          // tiles: of one matrix
+    int32_t K, tiles_i, tiles_j, tiles, tile0;   // tiles: of one matrix; tile0: the first one of the launch
     int32_t shares; float *part;                 // workgroups that share a tile's sum over k, and where they put their sums
     f16_t *out; int32_t out_ld;                  // GRAM: A, POLY: P, APPLY: X
     f16_t *out_t; int32_t out_t_ld;              // APPLY: X transposed
@@ -175,52 +180,67 @@ template <bool SPLIT> __device__ __forceinline__ void get8(const f16_t *m, int r
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = SPLIT ? (float)hi[e] + (float)lo[e] : (float)hi[e];
 }
-// eight neighbouring numbers of a row of the result, of which `left` are its
-__device__ __forceinline__ void put_result(const MuonArgs &a, int64_t row, int col, const float (&v)[8], int left) {
-    if (a.val) {
-        float *w = a.val + (a.first + row) * a.L + col;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) w[e] = a.keep * w[e] - a.step * v[e];
-        return;
-    }
-    const int64_t at = row * a.to_ld + col;
+// Eight neighbouring numbers of a row of the result, of which `left` are its: what is there already (of a step), and what is written.
+__device__ __forceinline__ void get_weights(const MuonArgs &a, int64_t row, int col, float (&w)[8], int left) {
+    const float *p = a.val + (a.first + row) * a.L + col;
     if (a.to_vec && left >= 8) {
+        const Vec<float, 8> x = load_vec<float, 8>(p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = x[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = e < left ? p[e] : 0.0f;
+    }
+}
+template <class T> __device__ __forceinline__ void put_numbers(T *p, const float (&v)[8], int left, bool vec) {
+    if (vec && left >= 8) {
         Vec<float, 8> x;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = v[e];
-        if (a.to_type == PS_F32) store_vec<float, 8>(reinterpret_cast<float *>(a.to) + at, x);
-        else if (a.to_type == PS_BF16) store_vec<bf16_t, 8>(reinterpret_cast<bf16_t *>(a.to) + at, x);
-        else store_vec<f16_t, 8>(reinterpret_cast<f16_t *>(a.to) + at, x);
-        return;
-    }
+        store_vec<T, 8>(p, x);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (e >= left) break;
-        if (a.to_type == PS_F32) reinterpret_cast<float *>(a.to)[at + e] = v[e];
-        else if (a.to_type == PS_BF16) reinterpret_cast<bf16_t *>(a.to)[at + e] = (bf16_t)v[e];
-        else reinterpret_cast<f16_t *>(a.to)[at + e] = (f16_t)v[e];
+        for (int e = 0; e < 8; ++e)
+            if (e < left) p[e] = (T)v[e];
     }
 }
+__device__ __forceinline__ void put_result(const MuonArgs &a, int64_t row, int col, const float (&v)[8], int left) {
+    if (a.to_type == PS_F32) put_numbers(reinterpret_cast<float *>(a.to) + row * a.to_ld + col, v, left, a.to_vec);
+    else if (a.to_type == PS_BF16) put_numbers(reinterpret_cast<bf16_t *>(a.to) + row * a.to_ld + col, v, left, a.to_vec);
+    else put_numbers(reinterpret_cast<f16_t *>(a.to) + row * a.to_ld + col, v, left, a.to_vec);
+}
 // Which tile a workgroup has, and which share of the sum over k.  Workgroups go to the compute dies in turn: each die gets
-// neighbouring tiles, whose rows its cache then holds.
-struct Place { int64_t b; int ti, tj, share, tile; };
+// neighbouring tiles, in bands of four rows or columns, whose operands its cache then holds (32 tiles at a time: 4 and 8 blocks of rows).
+struct Place { int64_t b; int ti, tj, share, slot; };
 template <int MODE>
 __device__ __forceinline__ Place place_of(const MuonArgs &a, uint32_t block, uint32_t all) {
     const uint32_t die = block % DIES, at = die * (all / DIES) + (die < all % DIES ? die : all % DIES) + block / DIES;
     Place p;
     p.share = (int)(at % (uint32_t)a.shares);
-    p.tile = (int)(at / (uint32_t)a.shares);
-    p.b = p.tile / a.tiles;
-    const int tile = p.tile % a.tiles;
-    if constexpr (MODE == MUON_GRAM || MODE == MUON_POLY) {                   // on and below the diagonal, row by row
-        p.ti = (int)((sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
-        while ((p.ti + 1) * (p.ti + 2) / 2 <= tile) ++p.ti;
-        while (p.ti * (p.ti + 1) / 2 > tile) --p.ti;
-        p.tj = tile - p.ti * (p.ti + 1) / 2;
+    p.slot = (int)(at / (uint32_t)a.shares);
+    p.b = (a.tile0 + p.slot) / a.tiles;
+    const int tile = (a.tile0 + p.slot) % a.tiles;
+    if constexpr (MODE == MUON_GRAM || MODE == MUON_POLY) {
+        // on and below the diagonal: bands of four rows; in a band the columns before the diagonal one by one, then its triangle
+        const auto row_of = [](int t) {
+            int i = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+            while ((i + 1) * (i + 2) / 2 <= t) ++i;
+            while (i * (i + 1) / 2 > t) --i;
+            return i;
+        };
+        const int first = row_of(tile) & ~3, r = tile - first * (first + 1) / 2, rows = a.tiles_i - first < 4 ? a.tiles_i - first : 4;
+        if (r < first * rows) {
+            p.ti = first + r % rows;
+            p.tj = r / rows;
+        } else {
+            const int t = r - first * rows, i = row_of(t);
+            p.ti = first + i;
+            p.tj = first + t - i * (i + 1) / 2;
+        }
     } else {
-        p.ti = tile % a.tiles_i;
-        p.tj = tile / a.tiles_i;
+        const int first = tile / (GJ * a.tiles_i) * GJ, r = tile - first * a.tiles_i, columns = a.tiles_j - first < GJ ? a.tiles_j - first : GJ;
+        p.ti = r / columns;
+        p.tj = first + r % columns;
     }
     return p;
 }
@@ -231,41 +251,71 @@ __device__ __forceinline__ Place place_of(const MuonArgs &a, uint32_t block, uin
 constexpr int SUMS_LD = 68;                      // a row of 64 sums in LDS: 32 rows' pieces of 16 bytes lie in all banks
 template <int FI, int FJ, int KS, bool SPLIT, int MODE>
 __device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, const floatx16 (&x)[FI][FJ], int i0, int j0, float *mine, const float *sums, int group) {
-    constexpr float FACTOR = MODE == MUON_GRAM ? G_SCALE / (X_SCALE * X_SCALE) : MODE == MUON_APPLY ? 1.0f / P_SCALE : MODE == MUON_LAST ? 1.0f / (P_SCALE * X_SCALE) : 1.0f;
-    const bool rows = !(MODE == MUON_LAST && a.tall);
-    const bool columns = MODE == MUON_APPLY || (MODE == MUON_LAST && a.tall) || ((MODE == MUON_GRAM || MODE == MUON_POLY) && p.ti != p.tj);
+    constexpr float FACTOR = MODE == MUON_GRAM ? G_SCALE / (X_SCALE * X_SCALE) : MODE == MUON_APPLY ? 1.0f / P_SCALE : MODE >= MUON_LAST ? 1.0f / (P_SCALE * X_SCALE) : 1.0f;
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int si = 0; si < FI / 2; ++si)
 #pragma unroll
         for (int sj = 0; sj < FJ / 2; ++sj) {
+            const int gi = i0 + si * 64, gj = j0 + sj * 64;
+            const bool turned = MODE >= MUON_LAST && a.tall;                   // X is the transposed matrix
 #pragma unroll
             for (int fi = 0; fi < 2; ++fi)
 #pragma unroll
-                for (int fj = 0; fj < 2; ++fj)
+                for (int fj = 0; fj < 2; ++fj) {
+                    const floatx16 v = x[2 * si + fi][2 * sj + fj];
+                    if (turned) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) mine[(fi * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) * SUMS_LD + fj * 32 + l32] = x[2 * si + fi][2 * sj + fj][e];
+                        for (int g = 0; g < 4; ++g)
+                            *reinterpret_cast<floatx4 *>(&mine[(fj * 32 + l32) * SUMS_LD + fi * 32 + 8 * g + 4 * h]) = floatx4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) mine[(fi * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) * SUMS_LD + fj * 32 + l32] = v[e];
+                    }
+                }
             if constexpr (KS > 1) __syncthreads();
             else asm volatile("" ::: "memory");                                // (a wavefront's accesses to LDS stay in order)
-            const int gi = i0 + si * 64, gj = j0 + sj * 64;
-            for (int way = rows ? 0 : 1; way < (columns ? 2 : 1); ++way) {
-#pragma unroll 2
-                for (int q = group; q < 8; q += KS) {
-                    const int r = (q & 1) * 32 + l32, c = (q >> 1) * 16 + h * 8;   // row r of what is written, numbers c .. c + 7
-                    float v[8];
+            const auto sum = [&](int w) {
+                float v = sums[w];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int w = way ? (c + e) * SUMS_LD + r : r * SUMS_LD + c + e;
-                        v[e] = sums[w];
+                for (int k = 1; k < KS; ++k) v += sums[k * (64 * SUMS_LD) + w];
+                return v * FACTOR;
+            };
+            if constexpr (MODE >= MUON_LAST) {
+                // eight rows at a time, eight lanes a row; of a step the weights of all of them first
+                const int R0 = (turned ? gj : gi) + group * 8 + (lane >> 3), c = (lane & 7) * 8, C = (turned ? gi : gj) + c, height = turned ? a.m : a.n, left = (turned ? a.n : a.m) - C;
+                const auto at = [&](int q) { return (q * KS * 8 + group * 8 + (lane >> 3)) * SUMS_LD + c; };
+                if constexpr (MODE == MUON_STEP) {
+                    float w[8 / KS][8];
 #pragma unroll
-                        for (int k = 1; k < KS; ++k) v[e] += sums[k * (64 * SUMS_LD) + w];
-                        v[e] *= FACTOR;
+                    for (int q = 0; q < 8 / KS; ++q)
+                        if (R0 + q * KS * 8 < height) get_weights(a, p.b * height + R0 + q * KS * 8, C, w[q], left);
+#pragma unroll
+                    for (int q = 0; q < 8 / KS; ++q) {
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = a.keep * w[q][e] - a.step * sum(at(q) + e);
+                        if (R0 + q * KS * 8 < height) put_numbers(a.val + (a.first + p.b * height + R0 + q * KS * 8) * a.L + C, v, left, a.to_vec);
                     }
-                    const int R = (way ? gj : gi) + r, C = (way ? gi : gj) + c;
-                    if constexpr (MODE == MUON_LAST) {
-                        const int height = way ? a.m : a.n, width = way ? a.n : a.m;
-                        if (R < height && C < width) put_result(a, p.b * height + R, C, v, width - C);
-                    } else {
+                } else {
+#pragma unroll 1
+                    for (int q = 0; q < 8 / KS; ++q) {
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = sum(at(q) + e);
+                        if (R0 + q * KS * 8 < height) put_result(a, p.b * height + R0 + q * KS * 8, C, v, left);
+                    }
+                }
+            } else {
+                const bool columns = MODE == MUON_APPLY || p.ti != p.tj;
+                for (int way = 0; way < (columns ? 2 : 1); ++way) {
+#pragma unroll 2
+                    for (int q = group; q < 8; q += KS) {
+                        const int r = (q & 1) * 32 + l32, c = (q >> 1) * 16 + h * 8;   // row r of what is written, numbers c .. c + 7
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = sum(way ? (c + e) * SUMS_LD + r : r * SUMS_LD + c + e);
+                        const int R = (way ? gj : gi) + r, C = (way ? gi : gj) + c;
                         if constexpr (MODE == MUON_POLY) {                    // (A is symmetric: it is read as the result is written)
                             float g[8];
                             get8<SPLIT>(a.lhs + p.b * a.lhs_size, R, C, a.K, g);
@@ -361,7 +411,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
         s.cut();
     }
-    if (MODE == MUON_LAST && a.val && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
+    if (MODE == MUON_STEP && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
     put_tile<2, 2, KS, SPLIT, MODE>(a, p, s.all(), i0, j0, lds[group], lds[0], group);
 }
 
@@ -454,10 +504,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu((FI + FJ) *
         s.cut();
     }
     wait_and_meet<0>();                                                       // (nothing is on its way to LDS, and all stages have been read)
-    if (MODE == MUON_LAST && a.val && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
+    if (MODE == MUON_STEP && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
     if (a.shares > 1) {
         // a share of the sums: 16 bytes per lane at a time, as they are
-        floatx4 *to = reinterpret_cast<floatx4 *>(a.part) + ((int64_t)(p.tile * a.shares + p.share) * 4 + wave) * (FI * FJ * 4 * 64) + lane;
+        floatx4 *to = reinterpret_cast<floatx4 *>(a.part) + ((int64_t)(p.slot * a.shares + p.share) * 4 + wave) * (FI * FJ * 4 * 64) + lane;
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
@@ -473,51 +523,240 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu((FI + FJ) *
     put_tile<FI, FJ, 1, SPLIT, MODE>(a, p, s.all(), p.ti * TI + wi * FI * 32, p.tj * TJ + wj * FJ * 32, mine, mine, 0);
 }
 
-// The shares of the sums added, in order; a wavefront has what one had in the kernel before.
+// The shares of the sums added: a workgroup for 64 x 64 of a tile, each wavefront every fourth share, and then the four.
 template <int FI, int FJ, bool SPLIT, int MODE>
-__global__ __launch_bounds__(64) void k_muon_join(MuonArgs a, int32_t shares) {
-    __shared__ __attribute__((aligned(16))) float lds[64 * SUMS_LD];
-    const Place p = place_of<MODE>(a, blockIdx.x >> 2, gridDim.x >> 2);       // (a.shares is 1 here)
-    const int wave = blockIdx.x & 3, lane = threadIdx.x;
-    floatx16 x[FI][FJ];
+__global__ __launch_bounds__(256) void k_muon_join(MuonArgs a, int32_t shares) {
+    constexpr int KS = 4, PARTS = 4 * (FI / 2) * (FJ / 2);
+    __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];
+    const Place p = place_of<MODE>(a, blockIdx.x / PARTS, gridDim.x / PARTS);  // (a.shares is 1 here)
+    const int part = blockIdx.x % PARTS, wave = part & 3, si = (part >> 2) / (FJ / 2), sj = (part >> 2) % (FJ / 2);
+    const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    floatx16 x[2][2];
 #pragma unroll
-    for (int i = 0; i < FI; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < FJ; ++j) x[i][j] = floatx16{};
-    const floatx4 *from = reinterpret_cast<const floatx4 *>(a.part) + ((int64_t)p.tile * shares * 4 + wave) * (FI * FJ * 4 * 64) + lane;
-    for (int k = 0; k < shares; ++k) {
+        for (int j = 0; j < 2; ++j) x[i][j] = floatx16{};
+    for (int k = group; k < shares; k += KS) {
+        const floatx4 *from = reinterpret_cast<const floatx4 *>(a.part) + ((int64_t)(p.slot * shares + k) * 4 + wave) * (FI * FJ * 4 * 64) + lane;
 #pragma unroll
-        for (int i = 0; i < FI; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < FJ; ++j)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const floatx4 v = from[(int64_t)k * (4 * FI * FJ * 4 * 64) + ((i * FJ + j) * 4 + g) * 64];
+                    const floatx4 v = from[(((2 * si + i) * FJ + 2 * sj + j) * 4 + g) * 64];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[i][j][4 * g + e] += v[e];
                 }
     }
-    put_tile<FI, FJ, 1, SPLIT, MODE>(a, p, x, p.ti * 64 * FI + (wave >> 1) * FI * 32, p.tj * 64 * FJ + (wave & 1) * FJ * 32, lds, lds, 0);
+    put_tile<2, 2, KS, SPLIT, MODE>(a, p, x, p.ti * 64 * FI + ((wave >> 1) * FI + 2 * si) * 32, p.tj * 64 * FJ + ((wave & 1) * FJ + 2 * sj) * 32, lds[group], lds[0], group);
+}
+
+// ---- matrices of up to 128 x 128: all steps in one launch --------------------------------------------------------------
+// A workgroup of eight wavefronts has a matrix; of the frame of 128 x 128 (or 64 in either direction) a wavefront has 64 x 32, as the sums of the
+// matrix instruction lie: two pieces of 32 x 32.  X stays in registers as 32-bit numbers; LDS has one operand of X - its rows for A = X X', then
+// its columns for P X - and A, then P.  The norm and, of a step, momentum and weights are read and written as they lie in registers.
+// What several launches per step cost - 5 us each for a few microseconds of products - is what this saves.
+constexpr int ONE_SIDE = 128, ONE_THREADS = 512;
+
+// The 4 x 4 numbers of four lanes transposed: v[e] of lane q becomes v[q] of lane e.
+__device__ __forceinline__ void turn_quad(uint32_t (&v)[4]) {
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    const auto from = [](uint32_t x, auto perm) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(perm)::value, 0xf, 0xf, true); };
+    const std::integral_constant<int, 0xB1> by_one{};                         // lanes 1 0 3 2
+    const std::integral_constant<int, 0x4E> by_two{};                         // lanes 2 3 0 1
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+        const uint32_t got = from(odd ? v[e] : v[e + 1], by_one);
+        v[e] = odd ? got : v[e];
+        v[e + 1] = odd ? v[e + 1] : got;
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t got = from(high ? v[e] : v[e + 2], by_two);
+        v[e] = high ? got : v[e];
+        v[e + 2] = high ? v[e + 2] : got;
+    }
+}
+// high part in the lower half, low part in the upper one
+__device__ __forceinline__ uint32_t parts_of(float v) {
+    const f16_t hi = (f16_t)v, lo = (f16_t)(v - (float)hi);
+    return (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
+}
+
+struct MuonOne { MuonIn in; MuonArgs out; int32_t n, m, nq, mq, steps; };     // nq, mq: the frame
+
+template <class T, bool SPLIT, bool STEP>
+__global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32_t *err) {
+    constexpr int S = SPLIT ? 2 : 1;
+    extern __shared__ __attribute__((aligned(16))) f16_t one_lds[];
+    __shared__ double squares[ONE_THREADS / 64];
+    if (STEP && *(volatile const int32_t *)err) return;                       // (set before this launch: the same for all)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
+    const int i0 = (wave >> 2) * 64, j0 = (wave & 3) * 32, nq = a.nq, mq = a.mq;
+    const bool tall = a.out.tall, has_x = i0 < nq && j0 < mq, has_a = i0 < nq && j0 < nq;
+    f16_t *const r1 = one_lds, *const r2 = one_lds + nq * mq * S;
+    const int64_t row0 = (int64_t)blockIdx.x * a.in.rows;
+    const MuonIn &in = a.in;
+    // piece f, sum e: row i0 + 32 f + 8 (e / 4) + 4 h + e % 4, column j0 + l32 of X
+    const auto row_of = [&](int f, int e) { return i0 + 32 * f + 8 * (e >> 2) + 4 * h + (e & 3); };
+    floatx16 x[2];
+    double s = 0.0;
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int i = row_of(f, e), j = j0 + l32;
+            float v = 0.0f;
+            if (i < a.n && j < a.m) {
+                const int64_t row = row0 + (tall ? j : i), col = tall ? i : j;
+                v = (float)reinterpret_cast<const T *>(in.in)[row * in.ld + col];
+                if constexpr (STEP) {
+                    float *m = in.val + (in.first + row) * in.L + in.cols + col;
+                    const float moment = in.mu * *m + v;
+                    *m = moment;
+                    v = in.nesterov ? v + in.mu * moment : moment;
+                }
+            }
+            x[f][e] = v;
+            s += (double)v * (double)v;
+        }
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if (lane == 0) squares[wave] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < ONE_THREADS / 64; ++w) s += squares[w];
+    const float norm = (float)sqrt(s), scale = norm <= 3.0e38f ? X_SCALE / (norm + in.eps) : __builtin_nanf("");
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[f][e] *= scale;                        // (zero outside the matrix, or all NaN)
+
+    // the numbers v, rows and columns exchanged, into m of K numbers a row; the same as they are
+    const auto put_columns = [&](f16_t *m, int K, const floatx16 (&v)[2]) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int i = row_of(f, 4 * g), j = j0 + l32;
+                half4 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    hi[e] = (f16_t)v[f][4 * g + e];
+                    lo[e] = (f16_t)(v[f][4 * g + e] - (float)hi[e]);
+                }
+                f16_t *p = m + place8<SPLIT>(j, i & ~7, K) + (i & 4);
+                *reinterpret_cast<half4 *>(p) = hi;
+                if constexpr (SPLIT) *reinterpret_cast<half4 *>(p + 512) = lo;
+            }
+    };
+    const auto put_rows = [&](f16_t *m, int K, const floatx16 (&v)[2]) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t q[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[e] = parts_of(v[f][4 * g + e]);
+                turn_quad(q);
+                const int i = row_of(f, 4 * g) + (lane & 3), j = j0 + (l32 & ~3);
+                f16_t *p = m + place8<SPLIT>(i, j & ~7, K) + (j & 4);
+                uint32_t *hi = reinterpret_cast<uint32_t *>(p), *lo = reinterpret_cast<uint32_t *>(p + 512);
+                *reinterpret_cast<uint2 *>(hi) = uint2{(q[0] & 0xffffu) | q[1] << 16, (q[2] & 0xffffu) | q[3] << 16};
+                if constexpr (SPLIT) *reinterpret_cast<uint2 *>(lo) = uint2{q[0] >> 16 | (q[1] & 0xffff0000u), q[2] >> 16 | (q[3] & 0xffff0000u)};
+            }
+    };
+    // this wavefront's sums over the first `used` blocks of k, of rows of K numbers of l and r
+    const auto product = [&](const f16_t *l, const f16_t *r, int K, int used, floatx16 (&sum)[2]) {
+        const int blocks = K >> 4;
+        const f16_t *pl = l + (i0 >> 5) * blocks * (512 * S) + lane * 8, *pr = r + (j0 >> 5) * blocks * (512 * S) + lane * 8;
+        sum[0] = floatx16{};
+        sum[1] = floatx16{};
+#pragma unroll 2
+        for (int k = 0; k < used; ++k) {
+            half8 lf[2][S], rf[S];
+#pragma unroll
+            for (int e = 0; e < S; ++e) {
+                lf[0][e] = *reinterpret_cast<const half8 *>(pl + k * (512 * S) + e * 512);
+                lf[1][e] = *reinterpret_cast<const half8 *>(pl + (blocks + k) * (512 * S) + e * 512);
+                rf[e] = *reinterpret_cast<const half8 *>(pr + k * (512 * S) + e * 512);
+            }
+#pragma unroll
+            for (int e = SPLIT ? 2 : 0; e >= 0; --e)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) sum[f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lf[f][e == 2 ? S - 1 : 0], rf[e == 1 ? S - 1 : 0], sum[f], 0, 0, 0);
+        }
+    };
+    const int used_n = (a.n + 15) >> 4, used_m = (a.m + 15) >> 4;
+    for (int step = 0; step < a.steps; ++step) {
+        floatx16 g[2], q[2];
+        if (has_x) put_rows(r1, mq, x);
+        __syncthreads();
+        if (has_a) {
+            product(r1, r1, mq, used_m, g);
+            for (floatx16 &v : g) v *= G_SCALE / (X_SCALE * X_SCALE);
+            put_columns(r2, nq, g);                                           // (A is symmetric)
+        }
+        __syncthreads();
+        if (has_x) put_columns(r1, nq, x);
+        if (has_a) product(r2, r2, nq, used_n, q);
+        __syncthreads();
+        if (has_a) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    q[f][e] = q[f][e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g[f][e] * (NS_B * P_SCALE / G_SCALE) + (row_of(f, e) == j0 + l32 ? NS_A * P_SCALE : 0.0f);
+            put_columns(r2, nq, q);
+        }
+        __syncthreads();
+        if (has_x) {
+            product(r2, r1, nq, used_n, x);
+            for (floatx16 &v : x) v *= 1.0f / P_SCALE;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int i = row_of(f, e), j = j0 + l32;
+            if (i < a.n && j < a.m) {
+                const float v = x[f][e] * (1.0f / X_SCALE);
+                const int64_t row = row0 + (tall ? j : i), col = tall ? i : j;
+                if constexpr (STEP) {
+                    float *w = a.out.val + (a.out.first + row) * a.out.L + col;
+                    *w = a.out.keep * *w - a.out.step * v;
+                } else if (!SPLIT) reinterpret_cast<bf16_t *>(a.out.to)[row * a.out.to_ld + col] = (bf16_t)v;
+                else if (a.out.to_type == PS_F32) reinterpret_cast<float *>(a.out.to)[row * a.out.to_ld + col] = v;
+                else reinterpret_cast<f16_t *>(a.out.to)[row * a.out.to_ld + col] = (f16_t)v;
+            }
+        }
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
 // Sides count as multiples of the tile's.  256: large matrices of 16 bits; 128: where a quarter as many tiles of 128 as there
 // are numbers of them ... ; 64: the rest.
+#ifndef SMALLK
+#define SMALLK 1
+#define SMALLT 1024
+#endif
 #ifndef MIDN
 #define MIDN 256
 #endif
 struct MuonPlan {
     int32_t batch, n, m, tile, np, mp, blocks;
-    bool tall, split;
+    bool tall, split, one;
     size_t off_d, off_x, off_xt[2], off_g, off_p, off_part, bytes;
 };
 inline int64_t half_of(int64_t t) { return t * (t + 1) / 2; }
-constexpr int MOST_SHARES = 8, STAGES_AT_LEAST = 2;
-// Workgroups that share a tile's sum over k: where there are fewer tiles than compute units.
-int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t stages) {
+constexpr int MOST_SHARES = 8, TURNS_AT_LEAST = 2;
+// Workgroups that share a tile's sum over k, where there are fewer tiles than compute units.
+int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t K) {
     int64_t s = ps->num_cu / tiles;
     if (s > MOST_SHARES) s = MOST_SHARES;
-    if (s > stages / STAGES_AT_LEAST) s = stages / STAGES_AT_LEAST;
+    if (s > K / 64 / TURNS_AT_LEAST) s = K / 64 / TURNS_AT_LEAST;
     return s < 2 ? 1 : (int)s;
 }
 MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols, bool split, bool step) {
@@ -525,10 +764,12 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     p.batch = batch; p.tall = rows > cols; p.split = split;
     p.n = p.tall ? cols : rows; p.m = p.tall ? rows : cols;
     p.tile = 64;
+    p.one = p.m <= ONE_SIDE;
     if (p.n > MIDN) p.tile = 128;
     if (!split && half_of(ceil_div64(p.n, 256)) * batch >= ps->num_cu) p.tile = 256;
     p.np = (int32_t)(ceil_div64(p.n, p.tile) * p.tile); p.mp = (int32_t)(ceil_div64(p.m, p.tile) * p.tile);
-    const int64_t blocks = ceil_div64((int64_t)rows * cols, 4096);
+    if (p.one) return p;                          // (no scratch)
+    const int64_t blocks = ceil_div64((int64_t)rows * cols, 1024);
     p.blocks = (int32_t)(blocks < NORM_BLOCKS ? blocks : NORM_BLOCKS);
     const size_t size = split ? 4 : 2, nm = (size_t)batch * p.np * p.mp * size, nn = (size_t)batch * p.np * p.np * size;
     p.off_d = up256((size_t)batch * NORM_BLOCKS * sizeof(double));
@@ -539,17 +780,29 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     p.off_p = p.off_g + up256(nn);
     p.off_part = p.off_p + up256(nn);
     // (shares times tiles are at most as many as the compute units)
-    p.bytes = p.off_part + (p.tile == 128 ? (size_t)ps->num_cu * 128 * 128 * sizeof(float) : 0);
+    p.bytes = p.off_part + (p.tile > 64 ? (size_t)ps->num_cu * p.tile * p.tile * sizeof(float) : 0);
     return p;
 }
 
-template <int FI, int FJ, int KB, int STAGES, bool SPLIT, int MODE>
+template <int FI, int KB, int STAGES, bool SPLIT, int MODE>
 int large(dpaps_ps *ps, const MuonArgs &a, int64_t tiles, hipStream_t st) {
     static LdsAllowed allowed;
-    constexpr int STAGED = STAGES * 2 * (FI + FJ) * KB * (SPLIT ? 2 : 1) * 1024, SUMMED = 4 * 64 * SUMS_LD * 4, LDS = STAGED > SUMMED ? STAGED : SUMMED;
-    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_large<FI, FJ, KB, STAGES, SPLIT, MODE>), LDS);
+    constexpr int STAGED = STAGES * 4 * FI * KB * (SPLIT ? 2 : 1) * 1024, SUMMED = 4 * 64 * SUMS_LD * 4, LDS = STAGED > SUMMED ? STAGED : SUMMED;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_large<FI, FI, KB, STAGES, SPLIT, MODE>), LDS);
     if (rc) return rc;
-    k_muon_large<FI, FJ, KB, STAGES, SPLIT, MODE><<<(unsigned)(tiles * a.shares), 256, LDS, st>>>(a, ps->err);
+    k_muon_large<FI, FI, KB, STAGES, SPLIT, MODE><<<(unsigned)(tiles * a.shares), 256, LDS, st>>>(a, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+// Tiles tile0 .. tile0 + tiles - 1, fewer than compute units: with shared sums, if that can be.
+template <int FI, int KB, bool SPLIT, int MODE>
+int large_rest(dpaps_ps *ps, MuonArgs a, int64_t tiles, hipStream_t st) {
+    const int32_t shares = shares_of(ps, tiles, a.K);
+    a.shares = shares;
+    const int rc = large<FI, KB, 4, SPLIT, MODE>(ps, a, tiles, st);
+    if (rc || shares == 1) return rc;
+    a.shares = 1;
+    k_muon_join<FI, FI, SPLIT, MODE><<<(unsigned)(FI * FI * tiles), 256, 0, st>>>(a, shares);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
@@ -558,23 +811,26 @@ int product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
     constexpr bool HALF = MODE == MUON_GRAM || MODE == MUON_POLY;
     a.tiles = (int32_t)(HALF ? half_of(a.tiles_i) : (int64_t)a.tiles_i * a.tiles_j);
     a.shares = 1;
-    const int64_t tiles = (int64_t)a.tiles * batch;
+    const int64_t tiles = (int64_t)a.tiles * batch, cus = ps->num_cu;
     if constexpr (TILE == 64) {
         k_muon_small<SPLIT, MODE><<<(unsigned)tiles, 256, 0, st>>>(a, ps->err);
+        PS_HIP(ps, hipGetLastError());
     } else if constexpr (TILE == 256) {
-        return large<4, 4, 2, 4, SPLIT, MODE>(ps, a, tiles, st);
+        // as many tiles as make full rounds of the compute units, and the rest with shared sums
+        const int64_t rest = HALF && tiles % cus <= cus / 2 ? tiles % cus : 0;
+        const int rc = large<4, 2, 4, SPLIT, MODE>(ps, a, tiles - rest, st);
+        if (rc || rest == 0) return rc;
+        a.tile0 = (int32_t)(tiles - rest);
+        if constexpr (HALF) return large_rest<4, 2, SPLIT, MODE>(ps, a, rest, st);
     } else {
         constexpr int KB = SPLIT ? 2 : 4;                                     // so 128 KB of LDS; half of that where two workgroups share a compute unit
-        if constexpr (HALF) a.shares = shares_of(ps, tiles, a.K / 64);
-        const int rc = tiles > ps->num_cu ? large<2, 2, KB / 2, 4, SPLIT, MODE>(ps, a, tiles, st) : large<2, 2, KB, 4, SPLIT, MODE>(ps, a, tiles, st);
-        if (rc || a.shares == 1) return rc;
+        if (tiles > cus) return large<2, KB / 2, 4, SPLIT, MODE>(ps, a, tiles, st);
         if constexpr (HALF) {
-            const int32_t shares = a.shares;
-            a.shares = 1;
-            k_muon_join<2, 2, SPLIT, MODE><<<(unsigned)(4 * tiles), 64, 0, st>>>(a, shares);
-        }
+            // (with a short sum, tiles of 64)
+            if (SMALLK * a.K <= SMALLT && tiles < cus) { a.tiles_i *= 2; a.tiles_j *= 2; return product<64, SPLIT, MODE>(ps, a, batch, st); }
+            return large_rest<2, KB, SPLIT, MODE>(ps, a, tiles, st);
+        } else return large<2, KB, 4, SPLIT, MODE>(ps, a, tiles, st);
     }
-    PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
 
@@ -598,8 +854,10 @@ int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t s
         MuonArgs b = s + 1 == steps ? last : a;
         b.tiles_i = a.tiles_i; b.tiles_j = a.tiles_j; b.K = p.np;
         b.lhs = q; b.lhs_size = nn; b.rhs = xt; b.rhs_size = nm;
-        if (s + 1 == steps) rc = product<TILE, SPLIT, MUON_LAST>(ps, b, p.batch, st);
-        else {
+        if (s + 1 == steps) {
+            if constexpr (SPLIT) rc = last.val ? product<TILE, SPLIT, MUON_STEP>(ps, b, p.batch, st) : product<TILE, SPLIT, MUON_LAST>(ps, b, p.batch, st);
+            else rc = product<TILE, SPLIT, MUON_LAST>(ps, b, p.batch, st);
+        } else {
             // (X transposed is read by other workgroups while it is written: into the other place; X itself is not)
             b.out = x; b.out_ld = p.mp; b.out_t = xt_next; b.out_t_ld = p.np; b.out_size = nm;
             rc = product<TILE, SPLIT, MUON_APPLY>(ps, b, p.batch, st);
@@ -627,7 +885,29 @@ int norm_of(dpaps_ps *ps, const MuonPlan &p, const MuonIn &in, hipStream_t st) {
     return PS_OK;
 }
 
+template <class T, bool SPLIT, bool STEP>
+int one_of(dpaps_ps *ps, const MuonOne &a, int32_t batch, hipStream_t st) {
+    static LdsAllowed allowed;
+    constexpr size_t MOST = (size_t)2 * ONE_SIDE * ONE_SIDE * (SPLIT ? 4 : 2);
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_one<T, SPLIT, STEP>), MOST);
+    if (rc) return rc;
+    k_muon_one<T, SPLIT, STEP><<<(unsigned)batch, ONE_THREADS, (size_t)a.nq * (a.nq + a.mq) * (SPLIT ? 4 : 2), st>>>(a, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+template <class T>
+int one_launch(dpaps_ps *ps, const MuonPlan &p, const MuonIn &in, const MuonArgs &last, int32_t steps, hipStream_t st) {
+    MuonOne a{in, last, p.n, p.m, p.np, p.mp, steps};
+    if (in.val) return one_of<T, true, true>(ps, a, p.batch, st);
+    return p.split ? one_of<T, true, false>(ps, a, p.batch, st) : one_of<T, false, false>(ps, a, p.batch, st);
+}
+
 int orthogonalize(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t steps, hipStream_t st) {
+    last.n = p.n; last.m = p.m; last.tall = p.tall;
+    if (p.one) {
+        if (in.type == PS_F32) return one_launch<float>(ps, p, in, last, steps, st);
+        return in.type == PS_BF16 ? one_launch<bf16_t>(ps, p, in, last, steps, st) : one_launch<f16_t>(ps, p, in, last, steps, st);
+    }
     char *ws = (char *)ps->ws;
     in.squares = (double *)ws;
     in.blocks = p.blocks;
@@ -638,7 +918,6 @@ int orthogonalize(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int
     else rc = norm_of<f16_t>(ps, p, in, st);
     if (rc) return rc;
     if (in.val) { in.in = in.d; in.ld = in.cols; in.type = PS_F32; }
-    last.n = p.n; last.m = p.m; last.tall = p.tall;
     if (p.split) return p.tile == 128 ? iterate<128, true>(ps, p, in, last, steps, st) : iterate<64, true>(ps, p, in, last, steps, st);
     if (p.tile == 256) return iterate<256, false>(ps, p, in, last, steps, st);
     return p.tile == 128 ? iterate<128, false>(ps, p, in, last, steps, st) : iterate<64, false>(ps, p, in, last, steps, st);
@@ -682,7 +961,7 @@ extern "C" int muon_step(ps_handle ps, int32_t worker, int64_t first_key, int32_
     a.in = grad; a.ld = grad_ld; a.type = grad_type; a.rows = rows; a.cols = dim; a.eps = eps;
     a.val = ps->val; a.L = ps->L; a.first = first_key; a.mu = momentum; a.nesterov = nesterov != 0;
     MuonArgs last{};
-    last.val = ps->val; last.L = ps->L; last.first = first_key;
+    last.val = ps->val; last.L = ps->L; last.first = first_key; last.to_vec = ps->L % 4 == 0;
     last.keep = (float)(1.0 - (double)lr * weight_decay);
     last.step = (float)(lr * sqrt(rows > dim ? (double)rows / dim : 1.0));
     rc = orthogonalize(ps, p, a, last, steps, st);
