@@ -106,7 +106,6 @@ struct EmbSums {
     float *part;                                                 // two rows of D per range
     float *to; int64_t L;                                        // where a token's row is: the gradient (L = D) or the store
     float lr, eps;
-    int64_t clear_blocks;                                        // workgroups that clear the rows of tokens not mentioned
 };
 
 // What becomes of a token's sum: a row of the gradient, added to what is there, or a step of AdaGrad.
@@ -145,30 +144,16 @@ __device__ __forceinline__ bool emb_mentioned(const EmbSums &a, int64_t v) {
     return lo < a.n && (int64_t)a.skeys[lo] == v;
 }
 
-constexpr int CLEAR_ROWS = 16;                         // of a wavefront
-constexpr uint64_t NOKEY = ~0ull;
+constexpr int CLEAR_ROWS = 16;                         // rows of tokens not mentioned that a wavefront clears
+constexpr uint64_t NOKEY = ~0ull;                      // no token looks like this
 
-// A wavefront per range and 64 pieces of W values; UN rows are on their way together.  The first workgroups clear the rows of tokens
-// that are not mentioned (EMB_GRAD), the next ones count the statistics.
+// A wavefront per range and 64 pieces of W values; UN rows are on their way together.  The first workgroups count the statistics.
 template <class T, int W, int MODE>
 __global__ __launch_bounds__(256) void k_emb_sums(RouteArgs route, TokenIds t, EmbSums a, const int32_t *err) {
     constexpr int UN = MODE == EMB_ADAGRAD ? 8 : W >= 4 ? 8 : 16;
     const int32_t stop = flag_ahead(err);
     const int lane = threadIdx.x & 63;
     int64_t block = blockIdx.x;
-    if constexpr (MODE == EMB_GRAD) {
-        if (block < a.clear_blocks) {
-            if (blockIdx.y != 0 || stop) return;
-            const int64_t v0 = (block * 4 + (threadIdx.x >> 6)) * CLEAR_ROWS;
-            const bool clear = lane < CLEAR_ROWS && v0 + lane < a.count && !emb_mentioned(a, v0 + lane);
-            for (u64 left = __ballot(clear); left != 0; left &= left - 1ull) {
-                float *p = a.to + (v0 + __ffsll((long long)left) - 1) * a.L;
-                for (int c = lane * W; c < a.D; c += 64 * W) store_vec<float, W>(p + c, Vec<float, W>{});
-            }
-            return;
-        }
-        block -= a.clear_blocks;
-    }
     if constexpr (MODE == EMB_ADAGRAD) {
         __shared__ RouteLds l;
         if (block < route.blocks) {
@@ -231,19 +216,31 @@ __global__ __launch_bounds__(256) void k_emb_sums(RouteArgs route, TokenIds t, E
     }
 }
 
-// Tokens whose terms fill more than one range: the wavefront of the range in which they start adds the sums of the ranges behind
-// it, in order.  blockIdx.y: which 64 pieces.
-constexpr int JOIN_AHEAD = 32;
+// Tokens whose terms fill more than one range: the workgroup of the range in which they start adds the sums of the ranges behind it, each
+// wavefront a quarter of them in order, and then the four.  blockIdx.y: which 64 pieces.  The other workgroups, of a gradient that is not added to,
+// clear the rows of tokens that are not mentioned meanwhile: the few trips to memory, one behind the other, of a join hide behind that.
+constexpr int JOIN_AHEAD = 16;
 template <int W, int MODE>
-__global__ __launch_bounds__(256) void k_emb_join(EmbSums a, const int32_t *err) {
+__global__ __launch_bounds__(256) void k_emb_join(EmbSums a, int64_t joins, const int32_t *err) {
     const int32_t stop = flag_ahead(err);
-    const int lane = threadIdx.x & 63;
-    const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), R = a.range;
-    const int64_t q1 = (r + 1) * R;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (MODE == EMB_GRAD && blockIdx.x >= joins) {
+        if (blockIdx.y != 0 || stop) return;
+        const int64_t v0 = ((blockIdx.x - joins) * 4 + wave) * CLEAR_ROWS;
+        const bool clear = lane < CLEAR_ROWS && v0 + lane < a.count && !emb_mentioned(a, v0 + lane);
+        for (u64 left = __ballot(clear); left != 0; left &= left - 1ull) {
+            float *p = a.to + (v0 + __ffsll((long long)left) - 1) * a.L;
+            for (int c = lane * W; c < a.D; c += 64 * W) store_vec<float, W>(p + c, Vec<float, W>{});
+        }
+        return;
+    }
+    __shared__ Vec<float, W> sums[4][64];
+    const int64_t r = blockIdx.x, R = a.range, q1 = (r + 1) * R;
     if (q1 >= a.n) return;
     const uint64_t key = a.skeys[q1 - 1], next = a.skeys[q1];
+    const uint64_t start = r > 0 ? a.skeys[q1 - R] : NOKEY, before = r > 0 ? a.skeys[q1 - R - 1] : NOKEY;
     if (stop != 0 || next != key || (int64_t)key >= a.count) return;
-    if (r > 0 && a.skeys[q1 - R] == key && a.skeys[q1 - R - 1] == key) return;         // they started earlier
+    if (start == key && before == key) return;                                         // they started earlier
     // the ranges behind that begin with the token follow one another: 64 are looked at, spread over what is left
     const int64_t nranges = (a.n + R - 1) / R;
     int64_t lo = r + 1, hi = nranges, by = 1;
@@ -255,22 +252,153 @@ __global__ __launch_bounds__(256) void k_emb_join(EmbSums a, const int32_t *err)
         if (run > 0) lo += (run - 1) * by + 1;
         by = (hi - lo + 63) / 64;
     }
-    const int64_t m = lo - (r + 1);
+    // sum 0 is of range r, sum j of range r + j, j <= m
+    const int64_t m = lo - (r + 1), j0 = (m + 1) * wave / 4, j1 = (m + 1) * (wave + 1) / 4;
     const int c = blockIdx.y * 64 + lane;
-    if (c * W >= a.D) return;
-    const float *part = a.part + (int64_t)c * W;
+    const bool in = c * W < a.D;
+    const float *part = a.part + (in ? (int64_t)c * W : 0);
     Old<MODE, W> old;
-    emb_read<MODE, W>(old, a, (int64_t)key, c);
-    Vec<float, W> v = load_vec<float, W>(part + (2 * r + 1) * (int64_t)a.D);
-    for (int64_t j = 1; j <= m; j += JOIN_AHEAD) {
+    if (wave == 0 && in) emb_read<MODE, W>(old, a, (int64_t)key, c);
+    Vec<float, W> v = {};
+    for (int64_t j = j0; j < j1; j += JOIN_AHEAD) {
         Vec<float, W> d[JOIN_AHEAD];
 #pragma unroll
-        for (int i = 0; i < JOIN_AHEAD; ++i) d[i] = j + i <= m ? load_vec<float, W>(part + 2 * (r + j + i) * (int64_t)a.D) : Vec<float, W>{};
+        for (int i = 0; i < JOIN_AHEAD; ++i) d[i] = j + i < j1 ? load_vec<float, W>(part + (2 * (r + j + i) + (j + i == 0 ? 1 : 0)) * (int64_t)a.D) : Vec<float, W>{};
 #pragma unroll
         for (int i = 0; i < JOIN_AHEAD; ++i)
-            if (j + i <= m) v = v + d[i];
+            if (j + i < j1) v = v + d[i];
     }
-    emb_finish<MODE, W>(old, a, (int64_t)key, c, v);
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave == 0 && in) emb_finish<MODE, W>(old, a, (int64_t)key, c, sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]);
+}
+
+// ---- few tokens: one launch, without a sort -----------------------------------------------------------------------------
+// Every workgroup checks all tokens and has them in LDS.  A wavefront takes a position: if no position before it has the same token, the
+// positions that have it are the token's terms, in order.  They are added one after the other; more than FEW_OWN by the whole workgroup,
+// a sixteenth each, and then the sixteen.  Further workgroups clear the rows of tokens not mentioned, FEW_CLEAR each; the first ones count the
+// statistics.
+constexpr int FEW_THREADS = 1024, FEW_WAVES = FEW_THREADS / 64, FEW_OWN = 64, FEW_CLEAR = 64;
+template <class T, int W, int MODE>
+__global__ __launch_bounds__(FEW_THREADS) void k_emb_few(RouteArgs route, TokenIds t, EmbSums a, int32_t *err) {
+    constexpr size_t SUMS = (size_t)FEW_KEYS * 8, ALL = SUMS + (size_t)FEW_WAVES * 64 * W * 4;
+    __shared__ __attribute__((aligned(32))) unsigned char mem[ALL > sizeof(RouteLds) ? ALL : sizeof(RouteLds)];
+    __shared__ uint32_t many;                                          // which wavefronts' tokens the whole workgroup works on,
+    __shared__ u64 many_mask[FEW_WAVES][FEW_KEYS / 64], many_key[FEW_WAVES];   // and what they found of them
+    __shared__ int many_count[FEW_WAVES];
+    __shared__ bool named[FEW_CLEAR];
+    uint64_t *lk = reinterpret_cast<uint64_t *>(mem);
+    Vec<float, W> *sums = reinterpret_cast<Vec<float, W> *>(mem + SUMS);
+    const int n = (int)t.n;
+    if (threadIdx.x == 0) many = 0;
+    if (threadIdx.x < FEW_CLEAR) named[threadIdx.x] = false;
+    if (few_tokens_off<2>(t, err, [&](int64_t p, int64_t id) { lk[p] = id == t.pad ? NOKEY : (uint64_t)id; })) return;
+    int block = blockIdx.x;
+    if constexpr (MODE == EMB_ADAGRAD) {
+        if (block < route.blocks) {
+            __syncthreads();                                           // (the tokens in LDS are not needed here)
+            if (blockIdx.y == 0) route_tokens_block(route, t, *reinterpret_cast<RouteLds *>(mem), block, 0);
+            return;
+        }
+        block -= route.blocks;
+    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), chunks = (n + 63) / 64;
+    const int groups = (n + FEW_WAVES - 1) / FEW_WAVES;
+    if constexpr (MODE == EMB_GRAD) {
+        if (block >= groups) {
+            if (blockIdx.y != 0) return;
+            const int64_t v0 = (int64_t)(block - groups) * FEW_CLEAR;
+            for (int p = threadIdx.x; p < n; p += FEW_THREADS)
+                if (lk[p] - (uint64_t)v0 < FEW_CLEAR) named[lk[p] - (uint64_t)v0] = true;
+            __syncthreads();
+            for (int r = wave; r < FEW_CLEAR && v0 + r < a.count; r += FEW_WAVES)
+                if (!named[r])
+                    for (int c = lane * W; c < a.D; c += 64 * W) store_vec<float, W>(a.to + (v0 + r) * a.L + c, Vec<float, W>{});
+            return;
+        }
+    }
+    // (the positions dealt out to the workgroups in turn, shifted from turn to turn: frequent tokens are first named by the first
+    // positions, or at equal distances, and a workgroup takes its own one after the other)
+    const int mine = wave * groups + (block + 5 * wave) % groups;
+    const int c = blockIdx.y * 64 + lane;
+    const bool in = c * W < a.D;
+    const T *dout = reinterpret_cast<const T *>(a.dout) + (in ? (int64_t)c * W : 0);
+    u64 mask = 0;                                                      // lane i: which of the positions 64 i .. have the token
+    int count = 0;
+    uint64_t key = NOKEY;
+    const auto look = [&](int p) {
+        if (p >= n) return false;
+        key = lk[p];
+        key = readlane_u64(key, 0);
+        if (key == NOKEY) return false;
+        for (int i = 0; i < chunks; ++i) {
+            const u64 same = __ballot(64 * i + lane < n && lk[64 * i + lane] == key);
+            if (64 * i <= p && (64 * i + 63 < p ? same : same & ((1ull << (p & 63)) - 1ull)) != 0) return false;
+            count += __popcll(same);
+            mask = lane == i ? same : mask;
+        }
+        return true;
+    };
+    // the sum of the token's terms [lo, hi), one after the other
+    const auto sum = [&](int lo, int hi) {
+        constexpr int UN = W >= 4 ? 8 : 16;
+        Vec<float, W> v = {};
+        if (lo >= hi) return v;
+        int at = 0, seen = 0;                                          // the positions from 64 at on, `seen` terms are before those
+        u64 m = readlane_u64(mask, 0);
+        while (seen + __popcll(m) <= lo) { seen += __popcll(m); m = readlane_u64(mask, ++at); }
+        for (; seen < lo; ++seen) m &= m - 1ull;
+        while (lo < hi) {
+            Vec<float, W> d[UN];
+            int got = 0;
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+                d[u] = Vec<float, W>{};
+                if (lo + u < hi) {
+                    while (m == 0) m = readlane_u64(mask, ++at);
+                    const int p = 64 * at + __ffsll((long long)m) - 1;
+                    m &= m - 1ull;
+                    if (in) d[u] = load_vec<T, W>(dout + (int64_t)p * a.stride);
+                    ++got;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < UN; ++u)
+                if (u < got) v = v + d[u];
+            lo += got;
+        }
+        return v;
+    };
+    if (look(mine)) {
+        if (count <= FEW_OWN) {
+            Old<MODE, W> old;
+            if (in) emb_read<MODE, W>(old, a, (int64_t)key, c);
+            const Vec<float, W> v = sum(0, count);
+            if (in) emb_finish<MODE, W>(old, a, (int64_t)key, c, v);
+        } else {
+            if (lane < (int)FEW_KEYS / 64) many_mask[wave][lane] = mask;
+            if (lane == 0) { many_key[wave] = key; many_count[wave] = count; atomicOr(&many, 1u << wave); }
+        }
+    }
+    __syncthreads();
+    uint32_t left = (uint32_t)__builtin_amdgcn_readfirstlane((int)many);
+    while (left != 0) {
+        const int w = __ffs((int)left) - 1;
+        left &= left - 1u;
+        mask = lane < (int)FEW_KEYS / 64 ? many_mask[w][lane] : 0;
+        key = readlane_u64(many_key[w], 0);
+        count = __builtin_amdgcn_readfirstlane(many_count[w]);
+        sums[wave * 64 + lane] = sum(count * wave / FEW_WAVES, count * (wave + 1) / FEW_WAVES);
+        __syncthreads();
+        if (wave == 0 && in) {
+            Old<MODE, W> old;
+            emb_read<MODE, W>(old, a, (int64_t)key, c);
+            Vec<float, W> v = sums[lane];
+            for (int k = 1; k < FEW_WAVES; ++k) v = v + sums[k * 64 + lane];
+            emb_finish<MODE, W>(old, a, (int64_t)key, c, v);
+        }
+        __syncthreads();                                               // the sums' place is used again
+    }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
@@ -308,31 +436,39 @@ int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, 
     const auto fits = [&](int w) { return rows_allow(a.dout, dout_type, a.D, a.stride, w) && rows_allow(a.to, PS_F32, a.D, a.L, w); };
     const int W = dout_type != PS_F32 && mode != EMB_ADAGRAD && a.D > 256 && fits(8) ? 8 : a.D > 64 && fits(4) ? 4 : 1;
     const int64_t slices = (a.D / W + 63) / 64;
-    // ranges of 64 positions, shorter ones where those would be fewer wavefronts than the compute units hold
-    a.range = 64;
-    while (a.range > 8 && ceil_div64(t.n, a.range) * slices < 8 * (int64_t)ps->num_cu) a.range /= 2;
-    const int64_t nranges = ceil_div64(t.n, a.range);
-    const size_t off_skeys = up256((size_t)t.n * 8), off_spos = 2 * off_skeys, off_part = off_spos + up256((size_t)t.n * 4),
-                 off_sort = off_part + up256((size_t)nranges * 2 * (size_t)a.D * sizeof(float));
-    int rc = dpaps_ws_reserve(ps, off_sort + dpaps_sort_scratch_bytes(t.n, bits));
-    if (rc) return rc;
-    char *ws = (char *)ps->ws;
-    if (t.n > 0) {
+    a.n = t.n; a.count = t.count; a.first = t.first;
+    const bool few = t.n <= FEW_KEYS;
+    dim3 grid, join;
+    int64_t joins = 0;
+    if (few) {
+        grid = dim3((unsigned)((mode == EMB_GRAD ? ceil_div64(t.count, FEW_CLEAR) : 0) + route.blocks + ceil_div64(t.n, FEW_WAVES)), (unsigned)slices);
+    } else {
+        // ranges of 64 positions, shorter ones where those would be fewer wavefronts than the compute units hold
+        a.range = 64;
+        while (a.range > 8 && ceil_div64(t.n, a.range) * slices < 8 * (int64_t)ps->num_cu) a.range /= 2;
+        const int64_t nranges = ceil_div64(t.n, a.range);
+        const size_t off_skeys = up256((size_t)t.n * 8), off_spos = 2 * off_skeys, off_part = off_spos + up256((size_t)t.n * 4),
+                     off_sort = off_part + up256((size_t)nranges * 2 * (size_t)a.D * sizeof(float));
+        int rc = dpaps_ws_reserve(ps, off_sort + dpaps_sort_scratch_bytes(t.n, bits));
+        if (rc) return rc;
+        char *ws = (char *)ps->ws;
         k_emb_keys<<<grid_for(t.n, 256), 256, 0, st>>>(t, (int64_t *)ws, ps->err);
         PS_HIP(ps, hipGetLastError());
         rc = dpaps_sort_pairs(ps, (int64_t *)ws, t.n, bits, false, (uint64_t *)(ws + off_skeys), (uint32_t *)(ws + off_spos), ws + off_sort, st);
         if (rc) return rc;
+        a.skeys = (const uint64_t *)(ws + off_skeys); a.spos = (const uint32_t *)(ws + off_spos);
+        a.part = (float *)(ws + off_part);
+        joins = nranges - 1;
+        grid = dim3((unsigned)(route.blocks + ceil_div64(nranges, 4)), (unsigned)slices);
+        join = dim3((unsigned)(joins + (mode == EMB_GRAD ? ceil_div64(t.count, 4 * CLEAR_ROWS) : 0)), (unsigned)slices);
     }
-    a.skeys = (const uint64_t *)(ws + off_skeys); a.spos = (const uint32_t *)(ws + off_spos); a.n = t.n; a.count = t.count; a.first = t.first;
-    a.part = (float *)(ws + off_part);
-    a.clear_blocks = mode == EMB_GRAD ? ceil_div64(t.count, 4 * CLEAR_ROWS) : 0;
-    const dim3 grid((unsigned)(a.clear_blocks + route.blocks + ceil_div64(nranges, 4)), (unsigned)slices), join((unsigned)ceil_div64(nranges, 4), (unsigned)slices);
     if (grid.x == 0) return PS_OK;
 #define SUMS(T, WW, MODE)                                                                     \
     do {                                                                                      \
+        if (few) { k_emb_few<T, WW, MODE><<<grid, FEW_THREADS, 0, st>>>(route, t, a, ps->err); break; } \
         k_emb_sums<T, WW, MODE><<<grid, 256, 0, st>>>(route, t, a, ps->err);                  \
         PS_HIP(ps, hipGetLastError());                                                        \
-        if (nranges > 1) k_emb_join<WW, MODE><<<join, 256, 0, st>>>(a, ps->err);              \
+        k_emb_join<WW, MODE><<<join, 256, 0, st>>>(a, joins, ps->err);                        \
     } while (0)
 #define MODES(T, WW)                                                                          \
     do {                                                                                      \

@@ -13,15 +13,23 @@ struct TokenIds {
     __device__ __forceinline__ bool bad(int64_t t) const { return t != pad && (t < 0 || t >= count); }
 };
 
-// Whether a call of few tokens is to do nothing: few_keys_off, for tokens.
-__device__ __forceinline__ bool few_tokens_off(const TokenIds &t, int32_t *err) {
+// Whether a call of few tokens is to do nothing: few_keys_off, for tokens.  keep(p, id): called for every token as it is read.
+template <int AHEAD, class Keep>
+__device__ __forceinline__ bool few_tokens_off(const TokenIds &t, int32_t *err, Keep keep) {
     const bool was_off = *(volatile const int32_t *)err != 0;
     bool off = was_off;
-#pragma unroll 4
-    for (int64_t p = threadIdx.x; p < t.n; p += blockDim.x) off |= t.bad(t.at(p));
+#pragma unroll AHEAD
+    for (int64_t p = threadIdx.x; p < t.n; p += blockDim.x) {
+        const int64_t id = t.at(p);
+        keep(p, id);
+        off |= t.bad(id);
+    }
     const bool any = __syncthreads_or(off ? 1 : 0) != 0;
     if (any && threadIdx.x == 0 && !was_off) atomicExch(err, PS_EKEY);
     return any;
+}
+__device__ __forceinline__ bool few_tokens_off(const TokenIds &t, int32_t *err) {
+    return few_tokens_off<4>(t, err, [](int64_t, int64_t) {});
 }
 
 // The statistics of an access to the tokens' keys; padding is no access.
