@@ -87,15 +87,6 @@ __global__ __launch_bounds__(256) void k_emb_lookup(RouteArgs route, TokenIds t,
 }
 
 // ---- sums over sorted tokens ----------------------------------------------------------------------------------------
-// The keys that are sorted: the tokens; padding behind all of them.
-__global__ __launch_bounds__(256) void k_emb_keys(TokenIds t, int64_t *keys, int32_t *err) {
-    const int64_t p = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (p >= t.n) return;
-    const int64_t id = t.at(p);
-    if (t.bad(id)) atomicExch(err, PS_EKEY);
-    keys[p] = id == t.pad ? t.count : id;
-}
-
 struct EmbSums {
     const uint64_t *skeys; const uint32_t *spos; int64_t n;      // the sorted pairs
     int64_t count, first;                                        // tokens, the key of token 0
@@ -134,18 +125,41 @@ __device__ __forceinline__ void emb_finish(const Old<MODE, W> &o, const EmbSums 
     }
 }
 
-// whether a row is mentioned: the place of token v among the sorted ones
-__device__ __forceinline__ bool emb_mentioned(const EmbSums &a, int64_t v) {
-    int64_t lo = 0, hi = a.n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if ((int64_t)a.skeys[mid] < v) lo = mid + 1; else hi = mid;
-    }
-    return lo < a.n && (int64_t)a.skeys[lo] == v;
+// D zeros, by a wavefront (16 bytes a lane at most: neighbouring lanes' stores make whole lines)
+template <int W> __device__ __forceinline__ void clear_row(float *p, int D) {
+    constexpr int V = W < 4 ? W : 4;
+    for (int c = (threadIdx.x & 63) * V; c < D; c += 64 * V) store_vec<float, V>(p + c, Vec<float, V>{});
 }
 
 constexpr int CLEAR_ROWS = 16;                         // rows of tokens not mentioned that a wavefront clears
 constexpr uint64_t NOKEY = ~0ull;                      // no token looks like this
+
+// Which of the rows v0 .. v0 + CLEAR_ROWS - 1 are mentioned, a bit each, the same in all lanes: their first place among the sorted tokens, 64 places
+// looked at in one trip to memory, and the 64 tokens from there on; behind them - a token mentioned more often - again.
+__device__ __forceinline__ uint32_t emb_mentioned(const EmbSums &a, int64_t v0) {
+    const int lane = threadIdx.x & 63;
+    uint32_t rows = 0;
+    int64_t from = 0, v = v0;
+    while (true) {
+        int64_t lo = from, hi = a.n;                                   // the first place of a token v or above is one of these, or hi
+        while (hi - lo > 64) {
+            const int64_t by = (hi - lo + 63) / 64, at = lo + lane * by;
+            const int below = __popcll(__ballot(at < hi && (int64_t)a.skeys[at < hi ? at : lo] < v));
+            const int64_t base = lo;
+            if (below > 0) lo = base + (below - 1) * by + 1;
+            if (base + below * by < hi) hi = base + below * by;
+            if (below == 0) break;
+        }
+        const int64_t k = lo + lane < a.n ? (int64_t)a.skeys[lo + lane] : INT64_MAX;
+#pragma unroll
+        for (int i = 0; i < CLEAR_ROWS; ++i)
+            if (__ballot(k == v0 + i) != 0) rows |= 1u << i;
+        const int64_t last = (int64_t)readlane_u64((uint64_t)k, 63);
+        if (last >= v0 + CLEAR_ROWS - 1) return rows;
+        from = lo + 64;
+        v = last + 1;
+    }
+}
 
 // A wavefront per range and 64 pieces of W values; UN rows are on their way together.  The first workgroups count the statistics.
 template <class T, int W, int MODE>
@@ -227,11 +241,11 @@ __global__ __launch_bounds__(256) void k_emb_join(EmbSums a, int64_t joins, cons
     if (MODE == EMB_GRAD && blockIdx.x >= joins) {
         if (blockIdx.y != 0 || stop) return;
         const int64_t v0 = ((blockIdx.x - joins) * 4 + wave) * CLEAR_ROWS;
-        const bool clear = lane < CLEAR_ROWS && v0 + lane < a.count && !emb_mentioned(a, v0 + lane);
-        for (u64 left = __ballot(clear); left != 0; left &= left - 1ull) {
-            float *p = a.to + (v0 + __ffsll((long long)left) - 1) * a.L;
-            for (int c = lane * W; c < a.D; c += 64 * W) store_vec<float, W>(p + c, Vec<float, W>{});
-        }
+        if (v0 >= a.count) return;
+        const uint32_t mentioned = emb_mentioned(a, v0);
+        for (int i = 0; i < CLEAR_ROWS && v0 + i < a.count; ++i)
+            if (!(mentioned >> i & 1))
+                clear_row<W>(a.to + (v0 + i) * a.L, a.D);
         return;
     }
     __shared__ Vec<float, W> sums[4][64];
@@ -313,7 +327,7 @@ __global__ __launch_bounds__(FEW_THREADS) void k_emb_few(RouteArgs route, TokenI
             __syncthreads();
             for (int r = wave; r < FEW_CLEAR && v0 + r < a.count; r += FEW_WAVES)
                 if (!named[r])
-                    for (int c = lane * W; c < a.D; c += 64 * W) store_vec<float, W>(a.to + (v0 + r) * a.L + c, Vec<float, W>{});
+                    clear_row<W>(a.to + (v0 + r) * a.L, a.D);
             return;
         }
     }
@@ -432,9 +446,11 @@ int lookup(dpaps_ps *ps, const RouteArgs &a, const TokenIds &t, int32_t dim, flo
 // The sorted pairs and what the sums need, in the handle's scratch.
 int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, int32_t dout_type, int mode, hipStream_t st) {
     const int bits = dpaps_key_bits(t.count + 1);
-    // values of a lane, and so the wavefronts that a row takes
+    // Values of a lane, and so the wavefronts that a row takes.  16-bit rows 16 bytes at a time, unless rows of 32 bits are read and written as often: a
+    // wavefront's accesses to those then have gaps.  16,384 rows of 1024 into a gradient that is cleared: the sums 15 us with 8, 20 with 4;
+    // 262,144 of 512 added to one: 126 with 8, 118 with 4.
     const auto fits = [&](int w) { return rows_allow(a.dout, dout_type, a.D, a.stride, w) && rows_allow(a.to, PS_F32, a.D, a.L, w); };
-    const int W = dout_type != PS_F32 && mode != EMB_ADAGRAD && a.D > 256 && fits(8) ? 8 : a.D > 64 && fits(4) ? 4 : 1;
+    const int W = dout_type != PS_F32 && mode == EMB_GRAD && a.D > 256 && fits(8) ? 8 : a.D > 64 && fits(4) ? 4 : 1;
     const int64_t slices = (a.D / W + 63) / 64;
     a.n = t.n; a.count = t.count; a.first = t.first;
     const bool few = t.n <= FEW_KEYS;
@@ -443,20 +459,20 @@ int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, 
     if (few) {
         grid = dim3((unsigned)((mode == EMB_GRAD ? ceil_div64(t.count, FEW_CLEAR) : 0) + route.blocks + ceil_div64(t.n, FEW_WAVES)), (unsigned)slices);
     } else {
-        // ranges of 64 positions, shorter ones where those would be fewer wavefronts than the compute units hold
+        // ranges of 64 positions, shorter ones where those would be fewer wavefronts (of 256 values) than the compute units hold; by the
+        // number of tokens and the length of a row alone, so that a gradient that is added to gets the same sums
         a.range = 64;
-        while (a.range > 8 && ceil_div64(t.n, a.range) * slices < 8 * (int64_t)ps->num_cu) a.range /= 2;
+        while (a.range > 8 && ceil_div64(t.n, a.range) * ceil_div64(a.D, 256) < 16 * (int64_t)ps->num_cu) a.range /= 2;
         const int64_t nranges = ceil_div64(t.n, a.range);
-        const size_t off_skeys = up256((size_t)t.n * 8), off_spos = 2 * off_skeys, off_part = off_spos + up256((size_t)t.n * 4),
+        const size_t off_spos = up256((size_t)t.n * 8), off_part = off_spos + up256((size_t)t.n * 4),
                      off_sort = off_part + up256((size_t)nranges * 2 * (size_t)a.D * sizeof(float));
         int rc = dpaps_ws_reserve(ps, off_sort + dpaps_sort_scratch_bytes(t.n, bits));
         if (rc) return rc;
         char *ws = (char *)ps->ws;
-        k_emb_keys<<<grid_for(t.n, 256), 256, 0, st>>>(t, (int64_t *)ws, ps->err);
-        PS_HIP(ps, hipGetLastError());
-        rc = dpaps_sort_pairs(ps, (int64_t *)ws, t.n, bits, false, (uint64_t *)(ws + off_skeys), (uint32_t *)(ws + off_spos), ws + off_sort, st);
+        a.skeys = (const uint64_t *)ws;
+        a.spos = (const uint32_t *)(ws + off_spos);
+        rc = dpaps_sort_tokens(ps, t, (uint64_t *)ws, (uint32_t *)(ws + off_spos), ws + off_sort, st);
         if (rc) return rc;
-        a.skeys = (const uint64_t *)(ws + off_skeys); a.spos = (const uint32_t *)(ws + off_spos);
         a.part = (float *)(ws + off_part);
         joins = nranges - 1;
         grid = dim3((unsigned)(route.blocks + ceil_div64(nranges, 4)), (unsigned)slices);
@@ -473,8 +489,10 @@ int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, 
 #define MODES(T, WW)                                                                          \
     do {                                                                                      \
         if (mode == EMB_GRAD) SUMS(T, WW, EMB_GRAD);                                          \
-        else if (mode == EMB_GRAD_ADD) SUMS(T, WW, EMB_GRAD_ADD);                             \
-        else if constexpr (WW < 8) SUMS(T, WW, EMB_ADAGRAD);                                  \
+        else if constexpr (WW < 8) {                                                          \
+            if (mode == EMB_GRAD_ADD) SUMS(T, WW, EMB_GRAD_ADD);                              \
+            else SUMS(T, WW, EMB_ADAGRAD);                                                    \
+        }                                                                                     \
     } while (0)
 #define WIDTHS(T)                                                                             \
     do {                                                                                      \

@@ -26,8 +26,10 @@
 // Integer work only: the result is the same bit for bit whatever the scheduling.
 #include "common.h"
 #include "together.h"
+#include "token_ids.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -37,11 +39,23 @@ constexpr int SORT_MAX_BITS = 10;          // bits of a digit at most: 1024 buck
 
 __device__ __forceinline__ uint32_t digit_of(uint64_t key, int shift, uint32_t mask) { return (uint32_t)(key >> shift) & mask; }
 
-// FIRST: the input is the caller's key array (int64, checked to be in range or the handle is frozen) and the
-// positions are the indices; otherwise the pairs come from the previous pass.
-template <int ITEMS, bool FIRST>
-__global__ __launch_bounds__(SORT_THREADS) void k_sort_count(const int64_t *keys_in, const uint64_t *pk_in, int64_t n, int shift, int bits,
+// Keys: where the first pass has its keys from - the caller's key array (int64, checked to be in range or the handle is frozen), or the
+// caller's tokens -; the positions are the indices.  In the other passes (PairsIn) the pairs come from the previous pass.
+struct KeysIn { const int64_t *p; __device__ __forceinline__ uint64_t operator[](int64_t q) const { return (uint64_t)p[q]; } };
+// A token, padding behind all tokens, and behind that any other number
+struct TokensIn {
+    TokenIds t;
+    __device__ __forceinline__ uint64_t operator[](int64_t q) const {
+        const int64_t id = t.at(q);
+        return id == t.pad ? (uint64_t)t.count : id < 0 || id >= t.count ? (uint64_t)t.count + 1 : (uint64_t)id;
+    }
+};
+struct PairsIn { __device__ __forceinline__ uint64_t operator[](int64_t) const { return 0; } };
+template <class Keys> constexpr bool is_first() { return !std::is_same<Keys, PairsIn>::value; }
+template <int ITEMS, class Keys>
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_count(Keys keys_in, const uint64_t *pk_in, int64_t n, int shift, int bits,
                                                              int64_t num_tiles, uint32_t *hist, int64_t check_below, int32_t *err) {
+    constexpr bool FIRST = is_first<Keys>();
     const int32_t stop = flag_ahead(err);
     __shared__ uint32_t cnt[1 << SORT_MAX_BITS];
     const int R = 1 << bits;
@@ -51,7 +65,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_count(const int64_t *keys
 #pragma unroll
     for (int r = 0; r < ITEMS; ++r) {
         const int64_t q = base + (int64_t)r * SORT_THREADS + threadIdx.x;
-        key[r] = q < n ? (FIRST ? (uint64_t)keys_in[q] : pk_in[q]) : 0;
+        key[r] = q < n ? (FIRST ? keys_in[q] : pk_in[q]) : 0;
     }
     if (stop) return;
     for (int i = threadIdx.x; i < R; i += SORT_THREADS) cnt[i] = 0;
@@ -121,10 +135,11 @@ __global__ __launch_bounds__(256) void k_sort_scan(uint32_t *hist, int64_t num_t
     }
 }
 
-template <int ITEMS, bool FIRST>
-__global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(const int64_t *keys_in, const uint64_t *pk_in, const uint32_t *pp_in, int64_t n,
+template <int ITEMS, class Keys>
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(Keys keys_in, const uint64_t *pk_in, const uint32_t *pp_in, int64_t n,
                                                                int shift, int bits, int64_t num_tiles, const uint32_t *hist, uint64_t *pk_out,
                                                                uint32_t *pp_out, const int32_t *err) {
+    constexpr bool FIRST = is_first<Keys>();
     const int32_t stop = flag_ahead(err);
     __shared__ uint32_t wh[SORT_WAVES][1 << SORT_MAX_BITS];
     const int R = 1 << bits;
@@ -140,7 +155,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(const int64_t *ke
         const int64_t q = base + r * 64 + lane;
         key[r] = 0; pos[r] = 0;
         if (q < n) {
-            key[r] = FIRST ? (uint64_t)keys_in[q] : pk_in[q];
+            key[r] = FIRST ? keys_in[q] : pk_in[q];
             pos[r] = FIRST ? (uint32_t)q : pp_in[q];
         }
     }
@@ -210,9 +225,10 @@ constexpr int MID_THREADS = 512, MID_WAVES = MID_THREADS / 64, MID_MAX_TILES = 6
 constexpr int64_t MID_MAX = (int64_t)MID_THREADS * 4 * MID_MAX_TILES, MID_SHORT = MID_MAX / 4;
 static_assert(2 * MID_THREADS >= 1 << SORT_MAX_BITS, "two buckets per thread");
 
-template <int MID_ITEMS, bool FIRST>
-__global__ __launch_bounds__(MID_THREADS) void k_sort_mid_count(const int64_t *keys_in, const uint64_t *pk_in, int64_t n, int shift, int bits,
+template <int MID_ITEMS, class Keys>
+__global__ __launch_bounds__(MID_THREADS) void k_sort_mid_count(Keys keys_in, const uint64_t *pk_in, int64_t n, int shift, int bits,
                                                                 uint32_t *hist, int64_t check_below, int32_t *err) {
+    constexpr bool FIRST = is_first<Keys>();
     const int32_t stop = flag_ahead(err);
     __shared__ uint32_t cnt[1 << SORT_MAX_BITS];
     const int R = 1 << bits, tid = threadIdx.x;
@@ -222,7 +238,7 @@ __global__ __launch_bounds__(MID_THREADS) void k_sort_mid_count(const int64_t *k
 #pragma unroll
     for (int r = 0; r < MID_ITEMS; ++r) {
         const int64_t q = base + r * MID_THREADS + tid;
-        key[r] = q < n ? (FIRST ? (uint64_t)keys_in[q] : pk_in[q]) : 0;
+        key[r] = q < n ? (FIRST ? keys_in[q] : pk_in[q]) : 0;
     }
     if (stop) return;
     for (int i = tid; i < R; i += MID_THREADS) cnt[i] = 0;
@@ -238,10 +254,11 @@ __global__ __launch_bounds__(MID_THREADS) void k_sort_mid_count(const int64_t *k
     for (int i = tid; i < R; i += MID_THREADS) hist[(int64_t)blockIdx.x * R + i] = cnt[i];
 }
 
-template <int MID_ITEMS, bool FIRST>
-__global__ __launch_bounds__(MID_THREADS) void k_sort_mid_scatter(const int64_t *keys_in, const uint64_t *pk_in, const uint32_t *pp_in, int64_t n,
+template <int MID_ITEMS, class Keys>
+__global__ __launch_bounds__(MID_THREADS) void k_sort_mid_scatter(Keys keys_in, const uint64_t *pk_in, const uint32_t *pp_in, int64_t n,
                                                                   int shift, int bits, const uint32_t *hist, uint64_t *pk_out, uint32_t *pp_out,
                                                                   const int32_t *err) {
+    constexpr bool FIRST = is_first<Keys>();
     const int32_t stop = flag_ahead(err);
     __shared__ __attribute__((aligned(8))) uint32_t wh[MID_WAVES][1 << SORT_MAX_BITS];
     __shared__ uint32_t wave_sum[MID_WAVES];
@@ -255,7 +272,7 @@ __global__ __launch_bounds__(MID_THREADS) void k_sort_mid_scatter(const int64_t 
     for (int r = 0; r < MID_ITEMS; ++r) {
         const int64_t q = base + r * 64 + lane;
         const bool valid = q < n;
-        key[r] = valid ? (FIRST ? (uint64_t)keys_in[q] : pk_in[q]) : 0;
+        key[r] = valid ? (FIRST ? keys_in[q] : pk_in[q]) : 0;
         pos[r] = valid ? (FIRST ? (uint32_t)q : pp_in[q]) : 0u;
     }
     // this thread's two buckets: pairs in all tiles, and in the tiles before this one
@@ -346,9 +363,10 @@ struct BigLds {
     uint32_t sums[2][BIG_WAVES];
 };
 
-template <bool FIRST>
-__global__ __launch_bounds__(BIG_THREADS) void k_sort_big_count(const int64_t *keys_in, const uint64_t *pk_in, int64_t n, int shift, int bits, uint32_t *hist,
+template <class Keys>
+__global__ __launch_bounds__(BIG_THREADS) void k_sort_big_count(Keys keys_in, const uint64_t *pk_in, int64_t n, int shift, int bits, uint32_t *hist,
                                                                 int64_t check_below, int32_t *err) {
+    constexpr bool FIRST = is_first<Keys>();
     const int32_t stop = flag_ahead(err);
     __shared__ uint32_t cnt[1 << SORT_MAX_BITS];
     const int R = 1 << bits, tid = threadIdx.x;
@@ -358,7 +376,7 @@ __global__ __launch_bounds__(BIG_THREADS) void k_sort_big_count(const int64_t *k
 #pragma unroll
     for (int r = 0; r < BIG_ITEMS; ++r) {
         const int64_t q = base + r * BIG_THREADS + tid;
-        key[r] = q < n ? (FIRST ? (uint64_t)keys_in[q] : pk_in[q]) : 0;
+        key[r] = q < n ? (FIRST ? keys_in[q] : pk_in[q]) : 0;
     }
     if (stop) return;
     if (tid < R) cnt[tid] = 0;
@@ -379,9 +397,10 @@ __global__ __launch_bounds__(BIG_THREADS) void k_sort_big_count(const int64_t *k
     if (tid < R) hist[(int64_t)blockIdx.x * R + tid] = cnt[tid];
 }
 
-template <bool FIRST>
-__global__ __launch_bounds__(BIG_THREADS) void k_sort_big_scatter(const int64_t *keys_in, const uint64_t *pk_in, const uint32_t *pp_in, int64_t n, int shift,
+template <class Keys>
+__global__ __launch_bounds__(BIG_THREADS) void k_sort_big_scatter(Keys keys_in, const uint64_t *pk_in, const uint32_t *pp_in, int64_t n, int shift,
                                                                   int bits, const uint32_t *hist, uint64_t *pk_out, uint32_t *pp_out, const int32_t *err) {
+    constexpr bool FIRST = is_first<Keys>();
     const int32_t stop = flag_ahead(err);
     extern __shared__ __attribute__((aligned(16))) unsigned char big_mem[];
     BigLds &l = *reinterpret_cast<BigLds *>(big_mem);
@@ -396,7 +415,7 @@ __global__ __launch_bounds__(BIG_THREADS) void k_sort_big_scatter(const int64_t 
 #pragma unroll
     for (int r = 0; r < BIG_ITEMS; ++r) {
         const int q = first + r * 64 + lane;
-        key[r] = q < size ? (FIRST ? (uint64_t)keys_in[base + q] : pk_in[base + q]) : 0;
+        key[r] = q < size ? (FIRST ? keys_in[base + q] : pk_in[base + q]) : 0;
         pos[r] = q < size ? (FIRST ? (uint32_t)(base + q) : pp_in[base + q]) : 0u;
     }
     // this thread's bucket: pairs in all tiles, and in the tiles before this one
@@ -555,8 +574,8 @@ SortPlan sort_plan(int64_t n, int key_bits) {
 }
 
 // MID: up to MID_MAX pairs; ITEMS 0: BIG_MIN to BIG_MAX
-template <int ITEMS, bool MID>
-int sort_run(dpaps_ps *ps, const SortPlan &p, const int64_t *keys, int64_t n, int64_t check_below, uint64_t *skeys, uint32_t *spos, void *scratch,
+template <int ITEMS, bool MID, class Keys>
+int sort_run(dpaps_ps *ps, const SortPlan &p, const Keys &keys, int64_t n, int64_t check_below, uint64_t *skeys, uint32_t *spos, void *scratch,
              hipStream_t st) {
     uint64_t *alt_k = (uint64_t *)((char *)scratch + p.off_pk);
     uint32_t *alt_p = (uint32_t *)((char *)scratch + p.off_pp);
@@ -572,34 +591,34 @@ int sort_run(dpaps_ps *ps, const SortPlan &p, const int64_t *keys, int64_t n, in
         if constexpr (MID) {
             constexpr int TILE = MID_THREADS * ITEMS;
             const unsigned mid = (unsigned)((n + TILE - 1) / TILE);
-            if (i == 0) k_sort_mid_count<ITEMS, true><<<mid, MID_THREADS, 0, st>>>(keys, nullptr, n, shift, bits, hist, check_below, ps->err);
-            else k_sort_mid_count<ITEMS, false><<<mid, MID_THREADS, 0, st>>>(nullptr, in_k, n, shift, bits, hist, 0, ps->err);
+            if (i == 0) k_sort_mid_count<ITEMS, Keys><<<mid, MID_THREADS, 0, st>>>(keys, nullptr, n, shift, bits, hist, check_below, ps->err);
+            else k_sort_mid_count<ITEMS, PairsIn><<<mid, MID_THREADS, 0, st>>>(PairsIn{}, in_k, n, shift, bits, hist, 0, ps->err);
             PS_HIP(ps, hipGetLastError());
-            if (i == 0) k_sort_mid_scatter<ITEMS, true><<<mid, MID_THREADS, 0, st>>>(keys, nullptr, nullptr, n, shift, bits, hist, out_k, out_p, ps->err);
-            else k_sort_mid_scatter<ITEMS, false><<<mid, MID_THREADS, 0, st>>>(nullptr, in_k, in_p, n, shift, bits, hist, out_k, out_p, ps->err);
+            if (i == 0) k_sort_mid_scatter<ITEMS, Keys><<<mid, MID_THREADS, 0, st>>>(keys, nullptr, nullptr, n, shift, bits, hist, out_k, out_p, ps->err);
+            else k_sort_mid_scatter<ITEMS, PairsIn><<<mid, MID_THREADS, 0, st>>>(PairsIn{}, in_k, in_p, n, shift, bits, hist, out_k, out_p, ps->err);
             PS_HIP(ps, hipGetLastError());
         } else if constexpr (ITEMS == 0) {
             static LdsAllowed first, other;
-            int rc = dpaps_allow_lds(ps, first, reinterpret_cast<const void *>(&k_sort_big_scatter<true>), sizeof(BigLds));
-            if (!rc) rc = dpaps_allow_lds(ps, other, reinterpret_cast<const void *>(&k_sort_big_scatter<false>), sizeof(BigLds));
+            int rc = dpaps_allow_lds(ps, first, reinterpret_cast<const void *>(&k_sort_big_scatter<Keys>), sizeof(BigLds));
+            if (!rc) rc = dpaps_allow_lds(ps, other, reinterpret_cast<const void *>(&k_sort_big_scatter<PairsIn>), sizeof(BigLds));
             if (rc) return rc;
             const unsigned big = (unsigned)((n + BIG_TILE - 1) / BIG_TILE);
-            if (i == 0) k_sort_big_count<true><<<big, BIG_THREADS, 0, st>>>(keys, nullptr, n, shift, bits, hist, check_below, ps->err);
-            else k_sort_big_count<false><<<big, BIG_THREADS, 0, st>>>(nullptr, in_k, n, shift, bits, hist, 0, ps->err);
+            if (i == 0) k_sort_big_count<Keys><<<big, BIG_THREADS, 0, st>>>(keys, nullptr, n, shift, bits, hist, check_below, ps->err);
+            else k_sort_big_count<PairsIn><<<big, BIG_THREADS, 0, st>>>(PairsIn{}, in_k, n, shift, bits, hist, 0, ps->err);
             PS_HIP(ps, hipGetLastError());
-            if (i == 0) k_sort_big_scatter<true><<<big, BIG_THREADS, sizeof(BigLds), st>>>(keys, nullptr, nullptr, n, shift, bits, hist, out_k, out_p, ps->err);
-            else k_sort_big_scatter<false><<<big, BIG_THREADS, sizeof(BigLds), st>>>(nullptr, in_k, in_p, n, shift, bits, hist, out_k, out_p, ps->err);
+            if (i == 0) k_sort_big_scatter<Keys><<<big, BIG_THREADS, sizeof(BigLds), st>>>(keys, nullptr, nullptr, n, shift, bits, hist, out_k, out_p, ps->err);
+            else k_sort_big_scatter<PairsIn><<<big, BIG_THREADS, sizeof(BigLds), st>>>(PairsIn{}, in_k, in_p, n, shift, bits, hist, out_k, out_p, ps->err);
             PS_HIP(ps, hipGetLastError());
         } else {
-            if (i == 0) k_sort_count<ITEMS, true><<<tiles, SORT_THREADS, 0, st>>>(keys, nullptr, n, shift, bits, p.num_tiles, hist, check_below, ps->err);
-            else k_sort_count<ITEMS, false><<<tiles, SORT_THREADS, 0, st>>>(nullptr, in_k, n, shift, bits, p.num_tiles, hist, 0, ps->err);
+            if (i == 0) k_sort_count<ITEMS, Keys><<<tiles, SORT_THREADS, 0, st>>>(keys, nullptr, n, shift, bits, p.num_tiles, hist, check_below, ps->err);
+            else k_sort_count<ITEMS, PairsIn><<<tiles, SORT_THREADS, 0, st>>>(PairsIn{}, in_k, n, shift, bits, p.num_tiles, hist, 0, ps->err);
             PS_HIP(ps, hipGetLastError());
             k_sort_rowsum<<<R, 256, 0, st>>>(hist, p.num_tiles, tot, ps->err);
             PS_HIP(ps, hipGetLastError());
             k_sort_scan<<<R, 256, 0, st>>>(hist, p.num_tiles, tot, ps->err);
             PS_HIP(ps, hipGetLastError());
-            if (i == 0) k_sort_scatter<ITEMS, true><<<tiles, SORT_THREADS, 0, st>>>(keys, nullptr, nullptr, n, shift, bits, p.num_tiles, hist, out_k, out_p, ps->err);
-            else k_sort_scatter<ITEMS, false><<<tiles, SORT_THREADS, 0, st>>>(nullptr, in_k, in_p, n, shift, bits, p.num_tiles, hist, out_k, out_p, ps->err);
+            if (i == 0) k_sort_scatter<ITEMS, Keys><<<tiles, SORT_THREADS, 0, st>>>(keys, nullptr, nullptr, n, shift, bits, p.num_tiles, hist, out_k, out_p, ps->err);
+            else k_sort_scatter<ITEMS, PairsIn><<<tiles, SORT_THREADS, 0, st>>>(PairsIn{}, in_k, in_p, n, shift, bits, p.num_tiles, hist, out_k, out_p, ps->err);
             PS_HIP(ps, hipGetLastError());
         }
         in_k = out_k; in_p = out_p;
@@ -608,6 +627,16 @@ int sort_run(dpaps_ps *ps, const SortPlan &p, const int64_t *keys, int64_t n, in
         shift += bits;
     }
     return PS_OK;
+}
+
+template <class Keys>
+int sort_any(dpaps_ps *ps, const Keys &keys, int64_t n, int key_bits, int64_t check_below, uint64_t *skeys, uint32_t *spos, void *scratch, hipStream_t st) {
+    const SortPlan p = sort_plan(n, key_bits);
+    if (n <= MID_SHORT) return sort_run<2, true>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
+    if (n <= MID_MAX) return sort_run<4, true>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
+    if (n < BIG_MIN) return sort_run<4, false>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
+    if (n <= BIG_MAX) return sort_run<0, false>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
+    return sort_run<16, false>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
 }
 
 }  // namespace
@@ -637,10 +666,11 @@ int dpaps_sort_pairs(dpaps_ps *ps, const int64_t *keys, int64_t n, int key_bits,
         PS_HIP(ps, hipGetLastError());
         return PS_OK;
     }
-    const SortPlan p = sort_plan(n, key_bits);
-    if (n <= MID_SHORT) return sort_run<2, true>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
-    if (n <= MID_MAX) return sort_run<4, true>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
-    if (n < BIG_MIN) return sort_run<4, false>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
-    if (n <= BIG_MAX) return sort_run<0, false>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
-    return sort_run<16, false>(ps, p, keys, n, check_below, skeys, spos, scratch, st);
+    return sort_any(ps, KeysIn{keys}, n, key_bits, check_below, skeys, spos, scratch, st);
+}
+
+// The same for tokens, more than the few that a call takes without a sort: ordered by token, padding behind all of them (as token
+// t.count).  A token out of range sets the handle's error.  Scratch: that of keys of dpaps_key_bits(t.count + 1) bits.
+int dpaps_sort_tokens(dpaps_ps *ps, const TokenIds &t, uint64_t *skeys, uint32_t *spos, void *scratch, hipStream_t st) {
+    return sort_any(ps, TokensIn{t}, t.n, dpaps_key_bits(t.count + 1), t.count + 1, skeys, spos, scratch, st);
 }

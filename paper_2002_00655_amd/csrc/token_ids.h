@@ -44,3 +44,5 @@ __device__ __forceinline__ void route_tokens_block(const RouteArgs &a, const Tok
 // emb.hip: the statistics of a pull of the tokens' keys, and of a push of them right after it if `push`, in launches of their own, and with location
 // caches the replies
 int dpaps_route_tokens(dpaps_ps *ps, int32_t worker, const TokenIds &t, bool pull, bool push, hipStream_t st);
+// key_sort.hip: the pairs (token, position) ordered by token (see there)
+int dpaps_sort_tokens(dpaps_ps *ps, const TokenIds &t, uint64_t *skeys, uint32_t *spos, void *scratch, hipStream_t st);

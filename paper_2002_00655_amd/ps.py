@@ -289,10 +289,14 @@ class ParameterServer:
         at, kind, n = _tokens(tokens)
         dim = self.L if dim is None else dim
         if out is None:
-            out = torch.empty((*tokens.shape, dim), dtype=dtype, device=tokens.device)
-        elif out.shape != (*tokens.shape, dim):
-            raise ValueError(f"out must have the shape {(*tokens.shape, dim)}")
-        _, to, out_kind, stride = _rows(out, n, copy=False)
+            if dtype not in _TYPES:
+                raise TypeError(f"the result is float32, bfloat16 or float16, not {dtype}")
+            out = tokens.new_empty((*tokens.shape, dim), dtype=dtype)
+            to, out_kind, stride = out.data_ptr(), _TYPES[dtype], dim
+        else:
+            if out.shape != (*tokens.shape, dim):
+                raise ValueError(f"out must have the shape {(*tokens.shape, dim)}")
+            _, to, out_kind, stride = _rows(out, n, copy=False)
         self._check(_lib.emb_lookup(self._h, worker, first_key, self.K - first_key if num_tokens is None else num_tokens, dim, at, kind, n,
                                     _NO_PAD if pad_token is None else pad_token, scale, to, out_kind, stride, _stream()), "emb_lookup")
         return out
