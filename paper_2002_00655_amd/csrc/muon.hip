@@ -154,9 +154,7 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
 }
 
 // ---- the products ---------------------------------------------------------------------------------------------------
-#ifndef GJ
-#define GJ 4
-#endif
+constexpr int GJ = 4;                            // columns of a band
 constexpr uint32_t DIES = 8;                     // compute dies, each with a cache of its own
 constexpr int CHAIN = 12;                        // blocks of k whose products one chain of matrix instructions adds (a multiple of DEPTH and KB)
 enum MuonProduct { MUON_GRAM, MUON_POLY, MUON_APPLY, MUON_LAST, MUON_STEP };       // LAST, STEP: APPLY with the result put where it belongs
@@ -246,19 +244,78 @@ __device__ __forceinline__ Place place_of(const MuonArgs &a, uint32_t block, uin
 }
 
 // The sums leave by way of LDS, 64 x 64 at a time, so that rows of the result and rows of its mirror image are both written in whole
-// lines; the sums of KS wavefronts are added there.  x: 32 x 32 pieces, of which a lane has column lane % 32, rows
-// 8 g + 4 (lane / 32) + 0..3 for g = 0..3; from row i0, column j0 of matrix p.b.  mine: where this wavefront puts them, sums: the first one's place.
-constexpr int SUMS_LD = 68;                      // a row of 64 sums in LDS: 32 rows' pieces of 16 bytes lie in all banks
-template <int FI, int FJ, int KS, bool SPLIT, int MODE>
-__device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, const floatx16 (&x)[FI][FJ], int i0, int j0, float *mine, const float *sums, int group) {
+// lines.  SUMS_LD: a row of 64 sums there: 32 rows' pieces of 16 bytes lie in all banks.
+constexpr int SUMS_LD = 68;
+// From LDS, where KS wavefronts have put their shares of the sums, to where they belong: rows gi .., columns gj .. of matrix p.b.  group: of the KS wavefronts.
+template <int KS, bool SPLIT, int MODE>
+__device__ __forceinline__ void write_tile(const MuonArgs &a, const Place &p, int gi, int gj, const float *sums, int group) {
     constexpr float FACTOR = MODE == MUON_GRAM ? G_SCALE / (X_SCALE * X_SCALE) : MODE == MUON_APPLY ? 1.0f / P_SCALE : MODE >= MUON_LAST ? 1.0f / (P_SCALE * X_SCALE) : 1.0f;
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    const bool turned = MODE >= MUON_LAST && a.tall;
+                const auto sum = [&](int w) {
+                    float v = sums[w];
+    #pragma unroll
+                    for (int k = 1; k < KS; ++k) v += sums[k * (64 * SUMS_LD) + w];
+                    return v * FACTOR;
+                };
+                if constexpr (MODE >= MUON_LAST) {
+                    // eight rows at a time, eight lanes a row; of a step the weights of all of them first
+                    const int R0 = (turned ? gj : gi) + group * 8 + (lane >> 3), c = (lane & 7) * 8, C = (turned ? gi : gj) + c, height = turned ? a.m : a.n, left = (turned ? a.n : a.m) - C;
+                    const auto at = [&](int q) { return (q * KS * 8 + group * 8 + (lane >> 3)) * SUMS_LD + c; };
+                    if constexpr (MODE == MUON_STEP) {
+                        float w[8 / KS][8];
+    #pragma unroll
+                        for (int q = 0; q < 8 / KS; ++q)
+                            if (R0 + q * KS * 8 < height) get_weights(a, p.b * height + R0 + q * KS * 8, C, w[q], left);
+    #pragma unroll
+                        for (int q = 0; q < 8 / KS; ++q) {
+                            float v[8];
+    #pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = a.keep * w[q][e] - a.step * sum(at(q) + e);
+                            if (R0 + q * KS * 8 < height) put_numbers(a.val + (a.first + p.b * height + R0 + q * KS * 8) * a.L + C, v, left, a.to_vec);
+                        }
+                    } else {
+    #pragma unroll 1
+                        for (int q = 0; q < 8 / KS; ++q) {
+                            float v[8];
+    #pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = sum(at(q) + e);
+                            if (R0 + q * KS * 8 < height) put_result(a, p.b * height + R0 + q * KS * 8, C, v, left);
+                        }
+                    }
+                } else {
+                    const bool columns = MODE == MUON_APPLY || p.ti != p.tj;
+                    for (int way = 0; way < (columns ? 2 : 1); ++way) {
+    #pragma unroll 2
+                        for (int q = group; q < 8; q += KS) {
+                            const int r = (q & 1) * 32 + l32, c = (q >> 1) * 16 + h * 8;   // row r of what is written, numbers c .. c + 7
+                            float v[8];
+    #pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = sum(way ? (c + e) * SUMS_LD + r : r * SUMS_LD + c + e);
+                            const int R = (way ? gj : gi) + r, C = (way ? gi : gj) + c;
+                            if constexpr (MODE == MUON_POLY) {                    // (A is symmetric: it is read as the result is written)
+                                float g[8];
+                                get8<SPLIT>(a.lhs + p.b * a.lhs_size, R, C, a.K, g);
+    #pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    v[e] = v[e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g[e] * (NS_B * P_SCALE / G_SCALE) + (R == C + e ? NS_A * P_SCALE : 0.0f);
+                            }
+                            if (MODE == MUON_APPLY && way) put8<SPLIT>(a.out_t + p.b * a.out_size, R, C, a.out_t_ld, v);
+                            else put8<SPLIT>(a.out + p.b * a.out_size, R, C, a.out_ld, v);
+                        }
+                    }
+                }
+}
+// The numbers of the matrix instruction: x has 32 x 32 pieces, of which a lane has column lane % 32, rows 8 g + 4 (lane / 32) + 0..3 for
+// g = 0..3; from row i0, column j0 on.  mine: where this wavefront puts them, sums: the first one's place.
+template <int FI, int FJ, int KS, bool SPLIT, int MODE>
+__device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, const floatx16 (&x)[FI][FJ], int i0, int j0, float *mine, const float *sums, int group) {
+    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    const bool turned = MODE >= MUON_LAST && a.tall;                           // X is the transposed matrix
 #pragma unroll
     for (int si = 0; si < FI / 2; ++si)
 #pragma unroll
         for (int sj = 0; sj < FJ / 2; ++sj) {
-            const int gi = i0 + si * 64, gj = j0 + sj * 64;
-            const bool turned = MODE >= MUON_LAST && a.tall;                   // X is the transposed matrix
 #pragma unroll
             for (int fi = 0; fi < 2; ++fi)
 #pragma unroll
@@ -275,59 +332,7 @@ __device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, cons
                 }
             if constexpr (KS > 1) __syncthreads();
             else asm volatile("" ::: "memory");                                // (a wavefront's accesses to LDS stay in order)
-            const auto sum = [&](int w) {
-                float v = sums[w];
-#pragma unroll
-                for (int k = 1; k < KS; ++k) v += sums[k * (64 * SUMS_LD) + w];
-                return v * FACTOR;
-            };
-            if constexpr (MODE >= MUON_LAST) {
-                // eight rows at a time, eight lanes a row; of a step the weights of all of them first
-                const int R0 = (turned ? gj : gi) + group * 8 + (lane >> 3), c = (lane & 7) * 8, C = (turned ? gi : gj) + c, height = turned ? a.m : a.n, left = (turned ? a.n : a.m) - C;
-                const auto at = [&](int q) { return (q * KS * 8 + group * 8 + (lane >> 3)) * SUMS_LD + c; };
-                if constexpr (MODE == MUON_STEP) {
-                    float w[8 / KS][8];
-#pragma unroll
-                    for (int q = 0; q < 8 / KS; ++q)
-                        if (R0 + q * KS * 8 < height) get_weights(a, p.b * height + R0 + q * KS * 8, C, w[q], left);
-#pragma unroll
-                    for (int q = 0; q < 8 / KS; ++q) {
-                        float v[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = a.keep * w[q][e] - a.step * sum(at(q) + e);
-                        if (R0 + q * KS * 8 < height) put_numbers(a.val + (a.first + p.b * height + R0 + q * KS * 8) * a.L + C, v, left, a.to_vec);
-                    }
-                } else {
-#pragma unroll 1
-                    for (int q = 0; q < 8 / KS; ++q) {
-                        float v[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = sum(at(q) + e);
-                        if (R0 + q * KS * 8 < height) put_result(a, p.b * height + R0 + q * KS * 8, C, v, left);
-                    }
-                }
-            } else {
-                const bool columns = MODE == MUON_APPLY || p.ti != p.tj;
-                for (int way = 0; way < (columns ? 2 : 1); ++way) {
-#pragma unroll 2
-                    for (int q = group; q < 8; q += KS) {
-                        const int r = (q & 1) * 32 + l32, c = (q >> 1) * 16 + h * 8;   // row r of what is written, numbers c .. c + 7
-                        float v[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = sum(way ? (c + e) * SUMS_LD + r : r * SUMS_LD + c + e);
-                        const int R = (way ? gj : gi) + r, C = (way ? gi : gj) + c;
-                        if constexpr (MODE == MUON_POLY) {                    // (A is symmetric: it is read as the result is written)
-                            float g[8];
-                            get8<SPLIT>(a.lhs + p.b * a.lhs_size, R, C, a.K, g);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                v[e] = v[e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g[e] * (NS_B * P_SCALE / G_SCALE) + (R == C + e ? NS_A * P_SCALE : 0.0f);
-                        }
-                        if (MODE == MUON_APPLY && way) put8<SPLIT>(a.out_t + p.b * a.out_size, R, C, a.out_t_ld, v);
-                        else put8<SPLIT>(a.out + p.b * a.out_size, R, C, a.out_ld, v);
-                    }
-                }
-            }
+            write_tile<KS, SPLIT, MODE>(a, p, i0 + si * 64, j0 + sj * 64, sums, group);
             asm volatile("" ::: "memory");
         }
 }
@@ -378,8 +383,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];
     const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const Place p = place_of<MODE>(a, blockIdx.x, gridDim.x);
-    const int i0 = p.ti * 64, j0 = p.tj * 64, blocks = a.K >> 4, cnt = blocks / KS;               // (sides are multiples of 64)
-    const f16_t *l = a.lhs + p.b * a.lhs_size + ((int64_t)(i0 >> 5) * blocks + group) * (512 * S), *r = a.rhs + p.b * a.rhs_size + ((int64_t)(j0 >> 5) * blocks + group) * (512 * S);
+    const int i0 = p.ti * 64, j0 = p.tj * 64, blocks = a.K >> 4, turns = blocks / KS;             // (sides are multiples of 64)
+    const int first = turns * p.share / a.shares, cnt = turns * (p.share + 1) / a.shares - first, block0 = first * KS + group;
+    const f16_t *l = a.lhs + p.b * a.lhs_size + ((int64_t)(i0 >> 5) * blocks + block0) * (512 * S), *r = a.rhs + p.b * a.rhs_size + ((int64_t)(j0 >> 5) * blocks + block0) * (512 * S);
     const int64_t next_rows = (int64_t)blocks * (512 * S);
     half8 lf[DEPTH][2][S], rf[DEPTH][2][S];
     const auto load = [&](half8 (&x)[2][S], half8 (&y)[2][S], int t) {
@@ -412,7 +418,47 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         s.cut();
     }
     if (MODE == MUON_STEP && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
+    if (MODE == MUON_GRAM && a.shares > 1) {
+        // a share of the sums: 64 x 64, row by row
+        float *to = a.part + (int64_t)(p.slot * a.shares + p.share) * 4096;
+#pragma unroll
+        for (int fi = 0; fi < 2; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < 2; ++fj)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) lds[group][(fi * 32 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * SUMS_LD + fj * 32 + (lane & 31)] = s.all()[fi][fj][e];
+        __syncthreads();
+        for (int q = group; q < 16; q += KS) {
+            const int at = (q * 4 + (lane >> 4)) * SUMS_LD + (lane & 15) * 4;
+            floatx4 v = *reinterpret_cast<const floatx4 *>(&lds[0][at]);
+#pragma unroll
+            for (int k = 1; k < KS; ++k) v += *reinterpret_cast<const floatx4 *>(&lds[k][at]);
+            *reinterpret_cast<floatx4 *>(to + q * 256 + lane * 4) = v;
+        }
+        return;
+    }
     put_tile<2, 2, KS, SPLIT, MODE>(a, p, s.all(), i0, j0, lds[group], lds[0], group);
+}
+
+// The shares of a small tile's sums added: each wavefront every fourth share, and then the four.
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void k_muon_join_small(MuonArgs a, int32_t shares) {
+    constexpr int KS = 4;
+    __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];
+    const Place p = place_of<MUON_GRAM>(a, blockIdx.x, gridDim.x);             // (a.shares is 1 here)
+    const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    floatx4 x[16];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) x[q] = floatx4{};
+    for (int k = group; k < shares; k += KS) {
+        const float *from = a.part + (int64_t)(p.slot * shares + k) * 4096 + lane * 4;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) x[q] += *reinterpret_cast<const floatx4 *>(from + q * 256);
+    }
+#pragma unroll
+    for (int q = 0; q < 16; ++q) *reinterpret_cast<floatx4 *>(&lds[group][(q * 4 + (lane >> 4)) * SUMS_LD + (lane & 15) * 4]) = x[q];
+    __syncthreads();
+    write_tile<KS, SPLIT, MUON_GRAM>(a, p, p.ti * 64, p.tj * 64, lds[0], group);
 }
 
 // until at most N of this wavefront's loads are on their way and all it has asked of LDS is there, then until all wavefronts are so far
@@ -736,22 +782,18 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
-// Sides count as multiples of the tile's.  256: large matrices of 16 bits; 128: where a quarter as many tiles of 128 as there
-// are numbers of them ... ; 64: the rest.
-#ifndef SMALLK
-#define SMALLK 1
-#define SMALLT 1024
-#endif
-#ifndef MIDN
-#define MIDN 256
-#endif
+// Sides count as multiples of the tile's, 64, 128 or 256.  Tiles of 128 read a line of an operand half as often, tiles of 256 a quarter
+// as often, but few of them leave compute units idle.  Whole calls, tiles of 64 and of 128: 32 bits, 300 x 300 111 us and 151, 1024 x 1024 202 and
+// 261, four of 1024 x 1024 458 and 431, 1024 x 4096 429 and 372, 4096 x 4096 5,086 and 4,486; 16 of 512 x 512 297 and 284, 32 of 300 x 300 199 and 292
+// - the line is at 4 million numbers, a tile of 128 per compute unit.  16 bits, 128 and 256: 4096 x 4096 1,686 and 1,577, four of 2048 x 2048 926
+// and 975, 3000 x 3000 851 and 1,144.
 struct MuonPlan {
     int32_t batch, n, m, tile, np, mp, blocks;
     bool tall, split, one;
     size_t off_d, off_x, off_xt[2], off_g, off_p, off_part, bytes;
 };
 inline int64_t half_of(int64_t t) { return t * (t + 1) / 2; }
-constexpr int MOST_SHARES = 8, TURNS_AT_LEAST = 2;
+constexpr int MOST_SHARES = 8, TURNS_AT_LEAST = 2, SMALL_SHARES = 16, SMALL_TURNS = 4;
 // Workgroups that share a tile's sum over k, where there are fewer tiles than compute units.
 int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t K) {
     int64_t s = ps->num_cu / tiles;
@@ -759,14 +801,21 @@ int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t K) {
     if (s > K / 64 / TURNS_AT_LEAST) s = K / 64 / TURNS_AT_LEAST;
     return s < 2 ? 1 : (int)s;
 }
+// The same for tiles of 64, a long sum: at least SMALL_TURNS blocks of k for each wavefront.  A share more costs the join, 3 us, and saves a part of the sum's
+// time: 10 x 4096 in 32 bits 101 us instead of 211, 128 x 1024 106 instead of 117; 128 x 512, with two shares, 102 instead of 97.
+int small_shares(const dpaps_ps *ps, int64_t tiles, int32_t K) {
+    const int64_t by_K = K / 64 / SMALL_TURNS, most = ps->num_cu / tiles;
+    if (by_K < 4) return 1;
+    const int64_t s = by_K < most ? by_K : most;
+    return s < 2 ? 1 : s > SMALL_SHARES ? SMALL_SHARES : (int)s;
+}
 MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols, bool split, bool step) {
     MuonPlan p{};
     p.batch = batch; p.tall = rows > cols; p.split = split;
     p.n = p.tall ? cols : rows; p.m = p.tall ? rows : cols;
-    p.tile = 64;
     p.one = p.m <= ONE_SIDE;
-    if (p.n > MIDN) p.tile = 128;
-    if (!split && half_of(ceil_div64(p.n, 256)) * batch >= ps->num_cu) p.tile = 256;
+    p.tile = p.n > 256 && (int64_t)p.n * p.m * batch >= (int64_t)16384 * ps->num_cu ? 128 : 64;
+    if (!split && (p.n >= 4096 || half_of(ceil_div64(p.n, 256)) * batch >= ps->num_cu)) p.tile = 256;
     p.np = (int32_t)(ceil_div64(p.n, p.tile) * p.tile); p.mp = (int32_t)(ceil_div64(p.m, p.tile) * p.tile);
     if (p.one) return p;                          // (no scratch)
     const int64_t blocks = ceil_div64((int64_t)rows * cols, 1024);
@@ -780,7 +829,7 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     p.off_p = p.off_g + up256(nn);
     p.off_part = p.off_p + up256(nn);
     // (shares times tiles are at most as many as the compute units)
-    p.bytes = p.off_part + (p.tile > 64 ? (size_t)ps->num_cu * p.tile * p.tile * sizeof(float) : 0);
+    p.bytes = p.off_part + (size_t)ps->num_cu * p.tile * p.tile * sizeof(float);
     return p;
 }
 
@@ -813,11 +862,18 @@ int product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
     a.shares = 1;
     const int64_t tiles = (int64_t)a.tiles * batch, cus = ps->num_cu;
     if constexpr (TILE == 64) {
-        k_muon_small<SPLIT, MODE><<<(unsigned)tiles, 256, 0, st>>>(a, ps->err);
+        if constexpr (MODE == MUON_GRAM) a.shares = small_shares(ps, tiles, a.K);
+        k_muon_small<SPLIT, MODE><<<(unsigned)(tiles * a.shares), 256, 0, st>>>(a, ps->err);
         PS_HIP(ps, hipGetLastError());
+        if constexpr (MODE == MUON_GRAM) {
+            const int32_t shares = a.shares;
+            a.shares = 1;
+            if (shares > 1) k_muon_join_small<SPLIT><<<(unsigned)tiles, 256, 0, st>>>(a, shares);
+            PS_HIP(ps, hipGetLastError());
+        }
     } else if constexpr (TILE == 256) {
         // as many tiles as make full rounds of the compute units, and the rest with shared sums
-        const int64_t rest = HALF && tiles % cus <= cus / 2 ? tiles % cus : 0;
+        const int64_t rest = HALF && tiles > cus && tiles % cus <= cus / 2 ? tiles % cus : 0;
         const int rc = large<4, 2, 4, SPLIT, MODE>(ps, a, tiles - rest, st);
         if (rc || rest == 0) return rc;
         a.tile0 = (int32_t)(tiles - rest);
@@ -827,7 +883,7 @@ int product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
         if (tiles > cus) return large<2, KB / 2, 4, SPLIT, MODE>(ps, a, tiles, st);
         if constexpr (HALF) {
             // (with a short sum, tiles of 64)
-            if (SMALLK * a.K <= SMALLT && tiles < cus) { a.tiles_i *= 2; a.tiles_j *= 2; return product<64, SPLIT, MODE>(ps, a, batch, st); }
+            if (a.K <= 1024 && tiles < cus) { a.tiles_i *= 2; a.tiles_j *= 2; return product<64, SPLIT, MODE>(ps, a, batch, st); }
             return large_rest<2, KB, SPLIT, MODE>(ps, a, tiles, st);
         } else return large<2, KB, 4, SPLIT, MODE>(ps, a, tiles, st);
     }
