@@ -315,7 +315,7 @@ int kge_sgd_epoch(ps_handle ps, int64_t num_entities, int32_t dim, int64_t num_t
  * (dim <= value_len), so that several tables, and matrices, can share a server.  Tokens are int32 or int64 (PS_I32, PS_I64);
  * a token equal to pad_token (which may lie outside the vocabulary; PS_NO_PAD: none) is padding: no key is accessed for it.
  * Any other token outside [0, num_tokens) is an error found on the device (PS_EKEY, deferred, see the top): nothing is
- * changed then.  n = 0 is allowed everywhere; n < 2^31 (PS_ELIMIT).
+ * changed then.  n = 0 is allowed everywhere; n <= PS_EMB_MAX_TOKENS, num_tokens < 2^31, and a lookup's result has less than 2^34 elements (PS_ELIMIT).
  * Tensors other than the server's values are 32-bit floats or 16-bit ones (PS_F32, PS_BF16, PS_F16), in rows whose
  * elements are contiguous; strides count elements.  All sums are in 32 bits; a result is rounded to its type once.
  * The tensors of a call must not overlap the ones it writes.  None of these calls waits for the stream, except where
@@ -326,6 +326,7 @@ enum { PS_F32 = 0, PS_BF16 = 1, PS_F16 = 2 };    /* types of values */
 enum { PS_I32 = 0, PS_I64 = 1 };                 /* types of tokens */
 #define PS_NO_PAD INT64_MIN
 #define PS_EMB_MAX_DIM 65536
+#define PS_EMB_MAX_TOKENS 536870912
 
 /* out[p * out_stride + c] = scale * (value c of token p), rounded to out_type; zero where token p is padding.  An
  * access like ps_pull of the tokens' keys.  out_stride >= dim. */

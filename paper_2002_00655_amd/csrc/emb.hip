@@ -420,7 +420,10 @@ __global__ __launch_bounds__(FEW_THREADS) void k_emb_few(RouteArgs route, TokenI
 int token_ids(dpaps_ps *ps, int64_t first_key, int64_t num_tokens, bool in_store, const void *tokens, int32_t token_type, int64_t n, int64_t pad, TokenIds *t) {
     if (n < 0 || (n > 0 && !tokens) || num_tokens <= 0 || first_key < 0 || (token_type != PS_I32 && token_type != PS_I64)) return PS_EINVAL;
     if (in_store && (num_tokens > ps->K || first_key > ps->K - num_tokens)) return PS_EINVAL;
-    if (n >= ((int64_t)1 << 31)) return PS_ELIMIT;
+    if (n > PS_EMB_MAX_TOKENS || num_tokens >= ((int64_t)1 << 31)) {
+        ps->last_error = "tokens: at most 2^29 in a call, of a vocabulary of less than 2^31";
+        return PS_ELIMIT;
+    }
     t->ids = tokens; t->wide = token_type == PS_I64; t->n = n; t->first = first_key; t->count = num_tokens; t->pad = pad;
     return PS_OK;
 }
@@ -431,7 +434,9 @@ int lookup(dpaps_ps *ps, const RouteArgs &a, const TokenIds &t, int32_t dim, flo
 #define LOOKUP(W, AHEAD)                                                                                                                          \
     do {                                                                                                                                          \
         const uint32_t P = (uint32_t)(dim / W);                                                                                                   \
-        const unsigned grid = (unsigned)a.blocks + grid_for(t.n * P, 256 * AHEAD);                                                                \
+        const int64_t blocks = a.blocks + ceil_div64(t.n * P, 256 * AHEAD);                                                                       \
+        if (blocks >= ((int64_t)1 << 24)) { ps->last_error = "emb_lookup: the result is too large for one launch"; return PS_ELIMIT; }            \
+        const unsigned grid = (unsigned)blocks;                                                                                                   \
         k_emb_lookup<Out, W, AHEAD, false><<<grid, 256, 0, st>>>(a, t, P, 1.0 / P, ps->L, scale, ps->val, out, stride, ps->err);                  \
     } while (0)
     if (sizeof(Out) == 2 && fits(8)) LOOKUP(8, 2);

@@ -110,7 +110,13 @@ __global__ __launch_bounds__(256) void k_muon_norm(MuonIn a, uint32_t P, double 
     if (threadIdx.x == 0) a.squares[(int64_t)blockIdx.y * NORM_BLOCKS + blockIdx.x] = s;
 }
 
-// X_0 both ways, zero where the padded matrices go on.  A norm that is no number, or infinite, makes all of the matrix NaN, as the division would.
+// What a matrix's numbers are multiplied by to become X_0, scaled, in 64 bits: neither a norm above the largest 32-bit number nor one near the smallest
+// loses anything.  An infinity or NaN anywhere in the matrix makes all of X NaN, as the division and the products would.
+__device__ __forceinline__ double scale_of(double square, float eps) {
+    return square <= 1.7e308 ? (double)X_SCALE / (sqrt(square) + (double)eps) : __builtin_nan("");
+}
+
+// X_0 both ways, zero where the padded matrices go on.
 template <bool SPLIT>
 __device__ __forceinline__ void put8(f16_t *to, int r, int k, int K, const float (&v)[8]) {
     half8 hi, lo;
@@ -128,15 +134,14 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
     __shared__ float tile[64][65];
     const int64_t b = blockIdx.z;
     const double square = sum_of_256((int)threadIdx.x < a.blocks ? a.squares[b * NORM_BLOCKS + threadIdx.x] : 0.0);
-    const float norm = (float)sqrt(square);
-    const float f = norm <= 3.0e38f ? X_SCALE / (norm + a.eps) : __builtin_nanf("");
+    const double f = scale_of(square, a.eps);
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;                     // of X
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;                       // of the matrix itself
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
         const int r = wave + 4 * u, rr = r0 + r, cc = c0 + lane;
-        const float v = rr < a.rows && cc < a.cols ? f * element(a, b * a.rows + rr, cc) : 0.0f;
+        const float v = rr < a.rows && cc < a.cols ? (float)(f * (double)element(a, b * a.rows + rr, cc)) : 0.0f;
         if (tall) tile[lane][r] = v; else tile[r][lane] = v;
     }
     __syncthreads();
@@ -673,11 +678,11 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
     s = 0.0;
 #pragma unroll
     for (int w = 0; w < ONE_THREADS / 64; ++w) s += squares[w];
-    const float norm = (float)sqrt(s), scale = norm <= 3.0e38f ? X_SCALE / (norm + in.eps) : __builtin_nanf("");
+    const double scale = scale_of(s, in.eps);
 #pragma unroll
     for (int f = 0; f < 2; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[f][e] *= scale;                        // (zero outside the matrix, or all NaN)
+        for (int e = 0; e < 16; ++e) x[f][e] = (float)((double)x[f][e] * scale);      // (zero outside the matrix, or all NaN)
 
     // the numbers v, rows and columns exchanged, into m of K numbers a row; the same as they are
     const auto put_columns = [&](f16_t *m, int K, const floatx16 (&v)[2]) {
@@ -784,8 +789,8 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 // ---- host -----------------------------------------------------------------------------------------------------------
 // Sides count as multiples of the tile's, 64, 128 or 256.  Tiles of 128 read a line of an operand half as often, tiles of 256 a quarter
 // as often, but few of them leave compute units idle.  Whole calls, tiles of 64 and of 128: 32 bits, 300 x 300 111 us and 151, 1024 x 1024 202 and
-// 261, four of 1024 x 1024 458 and 431, 1024 x 4096 429 and 372, 4096 x 4096 5,086 and 4,486; 16 of 512 x 512 297 and 284, 32 of 300 x 300 199 and 292
-// - the line is at 4 million numbers, a tile of 128 per compute unit.  16 bits, 128 and 256: 4096 x 4096 1,686 and 1,577, four of 2048 x 2048 926
+// 261, two of them 292 and 320, 1500 x 2000 516 and 448, four of 1024 x 1024 458 and 431, 1024 x 4096 429 and 372, 4096 x 4096 5,086 and 4,486;
+// 32 of 300 x 300, which become 320 and 384, 199 and 292 - the line is at 2.9 million numbers, unless the larger tile makes them a quarter more.  16 bits, 128 and 256: 4096 x 4096 1,686 and 1,577, four of 2048 x 2048 926
 // and 975, 3000 x 3000 851 and 1,144.
 struct MuonPlan {
     int32_t batch, n, m, tile, np, mp, blocks;
@@ -814,7 +819,8 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     p.batch = batch; p.tall = rows > cols; p.split = split;
     p.n = p.tall ? cols : rows; p.m = p.tall ? rows : cols;
     p.one = p.m <= ONE_SIDE;
-    p.tile = p.n > 256 && (int64_t)p.n * p.m * batch >= (int64_t)16384 * ps->num_cu ? 128 : 64;
+    const auto padded = [&](int64_t t) { return ceil_div64(p.n, t) * t * ceil_div64(p.m, t) * t * batch; };
+    p.tile = padded(64) >= (int64_t)11264 * ps->num_cu && 4 * padded(128) <= 5 * padded(64) ? 128 : 64;
     if (!split && (p.n >= 4096 || half_of(ceil_div64(p.n, 256)) * batch >= ps->num_cu)) p.tile = 256;
     p.np = (int32_t)(ceil_div64(p.n, p.tile) * p.tile); p.mp = (int32_t)(ceil_div64(p.m, p.tile) * p.tile);
     if (p.one) return p;                          // (no scratch)
