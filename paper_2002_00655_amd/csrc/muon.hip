@@ -54,12 +54,6 @@ struct MuonIn {
     int32_t blocks;
     float eps;
 };
-__device__ __forceinline__ float element(const MuonIn &a, int64_t row, int col) {
-    const int64_t i = row * a.ld + col;
-    if (a.type == PS_F32) return reinterpret_cast<const float *>(a.in)[i];
-    return a.type == PS_BF16 ? (float)reinterpret_cast<const bf16_t *>(a.in)[i] : (float)reinterpret_cast<const f16_t *>(a.in)[i];
-}
-
 // The sum of a workgroup's 256 numbers, in a fixed order; the same in all threads.
 __device__ __forceinline__ double sum_of_256(double x) {
     __shared__ double lds[4];
@@ -129,20 +123,25 @@ __device__ __forceinline__ void put8(f16_t *to, int r, int k, int K, const float
     *reinterpret_cast<half8 *>(p) = hi;
     if constexpr (SPLIT) *reinterpret_cast<half8 *>(p + 512) = lo;
 }
-template <bool SPLIT>
+template <class T, bool SPLIT>
 __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np, int mp, f16_t *x, f16_t *xt) {
     __shared__ float tile[64][65];
     const int64_t b = blockIdx.z;
-    const double square = sum_of_256((int)threadIdx.x < a.blocks ? a.squares[b * NORM_BLOCKS + threadIdx.x] : 0.0);
-    const double f = scale_of(square, a.eps);
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;                     // of X
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;                       // of the matrix itself
+    const int r0 = tall ? j0 : i0, c0 = (tall ? i0 : j0) + lane;              // of the matrix itself
+    float v[16];
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
-        const int r = wave + 4 * u, rr = r0 + r, cc = c0 + lane;
-        const float v = rr < a.rows && cc < a.cols ? (float)(f * (double)element(a, b * a.rows + rr, cc)) : 0.0f;
-        if (tall) tile[lane][r] = v; else tile[r][lane] = v;
+        const int r = r0 + wave + 4 * u;
+        v[u] = r < a.rows && c0 < a.cols ? (float)reinterpret_cast<const T *>(a.in)[(b * a.rows + r) * a.ld + c0] : 0.0f;
+    }
+    const double square = sum_of_256((int)threadIdx.x < a.blocks ? a.squares[b * NORM_BLOCKS + threadIdx.x] : 0.0);
+    const double f = scale_of(square, a.eps);
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+        const float y = (float)(f * (double)v[u]);
+        if (tall) tile[lane][wave + 4 * u] = y; else tile[wave + 4 * u][lane] = y;
     }
     __syncthreads();
     x += b * (int64_t)np * mp * (SPLIT ? 2 : 1);
@@ -150,10 +149,10 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int r = u * 32 + (lane & 31), k = wave * 16 + (lane >> 5) * 8;
-        float v[8], w[8];
+        float y[8], w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { v[i] = tile[r][k + i]; w[i] = tile[k + i][r]; }
-        put8<SPLIT>(x, i0 + r, j0 + k, mp, v);
+        for (int i = 0; i < 8; ++i) { y[i] = tile[r][k + i]; w[i] = tile[k + i][r]; }
+        put8<SPLIT>(x, i0 + r, j0 + k, mp, y);
         put8<SPLIT>(xt, j0 + r, i0 + k, np, w);
     }
 }
@@ -259,7 +258,7 @@ __device__ __forceinline__ void write_tile(const MuonArgs &a, const Place &p, in
     const bool turned = MODE >= MUON_LAST && a.tall;
                 const auto sum = [&](int w) {
                     float v = sums[w];
-    #pragma unroll
+#pragma unroll
                     for (int k = 1; k < KS; ++k) v += sums[k * (64 * SUMS_LD) + w];
                     return v * FACTOR;
                 };
@@ -269,21 +268,21 @@ __device__ __forceinline__ void write_tile(const MuonArgs &a, const Place &p, in
                     const auto at = [&](int q) { return (q * KS * 8 + group * 8 + (lane >> 3)) * SUMS_LD + c; };
                     if constexpr (MODE == MUON_STEP) {
                         float w[8 / KS][8];
-    #pragma unroll
+#pragma unroll
                         for (int q = 0; q < 8 / KS; ++q)
                             if (R0 + q * KS * 8 < height) get_weights(a, p.b * height + R0 + q * KS * 8, C, w[q], left);
-    #pragma unroll
+#pragma unroll
                         for (int q = 0; q < 8 / KS; ++q) {
                             float v[8];
-    #pragma unroll
+#pragma unroll
                             for (int e = 0; e < 8; ++e) v[e] = a.keep * w[q][e] - a.step * sum(at(q) + e);
                             if (R0 + q * KS * 8 < height) put_numbers(a.val + (a.first + p.b * height + R0 + q * KS * 8) * a.L + C, v, left, a.to_vec);
                         }
                     } else {
-    #pragma unroll 1
+#pragma unroll 1
                         for (int q = 0; q < 8 / KS; ++q) {
                             float v[8];
-    #pragma unroll
+#pragma unroll
                             for (int e = 0; e < 8; ++e) v[e] = sum(at(q) + e);
                             if (R0 + q * KS * 8 < height) put_result(a, p.b * height + R0 + q * KS * 8, C, v, left);
                         }
@@ -291,17 +290,17 @@ __device__ __forceinline__ void write_tile(const MuonArgs &a, const Place &p, in
                 } else {
                     const bool columns = MODE == MUON_APPLY || p.ti != p.tj;
                     for (int way = 0; way < (columns ? 2 : 1); ++way) {
-    #pragma unroll 2
+#pragma unroll 2
                         for (int q = group; q < 8; q += KS) {
                             const int r = (q & 1) * 32 + l32, c = (q >> 1) * 16 + h * 8;   // row r of what is written, numbers c .. c + 7
                             float v[8];
-    #pragma unroll
+#pragma unroll
                             for (int e = 0; e < 8; ++e) v[e] = sum(way ? (c + e) * SUMS_LD + r : r * SUMS_LD + c + e);
                             const int R = (way ? gj : gi) + r, C = (way ? gi : gj) + c;
                             if constexpr (MODE == MUON_POLY) {                    // (A is symmetric: it is read as the result is written)
                                 float g[8];
                                 get8<SPLIT>(a.lhs + p.b * a.lhs_size, R, C, a.K, g);
-    #pragma unroll
+#pragma unroll
                                 for (int e = 0; e < 8; ++e)
                                     v[e] = v[e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g[e] * (NS_B * P_SCALE / G_SCALE) + (R == C + e ? NS_A * P_SCALE : 0.0f);
                             }
@@ -724,7 +723,6 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
         const f16_t *pl = l + (i0 >> 5) * blocks * (512 * S) + lane * 8, *pr = r + (j0 >> 5) * blocks * (512 * S) + lane * 8;
         sum[0] = floatx16{};
         sum[1] = floatx16{};
-#pragma unroll 2
         for (int k = 0; k < used; ++k) {
             half8 lf[2][S], rf[S];
 #pragma unroll
@@ -901,7 +899,10 @@ int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t s
     char *ws = (char *)ps->ws;
     f16_t *x = (f16_t *)(ws + p.off_x), *xt = (f16_t *)(ws + p.off_xt[0]), *xt_next = (f16_t *)(ws + p.off_xt[1]), *g = (f16_t *)(ws + p.off_g), *q = (f16_t *)(ws + p.off_p);
     const int64_t S = SPLIT ? 2 : 1, nm = (int64_t)p.np * p.mp * S, nn = (int64_t)p.np * p.np * S;
-    k_muon_scale<SPLIT><<<dim3((unsigned)(p.mp / 64), (unsigned)(p.np / 64), (unsigned)p.batch), 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
+    const dim3 grid((unsigned)(p.mp / 64), (unsigned)(p.np / 64), (unsigned)p.batch);
+    if (in.type == PS_F32) k_muon_scale<float, SPLIT><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
+    else if (in.type == PS_BF16) k_muon_scale<bf16_t, SPLIT><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
+    else k_muon_scale<f16_t, SPLIT><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
     PS_HIP(ps, hipGetLastError());
     for (int s = 0; s < steps; ++s) {
         MuonArgs a{};
