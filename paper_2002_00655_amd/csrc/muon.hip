@@ -33,6 +33,17 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Two numbers as high and low parts, each rounded to the nearest: two conversions, and two fused subtractions, which are exact
+typedef f16_t half2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+struct Parts { half2 hi, lo; };
+template <bool SPLIT> __device__ __forceinline__ Parts parts_of(float a, float b) {
+    Parts p;
+    p.hi = __builtin_convertvector(floatx2{a, b}, half2);
+    if constexpr (SPLIT) p.lo = __builtin_convertvector(floatx2{__builtin_fmaf((float)p.hi[0], -1.0f, a), __builtin_fmaf((float)p.hi[1], -1.0f, b)}, half2);
+    return p;
+}
+
 // A matrix in scratch lies as the matrix instruction takes it: 32 rows and 16 numbers of each are a block, in which lane l of a wavefront
 // finds its eight numbers, of row l % 32 from number 8 (l / 32) on, at 16 l bytes (SPLIT: the 64 lanes' high parts, then their
 // low parts); the blocks of the same rows follow one another.  So operands come into registers in whole lines, and never see LDS.
@@ -104,20 +115,37 @@ __global__ __launch_bounds__(256) void k_muon_norm(MuonIn a, uint32_t P, double 
     if (threadIdx.x == 0) a.squares[(int64_t)blockIdx.y * NORM_BLOCKS + blockIdx.x] = s;
 }
 
-// What a matrix's numbers are multiplied by to become X_0, scaled, in 64 bits: neither a norm above the largest 32-bit number nor one near the smallest
-// loses anything.  An infinity or NaN anywhere in the matrix makes all of X NaN, as the division and the products would.
-__device__ __forceinline__ double scale_of(double square, float eps) {
-    return square <= 1.7e308 ? (double)X_SCALE / (sqrt(square) + (double)eps) : __builtin_nan("");
-}
+// A matrix's numbers become X_0, scaled.  In 64 bits where the sum of squares is far from 1, so that neither a norm above the largest 32-bit number nor
+// one near the smallest loses anything (everywhere, 3 of the 49 us of 16 matrices of 100 x 100).  An infinity or NaN anywhere in the matrix makes all of X
+// NaN, as the division and the products would.
+struct Scale {
+    bool usual;
+    float f;
+    double wide;
+    __device__ __forceinline__ Scale(double square, float eps) : usual(square >= 1e-30 && square <= 1e30), f(0.0f), wide(0.0) {
+        if (usual) f = X_SCALE / (sqrtf((float)square) + eps);
+        else wide = square <= 1.7e308 ? (double)X_SCALE / (sqrt(square) + (double)eps) : __builtin_nan("");
+    }
+    template <int N> __device__ __forceinline__ void apply(float (&v)[N]) const {
+        if (usual) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = (float)((double)v[i] * wide);
+        }
+    }
+};
 
 // X_0 both ways, zero where the padded matrices go on.
 template <bool SPLIT>
 __device__ __forceinline__ void put8(f16_t *to, int r, int k, int K, const float (&v)[8]) {
     half8 hi, lo;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        hi[i] = (f16_t)v[i];
-        lo[i] = (f16_t)(v[i] - (float)hi[i]);
+    for (int i = 0; i < 8; i += 2) {
+        const Parts p = parts_of<SPLIT>(v[i], v[i + 1]);
+        hi[i] = p.hi[0]; hi[i + 1] = p.hi[1];
+        if constexpr (SPLIT) { lo[i] = p.lo[0]; lo[i + 1] = p.lo[1]; }
     }
     f16_t *p = to + place8<SPLIT>(r, k, K);
     *reinterpret_cast<half8 *>(p) = hi;
@@ -137,11 +165,10 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
         v[u] = r < a.rows && c0 < a.cols ? (float)reinterpret_cast<const T *>(a.in)[(b * a.rows + r) * a.ld + c0] : 0.0f;
     }
     const double square = sum_of_256((int)threadIdx.x < a.blocks ? a.squares[b * NORM_BLOCKS + threadIdx.x] : 0.0);
-    const double f = scale_of(square, a.eps);
+    Scale(square, a.eps).apply(v);
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
-        const float y = (float)(f * (double)v[u]);
-        if (tall) tile[lane][wave + 4 * u] = y; else tile[wave + 4 * u][lane] = y;
+        if (tall) tile[lane][wave + 4 * u] = v[u]; else tile[wave + 4 * u][lane] = v[u];
     }
     __syncthreads();
     x += b * (int64_t)np * mp * (SPLIT ? 2 : 1);
@@ -609,29 +636,16 @@ __global__ __launch_bounds__(256) void k_muon_join(MuonArgs a, int32_t shares) {
 // What several launches per step cost - 5 us each for a few microseconds of products - is what this saves.
 constexpr int ONE_SIDE = 128, ONE_THREADS = 512;
 
-// The 4 x 4 numbers of four lanes transposed: v[e] of lane q becomes v[q] of lane e.
-__device__ __forceinline__ void turn_quad(uint32_t (&v)[4]) {
-    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
-    const auto from = [](uint32_t x, auto perm) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(perm)::value, 0xf, 0xf, true); };
+// The 4 x 4 numbers of 16 bits of four lanes transposed: rows 0, 1 and rows 2, 3 of a lane's column become, of lane q, row q of the four columns.
+__device__ __forceinline__ void turn_quad(uint32_t &r01, uint32_t &r23) {
+    const auto other = [](uint32_t x, auto perm) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(perm)::value, 0xf, 0xf, true); };
     const std::integral_constant<int, 0xB1> by_one{};                         // lanes 1 0 3 2
     const std::integral_constant<int, 0x4E> by_two{};                         // lanes 2 3 0 1
-#pragma unroll
-    for (int e = 0; e < 4; e += 2) {
-        const uint32_t got = from(odd ? v[e] : v[e + 1], by_one);
-        v[e] = odd ? got : v[e];
-        v[e + 1] = odd ? v[e + 1] : got;
-    }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const uint32_t got = from(high ? v[e] : v[e + 2], by_two);
-        v[e] = high ? got : v[e];
-        v[e + 2] = high ? v[e + 2] : got;
-    }
-}
-// high part in the lower half, low part in the upper one
-__device__ __forceinline__ uint32_t parts_of(float v) {
-    const f16_t hi = (f16_t)v, lo = (f16_t)(v - (float)hi);
-    return (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
+    const bool high = threadIdx.x & 2;
+    const uint32_t got = other(high ? r01 : r23, by_two), a0 = high ? got : r01, a1 = high ? r23 : got;    // of columns q % 2 and q % 2 + 2
+    const uint32_t select = threadIdx.x & 1 ? 0x03020706u : 0x05040100u;
+    r01 = __builtin_amdgcn_perm(other(a0, by_one), a0, select);
+    r23 = __builtin_amdgcn_perm(other(a1, by_one), a1, select);
 }
 
 struct MuonOne { MuonIn in; MuonArgs out; int32_t n, m, nq, mq, steps; };     // nq, mq: the frame
@@ -650,7 +664,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
     const MuonIn &in = a.in;
     // piece f, sum e: row i0 + 32 f + 8 (e / 4) + 4 h + e % 4, column j0 + l32 of X
     const auto row_of = [&](int f, int e) { return i0 + 32 * f + 8 * (e >> 2) + 4 * h + (e & 3); };
-    floatx16 x[2];
+    float v0[32];
     double s = 0.0;
 #pragma unroll
     for (int f = 0; f < 2; ++f)
@@ -668,7 +682,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
                     v = in.nesterov ? v + in.mu * moment : moment;
                 }
             }
-            x[f][e] = v;
+            v0[f * 16 + e] = v;
             s += (double)v * (double)v;
         }
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
@@ -677,44 +691,46 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
     s = 0.0;
 #pragma unroll
     for (int w = 0; w < ONE_THREADS / 64; ++w) s += squares[w];
-    const double scale = scale_of(s, in.eps);
+    Scale(s, in.eps).apply(v0);                                               // (zero outside the matrix, or all NaN)
+    floatx16 x[2];
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[f][e] = (float)((double)x[f][e] * scale);      // (zero outside the matrix, or all NaN)
+    for (int i = 0; i < 32; ++i) x[i >> 4][i & 15] = v0[i];
 
-    // the numbers v, rows and columns exchanged, into m of K numbers a row; the same as they are
-    const auto put_columns = [&](f16_t *m, int K, const floatx16 (&v)[2]) {
+    // the numbers as parts: pair (f, 2 g + e): rows 4 g + 2 e and the next one of piece f
+    const auto split = [&](Parts (&q)[2][8], const floatx16 (&v)[2], float factor) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[f][e] = parts_of<SPLIT>(v[f][2 * e] * factor, v[f][2 * e + 1] * factor);
+    };
+    // into m of K numbers a row: rows and columns exchanged, four rows' numbers are neighbours; and as they are
+    const auto put_columns = [&](f16_t *m, int K, const Parts (&q)[2][8]) {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int i = row_of(f, 4 * g), j = j0 + l32;
-                half4 hi, lo;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    hi[e] = (f16_t)v[f][4 * g + e];
-                    lo[e] = (f16_t)(v[f][4 * g + e] - (float)hi[e]);
-                }
                 f16_t *p = m + place8<SPLIT>(j, i & ~7, K) + (i & 4);
-                *reinterpret_cast<half4 *>(p) = hi;
-                if constexpr (SPLIT) *reinterpret_cast<half4 *>(p + 512) = lo;
+                *reinterpret_cast<half4 *>(p) = __builtin_shufflevector(q[f][2 * g].hi, q[f][2 * g + 1].hi, 0, 1, 2, 3);
+                if constexpr (SPLIT) *reinterpret_cast<half4 *>(p + 512) = __builtin_shufflevector(q[f][2 * g].lo, q[f][2 * g + 1].lo, 0, 1, 2, 3);
             }
     };
-    const auto put_rows = [&](f16_t *m, int K, const floatx16 (&v)[2]) {
+    const auto put_rows = [&](f16_t *m, int K, const Parts (&q)[2][8]) {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                uint32_t q[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) q[e] = parts_of(v[f][4 * g + e]);
-                turn_quad(q);
                 const int i = row_of(f, 4 * g) + (lane & 3), j = j0 + (l32 & ~3);
                 f16_t *p = m + place8<SPLIT>(i, j & ~7, K) + (j & 4);
-                uint32_t *hi = reinterpret_cast<uint32_t *>(p), *lo = reinterpret_cast<uint32_t *>(p + 512);
-                *reinterpret_cast<uint2 *>(hi) = uint2{(q[0] & 0xffffu) | q[1] << 16, (q[2] & 0xffffu) | q[3] << 16};
-                if constexpr (SPLIT) *reinterpret_cast<uint2 *>(lo) = uint2{q[0] >> 16 | (q[1] & 0xffff0000u), q[2] >> 16 | (q[3] & 0xffff0000u)};
+                uint32_t a = __builtin_bit_cast(uint32_t, q[f][2 * g].hi), b = __builtin_bit_cast(uint32_t, q[f][2 * g + 1].hi);
+                turn_quad(a, b);
+                *reinterpret_cast<uint2 *>(p) = uint2{a, b};
+                if constexpr (SPLIT) {
+                    a = __builtin_bit_cast(uint32_t, q[f][2 * g].lo);
+                    b = __builtin_bit_cast(uint32_t, q[f][2 * g + 1].lo);
+                    turn_quad(a, b);
+                    *reinterpret_cast<uint2 *>(p + 512) = uint2{a, b};
+                }
             }
     };
     // this wavefront's sums over the first `used` blocks of k, of rows of K numbers of l and r
@@ -738,17 +754,22 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
         }
     };
     const int used_n = (a.n + 15) >> 4, used_m = (a.m + 15) >> 4;
+    float x_factor = 1.0f;                                                    // x holds this times the scaled X
     for (int step = 0; step < a.steps; ++step) {
         floatx16 g[2], q[2];
-        if (has_x) put_rows(r1, mq, x);
+        Parts parts[2][8], more[2][8];
+        if (has_x) {
+            split(parts, x, x_factor);
+            put_rows(r1, mq, parts);
+        }
         __syncthreads();
         if (has_a) {
             product(r1, r1, mq, used_m, g);
-            for (floatx16 &v : g) v *= G_SCALE / (X_SCALE * X_SCALE);
-            put_columns(r2, nq, g);                                           // (A is symmetric)
+            split(more, g, G_SCALE / (X_SCALE * X_SCALE));
+            put_columns(r2, nq, more);                                        // (A is symmetric)
         }
         __syncthreads();
-        if (has_x) put_columns(r1, nq, x);
+        if (has_x) put_columns(r1, nq, parts);
         if (has_a) product(r2, r2, nq, used_n, q);
         __syncthreads();
         if (has_a) {
@@ -756,14 +777,14 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
             for (int f = 0; f < 2; ++f)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    q[f][e] = q[f][e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g[f][e] * (NS_B * P_SCALE / G_SCALE) + (row_of(f, e) == j0 + l32 ? NS_A * P_SCALE : 0.0f);
-            put_columns(r2, nq, q);
+                    q[f][e] = q[f][e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) +
+                              (g[f][e] * (NS_B * P_SCALE / (X_SCALE * X_SCALE)) + (row_of(f, e) == j0 + l32 ? NS_A * P_SCALE : 0.0f));
+            split(more, q, 1.0f);
+            put_columns(r2, nq, more);
         }
         __syncthreads();
-        if (has_x) {
-            product(r2, r1, nq, used_n, x);
-            for (floatx16 &v : x) v *= 1.0f / P_SCALE;
-        }
+        if (has_x) product(r2, r1, nq, used_n, x);
+        x_factor = 1.0f / P_SCALE;
         __syncthreads();
     }
 #pragma unroll
@@ -772,7 +793,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
         for (int e = 0; e < 16; ++e) {
             const int i = row_of(f, e), j = j0 + l32;
             if (i < a.n && j < a.m) {
-                const float v = x[f][e] * (1.0f / X_SCALE);
+                const float v = x[f][e] * (x_factor / X_SCALE);
                 const int64_t row = row0 + (tall ? j : i), col = tall ? i : j;
                 if constexpr (STEP) {
                     float *w = a.out.val + (a.out.first + row) * a.out.L + col;
