@@ -6,9 +6,13 @@
 // was very small.
 //
 // All products are of fp16 numbers on the matrix cores with sums in 32 bits.  Numbers are held
-//   SPLIT    as the sum of two fp16 numbers, high + low: 22 bits and a sign each way, an error of 2^-24 of the number, so what a float has;
-//            a product is high high + high low + low high (what is left out is 2^-24 of it): three instructions;
-//   single   as one fp16 number, where the result is rounded to bf16: an error of 2^-12, an eighth of what that rounding costs.
+//   as pairs   the sum of two fp16 numbers, high + low: 11 bits each and a sign between them, an error of 2^-23 of the number at most;
+//              a product is high high + high low + low high (what is left out is 2^-22 of it at most, 2^-24 as a rule): three instructions;
+//   single     as one fp16 number: an error of 2^-11 at most, an eighth of what rounding to bf16 costs.
+// Pairs throughout for results of 32 bits and of fp16, and where one launch does it all.  Of other bf16 results all numbers are single, except X where the
+// first two steps multiply it by P: there an error of X goes into all directions alike, and the steps raise the weak ones by 3.4 each.
+// Matrices with a few strong directions are off by 0.008 of their norm without that, 0.002 with it (the rounding of the result: 0.0017); pairs in
+// the other products, or in later steps, change less than 0.0003.  It costs two instructions instead of one in two of fifteen products: 4096 x 4096 twice 3.32 ms instead of 2.84.
 // fp16 holds few magnitudes, so every number is scaled by a power of two: the spectral norms of X, A and P are at most 1.21,
 // 1.46 and 3.45 whatever D is (p of [0, 1.21] stays below 1.21), and so is every element; scaled they fill the
 // upper end of the type, and what is lost at the lower end is 2^-39 of the norm or less.
@@ -37,19 +41,19 @@ inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 typedef f16_t half2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 struct Parts { half2 hi, lo; };
-template <bool SPLIT> __device__ __forceinline__ Parts parts_of(float a, float b) {
+template <bool PAIR> __device__ __forceinline__ Parts parts_of(float a, float b) {
     Parts p;
     p.hi = __builtin_convertvector(floatx2{a, b}, half2);
-    if constexpr (SPLIT) p.lo = __builtin_convertvector(floatx2{__builtin_fmaf((float)p.hi[0], -1.0f, a), __builtin_fmaf((float)p.hi[1], -1.0f, b)}, half2);
+    if constexpr (PAIR) p.lo = __builtin_convertvector(floatx2{__builtin_fmaf((float)p.hi[0], -1.0f, a), __builtin_fmaf((float)p.hi[1], -1.0f, b)}, half2);
     return p;
 }
 
 // A matrix in scratch lies as the matrix instruction takes it: 32 rows and 16 numbers of each are a block, in which lane l of a wavefront
-// finds its eight numbers, of row l % 32 from number 8 (l / 32) on, at 16 l bytes (SPLIT: the 64 lanes' high parts, then their
+// finds its eight numbers, of row l % 32 from number 8 (l / 32) on, at 16 l bytes (pairs: the 64 lanes' high parts, then their
 // low parts); the blocks of the same rows follow one another.  So operands come into registers in whole lines, and never see LDS.
 // The eight numbers of row r from k on (k a multiple of 8), K numbers a row:
-template <bool SPLIT> __device__ __forceinline__ int64_t place8(int r, int k, int K) {
-    return ((int64_t)(r >> 5) * (K >> 4) + (k >> 4)) * (SPLIT ? 1024 : 512) + ((k & 8) * 4 + (r & 31)) * 8;
+template <bool PAIR> __device__ __forceinline__ int64_t place8(int r, int k, int K) {
+    return ((int64_t)(r >> 5) * (K >> 4) + (k >> 4)) * (PAIR ? 1024 : 512) + ((k & 8) * 4 + (r & 31)) * 8;
 }
 
 // ---- the norm, and the momentum -------------------------------------------------------------------------------------
@@ -138,20 +142,21 @@ struct Scale {
 };
 
 // X_0 both ways, zero where the padded matrices go on.
-template <bool SPLIT>
+template <bool PAIR>
 __device__ __forceinline__ void put8(f16_t *to, int r, int k, int K, const float (&v)[8]) {
     half8 hi, lo;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-        const Parts p = parts_of<SPLIT>(v[i], v[i + 1]);
+        const Parts p = parts_of<PAIR>(v[i], v[i + 1]);
         hi[i] = p.hi[0]; hi[i + 1] = p.hi[1];
-        if constexpr (SPLIT) { lo[i] = p.lo[0]; lo[i + 1] = p.lo[1]; }
+        if constexpr (PAIR) { lo[i] = p.lo[0]; lo[i + 1] = p.lo[1]; }
     }
-    f16_t *p = to + place8<SPLIT>(r, k, K);
+    f16_t *p = to + place8<PAIR>(r, k, K);
     *reinterpret_cast<half8 *>(p) = hi;
-    if constexpr (SPLIT) *reinterpret_cast<half8 *>(p + 512) = lo;
+    if constexpr (PAIR) *reinterpret_cast<half8 *>(p + 512) = lo;
 }
-template <class T, bool SPLIT>
+// PAIR: X as pairs, as X transposed always is
+template <class T, bool PAIR>
 __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np, int mp, f16_t *x, f16_t *xt) {
     __shared__ float tile[64][65];
     const int64_t b = blockIdx.z;
@@ -171,16 +176,16 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
         if (tall) tile[lane][wave + 4 * u] = v[u]; else tile[wave + 4 * u][lane] = v[u];
     }
     __syncthreads();
-    x += b * (int64_t)np * mp * (SPLIT ? 2 : 1);
-    xt += b * (int64_t)np * mp * (SPLIT ? 2 : 1);
+    x += b * (int64_t)np * mp * (PAIR ? 2 : 1);
+    xt += b * (int64_t)np * mp * 2;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int r = u * 32 + (lane & 31), k = wave * 16 + (lane >> 5) * 8;
         float y[8], w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) { y[i] = tile[r][k + i]; w[i] = tile[k + i][r]; }
-        put8<SPLIT>(x, i0 + r, j0 + k, mp, y);
-        put8<SPLIT>(xt, j0 + r, i0 + k, np, w);
+        put8<PAIR>(x, i0 + r, j0 + k, mp, y);
+        put8<true>(xt, j0 + r, i0 + k, np, w);
     }
 }
 
@@ -188,26 +193,31 @@ __global__ __launch_bounds__(256) void k_muon_scale(MuonIn a, bool tall, int np,
 constexpr int GJ = 4;                            // columns of a band
 constexpr uint32_t DIES = 8;                     // compute dies, each with a cache of its own
 constexpr int CHAIN = 12;                        // blocks of k whose products one chain of matrix instructions adds (a multiple of DEPTH and KB)
+// The numbers of the left and the right operand: single ones, or pairs in the right one, or in both.
+enum MuonKind { SINGLE, RIGHT_SPLIT, SPLIT };
+constexpr int left_parts(int kind) { return kind == SPLIT ? 2 : 1; }
+constexpr int right_parts(int kind) { return kind == SINGLE ? 1 : 2; }
+constexpr int products_of(int kind) { return left_parts(kind) + right_parts(kind) - 1; }
 enum MuonProduct { MUON_GRAM, MUON_POLY, MUON_APPLY, MUON_LAST, MUON_STEP };       // LAST, STEP: APPLY with the result put where it belongs
 struct MuonArgs {
     const f16_t *lhs, *rhs;                      // rows of K numbers
-    int64_t lhs_size, rhs_size, out_size;        // of one matrix, in elements as they are stored
+    int64_t lhs_size, rhs_size, out_size, out_t_size;   // of one matrix, in elements as they are stored
     int32_t K, tiles_i, tiles_j, tiles, tile0;   // tiles: of one matrix; tile0: the first one of the launch
     int32_t shares; float *part;                 // workgroups that share a tile's sum over k, and where they put their sums
     f16_t *out; int32_t out_ld;                  // GRAM: A, POLY: P, APPLY: X
-    f16_t *out_t; int32_t out_t_ld;              // APPLY: X transposed
+    f16_t *out_t; int32_t out_t_ld, out_t_pair;  // APPLY: X transposed; out_t_pair: as pairs, for RIGHT_SPLIT
     // LAST: the result
     void *to; int64_t to_ld; int32_t to_type, to_vec, tall, n, m;   // to_vec: eight numbers of a row can be written together
     float *val; int64_t L, first; float keep, step;    // of a step: W <- keep W - step X
 };
 
-template <bool SPLIT> __device__ __forceinline__ void get8(const f16_t *m, int r, int k, int K, float (&v)[8]) {
-    const f16_t *p = m + place8<SPLIT>(r, k, K);
+template <bool PAIR> __device__ __forceinline__ void get8(const f16_t *m, int r, int k, int K, float (&v)[8]) {
+    const f16_t *p = m + place8<PAIR>(r, k, K);
     const half8 hi = *reinterpret_cast<const half8 *>(p);
     half8 lo = {};
-    if constexpr (SPLIT) lo = *reinterpret_cast<const half8 *>(p + 512);
+    if constexpr (PAIR) lo = *reinterpret_cast<const half8 *>(p + 512);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = SPLIT ? (float)hi[e] + (float)lo[e] : (float)hi[e];
+    for (int e = 0; e < 8; ++e) v[e] = PAIR ? (float)hi[e] + (float)lo[e] : (float)hi[e];
 }
 // Eight neighbouring numbers of a row of the result, of which `left` are its: what is there already (of a step), and what is written.
 __device__ __forceinline__ void get_weights(const MuonArgs &a, int64_t row, int col, float (&w)[8], int left) {
@@ -278,7 +288,7 @@ __device__ __forceinline__ Place place_of(const MuonArgs &a, uint32_t block, uin
 // lines.  SUMS_LD: a row of 64 sums there: 32 rows' pieces of 16 bytes lie in all banks.
 constexpr int SUMS_LD = 68;
 // From LDS, where KS wavefronts have put their shares of the sums, to where they belong: rows gi .., columns gj .. of matrix p.b.  group: of the KS wavefronts.
-template <int KS, bool SPLIT, int MODE>
+template <int KS, int KIND, int MODE>
 __device__ __forceinline__ void write_tile(const MuonArgs &a, const Place &p, int gi, int gj, const float *sums, int group) {
     constexpr float FACTOR = MODE == MUON_GRAM ? G_SCALE / (X_SCALE * X_SCALE) : MODE == MUON_APPLY ? 1.0f / P_SCALE : MODE >= MUON_LAST ? 1.0f / (P_SCALE * X_SCALE) : 1.0f;
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
@@ -326,20 +336,22 @@ __device__ __forceinline__ void write_tile(const MuonArgs &a, const Place &p, in
                             const int R = (way ? gj : gi) + r, C = (way ? gi : gj) + c;
                             if constexpr (MODE == MUON_POLY) {                    // (A is symmetric: it is read as the result is written)
                                 float g[8];
-                                get8<SPLIT>(a.lhs + p.b * a.lhs_size, R, C, a.K, g);
+                                get8<KIND == SPLIT>(a.lhs + p.b * a.lhs_size, R, C, a.K, g);
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
                                     v[e] = v[e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + g[e] * (NS_B * P_SCALE / G_SCALE) + (R == C + e ? NS_A * P_SCALE : 0.0f);
                             }
-                            if (MODE == MUON_APPLY && way) put8<SPLIT>(a.out_t + p.b * a.out_size, R, C, a.out_t_ld, v);
-                            else put8<SPLIT>(a.out + p.b * a.out_size, R, C, a.out_ld, v);
+                            f16_t *const to = MODE == MUON_APPLY && way ? a.out_t + p.b * a.out_t_size : a.out + p.b * a.out_size;
+                            const int ld = MODE == MUON_APPLY && way ? a.out_t_ld : a.out_ld;
+                            if (KIND == RIGHT_SPLIT && way && a.out_t_pair) put8<true>(to, R, C, ld, v);
+                            else put8<KIND == SPLIT>(to, R, C, ld, v);
                         }
                     }
                 }
 }
 // The numbers of the matrix instruction: x has 32 x 32 pieces, of which a lane has column lane % 32, rows 8 g + 4 (lane / 32) + 0..3 for
 // g = 0..3; from row i0, column j0 on.  mine: where this wavefront puts them, sums: the first one's place.
-template <int FI, int FJ, int KS, bool SPLIT, int MODE>
+template <int FI, int FJ, int KS, int KIND, int MODE>
 __device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, const floatx16 (&x)[FI][FJ], int i0, int j0, float *mine, const float *sums, int group) {
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
     const bool turned = MODE >= MUON_LAST && a.tall;                           // X is the transposed matrix
@@ -363,37 +375,38 @@ __device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, cons
                 }
             if constexpr (KS > 1) __syncthreads();
             else asm volatile("" ::: "memory");                                // (a wavefront's accesses to LDS stay in order)
-            write_tile<KS, SPLIT, MODE>(a, p, i0 + si * 64, j0 + sj * 64, sums, group);
+            write_tile<KS, KIND, MODE>(a, p, i0 + si * 64, j0 + sj * 64, sums, group);
             asm volatile("" ::: "memory");
         }
 }
 
 // The sums of a wavefront: C[i][j] += sum_k L[i][k] R[j][k], 32 x 32 pieces (v_mfma_f32_32x32x16_f16).
 // The matrix instruction does not round its sums to the nearest: a chain of them loses up to a unit in the last place at each link, always the
-// same way.  (One row of 5,000 in a chain of 313: an error of 72 units of 2^-24.)  So with numbers of 24 bits the chains are cut, and their sums
+// same way.  (One row of 5,000 in a chain of 313: an error of 72 units of 2^-24.)  So with pairs the chains are cut, and their sums
 // added by ordinary additions.
-template <int FI, int FJ, bool SPLIT> struct Sums {
-    floatx16 acc[FI][FJ], total[SPLIT ? FI : 1][SPLIT ? FJ : 1];
+template <int FI, int FJ, int KIND> struct Sums {
+    static constexpr int L = left_parts(KIND), R = right_parts(KIND);
+    floatx16 acc[FI][FJ], total[KIND == SPLIT ? FI : 1][KIND == SPLIT ? FJ : 1];
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
             for (int j = 0; j < FJ; ++j) {
                 acc[i][j] = floatx16{};
-                if constexpr (SPLIT) total[i][j] = floatx16{};
+                if constexpr (KIND == SPLIT) total[i][j] = floatx16{};
             }
     }
-    template <int S> __device__ __forceinline__ void add(const half8 (&l)[FI][S], const half8 (&r)[FJ][S]) {
+    __device__ __forceinline__ void add(const half8 (&l)[FI][L], const half8 (&r)[FJ][R]) {
 #pragma unroll
-        for (int e = SPLIT ? 2 : 0; e >= 0; --e)                              // low high, high low, high high
+        for (int e = products_of(KIND) - 1; e >= 0; --e)                      // low high and high low, as there are parts, then high high
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
                 for (int j = 0; j < FJ; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][e == 2 ? S - 1 : 0], r[j][e == 1 ? S - 1 : 0], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[i][e == 2 ? L - 1 : 0], r[j][e == 1 ? R - 1 : 0], acc[i][j], 0, 0, 0);
     }
     __device__ __forceinline__ void cut() {
-        if constexpr (SPLIT) {
+        if constexpr (KIND == SPLIT) {
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
@@ -401,35 +414,34 @@ template <int FI, int FJ, bool SPLIT> struct Sums {
         }
     }
     __device__ __forceinline__ const floatx16 (&all() const)[FI][FJ] {
-        if constexpr (SPLIT) return total;
+        if constexpr (KIND == SPLIT) return total;
         else return acc;
     }
 };
 
 // Few or small tiles: 64 x 64 per workgroup, and its four wavefronts share the sum over k, a block in turn.  Operands come straight
 // from memory, DEPTH blocks ahead; nobody waits for anybody before the end.
-template <bool SPLIT, int MODE>
+template <int KIND, int MODE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_muon_small(MuonArgs a, const int32_t *err) {
-    constexpr int KS = 4, S = SPLIT ? 2 : 1, DEPTH = SPLIT ? 3 : 4;
+    constexpr int KS = 4, L = left_parts(KIND), R = right_parts(KIND), DEPTH = KIND == SPLIT ? 3 : 4;
     __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];
     const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const Place p = place_of<MODE>(a, blockIdx.x, gridDim.x);
     const int i0 = p.ti * 64, j0 = p.tj * 64, blocks = a.K >> 4, turns = blocks / KS;             // (sides are multiples of 64)
     const int first = turns * p.share / a.shares, cnt = turns * (p.share + 1) / a.shares - first, block0 = first * KS + group;
-    const f16_t *l = a.lhs + p.b * a.lhs_size + ((int64_t)(i0 >> 5) * blocks + block0) * (512 * S), *r = a.rhs + p.b * a.rhs_size + ((int64_t)(j0 >> 5) * blocks + block0) * (512 * S);
-    const int64_t next_rows = (int64_t)blocks * (512 * S);
-    half8 lf[DEPTH][2][S], rf[DEPTH][2][S];
-    const auto load = [&](half8 (&x)[2][S], half8 (&y)[2][S], int t) {
-        const int64_t off = (int64_t)t * (KS * 512 * S);
+    const f16_t *l = a.lhs + p.b * a.lhs_size + ((int64_t)(i0 >> 5) * blocks + block0) * (512 * L), *r = a.rhs + p.b * a.rhs_size + ((int64_t)(j0 >> 5) * blocks + block0) * (512 * R);
+    const int64_t rows32 = (int64_t)blocks * 512;                              // elements to the next 32 rows, of a part
+    half8 lf[DEPTH][2][L], rf[DEPTH][2][R];
+    const auto load = [&](half8 (&x)[2][L], half8 (&y)[2][R], int t) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int f = 0; f < 2; ++f) {
 #pragma unroll
-            for (int e = 0; e < S; ++e) {
-                x[f][e] = *reinterpret_cast<const half8 *>(l + off + f * next_rows + e * 512 + lane * 8);
-                y[f][e] = *reinterpret_cast<const half8 *>(r + off + f * next_rows + e * 512 + lane * 8);
-            }
+            for (int e = 0; e < L; ++e) x[f][e] = *reinterpret_cast<const half8 *>(l + (int64_t)t * (KS * 512 * L) + f * (rows32 * L) + e * 512 + lane * 8);
+#pragma unroll
+            for (int e = 0; e < R; ++e) y[f][e] = *reinterpret_cast<const half8 *>(r + (int64_t)t * (KS * 512 * R) + f * (rows32 * R) + e * 512 + lane * 8);
+        }
     };
-    Sums<2, 2, SPLIT> s;
+    Sums<2, 2, KIND> s;
     s.clear();
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d)
@@ -468,11 +480,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
         return;
     }
-    put_tile<2, 2, KS, SPLIT, MODE>(a, p, s.all(), i0, j0, lds[group], lds[0], group);
+    put_tile<2, 2, KS, KIND, MODE>(a, p, s.all(), i0, j0, lds[group], lds[0], group);
 }
 
 // The shares of a small tile's sums added: each wavefront every fourth share, and then the four.
-template <bool SPLIT>
+template <int KIND>
 __global__ __launch_bounds__(256) void k_muon_join_small(MuonArgs a, int32_t shares) {
     constexpr int KS = 4;
     __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];
@@ -489,7 +501,7 @@ __global__ __launch_bounds__(256) void k_muon_join_small(MuonArgs a, int32_t sha
 #pragma unroll
     for (int q = 0; q < 16; ++q) *reinterpret_cast<floatx4 *>(&lds[group][(q * 4 + (lane >> 4)) * SUMS_LD + (lane & 15) * 4]) = x[q];
     __syncthreads();
-    write_tile<KS, SPLIT, MUON_GRAM>(a, p, p.ti * 64, p.tj * 64, lds[0], group);
+    write_tile<KS, KIND, MUON_GRAM>(a, p, p.ti * 64, p.tj * 64, lds[0], group);
 }
 
 // until at most N of this wavefront's loads are on their way and all it has asked of LDS is there, then until all wavefronts are so far
@@ -510,51 +522,57 @@ template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinlin
     if constexpr (I + 1 < PRODUCTS) interleave<PRODUCTS, READS, LOADS, I + 1>();
 }
 
-// Larger ones: 64 FI x 64 FJ per workgroup, a quarter per wavefront, operands by way of LDS, so that a line is read from the die's cache by
+// Larger ones: 64 FI x 64 FI per workgroup, a quarter per wavefront, operands by way of LDS, so that a line is read from the die's cache by
 // one wavefront and used by two.  A stage has KB blocks of k; STAGES of them are in LDS or on their way there, straight from memory.  A wavefront
 // asks for the next block's operands before it multiplies the ones it has, also across the meeting of the wavefronts at which a
 // stage is given up and the next one is known to be there.
-template <int FI, int FJ, int KB, int STAGES, bool SPLIT, int MODE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu((FI + FJ) * KB * (SPLIT ? 2 : 1) <= 8 ? 2 : 1))) void k_muon_large(MuonArgs a, const int32_t *err) {
-    constexpr int S = SPLIT ? 2 : 1, TI = 64 * FI, TJ = 64 * FJ, U = KB == 1 ? 2 : KB, PER = KB * S, PIECES = (2 * FI + 2 * FJ) * PER, MINE = PIECES / 4, STAGE = PIECES * 1024;
-    static_assert(STAGES >= 3 && U % 2 == 0 && PIECES % 4 == 0 && MINE % KB == 0 && (2 * FI * PER) % MINE == 0 && MINE % PER == 0, "a wavefront's pieces are whole rows of one operand");
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+constexpr int stage_pieces(int FI, int KB, int kind) { return 2 * FI * KB * (left_parts(kind) + right_parts(kind)); }   // of 1,024 bytes
+template <int FI, int KB, int STAGES, int KIND, int MODE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(STAGES * stage_pieces(FI, KB, KIND) <= 80 ? 2 : 1))) void k_muon_large(MuonArgs a, const int32_t *err) {
+    constexpr int L = left_parts(KIND), R = right_parts(KIND), T = 64 * FI, U = KB == 1 ? 2 : KB, OWN = FI / 2;
+    constexpr int PER_L = KB * L, PER_R = KB * R, ML = OWN * PER_L, MR = OWN * PER_R, MINE = ML + MR, RIGHT = 4 * ML, STAGE = 4 * MINE * 1024;
+    static_assert(STAGES >= 3 && U % 2 == 0 && FI % 2 == 0);
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
+    unsigned char *const lds = lds_bytes;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const Place p = place_of<MODE>(a, blockIdx.x, gridDim.x);
     const int blocks = a.K >> 4, turns = blocks / U, first = (int)((int64_t)turns * p.share / a.shares), cnt = (int)((int64_t)turns * (p.share + 1) / a.shares) - first;
-    // what this wavefront fetches of a stage: pieces of 1,024 bytes, PER of a block of rows
-    const char *from[MINE / PER];
+    // A stage in LDS: of each operand's 2 FI times 32 rows, KB blocks with their parts, 1,024 bytes each.  This wavefront fetches those of OWN times 32 rows
+    // of either operand.
+    const char *left[OWN], *right[OWN];
 #pragma unroll
-    for (int i = 0; i < MINE / PER; ++i) {
-        const int rows = wave * (MINE / PER) + i;                             // block of 32 rows: first the left operand's 2 FI, then the right one's
-        const f16_t *m = rows < 2 * FI ? a.lhs + p.b * a.lhs_size + (int64_t)(p.ti * (2 * FI) + rows) * blocks * (512 * S)
-                                       : a.rhs + p.b * a.rhs_size + (int64_t)(p.tj * (2 * FJ) + rows - 2 * FI) * blocks * (512 * S);
-        from[i] = reinterpret_cast<const char *>(m) + (int64_t)first * (U * S * 1024);
+    for (int i = 0; i < OWN; ++i) {
+        const int rows = wave * OWN + i;
+        left[i] = reinterpret_cast<const char *>(a.lhs + p.b * a.lhs_size + ((int64_t)(p.ti * (2 * FI) + rows) * blocks + first * U) * (512 * L));
+        right[i] = reinterpret_cast<const char *>(a.rhs + p.b * a.rhs_size + ((int64_t)(p.tj * (2 * FI) + rows) * blocks + first * U) * (512 * R));
     }
     const uint32_t lane16 = lane * 16;
     const int last = cnt * (U / KB) - 1;
     // a KB-th of stage t, into its slot; behind the last stage that one once more, into a slot that nobody reads, so that all turns are alike
     const auto fetch = [&](int slot, int t, int kb) {
-        const int64_t off = (int64_t)(t < last ? t : last) * (PER * 1024);
+        const int64_t at = t < last ? t : last;
 #pragma unroll
-        for (int i = kb * MINE / KB; i < (kb + 1) * MINE / KB; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from[i / PER] + off + (i % PER) * 1024 + lane16),
-                                             (__attribute__((address_space(3))) void *)(lds + slot * STAGE + (wave * MINE + i) * 1024), 16, 0, 0);
+        for (int i = kb * MINE / KB; i < (kb + 1) * MINE / KB; ++i) {
+            const int j = i < ML ? i : i - ML;
+            const char *from = i < ML ? left[j / PER_L % OWN] + at * (PER_L * 1024) + j % PER_L * 1024 : right[j / PER_R % OWN] + at * (PER_R * 1024) + j % PER_R * 1024;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + lane16),
+                                             (__attribute__((address_space(3))) void *)(lds + slot * STAGE + (i < ML ? wave * ML + j : RIGHT + wave * MR + j) * 1024), 16, 0, 0);
+        }
     };
     const int wi = wave >> 1, wj = wave & 1;
-    half8 lf[2][FI][S], rf[2][FJ][S];
-    const auto read = [&](half8 (&x)[FI][S], half8 (&y)[FJ][S], int slot, int kb) {
+    half8 lf[2][FI][L], rf[2][FI][R];
+    const auto read = [&](half8 (&x)[FI][L], half8 (&y)[FI][R], int slot, int kb) {
         const unsigned char *at = lds + slot * STAGE + lane * 16;
 #pragma unroll
         for (int f = 0; f < FI; ++f)
 #pragma unroll
-            for (int e = 0; e < S; ++e) x[f][e] = *reinterpret_cast<const half8 *>(at + ((wi * FI + f) * PER + kb * S + e) * 1024);
+            for (int e = 0; e < L; ++e) x[f][e] = *reinterpret_cast<const half8 *>(at + ((wi * FI + f) * PER_L + kb * L + e) * 1024);
 #pragma unroll
-        for (int f = 0; f < FJ; ++f)
+        for (int f = 0; f < FI; ++f)
 #pragma unroll
-            for (int e = 0; e < S; ++e) y[f][e] = *reinterpret_cast<const half8 *>(at + ((2 * FI + wj * FJ + f) * PER + kb * S + e) * 1024);
+            for (int e = 0; e < R; ++e) y[f][e] = *reinterpret_cast<const half8 *>(at + (RIGHT + (wj * FI + f) * PER_R + kb * R + e) * 1024);
     };
-    Sums<FI, FJ, SPLIT> s;
+    Sums<FI, FI, KIND> s;
     s.clear();
 #pragma unroll
     for (int t = 0; t < STAGES - 1; ++t)
@@ -574,7 +592,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu((FI + FJ) *
                 read(lf[(kb + 1) & 1], rf[(kb + 1) & 1], next, (kb + 1) % KB);
                 fetch(into, stage + STAGES - 1, kb % KB);
                 s.add(lf[kb & 1], rf[kb & 1]);
-                interleave<FI * FJ * (SPLIT ? 3 : 1), (FI + FJ) * S, MINE / KB>();
+                interleave<FI * FI * products_of(KIND), FI * (L + R), MINE / KB>();
                 if (end) { into = slot; slot = next; ++stage; }
             }
         }
@@ -584,29 +602,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu((FI + FJ) *
     if (MODE == MUON_STEP && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
     if (a.shares > 1) {
         // a share of the sums: 16 bytes per lane at a time, as they are
-        floatx4 *to = reinterpret_cast<floatx4 *>(a.part) + ((int64_t)(p.slot * a.shares + p.share) * 4 + wave) * (FI * FJ * 4 * 64) + lane;
+        floatx4 *to = reinterpret_cast<floatx4 *>(a.part) + ((int64_t)(p.slot * a.shares + p.share) * 4 + wave) * (FI * FI * 4 * 64) + lane;
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
-            for (int j = 0; j < FJ; ++j)
+            for (int j = 0; j < FI; ++j)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const floatx16 v = s.all()[i][j];
-                    to[((i * FJ + j) * 4 + g) * 64] = floatx4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+                    to[((i * FI + j) * 4 + g) * 64] = floatx4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
                 }
         return;
     }
     float *const mine = reinterpret_cast<float *>(lds) + wave * (64 * SUMS_LD);
-    put_tile<FI, FJ, 1, SPLIT, MODE>(a, p, s.all(), p.ti * TI + wi * FI * 32, p.tj * TJ + wj * FJ * 32, mine, mine, 0);
+    put_tile<FI, FI, 1, KIND, MODE>(a, p, s.all(), p.ti * T + wi * FI * 32, p.tj * T + wj * FI * 32, mine, mine, 0);
 }
 
 // The shares of the sums added: a workgroup for 64 x 64 of a tile, each wavefront every fourth share, and then the four.
-template <int FI, int FJ, bool SPLIT, int MODE>
+template <int FI, int KIND, int MODE>
 __global__ __launch_bounds__(256) void k_muon_join(MuonArgs a, int32_t shares) {
-    constexpr int KS = 4, PARTS = 4 * (FI / 2) * (FJ / 2);
+    constexpr int KS = 4, PARTS = FI * FI;
     __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];
     const Place p = place_of<MODE>(a, blockIdx.x / PARTS, gridDim.x / PARTS);  // (a.shares is 1 here)
-    const int part = blockIdx.x % PARTS, wave = part & 3, si = (part >> 2) / (FJ / 2), sj = (part >> 2) % (FJ / 2);
+    const int part = blockIdx.x % PARTS, wave = part & 3, si = (part >> 2) / (FI / 2), sj = (part >> 2) % (FI / 2);
     const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     floatx16 x[2][2];
 #pragma unroll
@@ -614,19 +632,19 @@ __global__ __launch_bounds__(256) void k_muon_join(MuonArgs a, int32_t shares) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) x[i][j] = floatx16{};
     for (int k = group; k < shares; k += KS) {
-        const floatx4 *from = reinterpret_cast<const floatx4 *>(a.part) + ((int64_t)(p.slot * shares + k) * 4 + wave) * (FI * FJ * 4 * 64) + lane;
+        const floatx4 *from = reinterpret_cast<const floatx4 *>(a.part) + ((int64_t)(p.slot * shares + k) * 4 + wave) * (FI * FI * 4 * 64) + lane;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const floatx4 v = from[(((2 * si + i) * FJ + 2 * sj + j) * 4 + g) * 64];
+                    const floatx4 v = from[(((2 * si + i) * FI + 2 * sj + j) * 4 + g) * 64];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[i][j][4 * g + e] += v[e];
                 }
     }
-    put_tile<2, 2, KS, SPLIT, MODE>(a, p, x, p.ti * 64 * FI + ((wave >> 1) * FI + 2 * si) * 32, p.tj * 64 * FJ + ((wave & 1) * FJ + 2 * sj) * 32, lds[group], lds[0], group);
+    put_tile<2, 2, KS, KIND, MODE>(a, p, x, p.ti * 64 * FI + ((wave >> 1) * FI + 2 * si) * 32, p.tj * 64 * FI + ((wave & 1) * FI + 2 * sj) * 32, lds[group], lds[0], group);
 }
 
 // ---- matrices of up to 128 x 128: all steps in one launch --------------------------------------------------------------
@@ -650,9 +668,9 @@ __device__ __forceinline__ void turn_quad(uint32_t &r01, uint32_t &r23) {
 
 struct MuonOne { MuonIn in; MuonArgs out; int32_t n, m, nq, mq, steps; };     // nq, mq: the frame
 
-template <class T, bool SPLIT, bool STEP>
+template <class T, bool STEP>
 __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32_t *err) {
-    constexpr int S = SPLIT ? 2 : 1;
+    constexpr int S = 2;
     extern __shared__ __attribute__((aligned(16))) f16_t one_lds[];
     __shared__ double squares[ONE_THREADS / 64];
     if (STEP && *(volatile const int32_t *)err) return;                       // (set before this launch: the same for all)
@@ -701,7 +719,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[f][e] = parts_of<SPLIT>(v[f][2 * e] * factor, v[f][2 * e + 1] * factor);
+            for (int e = 0; e < 8; ++e) q[f][e] = parts_of<true>(v[f][2 * e] * factor, v[f][2 * e + 1] * factor);
     };
     // into m of K numbers a row: rows and columns exchanged, four rows' numbers are neighbours; and as they are
     const auto put_columns = [&](f16_t *m, int K, const Parts (&q)[2][8]) {
@@ -710,9 +728,9 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int i = row_of(f, 4 * g), j = j0 + l32;
-                f16_t *p = m + place8<SPLIT>(j, i & ~7, K) + (i & 4);
+                f16_t *p = m + place8<true>(j, i & ~7, K) + (i & 4);
                 *reinterpret_cast<half4 *>(p) = __builtin_shufflevector(q[f][2 * g].hi, q[f][2 * g + 1].hi, 0, 1, 2, 3);
-                if constexpr (SPLIT) *reinterpret_cast<half4 *>(p + 512) = __builtin_shufflevector(q[f][2 * g].lo, q[f][2 * g + 1].lo, 0, 1, 2, 3);
+                *reinterpret_cast<half4 *>(p + 512) = __builtin_shufflevector(q[f][2 * g].lo, q[f][2 * g + 1].lo, 0, 1, 2, 3);
             }
     };
     const auto put_rows = [&](f16_t *m, int K, const Parts (&q)[2][8]) {
@@ -721,16 +739,14 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int i = row_of(f, 4 * g) + (lane & 3), j = j0 + (l32 & ~3);
-                f16_t *p = m + place8<SPLIT>(i, j & ~7, K) + (j & 4);
+                f16_t *p = m + place8<true>(i, j & ~7, K) + (j & 4);
                 uint32_t a = __builtin_bit_cast(uint32_t, q[f][2 * g].hi), b = __builtin_bit_cast(uint32_t, q[f][2 * g + 1].hi);
                 turn_quad(a, b);
                 *reinterpret_cast<uint2 *>(p) = uint2{a, b};
-                if constexpr (SPLIT) {
-                    a = __builtin_bit_cast(uint32_t, q[f][2 * g].lo);
-                    b = __builtin_bit_cast(uint32_t, q[f][2 * g + 1].lo);
-                    turn_quad(a, b);
-                    *reinterpret_cast<uint2 *>(p + 512) = uint2{a, b};
-                }
+                a = __builtin_bit_cast(uint32_t, q[f][2 * g].lo);
+                b = __builtin_bit_cast(uint32_t, q[f][2 * g + 1].lo);
+                turn_quad(a, b);
+                *reinterpret_cast<uint2 *>(p + 512) = uint2{a, b};
             }
     };
     // this wavefront's sums over the first `used` blocks of k, of rows of K numbers of l and r
@@ -748,7 +764,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
                 rf[e] = *reinterpret_cast<const half8 *>(pr + k * (512 * S) + e * 512);
             }
 #pragma unroll
-            for (int e = SPLIT ? 2 : 0; e >= 0; --e)
+            for (int e = 2; e >= 0; --e)
 #pragma unroll
                 for (int f = 0; f < 2; ++f) sum[f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lf[f][e == 2 ? S - 1 : 0], rf[e == 1 ? S - 1 : 0], sum[f], 0, 0, 0);
         }
@@ -798,7 +814,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
                 if constexpr (STEP) {
                     float *w = a.out.val + (a.out.first + row) * a.out.L + col;
                     *w = a.out.keep * *w - a.out.step * v;
-                } else if (!SPLIT) reinterpret_cast<bf16_t *>(a.out.to)[row * a.out.to_ld + col] = (bf16_t)v;
+                } else if (a.out.to_type == PS_BF16) reinterpret_cast<bf16_t *>(a.out.to)[row * a.out.to_ld + col] = (bf16_t)v;
                 else if (a.out.to_type == PS_F32) reinterpret_cast<float *>(a.out.to)[row * a.out.to_ld + col] = v;
                 else reinterpret_cast<f16_t *>(a.out.to)[row * a.out.to_ld + col] = (f16_t)v;
             }
@@ -817,6 +833,7 @@ struct MuonPlan {
     size_t off_d, off_x, off_xt[2], off_g, off_p, off_part, bytes;
 };
 inline int64_t half_of(int64_t t) { return t * (t + 1) / 2; }
+constexpr int PAIR_STEPS = 2;                    // of single numbers, the first steps, which read X as pairs
 constexpr int MOST_SHARES = 8, TURNS_AT_LEAST = 2, SMALL_SHARES = 16, SMALL_TURNS = 4;
 // Workgroups that share a tile's sum over k, where there are fewer tiles than compute units.
 int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t K) {
@@ -845,12 +862,12 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     if (p.one) return p;                          // (no scratch)
     const int64_t blocks = ceil_div64((int64_t)rows * cols, 1024);
     p.blocks = (int32_t)(blocks < NORM_BLOCKS ? blocks : NORM_BLOCKS);
-    const size_t size = split ? 4 : 2, nm = (size_t)batch * p.np * p.mp * size, nn = (size_t)batch * p.np * p.np * size;
+    const size_t size = split ? 4 : 2, nm = (size_t)batch * p.np * p.mp, nn = (size_t)batch * p.np * p.np * size;
     p.off_d = up256((size_t)batch * NORM_BLOCKS * sizeof(double));
     p.off_x = p.off_d + (step ? up256((size_t)batch * rows * cols * sizeof(float)) : 0);
-    p.off_xt[0] = p.off_x + up256(nm);
-    p.off_xt[1] = p.off_xt[0] + up256(nm);
-    p.off_g = p.off_xt[1] + up256(nm);
+    p.off_xt[0] = p.off_x + up256(nm * size);
+    p.off_xt[1] = p.off_xt[0] + up256(nm * 4);
+    p.off_g = p.off_xt[1] + up256(nm * 4);
     p.off_p = p.off_g + up256(nn);
     p.off_part = p.off_p + up256(nn);
     // (shares times tiles are at most as many as the compute units)
@@ -858,94 +875,116 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     return p;
 }
 
-template <int FI, int KB, int STAGES, bool SPLIT, int MODE>
+template <int FI, int KB, int STAGES, int KIND, int MODE>
 int large(dpaps_ps *ps, const MuonArgs &a, int64_t tiles, hipStream_t st) {
     static LdsAllowed allowed;
-    constexpr int STAGED = STAGES * 4 * FI * KB * (SPLIT ? 2 : 1) * 1024, SUMMED = 4 * 64 * SUMS_LD * 4, LDS = STAGED > SUMMED ? STAGED : SUMMED;
-    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_large<FI, FI, KB, STAGES, SPLIT, MODE>), LDS);
+    constexpr int STAGED = STAGES * stage_pieces(FI, KB, KIND) * 1024, SUMMED = 4 * 64 * SUMS_LD * 4, LDS = STAGED > SUMMED ? STAGED : SUMMED;
+    static_assert(LDS <= 160 * 1024);
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_large<FI, KB, STAGES, KIND, MODE>), LDS);
     if (rc) return rc;
-    k_muon_large<FI, FI, KB, STAGES, SPLIT, MODE><<<(unsigned)(tiles * a.shares), 256, LDS, st>>>(a, ps->err);
+    k_muon_large<FI, KB, STAGES, KIND, MODE><<<(unsigned)(tiles * a.shares), 256, LDS, st>>>(a, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
 // Tiles tile0 .. tile0 + tiles - 1, fewer than compute units: with shared sums, if that can be.
-template <int FI, int KB, bool SPLIT, int MODE>
+template <int FI, int KB, int KIND, int MODE>
 int large_rest(dpaps_ps *ps, MuonArgs a, int64_t tiles, hipStream_t st) {
     const int32_t shares = shares_of(ps, tiles, a.K);
     a.shares = shares;
-    const int rc = large<FI, KB, 4, SPLIT, MODE>(ps, a, tiles, st);
+    const int rc = large<FI, KB, 4, KIND, MODE>(ps, a, tiles, st);
     if (rc || shares == 1) return rc;
     a.shares = 1;
-    k_muon_join<FI, FI, SPLIT, MODE><<<(unsigned)(FI * FI * tiles), 256, 0, st>>>(a, shares);
+    k_muon_join<FI, KIND, MODE><<<(unsigned)(FI * FI * tiles), 256, 0, st>>>(a, shares);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
-template <int TILE, bool SPLIT, int MODE>
-int product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
-    constexpr bool HALF = MODE == MUON_GRAM || MODE == MUON_POLY;
-    a.tiles = (int32_t)(HALF ? half_of(a.tiles_i) : (int64_t)a.tiles_i * a.tiles_j);
+// X X' or A A', of which half of the tiles is computed
+template <int TILE, int KIND, int MODE>
+int half_product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
+    a.tiles = (int32_t)half_of(a.tiles_i);
     a.shares = 1;
     const int64_t tiles = (int64_t)a.tiles * batch, cus = ps->num_cu;
     if constexpr (TILE == 64) {
         if constexpr (MODE == MUON_GRAM) a.shares = small_shares(ps, tiles, a.K);
-        k_muon_small<SPLIT, MODE><<<(unsigned)(tiles * a.shares), 256, 0, st>>>(a, ps->err);
+        k_muon_small<KIND, MODE><<<(unsigned)(tiles * a.shares), 256, 0, st>>>(a, ps->err);
         PS_HIP(ps, hipGetLastError());
         if constexpr (MODE == MUON_GRAM) {
             const int32_t shares = a.shares;
             a.shares = 1;
-            if (shares > 1) k_muon_join_small<SPLIT><<<(unsigned)tiles, 256, 0, st>>>(a, shares);
+            if (shares > 1) k_muon_join_small<KIND><<<(unsigned)tiles, 256, 0, st>>>(a, shares);
             PS_HIP(ps, hipGetLastError());
         }
+        return PS_OK;
     } else if constexpr (TILE == 256) {
         // as many tiles as make full rounds of the compute units, and the rest with shared sums
-        const int64_t rest = HALF && tiles > cus && tiles % cus <= cus / 2 ? tiles % cus : 0;
-        const int rc = large<4, 2, 4, SPLIT, MODE>(ps, a, tiles - rest, st);
+        const int64_t rest = tiles > cus && tiles % cus <= cus / 2 ? tiles % cus : 0;
+        const int rc = large<4, 2, 4, KIND, MODE>(ps, a, tiles - rest, st);
         if (rc || rest == 0) return rc;
         a.tile0 = (int32_t)(tiles - rest);
-        if constexpr (HALF) return large_rest<4, 2, SPLIT, MODE>(ps, a, rest, st);
+        return large_rest<4, 2, KIND, MODE>(ps, a, rest, st);
     } else {
-        constexpr int KB = SPLIT ? 2 : 4;                                     // so 128 KB of LDS; half of that where two workgroups share a compute unit
-        if (tiles > cus) return large<2, KB / 2, 4, SPLIT, MODE>(ps, a, tiles, st);
-        if constexpr (HALF) {
-            // (with a short sum, tiles of 64)
-            if (a.K <= 1024 && tiles < cus) { a.tiles_i *= 2; a.tiles_j *= 2; return product<64, SPLIT, MODE>(ps, a, batch, st); }
-            return large_rest<2, KB, SPLIT, MODE>(ps, a, tiles, st);
-        } else return large<2, KB, 4, SPLIT, MODE>(ps, a, tiles, st);
+        constexpr int KB = KIND == SPLIT ? 2 : 4;                             // so 128 KB of LDS; half of that where two workgroups share a compute unit
+        if (tiles > cus) return large<2, KB / 2, 4, KIND, MODE>(ps, a, tiles, st);
+        if (a.K <= 1024 && tiles < cus) {                                     // (with a short sum, tiles of 64)
+            a.tiles_i *= 2;
+            return half_product<64, KIND, MODE>(ps, a, batch, st);
+        }
+        return large_rest<2, KB, KIND, MODE>(ps, a, tiles, st);
     }
-    return PS_OK;
+}
+// P X
+template <int TILE, int KIND, int MODE>
+int whole_product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
+    a.tiles = a.tiles_i * a.tiles_j;
+    a.shares = 1;
+    const int64_t tiles = (int64_t)a.tiles * batch;
+    if constexpr (TILE == 64) {
+        k_muon_small<KIND, MODE><<<(unsigned)tiles, 256, 0, st>>>(a, ps->err);
+        PS_HIP(ps, hipGetLastError());
+        return PS_OK;
+    } else if constexpr (TILE == 256) {
+        return large<4, 2, KIND == RIGHT_SPLIT ? 3 : 4, KIND, MODE>(ps, a, tiles, st);
+    } else {
+        // (96 to 128 KB of LDS; 64 or 72 where two workgroups share a compute unit)
+        constexpr int KB = KIND == SINGLE ? 4 : 2;
+        if (tiles > ps->num_cu) return large<2, KIND == RIGHT_SPLIT ? KB : KB / 2, KIND == RIGHT_SPLIT ? 3 : 4, KIND, MODE>(ps, a, tiles, st);
+        return large<2, KB, 4, KIND, MODE>(ps, a, tiles, st);
+    }
 }
 
-template <int TILE, bool SPLIT>
+template <int TILE, bool PAIR>
 int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t steps, hipStream_t st) {
+    constexpr int KIND = PAIR ? SPLIT : SINGLE;
     char *ws = (char *)ps->ws;
     f16_t *x = (f16_t *)(ws + p.off_x), *xt = (f16_t *)(ws + p.off_xt[0]), *xt_next = (f16_t *)(ws + p.off_xt[1]), *g = (f16_t *)(ws + p.off_g), *q = (f16_t *)(ws + p.off_p);
-    const int64_t S = SPLIT ? 2 : 1, nm = (int64_t)p.np * p.mp * S, nn = (int64_t)p.np * p.np * S;
+    const int64_t S = PAIR ? 2 : 1, nm = (int64_t)p.np * p.mp, nn = (int64_t)p.np * p.np * S;
     const dim3 grid((unsigned)(p.mp / 64), (unsigned)(p.np / 64), (unsigned)p.batch);
-    if (in.type == PS_F32) k_muon_scale<float, SPLIT><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
-    else if (in.type == PS_BF16) k_muon_scale<bf16_t, SPLIT><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
-    else k_muon_scale<f16_t, SPLIT><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
+    if (in.type == PS_F32) k_muon_scale<float, PAIR><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
+    else if (in.type == PS_BF16) k_muon_scale<bf16_t, PAIR><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
+    else k_muon_scale<f16_t, PAIR><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
     PS_HIP(ps, hipGetLastError());
     for (int s = 0; s < steps; ++s) {
         MuonArgs a{};
         a.tiles_i = p.np / TILE; a.tiles_j = p.mp / TILE;
         a.part = (float *)(ws + p.off_part);
-        a.lhs = a.rhs = x; a.lhs_size = a.rhs_size = nm; a.K = p.mp; a.out = g; a.out_ld = p.np; a.out_size = nn;
-        int rc = product<TILE, SPLIT, MUON_GRAM>(ps, a, p.batch, st);
+        a.lhs = a.rhs = x; a.lhs_size = a.rhs_size = nm * S; a.K = p.mp; a.out = g; a.out_ld = p.np; a.out_size = nn;
+        int rc = half_product<TILE, KIND, MUON_GRAM>(ps, a, p.batch, st);
         if (rc) return rc;
         a.lhs = a.rhs = g; a.lhs_size = a.rhs_size = nn; a.K = p.np; a.out = q;
-        rc = product<TILE, SPLIT, MUON_POLY>(ps, a, p.batch, st);
+        rc = half_product<TILE, KIND, MUON_POLY>(ps, a, p.batch, st);
         if (rc) return rc;
-        MuonArgs b = s + 1 == steps ? last : a;
+        const bool end = s + 1 == steps, pairs = !PAIR && s < PAIR_STEPS;
+        MuonArgs b = end ? last : a;
         b.tiles_i = a.tiles_i; b.tiles_j = a.tiles_j; b.K = p.np;
-        b.lhs = q; b.lhs_size = nn; b.rhs = xt; b.rhs_size = nm;
-        if (s + 1 == steps) {
-            if constexpr (SPLIT) rc = last.val ? product<TILE, SPLIT, MUON_STEP>(ps, b, p.batch, st) : product<TILE, SPLIT, MUON_LAST>(ps, b, p.batch, st);
-            else rc = product<TILE, SPLIT, MUON_LAST>(ps, b, p.batch, st);
-        } else {
-            // (X transposed is read by other workgroups while it is written: into the other place; X itself is not)
-            b.out = x; b.out_ld = p.mp; b.out_t = xt_next; b.out_t_ld = p.np; b.out_size = nm;
-            rc = product<TILE, SPLIT, MUON_APPLY>(ps, b, p.batch, st);
-        }
+        // (X transposed is read by other workgroups while it is written: into the other place; X itself is not)
+        b.lhs = q; b.lhs_size = nn; b.rhs = xt; b.rhs_size = nm * 2;
+        b.out = x; b.out_ld = p.mp; b.out_size = nm * S;
+        b.out_t = xt_next; b.out_t_ld = p.np; b.out_t_size = nm * 2; b.out_t_pair = s + 1 < PAIR_STEPS;
+        if constexpr (PAIR) {
+            if (!end) rc = whole_product<TILE, SPLIT, MUON_APPLY>(ps, b, p.batch, st);
+            else rc = last.val ? whole_product<TILE, SPLIT, MUON_STEP>(ps, b, p.batch, st) : whole_product<TILE, SPLIT, MUON_LAST>(ps, b, p.batch, st);
+        } else if (pairs) rc = end ? whole_product<TILE, RIGHT_SPLIT, MUON_LAST>(ps, b, p.batch, st) : whole_product<TILE, RIGHT_SPLIT, MUON_APPLY>(ps, b, p.batch, st);
+        else rc = end ? whole_product<TILE, SINGLE, MUON_LAST>(ps, b, p.batch, st) : whole_product<TILE, SINGLE, MUON_APPLY>(ps, b, p.batch, st);
         if (rc) return rc;
         f16_t *const t = xt; xt = xt_next; xt_next = t;
     }
@@ -969,21 +1008,20 @@ int norm_of(dpaps_ps *ps, const MuonPlan &p, const MuonIn &in, hipStream_t st) {
     return PS_OK;
 }
 
-template <class T, bool SPLIT, bool STEP>
+template <class T, bool STEP>
 int one_of(dpaps_ps *ps, const MuonOne &a, int32_t batch, hipStream_t st) {
     static LdsAllowed allowed;
-    constexpr size_t MOST = (size_t)2 * ONE_SIDE * ONE_SIDE * (SPLIT ? 4 : 2);
-    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_one<T, SPLIT, STEP>), MOST);
+    constexpr size_t MOST = (size_t)2 * ONE_SIDE * ONE_SIDE * 4;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_muon_one<T, STEP>), MOST);
     if (rc) return rc;
-    k_muon_one<T, SPLIT, STEP><<<(unsigned)batch, ONE_THREADS, (size_t)a.nq * (a.nq + a.mq) * (SPLIT ? 4 : 2), st>>>(a, ps->err);
+    k_muon_one<T, STEP><<<(unsigned)batch, ONE_THREADS, (size_t)a.nq * (a.nq + a.mq) * 4, st>>>(a, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
 template <class T>
 int one_launch(dpaps_ps *ps, const MuonPlan &p, const MuonIn &in, const MuonArgs &last, int32_t steps, hipStream_t st) {
-    MuonOne a{in, last, p.n, p.m, p.np, p.mp, steps};
-    if (in.val) return one_of<T, true, true>(ps, a, p.batch, st);
-    return p.split ? one_of<T, true, false>(ps, a, p.batch, st) : one_of<T, false, false>(ps, a, p.batch, st);
+    const MuonOne a{in, last, p.n, p.m, p.np, p.mp, steps};
+    return in.val ? one_of<T, true>(ps, a, p.batch, st) : one_of<T, false>(ps, a, p.batch, st);
 }
 
 int orthogonalize(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t steps, hipStream_t st) {
