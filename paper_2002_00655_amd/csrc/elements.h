@@ -22,18 +22,17 @@ __device__ __forceinline__ Vec<float, W> load_vec(const T *p) {
     }
 }
 // the same the other way: rounded to the nearest, ties to even; what is too large for T becomes infinite
-template <class T, int W, bool STREAM = false>
+template <class T, int W>
 __device__ __forceinline__ void store_vec(T *p, Vec<float, W> v) {
     if constexpr (W * sizeof(T) <= 16) {
         Vec<T, W> x;
         if constexpr (W == 1) x = (T)v;
         else x = __builtin_convertvector(v, Vec<T, W>);
-        if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<Vec<T, W> *>(p));
-        else *reinterpret_cast<Vec<T, W> *>(p) = x;
+        *reinterpret_cast<Vec<T, W> *>(p) = x;
     } else {
         static_assert(W == 8 && sizeof(T) == 4);
-        store_vec<T, 4, STREAM>(p, __builtin_shufflevector(v, v, 0, 1, 2, 3));
-        store_vec<T, 4, STREAM>(p + 4, __builtin_shufflevector(v, v, 4, 5, 6, 7));
+        store_vec<T, 4>(p, __builtin_shufflevector(v, v, 0, 1, 2, 3));
+        store_vec<T, 4>(p + 4, __builtin_shufflevector(v, v, 4, 5, 6, 7));
     }
 }
 

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void k_token_replies(TokenIds t, int32_t worke
 // ---- lookup ---------------------------------------------------------------------------------------------------------
 // The result in pieces of W values, P a row, a workgroup 256 * AHEAD consecutive pieces, a thread every 256th: its tokens,
 // then its pieces of the rows, are asked for together.  The first route.blocks workgroups count the statistics.
-template <class Out, int W, int AHEAD, bool STREAM>
+template <class Out, int W, int AHEAD>
 __global__ __launch_bounds__(256) void k_emb_lookup(RouteArgs route, TokenIds t, uint32_t P, double inv_P, int64_t L, float scale, const float *val, Out *out,
                                                     int64_t stride, int32_t *err) {
     const bool few = t.n <= FEW_KEYS;
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256) void k_emb_lookup(RouteArgs route, TokenIds t,
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-        if (first + u * 256 + threadIdx.x < total) store_vec<Out, W, STREAM>(out + (p0 + row[u]) * stride + (int64_t)c[u] * W, x[u]);
+        if (first + u * 256 + threadIdx.x < total) store_vec<Out, W>(out + (p0 + row[u]) * stride + (int64_t)c[u] * W, x[u]);
 }
 
 // ---- sums over sorted tokens ----------------------------------------------------------------------------------------
@@ -437,7 +437,7 @@ int lookup(dpaps_ps *ps, const RouteArgs &a, const TokenIds &t, int32_t dim, flo
         const int64_t blocks = a.blocks + ceil_div64(t.n * P, 256 * AHEAD);                                                                       \
         if (blocks >= ((int64_t)1 << 24)) { ps->last_error = "emb_lookup: the result is too large for one launch"; return PS_ELIMIT; }            \
         const unsigned grid = (unsigned)blocks;                                                                                                   \
-        k_emb_lookup<Out, W, AHEAD, false><<<grid, 256, 0, st>>>(a, t, P, 1.0 / P, ps->L, scale, ps->val, out, stride, ps->err);                  \
+        k_emb_lookup<Out, W, AHEAD><<<grid, 256, 0, st>>>(a, t, P, 1.0 / P, ps->L, scale, ps->val, out, stride, ps->err);                  \
     } while (0)
     if (sizeof(Out) == 2 && fits(8)) LOOKUP(8, 2);
     else if (fits(4)) LOOKUP(4, 4);

@@ -21,7 +21,8 @@
 //                      input order - the pass is stable - and every pair is stored.
 // Up to MID_MAX pairs the tiles are few and larger, and every workgroup of the scatter works out its offsets from all
 // tiles' counters itself: two launches per pass instead of four; so they are from BIG_MIN up to BIG_MAX pairs, in larger
-// tiles that are put in order in LDS before they are stored.  Up to FEW_MAX pairs one workgroup sorts them in LDS.
+// tiles that are put in order in LDS before they are stored.  Up to FEW_MAX pairs one workgroup sorts them in LDS, up to RANK_MAX tokens
+// are ranked by comparing each with all, in one launch.
 // A caller that has not checked its keys asks for it: the first kernel then sets the handle's error, which ends the rest.
 // Integer work only: the result is the same bit for bit whatever the scheduling.
 #include "common.h"
@@ -540,6 +541,64 @@ __global__ __launch_bounds__(FEW_THREADS) void k_sort_few(const int64_t *keys, i
     }
 }
 
+// ---- up to RANK_MAX tokens: one launch, a token's place is how many come before it ------------------------------------
+// A workgroup takes 64 tokens, or 64 / `parts` of them where that leaves compute units idle, and compares each with all n: a wavefront has R times 64
+// tokens in registers, one comparison is an instruction for 64 of them, and the scalar unit counts its bits.  Earlier positions come before their equals,
+// later ones do not: a token counts as 2 token, behind as 2 token + 1, and what is below 2 t + 1 comes before t.
+// The scalar unit, two instructions a comparison, bounds it, so it grows with n^2.  A gradient of 5,000 rows of 16, this way and in four launches:
+// 2,049 to 4,096 tokens 14 us and 23, 8,192 18.6 and 23.8; 16,384 35.4 and 25.3.
+constexpr int RANK_THREADS = 1024, RANK_WAVES = RANK_THREADS / 64, RANK_MAX = 8 * RANK_THREADS;
+template <int R>
+__global__ __launch_bounds__(RANK_THREADS) void k_sort_rank(TokensIn tokens, int parts, uint64_t *skeys, uint32_t *spos, int32_t *err) {
+    const int32_t stop = flag_ahead(err);
+    __shared__ uint32_t counts[RANK_WAVES][64];
+    const int n = (int)tokens.t.n, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int chunk = blockIdx.x / parts, each = 64 / parts, j0 = blockIdx.x % parts * each, own = chunk * 64 + lane;
+    int64_t id[R + 1];                                                 // (all on their way together)
+    const auto at = [&](int i) {
+        const int q = i == R ? own : (wave * R + i) * 64 + lane;
+        return q < n ? q : n - 1;
+    };
+    if (tokens.t.wide) {
+#pragma unroll
+        for (int i = 0; i <= R; ++i) id[i] = reinterpret_cast<const int64_t *>(tokens.t.ids)[at(i)];
+    } else {
+#pragma unroll
+        for (int i = 0; i <= R; ++i) id[i] = reinterpret_cast<const int32_t *>(tokens.t.ids)[at(i)];
+    }
+    const int64_t pad = tokens.t.pad;
+    const uint32_t padding = (uint32_t)tokens.t.count;                 // (below 2^31)
+    const uint32_t mine = own >= n ? ~0u : id[R] == pad ? padding : (uint32_t)id[R];
+    uint32_t x[R];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int from = wave * R + i;
+        bad |= tokens.t.bad(id[i]);
+        const uint32_t key = id[i] == pad ? padding : (uint32_t)id[i];
+        x[i] = from == chunk || from * 64 + lane >= n ? ~0u : 2u * key + (from > chunk ? 1u : 0u);
+    }
+    if (bad) atomicExch(err, PS_EKEY);
+    if (__syncthreads_or(bad || stop != 0)) return;
+    uint32_t count = 0;                                                // lane j: of the chunk's token j
+    for (int j = j0; j < j0 + each; ++j) {
+        const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)mine, j), up_to = 2u * t + 1u;
+        uint32_t c = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) c += (uint32_t)__popcll(__ballot(x[i] < up_to));
+        if (wave == 0) c += (uint32_t)__popcll(__ballot(mine < t || (mine == t && lane < j)));
+        count = lane == j ? c : count;
+    }
+    counts[wave][lane] = count;
+    __syncthreads();
+    if (wave == 0 && lane >= j0 && lane < j0 + each && own < n) {
+        uint32_t place = 0;
+        for (int w = 0; w < RANK_WAVES; ++w) place += counts[w][lane];
+        skeys[place] = mine;
+        spos[place] = (uint32_t)own;
+    }
+}
+
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct SortPlan {
@@ -672,5 +731,15 @@ int dpaps_sort_pairs(dpaps_ps *ps, const int64_t *keys, int64_t n, int key_bits,
 // The same for tokens, more than the few that a call takes without a sort: ordered by token, padding behind all of them (as token
 // t.count).  A token out of range sets the handle's error.  Scratch: that of keys of dpaps_key_bits(t.count + 1) bits.
 int dpaps_sort_tokens(dpaps_ps *ps, const TokenIds &t, uint64_t *skeys, uint32_t *spos, void *scratch, hipStream_t st) {
+    if (t.n <= RANK_MAX) {
+        const int chunks = (int)((t.n + 63) / 64);
+        int parts = 1;
+        while (parts < 8 && chunks * parts < ps->num_cu) parts *= 2;
+        const unsigned grid = (unsigned)(chunks * parts);
+        if (t.n <= RANK_MAX / 2) k_sort_rank<4><<<grid, RANK_THREADS, 0, st>>>(TokensIn{t}, parts, skeys, spos, ps->err);
+        else k_sort_rank<8><<<grid, RANK_THREADS, 0, st>>>(TokensIn{t}, parts, skeys, spos, ps->err);
+        PS_HIP(ps, hipGetLastError());
+        return PS_OK;
+    }
     return sort_any(ps, TokensIn{t}, t.n, dpaps_key_bits(t.count + 1), t.count + 1, skeys, spos, scratch, st);
 }

@@ -122,6 +122,37 @@ def test_gradient(n, V, D):
     srv.status()
 
 
+@pytest.mark.parametrize("n", [2049, 2112, 4095, 4096, 4097, 8128, 8191, 8192, 8193, 16_385, 131_073, 262_145])
+def test_every_term_is_added_once_whatever_sorts_the_tokens(n):
+    """Sums of small integers are exact, in any order: how often a token comes, and at which positions."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    srv = P.ParameterServer(1, 1, 1)
+    rng = np.random.default_rng(n)
+    for V, pad, wide in ((1, None, True), (130, 129, False), (70_000, 0, True), (100_000, -5, False)):
+        tokens = rng.integers(0, V, n)
+        if pad is not None:
+            tokens[rng.random(n) < 0.1] = pad
+        dout = np.stack([np.ones(n), np.arange(n) % 8, np.arange(n) // 8 % 8], 1).astype(np.float32)
+        got = srv.emb_grad(torch.from_numpy(tokens.astype(np.int64 if wide else np.int32)).cuda(), torch.from_numpy(dout).cuda(), V, pad_token=pad).cpu().numpy()
+        there = tokens != pad if pad is not None else np.ones(n, bool)
+        for c in range(3):
+            assert np.array_equal(got[:, c], np.bincount(tokens[there], weights=dout[there, c], minlength=V).astype(np.float32)), (V, c)
+
+
+@pytest.mark.parametrize("n", [2052, 4096, 4100, 8192, 8196, 131_072, 131_076])
+def test_terms_are_added_in_the_order_of_their_positions(n):
+    """Four terms a token, which lie in one range: the sums are those of 32-bit additions one after the other, bit for bit."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng = np.random.default_rng(n)
+    tokens = rng.permutation(np.repeat(np.arange(n // 4), 4))
+    dout = rng.standard_normal((n, 5)).astype(np.float32)
+    got = P.ParameterServer(1, 1, 1).emb_grad(torch.from_numpy(tokens).cuda(), torch.from_numpy(dout).cuda(), n // 4).cpu().numpy()
+    d = dout[np.argsort(tokens, kind="stable")].reshape(n // 4, 4, 5)
+    assert np.array_equal(got, ((d[:, 0] + d[:, 1]) + d[:, 2]) + d[:, 3])
+
+
 @pytest.mark.parametrize("what", ["one token", "all padding", "every token once", "two tokens in turn"])
 @pytest.mark.parametrize("n,D", [(65, 16), (4096, 128), (30_000, 72)])
 def test_gradient_of_extreme_batches(what, n, D):
