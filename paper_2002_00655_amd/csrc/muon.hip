@@ -647,12 +647,16 @@ __global__ __launch_bounds__(256) void k_muon_join(MuonArgs a, int32_t shares) {
     put_tile<2, 2, KS, KIND, MODE>(a, p, x, p.ti * 64 * FI + ((wave >> 1) * FI + 2 * si) * 32, p.tj * 64 * FI + ((wave & 1) * FI + 2 * sj) * 32, lds[group], lds[0], group);
 }
 
-// ---- matrices of up to 128 x 128: all steps in one launch --------------------------------------------------------------
-// A workgroup of eight wavefronts has a matrix; of the frame of 128 x 128 (or 64 in either direction) a wavefront has 64 x 32, as the sums of the
+// ---- matrices of up to 128 x 128 or 64 x 256: all steps in one launch ----------------------------------------------------
+// A workgroup of eight wavefronts has a matrix; of its frame, sides of multiples of 64, a wavefront has 64 x 32, as the sums of the
 // matrix instruction lie: two pieces of 32 x 32.  X stays in registers as 32-bit numbers; LDS has one operand of X - its rows for A = X X', then
 // its columns for P X - and A, then P.  The norm and, of a step, momentum and weights are read and written as they lie in registers.
-// What several launches per step cost - 5 us each for a few microseconds of products - is what this saves.
+// What several launches per step cost - 5 us each for a few microseconds of products - is what this saves: 64 x 256 39 us instead of 80 to 90, 10 x 200 30
+// instead of 75, 16 of 100 x 100 45 instead of 105.  What is left is a chain of four meetings a step, with a product of 4 to 16 blocks of k, or a change of
+// parts in LDS, between two of them.  Larger thin matrices in slices of 128 or 256 columns, a launch per step that adds the slices' A, are
+// slower than the several launches: 128 x 1024 156 us instead of 108.
 constexpr int ONE_SIDE = 128, ONE_THREADS = 512;
+inline bool one_fits(int32_t n, int32_t m) { return m <= ONE_SIDE || (n <= 64 && m <= 256); }
 
 // The 4 x 4 numbers of 16 bits of four lanes transposed: rows 0, 1 and rows 2, 3 of a lane's column become, of lane q, row q of the four columns.
 __device__ __forceinline__ void turn_quad(uint32_t &r01, uint32_t &r23) {
@@ -675,7 +679,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
     __shared__ double squares[ONE_THREADS / 64];
     if (STEP && *(volatile const int32_t *)err) return;                       // (set before this launch: the same for all)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
-    const int i0 = (wave >> 2) * 64, j0 = (wave & 3) * 32, nq = a.nq, mq = a.mq;
+    const int nq = a.nq, mq = a.mq, across = nq == 64 ? 8 : 4, i0 = wave / across * 64, j0 = wave % across * 32;
     const bool tall = a.out.tall, has_x = i0 < nq && j0 < mq, has_a = i0 < nq && j0 < nq;
     f16_t *const r1 = one_lds, *const r2 = one_lds + nq * mq * S;
     const int64_t row0 = (int64_t)blockIdx.x * a.in.rows;
@@ -690,7 +694,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
         for (int e = 0; e < 16; ++e) {
             const int i = row_of(f, e), j = j0 + l32;
             float v = 0.0f;
-            if (i < a.n && j < a.m) {
+            if (has_x && i < a.n && j < a.m) {
                 const int64_t row = row0 + (tall ? j : i), col = tall ? i : j;
                 v = (float)reinterpret_cast<const T *>(in.in)[row * in.ld + col];
                 if constexpr (STEP) {
@@ -749,7 +753,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
                 *reinterpret_cast<uint2 *>(p + 512) = uint2{a, b};
             }
     };
-    // this wavefront's sums over the first `used` blocks of k, of rows of K numbers of l and r
+    // this wavefront's sums over the first `used` blocks of k, 16 at most (so that chains are short: see Sums), of rows of K numbers of l and r
     const auto product = [&](const f16_t *l, const f16_t *r, int K, int used, floatx16 (&sum)[2]) {
         const int blocks = K >> 4;
         const f16_t *pl = l + (i0 >> 5) * blocks * (512 * S) + lane * 8, *pr = r + (j0 >> 5) * blocks * (512 * S) + lane * 8;
@@ -808,7 +812,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int i = row_of(f, e), j = j0 + l32;
-            if (i < a.n && j < a.m) {
+            if (has_x && i < a.n && j < a.m) {
                 const float v = x[f][e] * (x_factor / X_SCALE);
                 const int64_t row = row0 + (tall ? j : i), col = tall ? i : j;
                 if constexpr (STEP) {
@@ -854,12 +858,15 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     MuonPlan p{};
     p.batch = batch; p.tall = rows > cols; p.split = split;
     p.n = p.tall ? cols : rows; p.m = p.tall ? rows : cols;
-    p.one = p.m <= ONE_SIDE;
+    p.one = one_fits(p.n, p.m);
+    if (p.one) {                                  // (no scratch)
+        p.np = (int32_t)(ceil_div64(p.n, 64) * 64); p.mp = (int32_t)(ceil_div64(p.m, 64) * 64);
+        return p;
+    }
     const auto padded = [&](int64_t t) { return ceil_div64(p.n, t) * t * ceil_div64(p.m, t) * t * batch; };
     p.tile = padded(64) >= (int64_t)11264 * ps->num_cu && 4 * padded(128) <= 5 * padded(64) ? 128 : 64;
     if (!split && (p.n >= 4096 || half_of(ceil_div64(p.n, 256)) * batch >= ps->num_cu)) p.tile = 256;
     p.np = (int32_t)(ceil_div64(p.n, p.tile) * p.tile); p.mp = (int32_t)(ceil_div64(p.m, p.tile) * p.tile);
-    if (p.one) return p;                          // (no scratch)
     const int64_t blocks = ceil_div64((int64_t)rows * cols, 1024);
     p.blocks = (int32_t)(blocks < NORM_BLOCKS ? blocks : NORM_BLOCKS);
     const size_t size = split ? 4 : 2, nm = (size_t)batch * p.np * p.mp, nn = (size_t)batch * p.np * p.np * size;

@@ -101,6 +101,18 @@ def test_few_strong_directions_in_bfloat16(srv, batch, rows, cols, steps):
         assert err <= 2 * rounded + 2.0 ** -24, (i, err, rounded)
 
 
+@pytest.mark.parametrize("batch,rows,cols", [(1, 64, 256), (2, 256, 64), (1, 65, 256), (1, 64, 257), (2, 10, 250), (3, 129, 64), (300, 30, 40), (1000, 64, 64), (257, 100, 128)])
+def test_small_matrices_and_many_of_them(srv, batch, rows, cols):
+    """At the limits of what one workgroup takes; batches by which larger matrices would be cut into larger tiles."""
+    import torch
+    rng = np.random.default_rng(batch + rows + cols)
+    for kind in ("float32", "bfloat16"):
+        x = torch.from_numpy(gaussian(rng, batch, rows, cols)).cuda().to(getattr(torch, kind))
+        got = srv.muon_orthogonalize(x)
+        for i in {0, batch // 2, batch - 1}:
+            check(got[i].double().cpu().numpy(), x[i].double().cpu().numpy(), kind, 2.0 ** -12 if kind == "bfloat16" else 2.0 ** -24, f"{kind} {i}")
+
+
 @pytest.mark.parametrize("rows,cols", [(60, 60), (200, 90), (90, 300), (1030, 1030)])
 def test_every_matrix_of_a_batch_by_itself(srv, rows, cols):
     """Zeros, one direction, extreme magnitudes, infinities and NaN, side by side."""
