@@ -651,10 +651,11 @@ __global__ __launch_bounds__(256) void k_muon_join(MuonArgs a, int32_t shares) {
 // A workgroup of eight wavefronts has a matrix; of its frame, sides of multiples of 64, a wavefront has 64 x 32, as the sums of the
 // matrix instruction lie: two pieces of 32 x 32.  X stays in registers as 32-bit numbers; LDS has one operand of X - its rows for A = X X', then
 // its columns for P X - and A, then P.  The norm and, of a step, momentum and weights are read and written as they lie in registers.
-// What several launches per step cost - 5 us each for a few microseconds of products - is what this saves: 64 x 256 39 us instead of 80 to 90, 10 x 200 30
-// instead of 75, 16 of 100 x 100 45 instead of 105.  What is left is a chain of four meetings a step, with a product of 4 to 16 blocks of k, or a change of
-// parts in LDS, between two of them.  Larger thin matrices in slices of 128 or 256 columns, a launch per step that adds the slices' A, are
-// slower than the several launches: 128 x 1024 156 us instead of 108.
+// What several launches per step cost - 5 us each for a few microseconds of products - is what this saves.  32 bits, this way and by tiles: 64 x 256 39 us
+// and 74, 10 x 200 29 and 74, 16 of 100 x 100 45 and 83, 300 of 128 x 128 103 and 246; bf16 results, which have single numbers by tiles: 64 x 256 42 and 61,
+// 16 of 100 x 100 48 and 69.  What is left is a chain of four meetings a step, with a product of up to 16 blocks of k, or a change of parts in LDS,
+// between two of them.  Larger thin matrices in slices of 128 or 256 columns, with a launch per step that adds the slices' A, are slower than
+// by tiles: 128 x 1024 156 us instead of 108.
 constexpr int ONE_SIDE = 128, ONE_THREADS = 512;
 inline bool one_fits(int32_t n, int32_t m) { return m <= ONE_SIDE || (n <= 64 && m <= 256); }
 
@@ -827,10 +828,12 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 
 // ---- host -----------------------------------------------------------------------------------------------------------
 // Sides count as multiples of the tile's, 64, 128 or 256.  Tiles of 128 read a line of an operand half as often, tiles of 256 a quarter
-// as often, but few of them leave compute units idle.  Whole calls, tiles of 64 and of 128: 32 bits, 300 x 300 111 us and 151, 1024 x 1024 202 and
-// 261, two of them 292 and 320, 1500 x 2000 516 and 448, four of 1024 x 1024 458 and 431, 1024 x 4096 429 and 372, 4096 x 4096 5,086 and 4,486;
-// 32 of 300 x 300, which become 320 and 384, 199 and 292 - the line is at 2.9 million numbers, unless the larger tile makes them a quarter more.  16 bits, 128 and 256: 4096 x 4096 1,686 and 1,577, four of 2048 x 2048 926
-// and 975, 3000 x 3000 851 and 1,144.
+// as often, but few of them leave compute units idle, and they fill up more.  Whole calls, tiles of 64 and of 128: 32 bits, 300 x 300 111 us and 151,
+// 1024 x 1024 202 and 261, two of them 292 and 320, 1500 x 2000 516 and 448, four of 1024 x 1024 458 and 431, 1024 x 4096 429 and 372, 4096 x 4096 5,086
+// and 4,486; 32 of 300 x 300, which become 320 and 384, 199 and 292; bf16 results, 300 of 200 x 200 520 and 500, 100 of 300 x 700 545 and 671, 26 of
+// 1000 x 1010 1,535 and 1,133 - the line is at 2.9 million numbers, unless the larger tile makes them a quarter more.  Tiles of 128 and of 256, single numbers:
+// two of 4096 x 4096 3,520 and 3,320, 8192 x 8192 12,860 and 11,280, 5000 x 5000 3,475 and 3,160; 6000 x 6000, which become 6016 and 6144, 5,380 and
+// 5,508, 4200 x 4200 2,153 and 2,538; 64 of 1024 x 1024 2,557 and 2,757, 2000 x 8000 937 and 1,566.
 struct MuonPlan {
     int32_t batch, n, m, tile, np, mp, blocks;
     bool tall, split, one;
@@ -865,7 +868,7 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     }
     const auto padded = [&](int64_t t) { return ceil_div64(p.n, t) * t * ceil_div64(p.m, t) * t * batch; };
     p.tile = padded(64) >= (int64_t)11264 * ps->num_cu && 4 * padded(128) <= 5 * padded(64) ? 128 : 64;
-    if (!split && (p.n >= 4096 || half_of(ceil_div64(p.n, 256)) * batch >= ps->num_cu)) p.tile = 256;
+    if (!split && p.n >= 4096 && 50 * padded(256) <= 51 * padded(128)) p.tile = 256;
     p.np = (int32_t)(ceil_div64(p.n, p.tile) * p.tile); p.mp = (int32_t)(ceil_div64(p.m, p.tile) * p.tile);
     const int64_t blocks = ceil_div64((int64_t)rows * cols, 1024);
     p.blocks = (int32_t)(blocks < NORM_BLOCKS ? blocks : NORM_BLOCKS);

@@ -113,6 +113,23 @@ def test_small_matrices_and_many_of_them(srv, batch, rows, cols):
             check(got[i].double().cpu().numpy(), x[i].double().cpu().numpy(), kind, 2.0 ** -12 if kind == "bfloat16" else 2.0 ** -24, f"{kind} {i}")
 
 
+@pytest.mark.parametrize("batch,rows,cols,steps", [(1, 4300, 4340, 1), (2, 4340, 4300, 3), (1, 4100, 4400, 2)])
+def test_large_matrices_in_bfloat16(srv, batch, rows, cols, steps):
+    """A few directions a hundred times as strong as the others.  At most twice as far from the true result as that rounded to bfloat16 is."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(rows)
+    d = (torch.randn(batch, rows, cols, device="cuda", generator=g) + 100 * torch.randn(batch, rows, 1, device="cuda", generator=g)).to(torch.bfloat16)
+    got = srv.muon_orthogonalize(d, steps=steps)
+    for i in range(batch):
+        x = d[i].double() / (torch.linalg.norm(d[i].double()) + 1e-7)
+        for _ in range(steps):
+            a = x @ x.T
+            x = A * x + (B * a + C * a @ a) @ x
+        rounded, err = (float(torch.linalg.norm(t.double() - x) / torch.linalg.norm(x)) for t in (x.to(torch.bfloat16), got[i]))
+        print(f"  {i}: error {err:.2e}, of rounding alone {rounded:.2e}", flush=True)
+        assert err <= 2 * rounded, (i, err, rounded)
+
+
 @pytest.mark.parametrize("rows,cols", [(60, 60), (200, 90), (90, 300), (1030, 1030)])
 def test_every_matrix_of_a_batch_by_itself(srv, rows, cols):
     """Zeros, one direction, extreme magnitudes, infinities and NaN, side by side."""
