@@ -48,6 +48,9 @@ __global__ __launch_bounds__(256) void k_token_replies(TokenIds t, int32_t worke
 // ---- lookup ---------------------------------------------------------------------------------------------------------
 // The result in pieces of W values, P a row, a workgroup 256 * AHEAD consecutive pieces, a thread every 256th: its tokens,
 // then its pieces of the rows, are asked for together.  The first route.blocks workgroups count the statistics.
+// Memory bounds it: 65,537 tokens of 50,000, by rank, 512 numbers to bf16: 96 MB (the rows mentioned once, the result) in 20 us, 4.8 TB/s; with pieces of 4
+// instead of 8, whose stores are of 8 bytes, 25 us.  More than a few tokens are checked in a launch before it (4 us), so that a bad one leaves
+// the result as it was.
 template <class Out, int W, int AHEAD>
 __global__ __launch_bounds__(256) void k_emb_lookup(RouteArgs route, TokenIds t, uint32_t P, double inv_P, int64_t L, float scale, const float *val, Out *out,
                                                     int64_t stride, int32_t *err) {
@@ -162,6 +165,8 @@ __device__ __forceinline__ uint32_t emb_mentioned(const EmbSums &a, int64_t v0) 
 }
 
 // A wavefront per range and 64 pieces of W values; UN rows are on their way together.  The first workgroups count the statistics.
+// Memory bounds it where there are many terms: 262,144 of 512 bf16 numbers onto a gradient of 128,000, by rank: 268 MB of terms in any order, 200 MB of the
+// gradient, 119 us, 3.9 TB/s; AdaGrad of 65,536 49 us.  With 16,384 of 1024 (15 us) it is the chain of trips: tokens, rows, sums.
 template <class T, int W, int MODE>
 __global__ __launch_bounds__(256) void k_emb_sums(RouteArgs route, TokenIds t, EmbSums a, const int32_t *err) {
     constexpr int UN = MODE == EMB_ADAGRAD ? 8 : W >= 4 ? 8 : 16;
@@ -233,6 +238,9 @@ __global__ __launch_bounds__(256) void k_emb_sums(RouteArgs route, TokenIds t, E
 // Tokens whose terms fill more than one range: the workgroup of the range in which they start adds the sums of the ranges behind it, each
 // wavefront a quarter of them in order, and then the four.  blockIdx.y: which 64 pieces.  The other workgroups, of a gradient that is not added to,
 // clear the rows of tokens that are not mentioned meanwhile: the few trips to memory, one behind the other, of a join hide behind that.
+// 50,000 rows of 1024, 44,800 of them not mentioned: 184 MB in 29 us, 6.3 TB/s; without rows to clear, 4,096 ranges of 64 x 512, 17 us, most of it a frequent
+// token's thousands of ranges (8 or 16 wavefronts a range instead of 4: 25 and 55 us).  Clearing all of the gradient on a second stream beside
+// the sort costs more than it hides: 82 us instead of 60.
 constexpr int JOIN_AHEAD = 16;
 template <int W, int MODE>
 __global__ __launch_bounds__(256) void k_emb_join(EmbSums a, int64_t joins, const int32_t *err) {
@@ -292,7 +300,10 @@ __global__ __launch_bounds__(256) void k_emb_join(EmbSums a, int64_t joins, cons
 // positions that have it are the token's terms, in order.  They are added one after the other; more than FEW_OWN by the whole workgroup,
 // a sixteenth each, and then the sixteen.  Further workgroups clear the rows of tokens not mentioned, FEW_CLEAR each; the first ones count the
 // statistics.
-constexpr int FEW_THREADS = 1024, FEW_WAVES = FEW_THREADS / 64, FEW_OWN = 64, FEW_CLEAR = 64;
+// The launch and a few trips to memory bound it: 64 tokens of 128 numbers 6.5 us, 1,024 8 to 10 (of 5,000, bf16, evenly spread to as their rank),
+// where a sort and the sums take 11.4 and 14.  By 2,048 tokens the two meet: 11.9 us and 13.9 evenly spread, 14.4 and 13.9 by rank, a single
+// token, all of whose terms one workgroup adds, 38 and 18.  FEW_OWN 16: by rank 512 tokens 7.8 us and 1,024 10.0, with 64 13.7 and 13.7, with 8 7.9 and 10.0.
+constexpr int FEW_THREADS = 1024, FEW_WAVES = FEW_THREADS / 64, FEW_OWN = 16, FEW_CLEAR = 64;
 template <class T, int W, int MODE>
 __global__ __launch_bounds__(FEW_THREADS) void k_emb_few(RouteArgs route, TokenIds t, EmbSums a, int32_t *err) {
     constexpr size_t SUMS = (size_t)FEW_KEYS * 8, ALL = SUMS + (size_t)FEW_WAVES * 64 * W * 4;
@@ -465,7 +476,8 @@ int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, 
         grid = dim3((unsigned)((mode == EMB_GRAD ? ceil_div64(t.count, FEW_CLEAR) : 0) + route.blocks + ceil_div64(t.n, FEW_WAVES)), (unsigned)slices);
     } else {
         // ranges of 64 positions, shorter ones where those would be fewer wavefronts (of 256 values) than the compute units hold; by the
-        // number of tokens and the length of a row alone, so that a gradient that is added to gets the same sums
+        // number of tokens and the length of a row alone, so that a gradient that is added to gets the same sums (4,096 terms of 256: the whole call 15 us, with
+        // ranges of 64 33; 16,384 of 1024 39 and 51; 65,536 of 512 51 and 59)
         a.range = 64;
         while (a.range > 8 && ceil_div64(t.n, a.range) * ceil_div64(a.D, 256) < 16 * (int64_t)ps->num_cu) a.range /= 2;
         const int64_t nranges = ceil_div64(t.n, a.range);
