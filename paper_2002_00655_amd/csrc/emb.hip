@@ -134,7 +134,8 @@ template <int W> __device__ __forceinline__ void clear_row(float *p, int D) {
     for (int c = (threadIdx.x & 63) * V; c < D; c += 64 * V) store_vec<float, V>(p + c, Vec<float, V>{});
 }
 
-constexpr int CLEAR_ROWS = 16;                         // rows of tokens not mentioned that a wavefront clears
+constexpr int CLEAR_ROWS = 16;                         // rows of tokens not mentioned that a wavefront clears at a time
+constexpr int64_t CLEARERS = (int64_t)1 << 20;         // workgroups at most that clear rows
 constexpr uint64_t NOKEY = ~0ull;                      // no token looks like this
 
 // Which of the rows v0 .. v0 + CLEAR_ROWS - 1 are mentioned, a bit each, the same in all lanes: their first place among the sorted tokens, 64 places
@@ -257,12 +258,12 @@ __global__ __launch_bounds__(256) void k_emb_join(EmbSums a, int64_t joins, cons
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (MODE == EMB_GRAD && blockIdx.x >= joins) {
         if (blockIdx.y != 0 || stop) return;
-        const int64_t v0 = ((blockIdx.x - joins) * 4 + wave) * CLEAR_ROWS;
-        if (v0 >= a.count) return;
-        const uint32_t mentioned = emb_mentioned(a, v0);
-        for (int i = 0; i < CLEAR_ROWS && v0 + i < a.count; ++i)
-            if (!(mentioned >> i & 1))
-                clear_row<W>(a.to + (v0 + i) * a.L, a.D);
+        for (int64_t v0 = ((blockIdx.x - joins) * 4 + wave) * CLEAR_ROWS; v0 < a.count; v0 += (gridDim.x - joins) * 4 * CLEAR_ROWS) {
+            const uint32_t mentioned = emb_mentioned(a, v0);
+            for (int i = 0; i < CLEAR_ROWS && v0 + i < a.count; ++i)
+                if (!(mentioned >> i & 1))
+                    clear_row<W>(a.to + (v0 + i) * a.L, a.D);
+        }
         return;
     }
     __shared__ Vec<float, W> sums[4][64];
@@ -325,7 +326,6 @@ __global__ __launch_bounds__(FEW_THREADS) void k_emb_few(RouteArgs route, TokenI
     Vec<float, W> *sums = reinterpret_cast<Vec<float, W> *>(mem + SUMS);
     const int n = (int)t.n;
     if (threadIdx.x == 0) many = 0;
-    if (threadIdx.x < FEW_CLEAR) named[threadIdx.x] = false;
     if (few_tokens_off<2>(t, err, [&](int64_t p, int64_t id) { lk[p] = id == t.pad ? NOKEY : (uint64_t)id; })) return;
     int block = blockIdx.x;
     if constexpr (MODE == EMB_ADAGRAD) {
@@ -341,13 +341,17 @@ __global__ __launch_bounds__(FEW_THREADS) void k_emb_few(RouteArgs route, TokenI
     if constexpr (MODE == EMB_GRAD) {
         if (block >= groups) {
             if (blockIdx.y != 0) return;
-            const int64_t v0 = (int64_t)(block - groups) * FEW_CLEAR;
-            for (int p = threadIdx.x; p < n; p += FEW_THREADS)
-                if (lk[p] - (uint64_t)v0 < FEW_CLEAR) named[lk[p] - (uint64_t)v0] = true;
-            __syncthreads();
-            for (int r = wave; r < FEW_CLEAR && v0 + r < a.count; r += FEW_WAVES)
-                if (!named[r])
-                    clear_row<W>(a.to + (v0 + r) * a.L, a.D);
+            for (int64_t v0 = (int64_t)(block - groups) * FEW_CLEAR; v0 < a.count; v0 += (int64_t)((int)gridDim.x - groups) * FEW_CLEAR) {
+                if (threadIdx.x < FEW_CLEAR) named[threadIdx.x] = false;
+                __syncthreads();
+                for (int p = threadIdx.x; p < n; p += FEW_THREADS)
+                    if (lk[p] - (uint64_t)v0 < FEW_CLEAR) named[lk[p] - (uint64_t)v0] = true;
+                __syncthreads();
+                for (int r = wave; r < FEW_CLEAR && v0 + r < a.count; r += FEW_WAVES)
+                    if (!named[r])
+                        clear_row<W>(a.to + (v0 + r) * a.L, a.D);
+                __syncthreads();
+            }
             return;
         }
     }
@@ -457,6 +461,10 @@ int lookup(dpaps_ps *ps, const RouteArgs &a, const TokenIds &t, int32_t dim, flo
         const int64_t blocks = a.blocks + ceil_div64(t.n * P, 256 * AHEAD);                                                                       \
         if (blocks >= ((int64_t)1 << 24)) { ps->last_error = "emb_lookup: the result is too large for one launch"; return PS_ELIMIT; }            \
         const unsigned grid = (unsigned)blocks;                                                                                                   \
+        if (t.n > FEW_KEYS) {                                                                                                                     \
+            k_emb_check<<<grid_for(t.n, 256), 256, 0, st>>>(t, ps->err);                                                                          \
+            PS_HIP(ps, hipGetLastError());                                                                                                        \
+        }                                                                                                                                         \
         k_emb_lookup<Out, W, AHEAD><<<grid, 256, 0, st>>>(a, t, P, 1.0 / P, ps->L, scale, ps->val, out, stride, ps->err);                  \
     } while (0)
     if (sizeof(Out) == 2 && fits(8)) LOOKUP(8, 2);
@@ -479,10 +487,12 @@ int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, 
     const int64_t slices = (a.D / W + 63) / 64;
     a.n = t.n; a.count = t.count; a.first = t.first;
     const bool few = t.n <= FEW_KEYS;
+    // workgroups that clear `rows` rows at a time (a launch has less than 2^32 threads)
+    const auto clearers = [&](int64_t rows) { const int64_t all = ceil_div64(t.count, rows); return all < CLEARERS ? all : CLEARERS; };
     dim3 grid, join;
     int64_t joins = 0;
     if (few) {
-        grid = dim3((unsigned)((mode == EMB_GRAD ? ceil_div64(t.count, FEW_CLEAR) : 0) + route.blocks + ceil_div64(t.n, FEW_WAVES)), (unsigned)slices);
+        grid = dim3((unsigned)((mode == EMB_GRAD ? clearers(FEW_CLEAR) : 0) + route.blocks + ceil_div64(t.n, FEW_WAVES)), (unsigned)slices);
     } else {
         // ranges of 64 positions, shorter ones where those would be fewer wavefronts (of 256 values) than the compute units hold; by the
         // number of tokens and the length of a row alone, so that a gradient that is added to gets the same sums (4,096 terms of 256: the whole call 15 us, with
@@ -502,7 +512,7 @@ int sums_of(dpaps_ps *ps, const RouteArgs &route, const TokenIds &t, EmbSums a, 
         a.part = (float *)(ws + off_part);
         joins = nranges - 1;
         grid = dim3((unsigned)(route.blocks + ceil_div64(nranges, 4)), (unsigned)slices);
-        join = dim3((unsigned)(joins + (mode == EMB_GRAD ? ceil_div64(t.count, 4 * CLEAR_ROWS) : 0)), (unsigned)slices);
+        join = dim3((unsigned)(joins + (mode == EMB_GRAD ? clearers(4 * CLEAR_ROWS) : 0)), (unsigned)slices);
     }
     if (grid.x == 0) return PS_OK;
 #define SUMS(T, WW, MODE)                                                                     \
@@ -563,10 +573,6 @@ extern "C" int emb_lookup(ps_handle ps, int32_t worker, int64_t first_key, int64
     int rc = token_ids(ps, first_key, num_tokens, true, tokens, token_type, n, pad_token, &t);
     if (rc || n == 0) return rc;
     hipStream_t st = (hipStream_t)stream;
-    if (n > FEW_KEYS) {
-        k_emb_check<<<grid_for(n, 256), 256, 0, st>>>(t, ps->err);
-        PS_HIP(ps, hipGetLastError());
-    }
     RouteArgs a{};
     if (!ps->loc) a = dpaps_route_args(ps, worker, n, PS_STAT_PULL_LOCAL, PS_STAT_PULL_REMOTE, -1, -1, st);
     if (out_type == PS_F32) rc = lookup(ps, a, t, dim, scale, (float *)out, out_type, out_stride, st);

@@ -153,6 +153,21 @@ def test_terms_are_added_in_the_order_of_their_positions(n):
     assert np.array_equal(got, ((d[:, 0] + d[:, 1]) + d[:, 2]) + d[:, 3])
 
 
+@pytest.mark.parametrize("n", [0, 100, 3000])
+def test_gradient_of_a_vocabulary_of_many_millions(n):
+    """More rows to clear than one workgroup each takes; the rest of a row of one number."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    V = 70_000_013
+    rng = np.random.default_rng(n)
+    tokens = rng.choice(V, n, replace=False) if n else np.zeros(0, np.int64)
+    tokens[:2] = (0, V - 1) if n else ()
+    dout = rng.standard_normal((n, 1)).astype(np.float32)
+    got = P.ParameterServer(1, 1, 1).emb_grad(torch.from_numpy(tokens).cuda(), torch.from_numpy(dout).cuda(), V, grad=torch.full((V, 1), 9.0, device="cuda"))
+    want = torch.zeros(V, 1, device="cuda").index_add_(0, torch.from_numpy(tokens).cuda(), torch.from_numpy(dout).cuda())
+    assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("what", ["one token", "all padding", "every token once", "two tokens in turn"])
 @pytest.mark.parametrize("n,D", [(65, 16), (4096, 128), (30_000, 72)])
 def test_gradient_of_extreme_batches(what, n, D):
