@@ -509,6 +509,83 @@ __global__ __launch_bounds__(256) void k_muon_join_small(MuonArgs a, int32_t sha
     write_tile<KS, KIND, MUON_GRAM>(a, p, p.ti * 64, p.tj * 64, lds[0], group);
 }
 
+// Thin matrices, A of 64 N x 64 N: the polynomial and P X in one launch.  A workgroup has 64 x 64 of P X; it works out the 64 rows of P that this takes by itself
+// - a wavefront 32 columns of P, or 32 x 32 -, into LDS, and goes on as k_muon_small, with its part of X on the way meanwhile.  Calls in 32 bits, this way and
+// with a launch for each: 10 x 300 60 us and 77, 127 x 333 81 and 92, 128 x 1024 96 and 108, 64 x 4096 89 and 106, 16 of 128 x 1024 125 and 135; where
+// there is work for all compute units P's rows worked out m / 64 times cost what the launch saves: 128 x 20000 204 and 202, 256 of 64 x 1024 331 and 325.
+template <int KIND, int MODE, int N>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_muon_poly_apply(MuonArgs a, const int32_t *err) {
+    constexpr int KS = 4, L = left_parts(KIND), R = right_parts(KIND), BLOCKS = 4 * N;
+    __shared__ __attribute__((aligned(16))) float lds[KS][64 * SUMS_LD];      // P's rows first, then the sums
+    static_assert(64 * 64 * N * L * 2 <= sizeof(lds));
+    f16_t *const rows = reinterpret_cast<f16_t *>(&lds[0][0]);
+    const int lane = threadIdx.x & 63, group = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
+    const Place p = place_of<MODE>(a, blockIdx.x, gridDim.x);
+    const f16_t *const A = a.lhs + p.b * a.lhs_size, *const x = a.rhs + p.b * a.rhs_size;
+    half8 rf[N][2][R];
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int e = 0; e < R; ++e) rf[t][f][e] = *reinterpret_cast<const half8 *>(x + ((int64_t)(p.tj * 2 + f) * BLOCKS + group + KS * t) * (512 * R) + e * 512 + lane * 8);
+    // columns 32 c .. of P, rows 32 (r + i) .. of the workgroup's: the matrix instruction gives them with rows and columns exchanged
+    const int c = N == 2 ? group : group & 1, r = N == 2 ? 0 : group >> 1;
+    floatx16 sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = floatx16{};
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        half8 lf[L], af[N][L];
+#pragma unroll
+        for (int e = 0; e < L; ++e) {
+            lf[e] = *reinterpret_cast<const half8 *>(A + (c * BLOCKS + b) * (512 * L) + e * 512 + lane * 8);
+#pragma unroll
+            for (int i = 0; i < N; ++i) af[i][e] = *reinterpret_cast<const half8 *>(A + ((p.ti * 2 + r + i) * BLOCKS + b) * (512 * L) + e * 512 + lane * 8);
+        }
+#pragma unroll
+        for (int e = 2 * (L - 1); e >= 0; --e)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lf[e == 2 ? L - 1 : 0], af[i][e == 1 ? L - 1 : 0], sum[i], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int row = (r + i) * 32 + l32, I = p.ti * 64 + row, k = c * 32 + 8 * g + 4 * h;
+            const f16_t *from = A + place8<L == 2>(I, k & ~7, 64 * N) + (k & 4);
+            const half4 hi = *reinterpret_cast<const half4 *>(from);
+            half4 lo = {};
+            if constexpr (L == 2) lo = *reinterpret_cast<const half4 *>(from + 512);
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float was = L == 2 ? (float)hi[e] + (float)lo[e] : (float)hi[e];
+                v[e] = sum[i][4 * g + e] * (NS_C * P_SCALE / (G_SCALE * G_SCALE)) + was * (NS_B * P_SCALE / G_SCALE) + (I == k + e ? NS_A * P_SCALE : 0.0f);
+            }
+            const Parts p0 = parts_of<L == 2>(v[0], v[1]), p1 = parts_of<L == 2>(v[2], v[3]);
+            f16_t *to = rows + place8<L == 2>(row, k & ~7, 64 * N) + (k & 4);
+            *reinterpret_cast<half4 *>(to) = __builtin_shufflevector(p0.hi, p1.hi, 0, 1, 2, 3);
+            if constexpr (L == 2) *reinterpret_cast<half4 *>(to + 512) = __builtin_shufflevector(p0.lo, p1.lo, 0, 1, 2, 3);
+        }
+    __syncthreads();
+    Sums<2, 2, KIND> s;
+    s.clear();
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        half8 lf[2][L];
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int e = 0; e < L; ++e) lf[f][e] = *reinterpret_cast<const half8 *>(rows + (f * BLOCKS + group + KS * t) * (512 * L) + e * 512 + lane * 8);
+        s.add(lf, rf[t]);
+    }
+    s.cut();
+    if (MODE == MUON_STEP && *(volatile const int32_t *)err) return;  // (set before this launch: the same for all)
+    __syncthreads();                                                          // (P has been read: its place is used again)
+    put_tile<2, 2, KS, KIND, MODE>(a, p, s.all(), p.ti * 64, p.tj * 64, lds[group], lds[0], group);
+}
+
 // until at most N of this wavefront's loads are on their way and all it has asked of LDS is there, then until all wavefronts are so far
 template <int N> __device__ __forceinline__ void wait_and_meet() {
     asm volatile("" ::: "memory");
@@ -665,7 +742,7 @@ __global__ __launch_bounds__(256) void k_muon_join(MuonArgs a, int32_t shares) {
 // and 74, 10 x 200 29 and 74, 16 of 100 x 100 45 and 83, 300 of 128 x 128 103 and 246; bf16 results, which have single numbers by tiles: 64 x 256 42 and 61,
 // 16 of 100 x 100 48 and 69.  What is left is a chain of four meetings a step, with a product of up to 16 blocks of k, or a change of parts in LDS,
 // between two of them.  Larger thin matrices in slices of 128 or 256 columns, with a launch per step that adds the slices' A, are slower than
-// by tiles: 128 x 1024 156 us instead of 108.
+// by tiles: 128 x 1024 156 us instead of 96.
 constexpr int ONE_SIDE = 128, ONE_THREADS = 512;
 inline bool one_fits(int32_t n, int32_t m) { return m <= ONE_SIDE || (n <= 64 && m <= 256); }
 
@@ -860,7 +937,8 @@ int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t K) {
     return s < 2 ? 1 : (int)s;
 }
 // The same for tiles of 64, a long sum: at least SMALL_TURNS blocks of k for each wavefront.  A share more costs the join, 3 us, and saves a part of the sum's
-// time: 10 x 4096 in 32 bits 101 us instead of 211, 128 x 1024 106 instead of 117; 128 x 512, with two shares, 102 instead of 97.
+// time: 10 x 4096 in 32 bits 101 us instead of 211, 128 x 1024 106 instead of 117; 128 x 512, with two shares, 102 instead of 97
+// (with the polynomial in a launch of its own).
 int small_shares(const dpaps_ps *ps, int64_t tiles, int32_t K) {
     const int64_t by_K = K / 64 / SMALL_TURNS, most = ps->num_cu / tiles;
     if (by_K < 4) return 1;
@@ -972,6 +1050,18 @@ int whole_product(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
     }
 }
 
+// the polynomial and P X of thin matrices
+template <int KIND, int MODE>
+int poly_apply(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
+    a.tiles = a.tiles_i * a.tiles_j;
+    a.shares = 1;
+    const unsigned grid = (unsigned)((int64_t)a.tiles * batch);
+    if (a.tiles_i == 1) k_muon_poly_apply<KIND, MODE, 1><<<grid, 256, 0, st>>>(a, ps->err);
+    else k_muon_poly_apply<KIND, MODE, 2><<<grid, 256, 0, st>>>(a, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+
 template <int TILE, bool PAIR>
 int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t steps, hipStream_t st) {
     constexpr int KIND = PAIR ? SPLIT : SINGLE;
@@ -983,6 +1073,7 @@ int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t s
     else if (in.type == PS_BF16) k_muon_scale<bf16_t, PAIR><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
     else k_muon_scale<f16_t, PAIR><<<grid, 256, 0, st>>>(in, p.tall, p.np, p.mp, x, xt);
     PS_HIP(ps, hipGetLastError());
+    const bool thin = TILE == 64 && p.np <= 128;
     for (int s = 0; s < steps; ++s) {
         MuonArgs a{};
         a.tiles_i = p.np / TILE; a.tiles_j = p.mp / TILE;
@@ -990,21 +1081,36 @@ int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t s
         a.lhs = a.rhs = x; a.lhs_size = a.rhs_size = nm * S; a.K = p.mp; a.out = g; a.out_ld = p.np; a.out_size = nn;
         int rc = half_product<TILE, KIND, MUON_GRAM>(ps, a, p.batch, st);
         if (rc) return rc;
-        a.lhs = a.rhs = g; a.lhs_size = a.rhs_size = nn; a.K = p.np; a.out = q;
-        rc = half_product<TILE, KIND, MUON_POLY>(ps, a, p.batch, st);
-        if (rc) return rc;
+        if (!thin) {
+            a.lhs = a.rhs = g; a.lhs_size = a.rhs_size = nn; a.out = q;
+            a.K = p.np;
+            rc = half_product<TILE, KIND, MUON_POLY>(ps, a, p.batch, st);
+            if (rc) return rc;
+        }
         const bool end = s + 1 == steps, pairs = !PAIR && s < PAIR_STEPS;
         MuonArgs b = end ? last : a;
         b.tiles_i = a.tiles_i; b.tiles_j = a.tiles_j; b.K = p.np;
         // (X transposed is read by other workgroups while it is written: into the other place; X itself is not)
-        b.lhs = q; b.lhs_size = nn; b.rhs = xt; b.rhs_size = nm * 2;
+        b.lhs = thin ? g : q; b.lhs_size = nn; b.rhs = xt; b.rhs_size = nm * 2;
         b.out = x; b.out_ld = p.mp; b.out_size = nm * S;
         b.out_t = xt_next; b.out_t_ld = p.np; b.out_t_size = nm * 2; b.out_t_pair = s + 1 < PAIR_STEPS;
+        const auto apply = [&](auto kind, auto mode) {
+            if constexpr (TILE == 64)
+                if (thin) return poly_apply<decltype(kind)::value, decltype(mode)::value>(ps, b, p.batch, st);
+            return whole_product<TILE, decltype(kind)::value, decltype(mode)::value>(ps, b, p.batch, st);
+        };
+        const std::integral_constant<int, MUON_APPLY> more{};
+        const std::integral_constant<int, MUON_LAST> result{};
         if constexpr (PAIR) {
-            if (!end) rc = whole_product<TILE, SPLIT, MUON_APPLY>(ps, b, p.batch, st);
-            else rc = last.val ? whole_product<TILE, SPLIT, MUON_STEP>(ps, b, p.batch, st) : whole_product<TILE, SPLIT, MUON_LAST>(ps, b, p.batch, st);
-        } else if (pairs) rc = end ? whole_product<TILE, RIGHT_SPLIT, MUON_LAST>(ps, b, p.batch, st) : whole_product<TILE, RIGHT_SPLIT, MUON_APPLY>(ps, b, p.batch, st);
-        else rc = end ? whole_product<TILE, SINGLE, MUON_LAST>(ps, b, p.batch, st) : whole_product<TILE, SINGLE, MUON_APPLY>(ps, b, p.batch, st);
+            const std::integral_constant<int, SPLIT> split{};
+            rc = !end ? apply(split, more) : last.val ? apply(split, std::integral_constant<int, MUON_STEP>{}) : apply(split, result);
+        } else if (pairs) {
+            const std::integral_constant<int, RIGHT_SPLIT> right{};
+            rc = end ? apply(right, result) : apply(right, more);
+        } else {
+            const std::integral_constant<int, SINGLE> single{};
+            rc = end ? apply(single, result) : apply(single, more);
+        }
         if (rc) return rc;
         f16_t *const t = xt; xt = xt_next; xt_next = t;
     }
