@@ -9,8 +9,9 @@
 //   as pairs   the sum of two fp16 numbers, high + low: 11 bits each and a sign between them, an error of 2^-23 of the number at most;
 //              a product is high high + high low + low high (what is left out is 2^-22 of it at most, 2^-24 as a rule): three instructions;
 //   single     as one fp16 number: an error of 2^-11 at most, an eighth of what rounding to bf16 costs.
-// Pairs throughout for results of 32 bits and of fp16, and where one launch does it all.  Of other bf16 results all numbers are single, except X where the
-// first two steps multiply it by P: there an error of X goes into all directions alike, and the steps raise the weak ones by 3.4 each.
+// Pairs throughout for results of 32 bits and of fp16, where one launch does it all, and where A is at most 64 x 64: the error of a few numbers of P is that of
+// all columns of X, so with single ones up to twice or, of 4 x 376, three times the rounding of a bf16 result (of 65 to 128 rows 1.2 times).  Of other
+// bf16 results all numbers are single, except X where the first two steps multiply it by P: there an error of X goes into all directions alike, and the steps raise the weak ones by 3.4 each.
 // Matrices with four directions 30 times as strong as the others are off by 0.008 of their norm without that, 0.002 with it (the rounding of the result:
 // 0.0017); pairs in the other products, or in later steps, change less than 0.0003.  It costs two instructions instead of one in two of fifteen products:
 // two of 4096 x 4096 3.32 ms instead of 2.84.  Directions 1,000 times as strong leave 0.011 (products of bf16 numbers: 0.3 to 1); pairs throughout, as
@@ -928,6 +929,7 @@ struct MuonPlan {
 };
 inline int64_t half_of(int64_t t) { return t * (t + 1) / 2; }
 constexpr int PAIR_STEPS = 2;                    // of single numbers, the first steps, which read X as pairs
+constexpr int PAIR_SIDE = 64;                    // pairs throughout where A is at most so large
 constexpr int MOST_SHARES = 8, TURNS_AT_LEAST = 2, SMALL_SHARES = 16, SMALL_TURNS = 4;
 // Workgroups that share a tile's sum over k, where there are fewer tiles than compute units.
 int shares_of(const dpaps_ps *ps, int64_t tiles, int32_t K) {
@@ -1056,8 +1058,8 @@ int poly_apply(dpaps_ps *ps, MuonArgs a, int32_t batch, hipStream_t st) {
     a.tiles = a.tiles_i * a.tiles_j;
     a.shares = 1;
     const unsigned grid = (unsigned)((int64_t)a.tiles * batch);
-    if (a.tiles_i == 1) k_muon_poly_apply<KIND, MODE, 1><<<grid, 256, 0, st>>>(a, ps->err);
-    else k_muon_poly_apply<KIND, MODE, 2><<<grid, 256, 0, st>>>(a, ps->err);
+    if (a.tiles_i == 2) k_muon_poly_apply<KIND, MODE, 2><<<grid, 256, 0, st>>>(a, ps->err);
+    else if constexpr (KIND == SPLIT) k_muon_poly_apply<KIND, MODE, 1><<<grid, 256, 0, st>>>(a, ps->err);     // (see PAIR_SIDE)
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
@@ -1181,7 +1183,7 @@ extern "C" int muon_orthogonalize(ps_handle ps, int32_t batch, int32_t rows, int
     if (batch == 0 || rows == 0 || cols == 0) return PS_OK;
     if (!in || !out || in_ld < cols || out_ld < cols) return PS_EINVAL;
     if (!sizes_allowed(batch, rows, cols)) return PS_ELIMIT;
-    const MuonPlan p = muon_plan(ps, batch, rows, cols, out_type != PS_BF16, false);
+    const MuonPlan p = muon_plan(ps, batch, rows, cols, out_type != PS_BF16 || (rows < cols ? rows : cols) <= PAIR_SIDE, false);
     const int rc = dpaps_ws_reserve(ps, p.bytes);
     if (rc) return rc;
     MuonIn a{};
