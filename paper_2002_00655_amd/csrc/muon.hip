@@ -9,13 +9,13 @@
 //   as pairs   the sum of two fp16 numbers, high + low: 11 bits each and a sign between them, an error of 2^-23 of the number at most;
 //              a product is high high + high low + low high (what is left out is 2^-22 of it at most, 2^-24 as a rule): three instructions;
 //   single     as one fp16 number: an error of 2^-11 at most, an eighth of what rounding to bf16 costs.
-// Pairs throughout for results of 32 bits and of fp16, where one launch does it all, and where A is at most 64 x 64: the error of a few numbers of P is that of
-// all columns of X, so with single ones up to twice or, of 4 x 376, three times the rounding of a bf16 result (of 65 to 128 rows 1.2 times).  Of other
-// bf16 results all numbers are single, except X where the first two steps multiply it by P: there an error of X goes into all directions alike, and the steps raise the weak ones by 3.4 each.
-// Matrices with four directions 30 times as strong as the others are off by 0.008 of their norm without that, 0.002 with it (the rounding of the result:
-// 0.0017); pairs in the other products, or in later steps, change less than 0.0003.  It costs two instructions instead of one in two of fifteen products:
-// two of 4096 x 4096 3.32 ms instead of 2.84.  Directions 1,000 times as strong leave 0.011 (products of bf16 numbers: 0.3 to 1); pairs throughout, as
-// for a result of 32 bits, would take 8.9 ms.
+// Pairs throughout for results of 32 bits and of fp16, where one launch does it all, and where A is at most 64 x 64: the error of one of a few numbers of P
+// is that of all columns of X, so single ones cost up to twice or, of 4 x 376, three times the rounding of a bf16 result (of 65 to 128 rows 1.2 times).
+// Of other bf16 results all numbers are single, except X where the first two steps multiply it by P: there an error of X goes into all directions
+// alike, and the steps raise the weak ones by 3.4 each.  Matrices with four directions 30 times as strong as the others are off by 0.008 of their
+// norm without that, 0.002 with it (the rounding of the result: 0.0017); pairs in the other products, or in later steps, change less than 0.0003.  It
+// costs two instructions instead of one in two of fifteen products: two of 4096 x 4096 3.32 ms instead of 2.84.  Directions 1,000 times as strong
+// leave 0.011 (products of bf16 numbers: 0.3 to 1); pairs throughout, as for a result of 32 bits, would take 8.9 ms.
 // fp16 holds few magnitudes, so every number is scaled by a power of two: the spectral norms of X, A and P are at most 1.21,
 // 1.46 and 3.45 whatever D is (p of [0, 1.21] stays below 1.21), and so is every element; scaled they fill the
 // upper end of the type, and what is lost at the lower end is 2^-39 of the norm or less.
@@ -306,7 +306,8 @@ __device__ __forceinline__ void write_tile(const MuonArgs &a, const Place &p, in
                 };
                 if constexpr (MODE >= MUON_LAST) {
                     // eight rows at a time, eight lanes a row; of a step the weights of all of them first
-                    const int R0 = (turned ? gj : gi) + group * 8 + (lane >> 3), c = (lane & 7) * 8, C = (turned ? gi : gj) + c, height = turned ? a.m : a.n, left = (turned ? a.n : a.m) - C;
+                    const int R0 = (turned ? gj : gi) + group * 8 + (lane >> 3), c = (lane & 7) * 8, C = (turned ? gi : gj) + c;
+                    const int height = turned ? a.m : a.n, left = (turned ? a.n : a.m) - C;
                     const auto at = [&](int q) { return (q * KS * 8 + group * 8 + (lane >> 3)) * SUMS_LD + c; };
                     if constexpr (MODE == MUON_STEP) {
                         float w[8 / KS][8];
@@ -435,7 +436,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const Place p = place_of<MODE>(a, blockIdx.x, gridDim.x);
     const int i0 = p.ti * 64, j0 = p.tj * 64, blocks = a.K >> 4, turns = blocks / KS;             // (sides are multiples of 64)
     const int first = turns * p.share / a.shares, cnt = turns * (p.share + 1) / a.shares - first, block0 = first * KS + group;
-    const f16_t *l = a.lhs + p.b * a.lhs_size + ((int64_t)(i0 >> 5) * blocks + block0) * (512 * L), *r = a.rhs + p.b * a.rhs_size + ((int64_t)(j0 >> 5) * blocks + block0) * (512 * R);
+    const f16_t *l = a.lhs + p.b * a.lhs_size + ((int64_t)(i0 >> 5) * blocks + block0) * (512 * L);
+    const f16_t *r = a.rhs + p.b * a.rhs_size + ((int64_t)(j0 >> 5) * blocks + block0) * (512 * R);
     const int64_t rows32 = (int64_t)blocks * 512;                              // elements to the next 32 rows, of a part
     half8 lf[DEPTH][2][L], rf[DEPTH][2][R];
     const auto load = [&](half8 (&x)[2][L], half8 (&y)[2][R], int t) {
