@@ -355,8 +355,8 @@ int emb_adagrad_step(ps_handle ps, int32_t worker, int64_t first_key, int64_t nu
  * are in_ld and out_ld >= cols elements apart.  A zero matrix stays zero; one that holds an infinity or no number becomes NaN, the others do not.
  * The products are carried out with numbers of 23 bits where the result has type PS_F32 or PS_F16, or one side is at most 64, or both
  * at most 128; where it is rounded to PS_BF16 (8 bits), else, with numbers of 11 bits, but for X in the first two steps, which has 23.  Sums are
- * in 32 bits.  (A PS_BF16 result is off by 0.0017 to 0.002 of its norm, by up to 0.011 where a few directions are 100 or more times as strong as all
- * others.)  1 <= steps <= 100, eps >= 0; the server's values have no part in it.  `out` must not overlap `in`.  Limits (PS_ELIMIT): sides of
+ * in 32 bits.  (A PS_BF16 result is off by 0.0017 to 0.002 of its norm, by up to 0.011 where some singular values are hundreds of times all
+ * others; a PS_F32 one by 2e-6, and 1e-4 there.)  1 <= steps <= 100, eps >= 0; the server's values have no part in it.  `out` must not overlap `in`.  Limits (PS_ELIMIT): sides of
  * PS_MUON_MAX_SIDE, PS_MUON_MAX_BATCH matrices.  Scratch: 20 bytes per element of the matrices (sides count as multiples of 64, 128
  * or 256) and up to 64 MiB, none where the sides are at most 128 and
  * 128, or 64 and 256; grown as needed. */

@@ -12,10 +12,10 @@
 // Pairs throughout for results of 32 bits and of fp16, where one launch does it all, and where A is at most 64 x 64: the error of one of a few numbers of P
 // is that of all columns of X, so single ones cost up to twice or, of 4 x 376, three times the rounding of a bf16 result (of 65 to 128 rows 1.2 times).
 // Of other bf16 results all numbers are single, except X where the first two steps multiply it by P: there an error of X goes into all directions
-// alike, and the steps raise the weak ones by 3.4 each.  Matrices with four directions 30 times as strong as the others are off by 0.008 of their
+// alike, and the steps raise the weak ones by 3.4 each.  Matrices with four singular values 150 to 240 times the others are off by 0.008 of their
 // norm without that, 0.002 with it (the rounding of the result: 0.0017); pairs in the other products, or in later steps, change less than 0.0003.  It
-// costs two instructions instead of one in two of fifteen products: two of 4096 x 4096 3.32 ms instead of 2.84.  Directions 1,000 times as strong
-// leave 0.011 (products of bf16 numbers: 0.3 to 1); pairs throughout, as for a result of 32 bits, would take 8.9 ms.
+// costs two instructions instead of one in two of fifteen products: two of 4096 x 4096 3.32 ms instead of 2.84.  Ratios of some
+// thousands leave 0.011 (products of bf16 numbers: 0.3 to 1); pairs throughout, as for a result of 32 bits, would take 8.9 ms.
 // fp16 holds few magnitudes, so every number is scaled by a power of two: the spectral norms of X, A and P are at most 1.21,
 // 1.46 and 3.45 whatever D is (p of [0, 1.21] stays below 1.21), and so is every element; scaled they fill the
 // upper end of the type, and what is lost at the lower end is 2^-39 of the norm or less.
