@@ -354,9 +354,12 @@ int emb_adagrad_step(ps_handle ps, int32_t worker, int64_t first_key, int64_t nu
  * (X' X and from the right where rows > cols, which is the same matrix).  Matrix i starts at row i * rows of `in` and `out`, whose rows
  * are in_ld and out_ld >= cols elements apart.  A zero matrix stays zero; one that holds an infinity or no number becomes NaN, the others do not.
  * The products are carried out with numbers of 23 bits where the result has type PS_F32 or PS_F16, or one side is at most 64, or both
- * at most 128; where it is rounded to PS_BF16 (8 bits), else, with numbers of 11 bits, but for X in the first two steps, which has 23.  Sums are
- * in 32 bits.  (A PS_BF16 result is off by 0.0017 to 0.002 of its norm, by up to 0.011 where some singular values are hundreds of times all
- * others; a PS_F32 one by 2e-6, and 1e-4 there.)  1 <= steps <= 100, eps >= 0; the server's values have no part in it.  `out` must not overlap `in`.  Limits (PS_ELIMIT): sides of
+ * at most 128; where it is rounded to PS_BF16 (8 bits), else, with numbers of 11 bits, but for X where all but the last two steps (in the first
+ * two, of fewer than four) multiply it, which has 23.  Sums are in 32 bits.  Relative to its norm, a PS_BF16 result is off by 0.0017 to 0.002 and a PS_F32
+ * one by 2e-6 after five steps.  Where some singular values are far above all others, what rounding leaves in the weak directions is raised by 3.4 in every
+ * step that follows: there a PS_BF16 result is off by up to 0.005, and either by up to 2^-21 3.4445^steps (2e-4 of five steps, 0.003 of seven, 0.1 of
+ * ten) beside that, as products in 32 bits are.  A caller who wants a PS_BF16 result of products of 23 bits throughout rounds a PS_F32 one.
+ * 1 <= steps <= 100, eps >= 0; the server's values have no part in it.  `out` must not overlap `in`.  Limits (PS_ELIMIT): sides of
  * PS_MUON_MAX_SIDE, PS_MUON_MAX_BATCH matrices.  Scratch: 20 bytes per element of the matrices (sides count as multiples of 64, 128
  * or 256) and up to 64 MiB, none where the sides are at most 128 and
  * 128, or 64 and 256; grown as needed. */

@@ -11,11 +11,13 @@
 //   single     as one fp16 number: an error of 2^-11 at most, an eighth of what rounding to bf16 costs.
 // Pairs throughout for results of 32 bits and of fp16, where one launch does it all, and where A is at most 64 x 64: the error of one of a few numbers of P
 // is that of all columns of X, so single ones cost up to twice or, of 4 x 376, three times the rounding of a bf16 result (of 65 to 128 rows 1.2 times).
-// Of other bf16 results all numbers are single, except X where the first two steps multiply it by P: there an error of X goes into all directions
-// alike, and the steps raise the weak ones by 3.4 each.  Matrices with four singular values 150 to 240 times the others are off by 0.008 of their
-// norm without that, 0.002 with it (the rounding of the result: 0.0017); pairs in the other products, or in later steps, change less than 0.0003.  It
-// costs two instructions instead of one in two of fifteen products: two of 4096 x 4096 3.32 ms instead of 2.84.  Ratios of some
-// thousands leave 0.011 (products of bf16 numbers: 0.3 to 1); pairs throughout, as for a result of 32 bits, would take 8.9 ms.
+// Of other bf16 results all numbers are single, except X where all but the last two steps multiply it by P: there an error of X goes into all directions
+// alike, and every step that is left raises the weak ones by 3.4 (an error of A or P moves strong directions a little, and is not raised).  Five steps of
+// matrices with one to 32 singular values 10^2 to 10^6 times all others, the roundings simulated in 64 bits: the result is off by up to 0.0039 of its norm
+// (its own rounding: 0.0017), with X single in the last three steps by 0.014, with X as pairs in all by 0.0037; ten steps 0.008, with X as pairs in the
+// first two alone 4.5.  (Products of bf16 numbers: 0.3 to 1.)  Errors of the sums, in 32 bits, are raised as well: 2^-21 3.4445^steps of the norm at most.
+// It costs two instructions instead of one in three of fifteen products: two of 4096 x 4096 3.88 ms, with X as pairs in two steps 3.65; pairs throughout,
+// as for a result of 32 bits, 9.33 ms.
 // fp16 holds few magnitudes, so every number is scaled by a power of two: the spectral norms of X, A and P are at most 1.21,
 // 1.46 and 3.45 whatever D is (p of [0, 1.21] stays below 1.21), and so is every element; scaled they fill the
 // upper end of the type, and what is lost at the lower end is 2^-39 of the norm or less.
@@ -930,7 +932,8 @@ struct MuonPlan {
     size_t off_d, off_x, off_xt[2], off_g, off_p, off_part, bytes;
 };
 inline int64_t half_of(int64_t t) { return t * (t + 1) / 2; }
-constexpr int PAIR_STEPS = 2;                    // of single numbers, the first steps, which read X as pairs
+// Of single numbers, the first steps, which read X as pairs: all but two, what the last ones raise an error of X by, and two at least.
+inline int pair_steps(int32_t steps) { return steps > 4 ? steps - 2 : 2; }
 constexpr int PAIR_SIDE = 64;                    // pairs throughout where A is at most so large
 constexpr int MOST_SHARES = 8, TURNS_AT_LEAST = 2, SMALL_SHARES = 16, SMALL_TURNS = 4;
 // Workgroups that share a tile's sum over k, where there are fewer tiles than compute units.
@@ -1091,13 +1094,13 @@ int iterate(dpaps_ps *ps, const MuonPlan &p, MuonIn in, MuonArgs last, int32_t s
             rc = half_product<TILE, KIND, MUON_POLY>(ps, a, p.batch, st);
             if (rc) return rc;
         }
-        const bool end = s + 1 == steps, pairs = !PAIR && s < PAIR_STEPS;
+        const bool end = s + 1 == steps, pairs = !PAIR && s < pair_steps(steps);
         MuonArgs b = end ? last : a;
         b.tiles_i = a.tiles_i; b.tiles_j = a.tiles_j; b.K = p.np;
         // (X transposed is read by other workgroups while it is written: into the other place; X itself is not)
         b.lhs = thin ? g : q; b.lhs_size = nn; b.rhs = xt; b.rhs_size = nm * 2;
         b.out = x; b.out_ld = p.mp; b.out_size = nm * S;
-        b.out_t = xt_next; b.out_t_ld = p.np; b.out_t_size = nm * 2; b.out_t_pair = s + 1 < PAIR_STEPS;
+        b.out_t = xt_next; b.out_t_ld = p.np; b.out_t_size = nm * 2; b.out_t_pair = s + 1 < pair_steps(steps);
         const auto apply = [&](auto kind, auto mode) {
             if constexpr (TILE == 64)
                 if (thin) return poly_apply<decltype(kind)::value, decltype(mode)::value>(ps, b, p.batch, st);

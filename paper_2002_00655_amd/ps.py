@@ -327,7 +327,8 @@ class ParameterServer:
                     "emb_adagrad_step")
 
     def muon_orthogonalize(self, x: torch.Tensor, steps: int = 5, eps: float = 1e-7, dtype: torch.dtype | None = None, out: torch.Tensor | None = None):
-        """Matrices [..., rows, cols] orthogonalised by Newton-Schulz products, in x's type or `dtype` (see include/dpaps.h)."""
+        """Matrices [..., rows, cols] orthogonalised by Newton-Schulz products, in x's type or `dtype`, of which the precision of the
+        products follows (see include/dpaps.h)."""
         batch, rows, cols = _matrices(x)
         if out is None:
             out = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
