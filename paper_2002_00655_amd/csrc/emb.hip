@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void k_token_replies(TokenIds t, int32_t worke
     const int64_t p = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (p >= t.n) return;
     const int64_t id = t.at(p);
-    if (id == t.pad) return;
+    if (t.padding(id)) return;
     const int32_t o = owner[t.first + id];
     if (o != worker) loc_row[t.first + id] = (int16_t)o;
 }
@@ -75,14 +75,14 @@ __global__ __launch_bounds__(256) void k_emb_lookup(RouteArgs route, TokenIds t,
         const uint32_t at = c0 + u * 256u + threadIdx.x;
         row[u] = (uint32_t)(((float)at + 0.5f) * inv_Pf);
         c[u] = at - row[u] * P;
-        id[u] = first + u * 256 + threadIdx.x < total ? t.at(p0 + row[u]) : t.pad;
+        id[u] = first + u * 256 + threadIdx.x < total ? t.at(p0 + row[u]) : 0;
     }
     if (few ? few_tokens_off(t, err) : stop != 0) return;
     Vec<float, W> x[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
         x[u] = Vec<float, W>{};
-        if (first + u * 256 + threadIdx.x < total && id[u] != t.pad) x[u] = load_vec<float, W>(val + (t.first + id[u]) * L + (int64_t)c[u] * W) * scale;
+        if (first + u * 256 + threadIdx.x < total && !t.padding(id[u])) x[u] = load_vec<float, W>(val + (t.first + id[u]) * L + (int64_t)c[u] * W) * scale;
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(FEW_THREADS) void k_emb_few(RouteArgs route, TokenI
     Vec<float, W> *sums = reinterpret_cast<Vec<float, W> *>(mem + SUMS);
     const int n = (int)t.n;
     if (threadIdx.x == 0) many = 0;
-    if (few_tokens_off<2>(t, err, [&](int64_t p, int64_t id) { lk[p] = id == t.pad ? NOKEY : (uint64_t)id; })) return;
+    if (few_tokens_off<2>(t, err, [&](int64_t p, int64_t id) { lk[p] = t.padding(id) ? NOKEY : (uint64_t)id; })) return;
     int block = blockIdx.x;
     if constexpr (MODE == EMB_ADAGRAD) {
         if (block < route.blocks) {
@@ -448,7 +448,7 @@ int token_ids(dpaps_ps *ps, int64_t first_key, int64_t num_tokens, bool in_store
         ps->last_error = "tokens: at most 2^29 in a call, of a vocabulary of less than 2^31";
         return PS_ELIMIT;
     }
-    t->ids = tokens; t->wide = token_type == PS_I64; t->n = n; t->first = first_key; t->count = num_tokens; t->pad = pad;
+    t->ids = tokens; t->wide = token_type == PS_I64; t->n = n; t->first = first_key; t->count = num_tokens; t->pad = pad; t->padded = pad != PS_NO_PAD;
     return PS_OK;
 }
 

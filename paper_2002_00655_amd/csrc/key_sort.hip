@@ -48,7 +48,7 @@ struct TokensIn {
     TokenIds t;
     __device__ __forceinline__ uint64_t operator[](int64_t q) const {
         const int64_t id = t.at(q);
-        return id == t.pad ? (uint64_t)t.count : id < 0 || id >= t.count ? (uint64_t)t.count + 1 : (uint64_t)id;
+        return t.padding(id) ? (uint64_t)t.count : id < 0 || id >= t.count ? (uint64_t)t.count + 1 : (uint64_t)id;
     }
 };
 struct PairsIn { __device__ __forceinline__ uint64_t operator[](int64_t) const { return 0; } };
@@ -566,16 +566,15 @@ __global__ __launch_bounds__(RANK_THREADS) void k_sort_rank(TokensIn tokens, int
 #pragma unroll
         for (int i = 0; i <= R; ++i) id[i] = reinterpret_cast<const int32_t *>(tokens.t.ids)[at(i)];
     }
-    const int64_t pad = tokens.t.pad;
     const uint32_t padding = (uint32_t)tokens.t.count;                 // (below 2^31)
-    const uint32_t mine = own >= n ? ~0u : id[R] == pad ? padding : (uint32_t)id[R];
+    const uint32_t mine = own >= n ? ~0u : tokens.t.padding(id[R]) ? padding : (uint32_t)id[R];
     uint32_t x[R];
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int from = wave * R + i;
         bad |= tokens.t.bad(id[i]);
-        const uint32_t key = id[i] == pad ? padding : (uint32_t)id[i];
+        const uint32_t key = tokens.t.padding(id[i]) ? padding : (uint32_t)id[i];
         x[i] = from == chunk || from * 64 + lane >= n ? ~0u : 2u * key + (from > chunk ? 1u : 0u);
     }
     if (bad) atomicExch(err, PS_EKEY);

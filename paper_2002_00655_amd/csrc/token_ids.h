@@ -5,12 +5,13 @@
 
 struct TokenIds {
     const void *ids = nullptr;   // int32 or int64 (wide), on the device; NULL: token p is p
-    int64_t n = 0, first = 0, count = 0, pad = INT64_MIN;
-    int32_t wide = 0;
+    int64_t n = 0, first = 0, count = 0, pad = 0;
+    int32_t wide = 0, padded = 0;   // padded: there is padding, the token `pad` (PS_NO_PAD is a token that a batch can hold, by mistake)
     __device__ __forceinline__ int64_t at(int64_t p) const {
         return !ids ? p : wide ? reinterpret_cast<const int64_t *>(ids)[p] : (int64_t)reinterpret_cast<const int32_t *>(ids)[p];
     }
-    __device__ __forceinline__ bool bad(int64_t t) const { return t != pad && (t < 0 || t >= count); }
+    __device__ __forceinline__ bool padding(int64_t t) const { return padded && t == pad; }
+    __device__ __forceinline__ bool bad(int64_t t) const { return (t < 0 || t >= count) && !padding(t); }
 };
 
 // Whether a call of few tokens is to do nothing: few_keys_off, for tokens.  keep(p, id): called for every token as it is read.
@@ -36,8 +37,9 @@ __device__ __forceinline__ bool few_tokens_off(const TokenIds &t, int32_t *err) 
 __device__ __forceinline__ void route_tokens_block(const RouteArgs &a, const TokenIds &t, RouteLds &l, int block, int32_t stop) {
     route_access_block(a, l, block, stop, [&](int64_t p, int64_t &k) {
         const int64_t id = t.at(p);
-        k = id == t.pad ? 0 : t.first + id;
-        return id != t.pad;
+        const bool padding = t.padding(id);
+        k = padding ? 0 : t.first + id;
+        return !padding;
     });
 }
 

@@ -334,6 +334,29 @@ def test_a_bad_token_changes_nothing(n, bad):
     srv.status()
 
 
+@pytest.mark.parametrize("n", [1, 64, 2048, 2049, 5000, 10_000, 140_000])
+def test_the_lowest_token_is_a_bad_one_where_there_is_no_padding(n):
+    """PS_NO_PAD has a value that an int64 batch can hold: an error like any other token that is not there."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng = np.random.default_rng(n)
+    srv, values = _server(900, 16, W=3)
+    tokens = rng.integers(0, 640, size=n)
+    tokens[n // 2] = -(1 << 63)
+    t = torch.from_numpy(tokens).cuda()
+    out, grad, dout = torch.full((n, 16), 7.0, device="cuda"), torch.full((640, 8), 7.0, device="cuda"), torch.ones(n, 8, device="cuda")
+    stats = srv.stats()
+    for call in (lambda: srv.emb_lookup(t, num_tokens=640, out=out, worker=1), lambda: srv.emb_grad(t, dout, 640, grad=grad),
+                 lambda: srv.emb_grad(t, dout, 640, grad=grad, accumulate=True),
+                 lambda: srv.emb_adagrad_step(t, dout, 0.1, 1e-8, num_tokens=640, worker=1), lambda: srv.emb_lookup(t, num_tokens=640, out=out, pad_token=0),
+                 lambda: srv.emb_grad(t, dout, 640, grad=grad, pad_token=-1)):
+        call()
+        with pytest.raises(P.PSError) as e:
+            srv.status()
+        assert e.value.code == P.PS_EKEY
+    assert (out == 7.0).all() and (grad == 7.0).all() and np.array_equal(_all(srv), values) and srv.stats() == stats
+
+
 def test_refusals():
     import torch
     from paper_2002_00655_amd import ps as P
