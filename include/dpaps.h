@@ -352,7 +352,7 @@ int emb_adagrad_step(ps_handle ps, int32_t worker, int64_t first_key, int64_t nu
 /* Orthogonalise `batch` matrices of rows x cols, each X_0 = D / (|D|_F + eps) and then `steps` times
  *   A = X X',  X <- a X + (b A + c A^2) X,   (a, b, c) = (3.4445, -4.7750, 2.0315)
  * (X' X and from the right where rows > cols, which is the same matrix).  Matrix i starts at row i * rows of `in` and `out`, whose rows
- * are in_ld and out_ld >= cols elements apart.  A zero matrix stays zero; one that holds an infinity or no number becomes NaN, the others do not.
+ * are in_ld and out_ld >= cols elements apart.  A zero matrix stays zero, whatever eps; one that holds an infinity or no number becomes NaN, the others do not.
  * The products are carried out with numbers of 23 bits where the result has type PS_F32 or PS_F16, or one side is at most 64, or both
  * at most 128; where it is rounded to PS_BF16 (8 bits), else, with numbers of 11 bits, but for X where all but the last two steps (in the first
  * two, of fewer than four) multiply it, which has 23.  Sums are in 32 bits.  Relative to its norm, a PS_BF16 result is off by 0.0017 to 0.002 and a PS_F32

@@ -127,14 +127,14 @@ __global__ __launch_bounds__(256) void k_muon_norm(MuonIn a, uint32_t P, double 
 
 // A matrix's numbers become X_0, scaled.  In 64 bits where the sum of squares is far from 1, so that neither a norm above the largest 32-bit number nor
 // one near the smallest loses anything (everywhere, 3 of the 49 us of 16 matrices of 100 x 100).  An infinity or NaN anywhere in the matrix makes all of X
-// NaN, as the division and the products would.
+// NaN, as the division and the products would; a matrix of zeros stays one, also where eps is 0.
 struct Scale {
     bool usual;
     float f;
     double wide;
     __device__ __forceinline__ Scale(double square, float eps) : usual(square >= 1e-30 && square <= 1e30), f(0.0f), wide(0.0) {
         if (usual) f = X_SCALE / (sqrtf((float)square) + eps);
-        else wide = square <= 1.7e308 ? (double)X_SCALE / (sqrt(square) + (double)eps) : __builtin_nan("");
+        else if (square != 0.0) wide = square <= 1.7e308 ? (double)X_SCALE / (sqrt(square) + (double)eps) : __builtin_nan("");
     }
     template <int N> __device__ __forceinline__ void apply(float (&v)[N]) const {
         if (usual) {

@@ -204,6 +204,26 @@ def test_every_matrix_of_a_batch_by_itself(srv, rows, cols):
     check(got[6], x[6], "float32", 2.0 ** -24, "plain", eps)
 
 
+@pytest.mark.parametrize("batch,rows,cols", [(2, 1, 1), (3, 60, 60), (2, 10, 300), (3, 300, 100), (2, 200, 190), (4, 850, 900), (2, 4352, 4352)])
+@pytest.mark.parametrize("eps", [0.0, 1e-7])
+def test_a_matrix_of_zeros_stays_zero(srv, batch, rows, cols, eps):
+    """Beside one that does not, and in the step: weights whose gradient and momentum are zero only decay."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(rows)
+    x = torch.randn(batch, rows, cols, device="cuda", generator=g)
+    x[0] = 0
+    for kind in (torch.float32, torch.bfloat16):
+        got = srv.muon_orthogonalize(x, eps=eps, dtype=kind)
+        assert (got[0] == 0).all() and torch.isfinite(got[1:].float()).all() and (got[1:] != 0).any()
+    if cols <= 512:
+        w = torch.randn(rows, 2 * cols, device="cuda", generator=g)
+        w[:, cols:] = 0
+        s = server(w.cpu().numpy())
+        s.muon_step(0, torch.zeros(rows, cols, device="cuda"), 0.5, weight_decay=0.25, eps=eps)
+        w[:, :cols] *= 0.875
+        assert torch.equal(s.pull(torch.arange(rows, device="cuda")), w)
+
+
 @pytest.mark.parametrize("steps", [1, 2, 5, 9])
 def test_number_of_steps(srv, steps):
     import torch
