@@ -354,11 +354,12 @@ int emb_adagrad_step(ps_handle ps, int32_t worker, int64_t first_key, int64_t nu
  * (X' X and from the right where rows > cols, which is the same matrix).  Matrix i starts at row i * rows of `in` and `out`, whose rows
  * are in_ld and out_ld >= cols elements apart.  A zero matrix stays zero, whatever eps; one that holds an infinity or no number becomes NaN, the others do not.
  * The products are carried out with numbers of 23 bits where the result has type PS_F32 or PS_F16, or one side is at most 64, or both
- * at most 128; where it is rounded to PS_BF16 (8 bits), else, with numbers of 11 bits, but for X where all but the last two steps (in the first
- * two, of fewer than four) multiply it, which has 23.  Sums are in 32 bits.  Relative to its norm, a PS_BF16 result is off by 0.0017 to 0.002 and a PS_F32
+ * at most 128; where it is rounded to PS_BF16 (8 bits), else, with numbers of 11 bits, but for X where all but the last two steps (of up to
+ * three: the first two) multiply it, which has 23.  Sums are in 32 bits.  Relative to its norm, a PS_BF16 result is off by 0.0017 to 0.002 and a PS_F32
  * one by 2e-6 after five steps.  Where some singular values are far above all others, what rounding leaves in the weak directions is raised by 3.4 in every
  * step that follows: there a PS_BF16 result is off by up to 0.005, and either by up to 2^-21 3.4445^steps (2e-4 of five steps, 0.003 of seven, 0.1 of
- * ten) beside that, as products in 32 bits are.  A caller who wants a PS_BF16 result of products of 23 bits throughout rounds a PS_F32 one.
+ * ten) beside that, as products in 32 bits are.  Every element of X is off by up to
+ * 2^-39 besides, which matters where |D|_F is far below eps and X_0 as small as |D|_F / eps (where it is a millionth, 0.0007 of the norm of a result of 600 x 600, 0.002 of 1800 x 1700).  A caller who wants a PS_BF16 result of products of 23 bits throughout rounds a PS_F32 one.
  * 1 <= steps <= 100, eps >= 0; the server's values have no part in it.  `out` must not overlap `in`.  Limits (PS_ELIMIT): sides of
  * PS_MUON_MAX_SIDE, PS_MUON_MAX_BATCH matrices.  Scratch: 20 bytes per element of the matrices (sides count as multiples of 64, 128
  * or 256) and up to 64 MiB, none where the sides are at most 128 and

@@ -20,7 +20,8 @@
 // as for a result of 32 bits, 9.33 ms.
 // fp16 holds few magnitudes, so every number is scaled by a power of two: the spectral norms of X, A and P are at most 1.21,
 // 1.46 and 3.45 whatever D is (p of [0, 1.21] stays below 1.21), and so is every element; scaled they fill the
-// upper end of the type, and what is lost at the lower end is 2^-39 of the norm or less.
+// upper end of the type, and what is lost at the lower end is 2^-39 or less of each element - of X_0's norm, where |D| is not far below eps; where it is, X_0 is
+// as small as |D| / eps, and its elements have so many digits less: of 600 x 600, |D| a millionth of eps, 2^-39 is 0.0007 of the norm.
 // All three products have the form sum_k L[i][k] R[j][k] with both operands' rows contiguous in k: A = X X' and
 // A^2 = A A' (A is symmetric) as they are, P X with X transposed - so X is written both ways.  Of the symmetric ones only the tiles on and below
 // the diagonal are computed; a tile is written to its mirror place as well.

@@ -204,6 +204,33 @@ def test_every_matrix_of_a_batch_by_itself(srv, rows, cols):
     check(got[6], x[6], "float32", 2.0 ** -24, "plain", eps)
 
 
+@pytest.mark.parametrize("rows,cols", [(60, 60), (10, 300), (300, 100), (200, 190), (600, 600), (1800, 1700)])
+@pytest.mark.parametrize("ratio", [1.0, 1e-3, 1e-6])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_matrices_whose_norm_is_below_eps(srv, rows, cols, ratio, kind):
+    """X_0 is as small as |D| / eps, and every step raises it 3.4 times.  A step's roundings: 8 units of the numbers as everywhere here, relatively, and 2^-39 of
+    each element, which the steps that are left raise; for bfloat16 the header's 0.005 beside that."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(rows)
+    eps, steps = 1e-7, 5
+    d = torch.randn(2, rows, cols, device="cuda", dtype=torch.float64, generator=g)
+    d = (d / torch.linalg.vector_norm(d, dim=(1, 2), keepdim=True) * (eps * ratio)).float()
+    got = srv.muon_orthogonalize(d, eps=eps, dtype=getattr(torch, kind))
+    for i in range(2):
+        x = d[i].double() / (torch.linalg.vector_norm(d[i].double()) + np.float64(np.float32(eps)))
+        off = 0.0
+        for k in range(steps):
+            left = A ** (steps - k)
+            off += left * (2.0 ** -21 * float(torch.linalg.vector_norm(x)) + 2.0 ** -39 * (rows * cols) ** 0.5)
+            a = x @ x.T
+            x = A * x + (B * a + C * a @ a) @ x
+        norm = float(torch.linalg.vector_norm(x))
+        err = float(torch.linalg.vector_norm(got[i].double() - x))
+        off += (0.005 if kind == "bfloat16" else 2.0 ** -24) * norm
+        print(f"  {i}: error {err / norm:.2e}, allowed {off / norm:.2e}", flush=True)
+        assert err <= off, (i, err, off)
+
+
 @pytest.mark.parametrize("batch,rows,cols", [(2, 1, 1), (3, 60, 60), (2, 10, 300), (3, 300, 100), (2, 200, 190), (4, 850, 900), (2, 4352, 4352)])
 @pytest.mark.parametrize("eps", [0.0, 1e-7])
 def test_a_matrix_of_zeros_stays_zero(srv, batch, rows, cols, eps):
