@@ -106,9 +106,11 @@ def _tokens(t: torch.Tensor) -> tuple[int, int, int]:
     return t.data_ptr(), kind, t.numel()
 
 
-def _rows(t: torch.Tensor, n: int, copy: bool = True) -> tuple[torch.Tensor, int, int, int]:
+def _rows(t: torch.Tensor, n: int, copy: bool = True, apart: bool = False) -> tuple[torch.Tensor, int, int, int]:
     """A tensor of n rows (its last dimension a row, the others counted together): what has to stay alive until the call is made, where
-    it is, its type, the rows' distance in elements.  Rows that do not lie at one distance are copied, or refused."""
+    it is, its type, the rows' distance in elements.  What is read (copy): a matrix is taken as it lies, or refused where it is transposed; rows of
+    more dimensions that do not lie at one distance are copied, and so are numbers that were expanded to rows (the gradient of a sum) and, if they
+    have to be apart, rows that were expanded.  What is written lies as the call can write it, or is refused."""
     kind = _TYPES.get(t.dtype)
     if kind is None or not t.is_cuda or t.dim() == 0:
         raise TypeError(f"expected a CUDA tensor of float32, bfloat16 or float16, got {t.dtype} on {t.device}")
@@ -118,6 +120,11 @@ def _rows(t: torch.Tensor, n: int, copy: bool = True) -> tuple[torch.Tensor, int
             raise ValueError(f"the rows of a result have to lie at one distance, got shape {tuple(t.shape)}, strides {t.stride()}")
         t = r
     rows, cols = t.shape
+    if copy and rows == n > 0 and cols > 1:
+        if t.stride(1) == 0:
+            t = t[:1].contiguous().expand(n, cols) if t.stride(0) == 0 else t.contiguous()
+        if apart and n > 1 and t.stride(0) == 0:
+            t = t.contiguous()
     if rows != n or (n > 0 and cols > 1 and t.stride(1) != 1):
         raise ValueError(f"expected {n} rows whose elements are contiguous, got shape {tuple(t.shape)}, strides {t.stride()}")
     return t, t.data_ptr(), kind, (t.stride(0) if n > 1 else cols)
@@ -334,7 +341,7 @@ class ParameterServer:
             out = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
         elif out.shape != x.shape:
             raise ValueError(f"out must have the shape {tuple(x.shape)}")
-        kept, frm, in_kind, in_ld = _rows(x, batch * rows)
+        kept, frm, in_kind, in_ld = _rows(x, batch * rows, apart=True)
         _, to, out_kind, out_ld = _rows(out, batch * rows, copy=False)
         self._check(_lib.muon_orthogonalize(self._h, batch, rows, cols, frm, in_kind, in_ld, to, out_kind, out_ld, steps, eps, _stream()), "muon_orthogonalize")
         return out
@@ -343,7 +350,7 @@ class ParameterServer:
                   steps: int = 5, eps: float = 1e-7, worker: int = -1) -> None:
         """One step of weight matrices in the server, from their gradients [..., rows, dim] (see include/dpaps.h)."""
         batch, rows, dim = _matrices(grad)
-        kept, frm, kind, ld = _rows(grad, batch * rows)
+        kept, frm, kind, ld = _rows(grad, batch * rows, apart=True)
         self._check(_lib.muon_step(self._h, worker, first_key, batch, rows, dim, frm, kind, ld, lr, momentum, int(nesterov), weight_decay, steps, eps,
                                    _stream()), "muon_step")
 

@@ -217,6 +217,31 @@ def test_gradient_of_broadcast_strided_and_misaligned_rows(kind):
         assert torch.equal(srv.emb_grad(tokens, rows, 50).double(), want)
 
 
+@pytest.mark.parametrize("n", [1, 60, 3000])
+def test_gradient_of_expanded_numbers(n):
+    """What a sum of a lookup's output, or of its rows' sums, passes back: strides of 0."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    rng, D = np.random.default_rng(n), 36
+    tokens = torch.from_numpy(rng.integers(0, 50, size=n)).cuda()
+    srv, _ = _server(50, 2 * D)
+    ref, _ = _server(50, 2 * D)
+    row = torch.from_numpy(rng.integers(-8, 9, size=(n, 1)).astype(np.float32)).cuda()
+    for dout in (torch.full((), 2.0, device="cuda").expand(n, D), row.expand(n, D), row[:1, :1].to(torch.bfloat16).expand(n, D)):
+        want = srv.emb_grad(tokens, dout.contiguous(), 50)
+        assert torch.equal(srv.emb_grad(tokens, dout, 50), want)
+        if n == 60:
+            assert torch.equal(srv.emb_grad(tokens.view(5, 12), dout.view(5, 12, D) if dout.stride(0) else dout[:1].expand(60, D).reshape(5, 12, D), 50), want)
+        srv.emb_adagrad_step(tokens, dout, 0.1, 1e-8)
+        ref.emb_adagrad_step(tokens, dout.contiguous(), 0.1, 1e-8)
+    out = torch.full((), 3.0, device="cuda").expand(5, 12, D)
+    assert torch.equal(srv.emb_grad(tokens[:1].expand(60).contiguous().view(5, 12), out, 50), srv.emb_grad(tokens[:1].expand(60).contiguous(), out.reshape(60, D).contiguous(), 50))
+    assert np.array_equal(_all(srv), _all(ref))
+    with pytest.raises(ValueError):
+        srv.emb_lookup(tokens[:1].expand(7).contiguous(), dim=D, out=torch.zeros(7, 1, device="cuda").expand(7, D))
+    srv.status()
+
+
 def test_gradient_against_differences():
     """<dout, lookup(E + h X) - lookup(E - h X)> / 2h = <grad, X>: the lookup is linear, so no more than roundings."""
     import torch

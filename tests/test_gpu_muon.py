@@ -278,6 +278,24 @@ def test_strided_matrices(srv, kind):
         assert (to == 7.0).all()
 
 
+@pytest.mark.parametrize("rows,cols", [(60, 60), (300, 40), (300, 130)])
+def test_expanded_matrices(srv, rows, cols):
+    """Gradients as sums pass them back: one number, a number of each row, or a row for all; of two and three dimensions."""
+    import torch
+    rng = np.random.default_rng(rows + cols)
+    col, row, number = (torch.from_numpy(gaussian(rng, *s)).cuda() for s in ((rows, 1), (1, cols), ()))
+    a, b = server(np.ones((2 * rows, 2 * cols), np.float32)), server(np.ones((2 * rows, 2 * cols), np.float32))
+    for x in (number.expand(rows, cols), col.expand(rows, cols), row.expand(rows, cols)):
+        for d in (x, x.expand(2, rows, cols)):
+            assert torch.equal(srv.muon_orthogonalize(d), srv.muon_orthogonalize(d.contiguous()))
+            a.muon_step(0, d, 0.1)
+            b.muon_step(0, d.contiguous(), 0.1)
+    keys = torch.arange(2 * rows, device="cuda")
+    assert torch.equal(a.pull(keys), b.pull(keys))
+    with pytest.raises(ValueError):
+        srv.muon_orthogonalize(col.expand(rows, cols), out=torch.zeros(rows, 1, device="cuda").expand(rows, cols))
+
+
 def server(values, W=1):
     import torch
     from paper_2002_00655_amd import ps as P
