@@ -132,6 +132,40 @@ def test_few_rows_in_bfloat16(srv, rows, cols, strong):
         assert err <= 1.02 * rounded, (i, err, rounded)
 
 
+@pytest.mark.parametrize("batch,rows,cols", [(1, 4096, 1024), (1, 1000, 4000), (1, 700, 6000), (6, 900, 640), (9, 370, 1200), (1, 1700, 1750), (8, 900, 1000)])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_millions_of_numbers(srv, batch, rows, cols, kind):
+    """Tiles of 128 where there are fewer than compute units: sums over k that several workgroups share, and short ones, which go by tiles of 64."""
+    import torch
+    rng = np.random.default_rng(rows + cols)
+    x = torch.from_numpy(gaussian(rng, batch, rows, cols)).cuda().to(getattr(torch, kind))
+    got = srv.muon_orthogonalize(x)
+    assert torch.equal(srv.muon_orthogonalize(x), got)
+    for i in sorted({0, batch - 1}):
+        check(got[i].double().cpu().numpy(), x[i].double().cpu().numpy(), kind, 2.0 ** -12 if kind == "bfloat16" else 2.0 ** -24, f"{kind} {i}")
+        if kind == "bfloat16":                                                          # (the header's bound is nearer)
+            want, _ = reference(x[i].double().cpu().numpy())
+            assert np.linalg.norm(got[i].double().cpu().numpy() - want) <= 0.005 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(2, 4352, 4300), (2, 4350, 4600), (1, 6100, 5888)])
+def test_the_largest_tiles_through_five_steps(srv, batch, rows, cols):
+    """Sides that tiles of 256 fill: single numbers and pairs one after the other, full rounds of the compute units and a rest whose sums are
+    shared, both ways round.  At most a fifth further from the true result than that rounded to bfloat16 is."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(rows)
+    d = torch.randn(batch, rows, cols, device="cuda", generator=g).to(torch.bfloat16)
+    got = srv.muon_orthogonalize(d)
+    for i in range(batch):
+        x = d[i].double() / (torch.linalg.norm(d[i].double()) + 1e-7)
+        for _ in range(5):
+            a = x @ x.T
+            x = A * x + (B * a + C * a @ a) @ x
+        rounded, err = (float(torch.linalg.norm(t.double() - x) / torch.linalg.norm(x)) for t in (x.to(torch.bfloat16), got[i]))
+        print(f"  {i}: error {err:.2e}, of rounding alone {rounded:.2e}", flush=True)
+        assert err <= 1.2 * rounded, (i, err, rounded)
+
+
 @pytest.mark.parametrize("batch,rows,cols,steps", [(1, 4300, 4340, 1), (2, 4340, 4300, 3), (1, 4100, 4400, 2)])
 def test_large_matrices_in_bfloat16(srv, batch, rows, cols, steps):
     """A few directions a hundred times as strong as the others.  At most twice as far from the true result as that rounded to bfloat16 is."""
@@ -339,6 +373,40 @@ def test_step(batch, rows, dim, L, first, kind):
         rest = np.ones(values.shape, bool)
         rest[at, :2 * dim] = False
         assert np.array_equal(got[rest], values[rest])
+    srv.status()
+
+
+@pytest.mark.parametrize("batch,rows,dim,L,first,kind", [(8, 2048, 512, 1024, 2, "bfloat16"), (5, 1500, 471, 943, 7, "float32"), (20, 300, 500, 1001, 1, "float16"),
+                                                         (12, 471, 500, 1000, 0, "bfloat16")])
+def test_step_of_many_numbers(batch, rows, dim, L, first, kind):
+    """Batches that are cut into tiles of 128: more of them than compute units and fewer, sums that are shared, sums that are short; rows of the server that
+    cannot be written eight numbers at a time.  Tolerances as in test_step."""
+    import torch
+    rng = np.random.default_rng(rows + dim)
+    print(f"case {batch} x {rows} x {dim} {kind}", flush=True)
+    keys = batch * rows
+    values = gaussian(rng, first + keys + 3, L) * np.float32(0.05)
+    srv = server(values)
+    lr, wd, mu = 0.02, 0.1, 0.9
+    f = lambda v: float(np.float32(v))  # noqa: E731
+    grad = torch.from_numpy(gaussian(rng, batch, rows, dim)).cuda().to(getattr(torch, kind))
+    srv.muon_step(first, grad, lr, momentum=mu, nesterov=True, weight_decay=wd)
+    got = srv.pull(torch.arange(first + keys + 3, device="cuda")).cpu().numpy()
+    g = grad.double().cpu().numpy().reshape(keys, dim)
+    at, step = slice(first, first + keys), f(lr) * np.sqrt(max(1.0, rows / dim))
+    M = f(mu) * values[at, dim:2 * dim].astype(np.float64) + g
+    for i in sorted({0, 1, batch // 2, batch - 1}):
+        r = slice(i * rows, (i + 1) * rows)
+        o, off = reference(g[r] + f(mu) * M[r])
+        W = (1 - f(lr) * f(wd)) * values[at, :dim][r].astype(np.float64) - step * o
+        tol = step * off + 8 * 2.0 ** -24 * (np.linalg.norm(W) + step * np.sqrt(min(rows, dim)))
+        err = np.linalg.norm(got[at, :dim][r] - W)
+        print(f"  {i}: error {err:.2e}, allowed {tol:.2e}", flush=True)
+        assert err <= tol, (i, err, tol)
+    assert np.abs(got[at, dim:2 * dim] - M).max() <= 4 * 2.0 ** -24 * max(1.0, np.abs(M).max())
+    rest = np.ones(values.shape, bool)
+    rest[at, :2 * dim] = False
+    assert np.array_equal(got[rest], values[rest])
     srv.status()
 
 
