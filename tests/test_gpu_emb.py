@@ -140,6 +140,68 @@ def test_every_term_is_added_once_whatever_sorts_the_tokens(n):
             assert np.array_equal(got[:, c], np.bincount(tokens[there], weights=dout[there, c], minlength=V).astype(np.float32)), (V, c)
 
 
+@pytest.mark.parametrize("n", [262_144, 2_097_152, 2_097_153, 5_000_001])
+@pytest.mark.parametrize("V,pad,wide", [(1, None, True), (2, None, False), (130, 129, False), (100_000, -5, True), (70_000_000, 0, False)])
+def test_every_term_is_added_once_of_millions(n, V, pad, wide):
+    """As above, up to the tiles of the longest sorts; sums stay below 2^24.  One token or two: one workgroup joins all ranges."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    print(f"case n={n} V={V}", flush=True)
+    g = torch.Generator("cuda").manual_seed(n + V)
+    tokens = torch.randint(0, V, (n,), device="cuda", generator=g)
+    if pad is not None:
+        tokens[torch.rand(n, device="cuda", generator=g) < 0.1] = pad
+    q = torch.arange(n, device="cuda")
+    dout = torch.stack([torch.ones_like(q), q % 2, q // 2 % 3 // 2], 1).float()
+    srv = P.ParameterServer(1, 1, 1)
+    got = srv.emb_grad(tokens if wide else tokens.int(), dout, V, pad_token=pad)
+    there = tokens != pad if pad is not None else torch.ones_like(tokens, dtype=torch.bool)
+    for c in range(3):
+        want = torch.zeros(V, dtype=torch.float64, device="cuda").index_add_(0, tokens[there], dout[there, c].double())
+        assert torch.equal(got[:, c].double(), want), c
+    srv.status()
+
+
+def test_offsets_past_32_bits():
+    """A result, a gradient of the result and a server of more than 2^31 numbers: their last rows."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    # the result: 4,300,000 rows of 512
+    rng, n = np.random.default_rng(0), 4_300_000
+    srv, values = _server(900, 512)
+    rows = torch.from_numpy(values).cuda()
+    tokens = torch.randint(0, 900, (n,), device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    out = srv.emb_lookup(tokens, dtype=torch.bfloat16)
+    for a in (0, n // 2, 4_194_300, n - 1000):                                             # (the 4,194,304th row starts at number 2^31)
+        assert torch.equal(out[a:a + 1000], rows[tokens[a:a + 1000]].to(torch.bfloat16))
+    # its gradient, every 500th row of it
+    out.zero_()
+    some = torch.arange(0, n, 500, device="cuda")
+    dout = out[::500]
+    dout.copy_(torch.from_numpy(rng.integers(-8, 9, size=(some.numel(), 512)).astype(np.float32)))
+    want = torch.zeros(900, 512, dtype=torch.float64, device="cuda").index_add_(0, tokens[some], dout.double())
+    assert dout.stride(0) * (some.numel() - 1) > 1 << 31 and torch.equal(srv.emb_grad(tokens[some], dout, 900).double(), want)
+    del out, dout, srv
+    # the server: 2,200,000 keys of 1,024
+    K, first = 2_200_000, 2_100_000
+    srv = P.ParameterServer(K, 1024, 1)
+    keys = torch.arange(first - 5, K, device="cuda")
+    at = torch.randint(0, K - first, (3000,), device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    was = torch.rand(keys.numel(), 1024, device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    srv.push(keys, was)
+    assert torch.equal(srv.emb_lookup(at, first_key=first), was[5 + at])
+    srv.emb_adagrad_step(at, torch.ones(3000, 512, device="cuda"), 0.5, 1.0, first_key=first)
+    got, count = srv.pull(keys), torch.bincount(at, minlength=K - first)
+    hit = torch.cat([torch.zeros(5, device="cuda"), count.float()])[:, None]
+    acc = was[:, 512:] + hit * hit
+    assert torch.equal(got[:, 512:], acc)
+    want = was[:, :512].double() - 0.5 * hit.double() / torch.sqrt(acc.double() + 1.0)
+    assert float((got[:, :512].double() - want).abs().max()) <= 4 * 2.0 ** -24
+    same = hit[:, 0] == 0
+    assert torch.equal(got[same], was[same])
+    srv.status()
+
+
 @pytest.mark.parametrize("n", [2052, 4096, 4100, 8192, 8196, 131_072, 131_076])
 def test_terms_are_added_in_the_order_of_their_positions(n):
     """Four terms a token, which lie in one range: the sums are those of 32-bit additions one after the other, bit for bit."""
