@@ -924,9 +924,13 @@ __global__ __launch_bounds__(ONE_THREADS) void k_muon_one(MuonOne a, const int32
 // as often, but few of them leave compute units idle, and they fill up more.  Whole calls, tiles of 64 and of 128: 32 bits, 300 x 300 111 us and 151,
 // 1024 x 1024 202 and 261, two of them 292 and 320, 1500 x 2000 516 and 448, four of 1024 x 1024 458 and 431, 1024 x 4096 429 and 372, 4096 x 4096 5,086
 // and 4,486; 32 of 300 x 300, which become 320 and 384, 199 and 292; bf16 results, 300 of 200 x 200 520 and 500, 100 of 300 x 700 545 and 671, 26 of
-// 1000 x 1010 1,535 and 1,133 - the line is at 2.9 million numbers, unless the larger tile makes them a quarter more.  Tiles of 128 and of 256, single numbers:
-// two of 4096 x 4096 3,520 and 3,320, 8192 x 8192 12,860 and 11,280, 5000 x 5000 3,475 and 3,160; 6000 x 6000, which become 6016 and 6144, 5,380 and
-// 5,508, 4200 x 4200 2,153 and 2,538; 64 of 1024 x 1024 2,557 and 2,757, 2000 x 8000 937 and 1,566.
+// 1000 x 1010 1,535 and 1,133 - the line is at 2.9 million numbers, unless the larger tile makes them a quarter more.  Tiles of 128 and of 256 for bf16
+// results: it is the rounds of the compute units that the 256s fill which count - seven tenths of them in P X, half of one in X X' -, and sides above 2048.
+// P X fills 0.77 to 1 of its rounds: 4096 x 4096 1,970 and 1,847, two of them 3,667 and 3,379, two of 3584 x 3584 2,609 and 2,376, four of 2560 x 2560 1,971
+// and 1,850, 5000 x 5000 3,593 and 3,205, 8192 x 8192 13,593 and 11,882; 0.70 to 0.75: 4864 x 4864 3,001 and 2,980, 4352 x 8704 4,070 and 3,973, three of
+// 2816 x 2816 1,876 and 1,918; 0.56 to 0.66: 4352 x 4352 2,295 and 2,593, two of 3328 x 3328 2,060 and 2,150, three of 2560 x 2560 1,487 and 1,716.  X X' fills
+// less than half of a round: 3584 x 7168 2,305 and 2,510, 2000 x 8000 921 and 1,578.  Short sums: eight of 2048 x 2048 2,063 and 2,136 (16 of them 4,156
+// and 3,988), 16 of 1536 x 1536 1,888 and 2,163, 64 of 1024 x 1024 2,629 and 2,780.  And no more than a fiftieth more numbers: 4200 x 4200 by tiles of 256 is 4352 x 4352.
 struct MuonPlan {
     int32_t batch, n, m, tile, np, mp, blocks;
     bool tall, split, one;
@@ -964,7 +968,10 @@ MuonPlan muon_plan(const dpaps_ps *ps, int32_t batch, int32_t rows, int32_t cols
     }
     const auto padded = [&](int64_t t) { return ceil_div64(p.n, t) * t * ceil_div64(p.m, t) * t * batch; };
     p.tile = padded(64) >= (int64_t)11264 * ps->num_cu && 4 * padded(128) <= 5 * padded(64) ? 128 : 64;
-    if (!split && p.n >= 4096 && 50 * padded(256) <= 51 * padded(128)) p.tile = 256;
+    const int64_t whole = ceil_div64(p.n, 256) * ceil_div64(p.m, 256) * batch, cus = ps->num_cu;
+    if (!split && p.n > 2048 && 50 * padded(256) <= 51 * padded(128) && 2 * half_of(ceil_div64(p.n, 256)) * batch >= cus &&
+        10 * whole >= 7 * ceil_div64(whole, cus) * cus)
+        p.tile = 256;
     p.np = (int32_t)(ceil_div64(p.n, p.tile) * p.tile); p.mp = (int32_t)(ceil_div64(p.m, p.tile) * p.tile);
     const int64_t blocks = ceil_div64((int64_t)rows * cols, 1024);
     p.blocks = (int32_t)(blocks < NORM_BLOCKS ? blocks : NORM_BLOCKS);

@@ -148,6 +148,24 @@ def test_millions_of_numbers(srv, batch, rows, cols, kind):
             assert np.linalg.norm(got[i].double().cpu().numpy() - want) <= 0.005 * np.linalg.norm(want)
 
 
+@pytest.mark.parametrize("batch,rows,cols", [(1, 4096, 4096), (4, 2560, 2560), (2, 2300, 5100), (1, 4300, 4340), (8, 2048, 2048)])
+@pytest.mark.parametrize("steps", [1, 2, 4, 6])
+def test_on_both_sides_of_the_rule_for_the_largest_tiles(srv, batch, rows, cols, steps):
+    """One direction 10^4 times the others, the bounds of test_dominated_matrices..."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(rows + steps)
+    d = torch.randn(batch, rows, cols, device="cuda", generator=g) + 100 * rows ** 0.5 * torch.randn(batch, rows, 1, device="cuda", generator=g)
+    got = srv.muon_orthogonalize(d, steps=steps, dtype=torch.bfloat16)
+    for i in {0, batch - 1}:
+        x = d[i].double() / (torch.linalg.vector_norm(d[i].double()) + 1e-7)
+        for _ in range(steps):
+            a = x @ x.T
+            x = A * x + (B * a + C * a @ a) @ x
+        err = float(torch.linalg.vector_norm(got[i].double() - x) / torch.linalg.vector_norm(x))
+        print(f"  {i}: {err:.2e}", flush=True)
+        assert err <= 0.005 + 2.0 ** -21 * A ** steps, (i, err)
+
+
 @pytest.mark.parametrize("batch,rows,cols", [(2, 4352, 4300), (2, 4350, 4600), (1, 6100, 5888)])
 def test_the_largest_tiles_through_five_steps(srv, batch, rows, cols):
     """Sides that tiles of 256 fill: single numbers and pairs one after the other, full rounds of the compute units and a rest whose sums are
