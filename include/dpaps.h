@@ -320,6 +320,8 @@ int kge_sgd_epoch(ps_handle ps, int64_t num_entities, int32_t dim, int64_t num_t
  * elements are contiguous; strides count elements.  All sums are in 32 bits; a result is rounded to its type once.
  * The tensors of a call must not overlap the ones it writes.  None of these calls waits for the stream, except where
  * scratch of the library has to grow (as for ps_push: emb_grad and emb_adagrad_step, muon_orthogonalize and muon_step).
+ * Calls that need not grow it can be captured into a HIP graph.  The graph keeps the scratch of that moment: no later call on the handle (a ps_push or a
+ * knowledge-graph call among them) may outgrow it while the graph is replayed.  With more than 256 workers the forwards of replays are not counted.
  * worker: as for ps_pull / ps_push (locality statistics, of every token that is not padding); with location caches the
  * replies set the requester's entries, too. */
 enum { PS_F32 = 0, PS_BF16 = 1, PS_F16 = 2 };    /* types of values */

@@ -87,7 +87,8 @@ __device__ __forceinline__ double sum_of_256(double x) {
 // Of matrix blockIdx.y: sums of squares in 64 bits (no number of 32 bits overflows there); of a step, first M <- mu M + G, and
 // what is orthogonalised, D = G + mu M (Nesterov) or M.  V numbers of a row at a time, P = cols / V such pieces a row; a thread
 // goes through every (256 blocks)th piece of the matrix, AHEAD of them together.
-// Memory bounds it: a step of eight matrices of 2048 x 512, a bf16 gradient, 118 MB read and written in 24 us, 4.9 TB/s; two of 4096 x 4096 in bf16 29 us.
+// Memory bounds a step: eight matrices of 2048 x 512, a bf16 gradient, 118 MB read and written in 24 us, 4.9 TB/s.  Two of 4096 x 4096 in bf16 are 67 MB in
+// 29 us, 2.3 TB/s, half of a copy's rate: what a thread has on its way, four pieces of 8 bytes, and at most 256 workgroups a matrix bound that.
 template <class T, int V, bool STEP>
 __global__ __launch_bounds__(256) void k_muon_norm(MuonIn a, uint32_t P, double inv_P, const int32_t *err) {
     constexpr int AHEAD = STEP ? 2 : 4;
@@ -392,7 +393,7 @@ __device__ __forceinline__ void put_tile(const MuonArgs &a, const Place &p, cons
 // The sums of a wavefront: C[i][j] += sum_k L[i][k] R[j][k], 32 x 32 pieces (v_mfma_f32_32x32x16_f16).
 // The matrix instruction does not round its sums to the nearest: a chain of them loses up to a unit in the last place at each link, always the
 // same way.  (One row of 5,000 in a chain of 313: an error of 72 units of 2^-24.)  So with pairs the chains are cut, and their sums
-// added by ordinary additions.
+// added by ordinary additions.  (The sums of at most 16 blocks of k in k_muon_one and of the polynomial in k_muon_poly_apply are one chain.)
 template <int FI, int FJ, int KIND> struct Sums {
     static constexpr int L = left_parts(KIND), R = right_parts(KIND);
     floatx16 acc[FI][FJ], total[KIND == SPLIT ? FI : 1][KIND == SPLIT ? FJ : 1];
@@ -615,7 +616,7 @@ template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinlin
 // asks for the next block's operands before it multiplies the ones it has, also across the meeting of the wavefronts at which a
 // stage is given up and the next one is known to be there.
 // The matrix units bound the large ones (a library's product of 8192 x 8192 fp16 numbers: 1,071 TFLOP/s).  Two of 4096 x 4096, tiles of 256: P X 275 GFLOP in
-// 255 us, 1,078 TFLOP/s, with pairs on the right 550 in 467, 1,178; X X' 146 in 162 with its rest and the join, 901.  Tiles of 128, pairs: P X of 1024 x 1024
+// 252 us, 1,091 TFLOP/s, with pairs on the right 550 in 452, 1,216; X X' 146 in 164 with its rest and the join, 890.  Tiles of 128, pairs: P X of 1024 x 1024
 // by 4096, 25.8 GFLOP in 33 us: 23 of them at 1,120 TFLOP/s, the rest launch, first operands and the way out; X X' 13.5 in 28 with the join.
 // (Operands straight from memory into registers are slower: the die's cache bounds it then.)
 constexpr int stage_pieces(int FI, int KB, int kind) { return 2 * FI * KB * (left_parts(kind) + right_parts(kind)); }   // of 1,024 bytes
