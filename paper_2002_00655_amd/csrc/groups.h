@@ -1,0 +1,51 @@
+// Rows grouped by the matrix that they use (group_rows): where a group's rows stand in the order, and the tiles of rows of one group.
+#pragma once
+#include "token_ids.h"
+
+// What a call is given of the groups.  order: the rows, group by group, those of no group behind; offsets: groups + 1 places where they start.  Both come
+// from the caller's memory, so whatever is read from them is brought into range before it is used.
+struct RowGroups {
+    const int32_t *order = nullptr, *offsets = nullptr;
+    int32_t groups = 0;
+    int32_t n = 0;                               // rows
+    __device__ __forceinline__ int start(int e) const {
+        const int o = offsets[e];
+        return o < 0 ? 0 : o > n ? n : o;
+    }
+};
+
+// The rows of one group from place `first` on, `rows` of them.  group == groups: rows of no group.
+struct RowTile { int group, first, rows; };
+
+// Tiles of BM places that hold rows of one group only.  Group e's tiles have the numbers from floor(start_e / BM) + e on: as ceil(c / BM) is at most
+// floor((s + c) / BM) + 1 - floor(s / BM), they end before the next group's, and no tile's number has to be looked up in a sum over the groups.
+// Numbers that belong to no tile have no rows.
+inline int64_t row_tiles(int64_t n, int32_t groups, int BM) { return n / BM + groups + 1; }
+__device__ __forceinline__ RowTile row_tile(const RowGroups &g, int tile, int BM) {
+    // the last e with floor(start_e / BM) + e <= tile: the wavefront's lanes look at 64 of them at once
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = g.groups;
+    while (lo < hi) {
+        const int step = (hi - lo) / 64 + 1, e = lo + lane * step;
+        const bool at = e <= hi && g.start(e) / BM + e <= tile;
+        const int c = __popcll(__ballot(at));
+        lo += (c > 1 ? c - 1 : 0) * step;
+        hi = hi < lo + step - 1 ? hi : lo + step - 1;
+        if (step == 1) break;
+    }
+    RowTile t;
+    t.group = __builtin_amdgcn_readfirstlane(lo < g.groups ? lo : g.groups);
+    const int s = g.start(t.group), end = t.group < g.groups ? g.start(t.group + 1) : g.n;
+    t.first = s + (tile - s / BM - t.group) * BM;
+    t.rows = end - t.first;
+    if (t.first < s || t.rows < 0) t.rows = 0;
+    if (t.rows > BM) t.rows = BM;
+    return t;
+}
+
+// group_rows.hip: the statistics of a pull of the groups' keys: those of a matrix for all (`shared` keys from `first` on, shared_keys may be 0), and for every
+// group that has rows, `each` keys from first_a + group * each on and, if first_b >= 0, from first_b + group * each on
+struct GroupKeys { int64_t first = 0, shared = 0, first_a = 0, first_b = -1; int32_t each = 0; };
+int dpaps_route_groups(dpaps_ps *ps, int32_t worker, const RowGroups &g, const GroupKeys &k, hipStream_t st);
+// group_rows.hip: what all calls check of the groups that they are given
+int dpaps_row_groups(dpaps_ps *ps, const int32_t *order, const int32_t *offsets, int32_t groups, int64_t n, RowGroups *g);

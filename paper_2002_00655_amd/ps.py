@@ -26,7 +26,7 @@ OPT_MF_EXACT, OPT_MF_CACHE_ROWS, OPT_MF_WAVES, OPT_MF_PROFILE, OPT_MF_GROUPED, O
 EXPORTS = ["ps_create", "ps_destroy", "ps_pull", "ps_push", "ps_push_noalloc", "ps_localize", "ps_owner", "ps_stats", "ps_status",
            "ps_set_option", "ps_last_error", "mf_block_ratings", "mf_load_ratings", "mf_sgd_epoch", "mf_sgd_epoch_handoff", "mf_train_sse",
            "mf_profile_read", "kge_sgd_step", "kge_sgd_epoch", "emb_lookup", "emb_grad", "emb_adagrad_step",
-           "muon_orthogonalize", "muon_step"]
+           "muon_orthogonalize", "muon_step", "group_rows", "expert_matmul", "expert_grad", "adapter_matmul", "adapter_grad"]
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}         # PS_F32, PS_BF16, PS_F16
 _TOKENS = {torch.int32: 0, torch.int64: 1}                              # PS_I32, PS_I64
@@ -70,6 +70,11 @@ def load_library() -> C.CDLL:
     lib.emb_adagrad_step.argtypes = [vp, i32, i64, i64, i32, vp, i32, i64, i64, f32, vp, i32, i64, f32, f32, vp]
     lib.muon_orthogonalize.argtypes = [vp, i32, i32, i32, vp, i32, i64, vp, i32, i64, i32, f32, vp]
     lib.muon_step.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32, i64, f32, f32, i32, f32, i32, f32, vp]
+    lib.group_rows.argtypes = [vp, i32, vp, i32, i64, i64, vp, vp, vp]
+    lib.expert_matmul.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, i64, vp, i32, i64, i32, vp, i32, i64, i32, vp]
+    lib.expert_grad.argtypes = [vp, i32, i32, i32, vp, vp, i64, vp, i64, i32, vp, i64, i32, i32, vp, i32, vp]
+    lib.adapter_matmul.argtypes = [vp, i32, i64, i32, i32, i64, i64, i32, i32, f32, vp, vp, i64, vp, i32, i64, vp, i32, i64, vp]
+    lib.adapter_grad.argtypes = [vp, i32, i64, i32, i32, i64, i64, i32, i32, f32, vp, vp, i64, vp, i64, vp, i64, i32, vp, i32, i64, vp, vp, vp]
     for name in EXPORTS:
         if name != "ps_last_error":
             getattr(lib, name).restype = C.c_int
@@ -137,6 +142,32 @@ def _matrices(t: torch.Tensor) -> tuple[int, int, int]:
     for d in t.shape[:-2]:
         batch *= d
     return batch, t.shape[-2], t.shape[-1]
+
+
+def _groups(groups) -> tuple[int, int, int, int]:
+    """What group_rows has returned: where the order and the offsets are, the number of groups, of rows."""
+    order, offsets = groups
+    _dev(order, torch.int32), _dev(offsets, torch.int32)
+    if offsets.numel() < 2:
+        raise ValueError("the offsets of groups are one more than there are groups")
+    return order.data_ptr(), offsets.data_ptr(), offsets.numel() - 1, order.numel()
+
+
+def _count_of(t: torch.Tensor) -> int:
+    n = 1
+    for d in t.shape[:-1]:
+        n *= d
+    return n
+
+
+def _pairs_of(t: torch.Tensor, n: int, what: str) -> tuple[int, int]:
+    """Rows of a tensor that stand for n rows, and for how many each of them stands."""
+    rows = _count_of(t) if t.dim() else 0
+    if n == 0 and rows == 0:
+        return 0, 1
+    if rows <= 0 or n % rows or n == 0:
+        raise ValueError(f"{what} has {rows} rows, which cannot stand for the {n} of the groups")
+    return rows, n // rows
 
 
 def _host(a, dtype) -> np.ndarray:
@@ -353,6 +384,95 @@ class ParameterServer:
         kept, frm, kind, ld = _rows(grad, batch * rows, apart=True)
         self._check(_lib.muon_step(self._h, worker, first_key, batch, rows, dim, frm, kind, ld, lr, momentum, int(nesterov), weight_decay, steps, eps,
                                    _stream()), "muon_step")
+
+    # -- models of many matrices ------------------------------------------------------
+    def group_rows(self, ids: torch.Tensor, num_groups: int, pad: int | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+        """The rows, numbered as `ids` lie, ordered by the group that they name, and where the groups start, num_groups + 1 places; rows whose id is `pad`
+        are of no group (see include/dpaps.h)."""
+        at, kind, n = _tokens(ids)
+        order = torch.empty(n, dtype=torch.int32, device=ids.device)
+        offsets = torch.empty(num_groups + 1, dtype=torch.int32, device=ids.device)
+        self._check(_lib.group_rows(self._h, num_groups, at, kind, n, _NO_PAD if pad is None else pad, order.data_ptr(), offsets.data_ptr(), _stream()), "group_rows")
+        return order, offsets
+
+    def expert_matmul(self, x: torch.Tensor, groups, first_key: int, rows: int, dim: int | None = None, transposed: bool = False, sum_pairs: int = 1,
+                      worker: int = -1, dtype: torch.dtype | None = None, out: torch.Tensor | None = None):
+        """The grouped rows times their expert's matrix (rows x dim, keys of the server), or its transpose; `groups` from group_rows (see include/dpaps.h).  x has
+        the groups' n rows, or fewer, each of which then stands for as many neighbouring ones.  The result, in x's type or `dtype`, is [n / sum_pairs, columns]:
+        of sum_pairs neighbouring rows the sum."""
+        order, offsets, experts, n = _groups(groups)
+        dim = self.L if dim is None else dim
+        given, columns = (rows, dim) if transposed else (dim, rows)
+        if x.dim() == 0 or x.shape[-1] != given:
+            raise ValueError(f"expected rows of {given} numbers, got shape {tuple(x.shape)}")
+        x_rows, x_pairs = _pairs_of(x, n, "x")
+        if sum_pairs < 1 or n % sum_pairs:
+            raise ValueError(f"sums of {sum_pairs} of {n} rows")
+        shape = (n // sum_pairs, columns)
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
+        elif out.shape[-1:] != shape[1:] or _count_of(out) != shape[0]:
+            raise ValueError(f"out must have the shape {shape}")
+        kept, frm, kind, stride = _rows(x, x_rows)
+        _, to, out_kind, out_stride = _rows(out, shape[0], copy=False)
+        self._check(_lib.expert_matmul(self._h, worker, first_key, experts, rows, dim, int(transposed), order, offsets, n, frm, kind, stride, x_pairs, to, out_kind,
+                                       out_stride, sum_pairs, _stream()), "expert_matmul")
+        return out
+
+    def expert_grad(self, left: torch.Tensor, right: torch.Tensor, groups, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None):
+        """Per group the sum of its rows' products left_i right_j, [groups, rows, dim]: the gradients of experts' matrices (see include/dpaps.h)."""
+        order, offsets, experts, n = _groups(groups)
+        if left.dtype != right.dtype:
+            raise TypeError(f"left and right have one type, not {left.dtype} and {right.dtype}")
+        (left_rows, left_pairs), (right_rows, right_pairs) = _pairs_of(left, n, "left"), _pairs_of(right, n, "right")
+        shape = (experts, left.shape[-1], right.shape[-1])
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=left.device)
+        elif out.shape != shape or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous and have the shape {shape}")
+        kept_left, l, kind, l_stride = _rows(left, left_rows)
+        kept_right, r, _, r_stride = _rows(right, right_rows)
+        _, to, out_kind, _ = _rows(out, experts * shape[1], copy=False)
+        self._check(_lib.expert_grad(self._h, experts, shape[1], shape[2], order, offsets, n, l, l_stride, left_pairs, r, r_stride, right_pairs, kind, to, out_kind,
+                                     _stream()), "expert_grad")
+        return out
+
+    def adapter_matmul(self, x: torch.Tensor, groups, first_key: int, rows: int, first_a: int, first_b: int, rank: int, scale: float = 1.0, dim: int | None = None,
+                       worker: int = -1, dtype: torch.dtype | None = None, out: torch.Tensor | None = None):
+        """Rows [..., dim] times a shared matrix and, beside it, scaled, their adapter's two of low rank, [..., rows]; `groups` from group_rows of the rows' adapters (see
+        include/dpaps.h)."""
+        order, offsets, adapters, n = _groups(groups)
+        dim = self.L if dim is None else dim
+        if x.dim() == 0 or x.shape[-1] != dim or _count_of(x) != n:
+            raise ValueError(f"expected {n} rows of {dim} numbers, got shape {tuple(x.shape)}")
+        if out is None:
+            out = torch.empty((*x.shape[:-1], rows), dtype=x.dtype if dtype is None else dtype, device=x.device)
+        elif out.shape != (*x.shape[:-1], rows):
+            raise ValueError(f"out must have the shape {(*x.shape[:-1], rows)}")
+        kept, frm, kind, stride = _rows(x, n)
+        _, to, out_kind, out_stride = _rows(out, n, copy=False)
+        self._check(_lib.adapter_matmul(self._h, worker, first_key, rows, dim, first_a, first_b, adapters, rank, scale, order, offsets, n, frm, kind, stride, to, out_kind,
+                                        out_stride, _stream()), "adapter_matmul")
+        return out
+
+    def adapter_grad(self, x: torch.Tensor, dout: torch.Tensor, groups, first_key: int, first_a: int, first_b: int, rank: int, scale: float = 1.0, worker: int = -1,
+                     want_dx: bool = True, dtype: torch.dtype | None = None):
+        """The gradients of adapter_matmul with respect to x (or None), in x's type or `dtype`, and to all adapters' A and B transposed, fp32, [adapters, rank, dim] and
+        [adapters, rank, rows] (see include/dpaps.h)."""
+        order, offsets, adapters, n = _groups(groups)
+        if x.dtype != dout.dtype:
+            raise TypeError(f"x and dout have one type, not {x.dtype} and {dout.dtype}")
+        if x.dim() == 0 or dout.shape[:-1] != x.shape[:-1] or _count_of(x) != n:
+            raise ValueError(f"expected {n} rows, got shapes {tuple(x.shape)} and {tuple(dout.shape)}")
+        dim, rows = x.shape[-1], dout.shape[-1]
+        dx = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device) if want_dx else None
+        da, db = (torch.empty((adapters, rank, c), dtype=torch.float32, device=x.device) for c in (dim, rows))
+        kept_x, frm, kind, stride = _rows(x, n)
+        kept_d, d, _, d_stride = _rows(dout, n)
+        to, to_kind, to_stride = (_rows(dx, n, copy=False)[1:]) if want_dx else (None, kind, dim)
+        self._check(_lib.adapter_grad(self._h, worker, first_key, rows, dim, first_a, first_b, adapters, rank, scale, order, offsets, n, frm, stride, d, d_stride, kind, to,
+                                      to_kind, to_stride, da.data_ptr(), db.data_ptr(), _stream()), "adapter_grad")
+        return dx, da, db
 
 
 def mf_block_ratings(m, n, rows, cols, vals, row_bounds, col_bounds):
