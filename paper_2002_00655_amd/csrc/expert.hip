@@ -9,18 +9,9 @@
 
 namespace {
 
-constexpr int BR = 128, BC = 128, TILE_THREADS = 256;
-
-__device__ __forceinline__ int row_at(const RowGroups &g, int place, int32_t *err) {
-    const int q = g.order[place];
-    if (q >= 0 && q < g.n) return q;
-    atomicExch(err, PS_EKEY);
-    return -1;
-}
-
-template <class CT, class XT, bool TURNED>
-__global__ __launch_bounds__(TILE_THREADS) void k_expert(ExpertArgs a, int32_t col_tiles, int32_t *err) {
-    constexpr int KU = unit_of<CT>();
+template <class CT, class XT, bool TURNED, class T>
+__global__ __launch_bounds__(T::THREADS) void k_expert(ExpertArgs a, int32_t col_tiles, int32_t *err) {
+    constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
     __shared__ Vec<CT, KU> lds[2][(BR + BC) * UNITS];
     __shared__ int at[BR];                                           // the rows' numbers; -1: none
     __shared__ int off;
@@ -29,13 +20,16 @@ __global__ __launch_bounds__(TILE_THREADS) void k_expert(ExpertArgs a, int32_t c
     const int c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * BC, tid = threadIdx.x;
     __syncthreads();
     if (off || t.rows == 0) return;
-    if (tid < BR) at[tid] = tid < t.rows ? row_at(a.g, t.first + tid, err) : -1;
+    for (int r = tid; r < BR; r += T::THREADS) {
+        at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
+        if (a.group_of && c0 == 0 && r < t.rows) a.group_of[t.first + r] = t.group;
+    }
     __syncthreads();
-    floatx16 acc[2][2] = {};
-    const int wave = tid >> 6, wc = (wave & 1) * 64, wr = (wave >> 1) * 64, cols = a.N - c0;
+    floatx16 acc[T::MC][T::MR] = {};
+    const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR, cols = a.N - c0;
     if (t.group < a.g.groups) {
         const float *w = a.w + (int64_t)t.group * a.each * a.L;
-        KMajor<XT, CT, BR, TILE_THREADS> rows;
+        KMajor<XT, CT, BR, T::THREADS> rows;
         rows.init([&](int r) { return at[r] < 0 ? nullptr : reinterpret_cast<const XT *>(a.x) + a.x_shared(at[r]) * a.x_stride; });
         const int steps = (a.K + step_of<CT>() - 1) / step_of<CT>();
         auto loop = [&](auto load, auto &columns) {
@@ -46,28 +40,28 @@ __global__ __launch_bounds__(TILE_THREADS) void k_expert(ExpertArgs a, int32_t c
             __syncthreads();
             for (int s = 0; s < steps; ++s) {
                 if (s + 1 < steps) { rows.load(s + 1, a.K); load(s + 1); }
-                step_products<CT, 2, 2>(lds[s & 1] + BR * UNITS, lds[s & 1], wc, wr, UNITS, acc);
+                step_products<CT, T::MC, T::MR>(lds[s & 1] + BR * UNITS, lds[s & 1], wc, wr, UNITS, acc);
                 if (s + 1 < steps) { rows.put(lds[(s + 1) & 1]); columns.put(lds[(s + 1) & 1] + BR * UNITS); }
                 __syncthreads();
             }
         };
         if constexpr (TURNED) {
-            NMajor<float, CT, BC, TILE_THREADS> columns;
+            NMajor<float, CT, BC, T::THREADS> columns;
             loop([&](int s) { columns.load(s, a.K, cols, [&](int k) { return w + (int64_t)k * a.L + c0; }); }, columns);
         } else {
-            KMajor<float, CT, BC, TILE_THREADS> columns;
+            KMajor<float, CT, BC, T::THREADS> columns;
             columns.init([&](int c) { return c < cols ? w + (int64_t)(c0 + c) * a.L : nullptr; });
             loop([&](int s) { columns.load(s, a.K); }, columns);
         }
     }
     const int l32 = tid & 31, h = (tid & 63) >> 5;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < T::MR; ++j) {
         const int r = wr + 32 * j + l32;
         if (at[r] < 0) continue;
         const int64_t to = (int64_t)(a.by_place ? t.first + r : at[r]) * a.out_stride;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < T::MC; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int c = wc + 32 * i + 8 * q + 4 * h;
@@ -77,33 +71,78 @@ __global__ __launch_bounds__(TILE_THREADS) void k_expert(ExpertArgs a, int32_t c
     }
 }
 
-// Group blockIdx.y's sum of products, a tile of it.  Left and right in the order of the places of the group's rows.
-template <class CT, class LT, class RT>
-__global__ __launch_bounds__(TILE_THREADS) void k_outer(OuterArgs a, int32_t row_tiles, int32_t col_tiles, int32_t *err) {
-    constexpr int KU = unit_of<CT>();
-    __shared__ Vec<CT, KU> lds[2][(BR + BC) * UNITS];
+// Groups of few rows.
+template <class CT, class XT, bool TURNED, int MT>
+__global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expert_few(ExpertArgs a, int32_t col_tiles, int32_t *err) {
+    typedef FewRows<CT, XT, TURNED, MT> F;
+    __shared__ float sums[F::SUMS];
+    __shared__ int at[16 * MT];
     __shared__ int off;
     look_for_all(err, &off);
-    const int tid = threadIdx.x, group = (int)(blockIdx.x / (uint32_t)(row_tiles * col_tiles)), tile = (int)(blockIdx.x % (uint32_t)(row_tiles * col_tiles));
-    const int r0 = tile / col_tiles * BR, c0 = tile % col_tiles * BC;
-    const int first = a.g.start(group), end = a.g.start(group + 1), K = end > first ? end - first : 0;
+    const RowTile t = row_tile(a.g, (int)(blockIdx.x / (uint32_t)col_tiles), 16 * MT);
+    const int c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * F::COLS, tid = threadIdx.x;
+    __syncthreads();
+    if (off || t.rows == 0) return;
+    if (tid < 16 * MT) {
+        at[tid] = tid < t.rows ? row_at(a.g, t.first + tid, err) : -1;
+        if (a.group_of && c0 == 0 && tid < t.rows) a.group_of[t.first + tid] = t.group;
+    }
+    __syncthreads();
+    if (t.group < a.g.groups) {
+        F f;
+        f.run(a.w + (int64_t)t.group * a.each * a.L, a.L, a.K, c0, a.N,
+              [&](int r) { return reinterpret_cast<const XT *>(a.x) + a.x_shared(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
+        f.put(sums);
+    }
+    __syncthreads();
+    for (int p = tid; p < F::PIECES; p += F::THREADS) {
+        const int r = F::row_of(p), c = F::col_of(p), left = a.N - c0 - c;
+        if (at[r] < 0 || left <= 0) continue;
+        const Vec<float, 4> v = t.group < a.g.groups ? a.scale * F::sum(sums, p) : Vec<float, 4>{};
+        put_typed(a.out, a.out_type, (int64_t)(a.by_place ? t.first + r : at[r]) * a.out_stride + c0 + c, v, left);
+    }
+}
+
+// A group's sum of products, a tile of it, over `chunk` places of its rows: a group of more than that has several workgroups for a tile.  The first of them
+// writes to the result, or, where that is not of 32 bits, to a slot of part; the others to slots that are told apart by their first place, whole chunks:
+// floor(first / chunk) differs between all chunks but the first ones of groups of several, as it does between the first ones.
+struct OuterTiles { int32_t rows, cols, chunk; float *part; int32_t slots; };
+__device__ __forceinline__ float *outer_slot(const OuterArgs &a, const OuterTiles &o, int group, int start, int first) {
+    const int64_t size = (int64_t)a.rows * a.cols;
+    if (first > start) return o.part + first / o.chunk * size;
+    return a.out_type == PS_F32 ? reinterpret_cast<float *>(a.out) + group * size : o.part + (o.slots + first / o.chunk) * size;
+}
+template <class CT, class LT, class RT, class T>
+__global__ __launch_bounds__(T::THREADS) void k_outer(OuterArgs a, OuterTiles o, int32_t *err) {
+    constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
+    __shared__ Vec<CT, KU> lds[2][(BR + BC) * UNITS];
+    extern __shared__ int at[];                                      // the rows' numbers of the chunk
+    __shared__ int off;
+    look_for_all(err, &off);
+    const int tid = threadIdx.x, tiles = o.rows * o.cols, tile = (int)(blockIdx.x % (uint32_t)tiles);
+    const int r0 = tile / o.cols * BR, c0 = tile % o.cols * BC;
+    const RowTile t = row_tile(a.g, (int)(blockIdx.x / (uint32_t)tiles), o.chunk);
+    if (t.group >= a.g.groups) return;
+    const int start = a.g.start(t.group), end = a.g.start(t.group + 1);
+    const bool empty = start >= end;
+    // (a group without rows has one chunk, of none: its matrix is cleared)
+    if (t.rows == 0 && !(empty && (int)(blockIdx.x / (uint32_t)tiles) == start / o.chunk + t.group)) return;
+    for (int p = tid; p < t.rows; p += T::THREADS) {
+        const int q = row_at(a.g, t.first + p, err);
+        at[p] = q < 0 ? 0 : q;                                       // (row 0 is read in its place; the error is set)
+    }
     __syncthreads();
     if (off) return;
-    floatx16 acc[2][2] = {};
-    const int wave = tid >> 6, wc = (wave & 1) * 64, wr = (wave >> 1) * 64;
-    NMajor<LT, CT, BR, TILE_THREADS> left;
-    NMajor<RT, CT, BC, TILE_THREADS> right;
-    const int steps = (K + step_of<CT>() - 1) / step_of<CT>();
-    // (a row out of range is left out: row 0 would be read in its place, so its number is looked at first)
-    const auto number = [&](int p) {
-        const int q = row_at(a.g, first + p, err);
-        return q < 0 ? 0 : q;
-    };
+    floatx16 acc[T::MC][T::MR] = {};
+    const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
+    NMajor<LT, CT, BR, T::THREADS> left;
+    NMajor<RT, CT, BC, T::THREADS> right;
+    const int steps = (t.rows + step_of<CT>() - 1) / step_of<CT>();
     const auto load = [&](int s) {
-        left.load(s, K, a.rows - r0, [&](int p) {
-            return reinterpret_cast<const LT *>(a.left) + (int64_t)(a.left_by_place ? first + p : a.left_shared(number(p))) * a.left_stride + r0;
+        left.load(s, t.rows, a.rows - r0, [&](int p) {
+            return reinterpret_cast<const LT *>(a.left) + (int64_t)(a.left_by_place ? t.first + p : a.left_shared(at[p])) * a.left_stride + r0;
         });
-        right.load(s, K, a.cols - c0, [&](int p) { return reinterpret_cast<const RT *>(a.right) + (int64_t)a.right_shared(number(p)) * a.right_stride + c0; });
+        right.load(s, t.rows, a.cols - c0, [&](int p) { return reinterpret_cast<const RT *>(a.right) + (int64_t)a.right_shared(at[p]) * a.right_stride + c0; });
     };
     if (steps > 0) {
         load(0);
@@ -113,23 +152,42 @@ __global__ __launch_bounds__(TILE_THREADS) void k_outer(OuterArgs a, int32_t row
     }
     for (int s = 0; s < steps; ++s) {
         if (s + 1 < steps) load(s + 1);
-        step_products<CT, 2, 2>(lds[s & 1] + BR * UNITS, lds[s & 1], wc, wr, UNITS, acc);
+        step_products<CT, T::MC, T::MR>(lds[s & 1] + BR * UNITS, lds[s & 1], wc, wr, UNITS, acc);
         if (s + 1 < steps) { left.put(lds[(s + 1) & 1]); right.put(lds[(s + 1) & 1] + BR * UNITS); }
         __syncthreads();
     }
+    const bool whole = end - start <= o.chunk;
+    void *out = whole ? a.out : outer_slot(a, o, t.group, start, t.first);
+    const int32_t type = whole ? a.out_type : PS_F32;
+    const int64_t base = whole ? (int64_t)t.group * a.rows * a.cols : 0;
     const int l32 = tid & 31, h = (tid & 63) >> 5;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < T::MR; ++j) {
         const int r = r0 + wr + 32 * j + l32;
         if (r >= a.rows) continue;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < T::MC; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int c = c0 + wc + 32 * i + 8 * q + 4 * h;
                 const Vec<float, 4> v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (c < a.cols) put_typed(a.out, a.out_type, ((int64_t)group * a.rows + r) * a.cols + c, v, a.cols - c);
+                if (c < a.cols) put_typed(out, type, base + (int64_t)r * a.cols + c, v, a.cols - c);
             }
+    }
+}
+// The chunks of groups of several, added up in their order.  blockIdx.y: the group
+__global__ __launch_bounds__(256) void k_outer_join(OuterArgs a, OuterTiles o, const int32_t *err) {
+    if (*(volatile const int32_t *)err) return;
+    const int64_t size = (int64_t)a.rows * a.cols;
+    for (int group = blockIdx.y; group < a.g.groups; group += gridDim.y) {
+        const int start = a.g.start(group), end = a.g.start(group + 1);
+        if (end - start <= o.chunk) continue;
+        for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
+            const int left = size - i < 4 ? (int)(size - i) : 4;
+            Vec<float, 4> v = {};
+            for (int first = start; first < end; first += o.chunk) v = v + load_some<float, 4>(outer_slot(a, o, group, start, first) + i, left);
+            put_typed(a.out, a.out_type, group * size + i, v, left);
+        }
     }
 }
 
@@ -153,42 +211,87 @@ int too_large(dpaps_ps *ps, const char *what) {
 
 }  // namespace
 
-int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
-    const int32_t col_tiles = (a.N + BC - 1) / BC;
-    const int64_t grid = row_tiles(a.g.n, a.g.groups, BR) * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "expert_matmul");
-#define EXPERT(CT, XT)                                                                                      \
-    do {                                                                                                    \
-        if (a.turned) k_expert<CT, XT, true><<<(unsigned)grid, TILE_THREADS, 0, st>>>(a, col_tiles, ps->err); \
-        else k_expert<CT, XT, false><<<(unsigned)grid, TILE_THREADS, 0, st>>>(a, col_tiles, ps->err);         \
-    } while (0)
-    if (a.x_type == PS_F32) EXPERT(float, float);
-    else if (a.x_type == PS_BF16) {
-        if (a.precise) EXPERT(float, bf16_t);
-        else EXPERT(bf16_t, bf16_t);
-    } else {
-        if (a.precise) EXPERT(float, f16_t);
-        else EXPERT(f16_t, f16_t);
-    }
-#undef EXPERT
+namespace {
+template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
+    const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
+    const int64_t grid = row_tiles(a.g.n, a.g.groups, T::ROWS) * col_tiles;
+    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "product");
+    k_expert<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, 0, st>>>(a, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
-
-int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs &a, hipStream_t st) {
-    const int32_t row_tiles = (a.rows + BR - 1) / BR, col_tiles = (a.cols + BC - 1) / BC;
-    const int64_t grid = (int64_t)a.g.groups * row_tiles * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "expert_grad");
-#define OUTER(CT, LT, RT) k_outer<CT, LT, RT><<<(unsigned)grid, TILE_THREADS, 0, st>>>(a, row_tiles, col_tiles, ps->err)
-    if (a.left_type == PS_F32) {
-        if (a.right_type == PS_F32) OUTER(float, float, float);
-        else if (a.right_type == PS_BF16) OUTER(float, float, bf16_t);
-        else OUTER(float, float, f16_t);
-    } else if (a.left_type == PS_BF16) OUTER(bf16_t, bf16_t, bf16_t);
-    else OUTER(f16_t, f16_t, f16_t);
-#undef OUTER
+template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
+    typedef FewRows<CT, XT, TURNED, MT> F;
+    const int32_t col_tiles = (a.N + F::COLS - 1) / F::COLS;
+    const int64_t grid = row_tiles(a.g.n, a.g.groups, 16 * MT) * col_tiles;
+    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "product");
+    k_expert_few<CT, XT, TURNED, MT><<<(unsigned)grid, F::THREADS, 0, st>>>(a, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
+}
+template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
+    const int64_t n = a.g.n, groups = a.g.groups;
+    if (n <= 8 * groups || n <= 16) return few_of<CT, XT, TURNED, 1>(ps, a, st);
+    if (n <= 24 * groups || n <= 64) return few_of<CT, XT, TURNED, 2>(ps, a, st);
+    if (a.N <= 32) return tiles_of<CT, XT, TURNED, Narrow>(ps, a, st);
+    if (ceil_div64(n, 128) * ceil_div64(a.N, 128) < 2 * ps->num_cu) return tiles_of<CT, XT, TURNED, Tile64>(ps, a, st);
+    return tiles_of<CT, XT, TURNED, Tile128>(ps, a, st);
+}
+template <class CT, class XT> int product_either(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
+    return a.turned ? product_of<CT, XT, true>(ps, a, st) : product_of<CT, XT, false>(ps, a, st);
+}
+}  // namespace
+
+int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
+    if (a.x_type == PS_F32) return product_either<float, float>(ps, a, st);
+    if (a.x_type == PS_BF16) return a.precise ? product_either<float, bf16_t>(ps, a, st) : product_either<bf16_t, bf16_t>(ps, a, st);
+    return a.precise ? product_either<float, f16_t>(ps, a, st) : product_either<f16_t, f16_t>(ps, a, st);
+}
+
+namespace {
+// The tiles of a sum, and how many of a group's rows a workgroup takes: as few as it needs for two workgroups a compute unit.
+template <class T> OuterTiles outer_tiles(const dpaps_ps *ps, const OuterArgs &a) {
+    OuterTiles o{};
+    o.rows = (a.rows + T::ROWS - 1) / T::ROWS;
+    o.cols = (a.cols + T::COLS - 1) / T::COLS;
+    o.chunk = 2048;
+    while (o.chunk > 256 && (int64_t)o.rows * o.cols * ceil_div64(a.g.n, o.chunk) < 2 * ps->num_cu) o.chunk /= 2;
+    o.slots = a.g.n / o.chunk + 1;
+    return o;
+}
+bool outer_narrow(const OuterArgs &a) { return a.rows <= 64; }
+template <class CT, class LT, class RT, class T> int outer_of(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st) {
+    OuterTiles o = outer_tiles<T>(ps, a);
+    o.part = part;
+    const int64_t grid = row_tiles(a.g.n, a.g.groups, o.chunk) * o.rows * o.cols;
+    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "expert_grad");
+    static LdsAllowed allowed;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer<CT, LT, RT, T>), 2048 * sizeof(int));
+    if (rc) return rc;
+    k_outer<CT, LT, RT, T><<<(unsigned)grid, T::THREADS, o.chunk * sizeof(int), st>>>(a, o, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    if (a.g.n <= o.chunk) return PS_OK;
+    const int64_t x = ceil_div64((int64_t)a.rows * a.cols, 1024);
+    k_outer_join<<<dim3((unsigned)(x < 256 ? x : 256), (unsigned)(a.g.groups < 1024 ? a.g.groups : 1024)), 256, 0, st>>>(a, o, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+template <class CT, class LT, class RT> int outer_any(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st) {
+    return outer_narrow(a) ? outer_of<CT, LT, RT, Low>(ps, a, part, st) : outer_of<CT, LT, RT, Tile128>(ps, a, part, st);
+}
+}  // namespace
+
+size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs &a) {
+    const OuterTiles o = outer_narrow(a) ? outer_tiles<Low>(ps, a) : outer_tiles<Tile128>(ps, a);
+    if (a.g.n <= o.chunk) return 0;
+    return (size_t)o.slots * (a.out_type == PS_F32 ? 1 : 2) * (size_t)a.rows * (size_t)a.cols * sizeof(float);
+}
+int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st) {
+    if (a.left_type == PS_F32) {
+        if (a.right_type == PS_F32) return outer_any<float, float, float>(ps, a, part, st);
+        return a.right_type == PS_BF16 ? outer_any<float, float, bf16_t>(ps, a, part, st) : outer_any<float, float, f16_t>(ps, a, part, st);
+    }
+    return a.left_type == PS_BF16 ? outer_any<bf16_t, bf16_t, bf16_t>(ps, a, part, st) : outer_any<f16_t, f16_t, f16_t>(ps, a, part, st);
 }
 
 extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed,
@@ -234,12 +337,13 @@ extern "C" int expert_grad(ps_handle ps, int32_t num_experts, int32_t rows, int3
                            void *out, int32_t out_type, void *stream) {
     if (!ps || num_experts <= 0 || rows <= 0 || dim <= 0 || !is_element_type(type) || !is_element_type(out_type) || !out) return PS_EINVAL;
     RowGroups g;
-    const int rc = dpaps_row_groups(ps, order, offsets, num_experts, n, &g);
+    int rc = dpaps_row_groups(ps, order, offsets, num_experts, n, &g);
     if (rc) return rc;
     if (left_pairs < 1 || right_pairs < 1 || n % left_pairs || n % right_pairs || (n > 0 && (!left || !right || left_stride < 0 || right_stride < 0))) return PS_EINVAL;
     OuterArgs a{};
     a.g = g; a.left = left; a.left_stride = left_stride; a.left_type = type; a.left_shared = Quotient(left_pairs);
     a.right = right; a.right_stride = right_stride; a.right_type = type; a.right_shared = Quotient(right_pairs);
     a.rows = rows; a.cols = dim; a.out = out; a.out_type = out_type;
-    return dpaps_outer_sums(ps, a, (hipStream_t)stream);
+    rc = dpaps_ws_reserve(ps, dpaps_outer_bytes(ps, a));
+    return rc ? rc : dpaps_outer_sums(ps, a, (float *)ps->ws, (hipStream_t)stream);
 }

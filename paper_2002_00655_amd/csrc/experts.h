@@ -12,6 +12,7 @@ struct ExpertArgs {
     float scale;
     void *out; int64_t out_stride; int32_t out_type, by_place;               // by_place: the row at place p goes to row p of out
     int32_t precise;                                                         // products of numbers of 32 bits
+    int32_t *group_of;                                                       // not NULL: the group of the row at place p
 };
 int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st);
 
@@ -23,7 +24,18 @@ struct OuterArgs {
     int32_t rows, cols;
     void *out; int32_t out_type;
 };
-int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs &a, hipStream_t st);
+// part: scratch of dpaps_outer_bytes(...) bytes
+size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs &a);
+int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st);
+
+
+// The row number that stands at a place; -1, and the handle's error, where there is no such row.
+__device__ __forceinline__ int row_at(const RowGroups &g, int place, int32_t *err) {
+    const int q = g.order[place];
+    if (q >= 0 && q < g.n) return q;
+    atomicExch(err, PS_EKEY);
+    return -1;
+}
 
 // out_p = M x_p + sum_r low[place of p][r] B_e[r], with a matrix M for all rows (or its transpose), low: fp32, of rows of a group, scaled already
 struct AdapterArgs {
@@ -32,6 +44,88 @@ struct AdapterArgs {
     const float *w; int64_t L;
     int32_t K, N, turned;
     const float *low; int64_t low_stride; int32_t rank;
+    const int32_t *group_of;                                                 // the group of the row at place p
     const float *b;                                                          // group e's rank rows from b + e * rank * L on
     void *out; int64_t out_stride; int32_t out_type;
+};
+
+// Few rows: MT tiles of 16 rows by the columns of a workgroup, whose wavefronts share the sum over k.  Both operands come straight from memory into the registers
+// that the matrix instruction reads, and nothing but the wavefronts' sums sees LDS: what counts is that all of the matrix is on its way at once.
+//   M as it is:  16 columns; lane l has column l % 16, and of a step's 4 units the one l / 16
+//   turned:      64 columns; lane l has the four columns from 4 (l % 16) on, for the numbers of unit l / 16: operand j is column 4 i + j of lane i
+// out[row][column] of wavefront w in sums, [w][16 MT][columns].
+template <class CT, class XT, bool TURNED, int MT> struct FewRows {
+    static constexpr int KU = unit_of<CT>(), COLS = TURNED ? 64 : 16, OPS = TURNED ? 4 : 1, WAVES = TURNED && MT == 4 ? 4 : 8, THREADS = 64 * WAVES, STEP = 4 * KU;
+    static constexpr int AHEAD = TURNED ? (KU == 8 ? 2 : 4) : (KU == 8 ? 4 : 8);
+    static constexpr int SUMS = WAVES * 16 * MT * COLS;
+    floatx4 acc[OPS][MT];
+    // w: where the matrix starts; c0: its first column here; x_of(r): where row r < 16 MT of the tile is (any row where there is none)
+    template <class F> __device__ __forceinline__ void run(const float *w, int64_t L, int K, int c0, int N, F x_of) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+        const int steps = (K + STEP - 1) / STEP, s0 = steps * wave / WAVES, s1 = steps * (wave + 1) / WAVES;
+        const float *mine = TURNED ? w + c0 + 4 * l16 : w + (int64_t)(c0 + l16 < N ? c0 + l16 : N - 1) * L;
+        const int cols = N - c0 - 4 * l16;
+#pragma unroll
+        for (int j = 0; j < OPS; ++j)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[j][m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        const XT *x[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) x[m] = x_of(16 * m + l16);
+        for (int s = s0; s < s1; s += AHEAD) {
+            Vec<float, KU> wv[AHEAD][OPS];
+            Vec<XT, KU> xv[AHEAD][MT];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int k = (s + u) * STEP + g * KU, left = s + u < s1 ? K - k : 0;
+                if constexpr (TURNED) {
+                    Vec<float, 4> rows[KU];
+#pragma unroll
+                    for (int i = 0; i < KU; ++i) {
+                        rows[i] = Vec<float, 4>{};
+                        if (i < left && cols > 0) rows[i] = load_some<float, 4>(mine + (int64_t)(k + i) * L, cols);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < KU; ++i) wv[u][j][i] = rows[i][j];
+                } else {
+                    wv[u][0] = Vec<float, KU>{};
+                    if (left > 0) wv[u][0] = load_some<float, KU>(mine + k, left);
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    xv[u][m] = Vec<XT, KU>{};
+                    if (left > 0) xv[u][m] = load_some<XT, KU>(x[m] + k, left);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int j = 0; j < OPS; ++j)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[j][m] = mfma_small<CT>(as_type<CT, float, KU>(wv[u][j]), as_type<CT, XT, KU>(xv[u][m]), acc[j][m]);
+        }
+    }
+    __device__ __forceinline__ void put(float *sums) const {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float *to = sums + ((wave * MT + m) * 16 + l16) * COLS + (TURNED ? 16 : 4) * g;
+            if constexpr (TURNED) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<Vec<float, 4> *>(to + 4 * i) = Vec<float, 4>{acc[0][m][i], acc[1][m][i], acc[2][m][i], acc[3][m][i]};
+            } else *reinterpret_cast<Vec<float, 4> *>(to) = acc[0][m];
+        }
+    }
+    // the sum of all wavefronts, of four neighbouring columns: piece p of 16 MT COLS / 4, its row and its first column
+    static constexpr int PIECES = 16 * MT * COLS / 4;
+    __device__ static __forceinline__ int row_of(int p) { return p / (COLS / 4); }
+    __device__ static __forceinline__ int col_of(int p) { return p % (COLS / 4) * 4; }
+    __device__ static __forceinline__ Vec<float, 4> sum(const float *sums, int p) {
+        Vec<float, 4> v = *reinterpret_cast<const Vec<float, 4> *>(sums + p * 4);
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v = v + *reinterpret_cast<const Vec<float, 4> *>(sums + w * 16 * MT * COLS + p * 4);
+        return v;
+    }
 };

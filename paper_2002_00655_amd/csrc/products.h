@@ -61,8 +61,9 @@ template <class ST, class CT, int ROWS, int THREADS> struct KMajor {
 
 // COLS columns that follow each other, for every k.
 template <class ST, class CT, int COLS, int THREADS> struct NMajor {
-    static constexpr int KU = unit_of<CT>(), N = COLS / 4 * UNITS / THREADS;
-    static_assert(N * THREADS == COLS / 4 * UNITS && (COLS / 4) % 1 == 0);
+    static constexpr int KU = unit_of<CT>(), BLOCKS = COLS / 4 * UNITS, N = BLOCKS < THREADS ? 1 : BLOCKS / THREADS;
+    static constexpr bool ALL = N * THREADS == BLOCKS;                         // else only the first threads have one
+    static_assert(ALL || BLOCKS < THREADS);
     Vec<ST, 4> raw[N][KU];
     // row_of(k): where the columns are for this k (below K); cols: those that there are
     template <class F> __device__ __forceinline__ void load(int step, int K, int cols, F row_of) {
@@ -72,7 +73,7 @@ template <class ST, class CT, int COLS, int THREADS> struct NMajor {
 #pragma unroll
             for (int i = 0; i < KU; ++i) {
                 raw[b][i] = Vec<ST, 4>{};
-                if (k + i < K && c < cols) raw[b][i] = load_some<ST, 4>(row_of(k + i) + c, cols - c);
+                if (k + i < K && c < cols && (ALL || at < BLOCKS)) raw[b][i] = load_some<ST, 4>(row_of(k + i) + c, cols - c);
             }
         }
     }
@@ -80,6 +81,7 @@ template <class ST, class CT, int COLS, int THREADS> struct NMajor {
 #pragma unroll
         for (int b = 0; b < N; ++b) {
             const int at = b * THREADS + (int)threadIdx.x, c = at % (COLS / 4) * 4, u = at / (COLS / 4);
+            if (!ALL && at >= BLOCKS) return;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 Vec<ST, KU> v;
@@ -121,6 +123,17 @@ __device__ __forceinline__ void step_products(const Vec<CT, unit_of<CT>()> *cols
     }
 }
 
+// The instruction for 16 columns by 16 rows, as many units as there are lanes.
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+template <class CT> __device__ __forceinline__ floatx4 mfma_small(Vec<CT, unit_of<CT>()> a, Vec<CT, unit_of<CT>()> b, floatx4 c) {
+    if constexpr (sizeof(CT) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    } else if constexpr (std::is_same<CT, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 // A quotient by a number that is known before the launch: of q < 2^29.
 struct Quotient {
     uint32_t by = 1, m = 1;
@@ -147,3 +160,12 @@ __device__ __forceinline__ void put_typed(void *to, int32_t type, int64_t at, Ve
     else if (type == PS_BF16) put_some(reinterpret_cast<bf16_t *>(to) + at, v, left);
     else put_some(reinterpret_cast<f16_t *>(to) + at, v, left);
 }
+
+// A tile's form: WC x WR wavefronts of 32 MC columns by 32 MR rows each.
+template <int MC_, int MR_, int WC_, int WR_> struct Form {
+    static constexpr int MC = MC_, MR = MR_, WC = WC_, WR = WR_, COLS = 32 * MC * WC, ROWS = 32 * MR * WR, THREADS = 64 * WC * WR;
+};
+typedef Form<1, 1, 2, 2> Tile64;
+typedef Form<2, 2, 2, 2> Tile128;
+typedef Form<1, 1, 1, 4> Narrow;                                     // 32 columns, 128 rows
+typedef Form<1, 1, 4, 1> Low;                                        // 128 columns, 32 rows
