@@ -12,9 +12,10 @@
 namespace {
 
 template <class CT, class XT, bool TURNED, class T>
-__global__ __launch_bounds__(T::THREADS) void k_adapter(AdapterArgs a, int32_t col_tiles, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a, int32_t col_tiles, int32_t *err) {
     constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
-    __shared__ Vec<CT, KU> lds[2][(BR + BC) * UNITS];
+    extern __shared__ __align__(16) char shared[];
+    Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
     __shared__ int at[BR];
     __shared__ int off;
     look_for_all(err, &off);
@@ -25,32 +26,21 @@ __global__ __launch_bounds__(T::THREADS) void k_adapter(AdapterArgs a, int32_t c
     if (off) return;
     floatx16 acc[T::MC][T::MR] = {};
     const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR, cols = a.N - c0;
-    const auto loop = [&](int K, auto load_rows, auto &rows, auto load_columns, auto &columns) {
-        const int steps = (K + step_of<CT>() - 1) / step_of<CT>();
-        load_rows(0);
-        load_columns(0);
-        rows.put(lds[0]);
-        columns.put(lds[0] + BR * UNITS);
-        __syncthreads();
-        for (int s = 0; s < steps; ++s) {
-            if (s + 1 < steps) { load_rows(s + 1); load_columns(s + 1); }
-            const int left = K - s * step_of<CT>(), units = (left + KU - 1) / KU;
-            step_products<CT, T::MC, T::MR>(lds[s & 1] + BR * UNITS, lds[s & 1], wc, wr, units < UNITS ? units : UNITS, acc);
-            if (s + 1 < steps) { rows.put(lds[(s + 1) & 1]); columns.put(lds[(s + 1) & 1] + BR * UNITS); }
-            __syncthreads();
-        }
-    };
     {
         KMajor<XT, CT, BR, T::THREADS> rows;
-        rows.init([&](int r) { return at[r] < 0 ? nullptr : reinterpret_cast<const XT *>(a.x) + (int64_t)at[r] * a.x_stride; });
-        if constexpr (TURNED) {
-            NMajor<float, CT, BC, T::THREADS> columns;
-            loop(a.K, [&](int s) { rows.load(s, a.K); }, rows, [&](int s) { columns.load(s, a.K, cols, [&](int k) { return a.w + (int64_t)k * a.L + c0; }); }, columns);
-        } else {
-            KMajor<float, CT, BC, T::THREADS> columns;
-            columns.init([&](int c) { return c < cols ? a.w + (int64_t)(c0 + c) * a.L : nullptr; });
-            loop(a.K, [&](int s) { rows.load(s, a.K); }, rows, [&](int s) { columns.load(s, a.K); }, columns);
-        }
+        rows.init([&](int r) { return reinterpret_cast<const XT *>(a.x) + (int64_t)(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
+        std::conditional_t<TURNED, KeyRows<CT, BC, T::THREADS>, KeyColumns<CT, BC, T::THREADS>> columns;
+        if constexpr (TURNED) columns.init(a.w + c0, a.L);
+        else columns.init(a.w + c0 * a.L, a.L, cols);
+        tile_sum<CT, T>(a.K, lds, wc, wr,
+            [&](int s, auto tail) {
+                rows.template load<decltype(tail)::value>(s, a.K);
+                columns.template load<decltype(tail)::value>(s, a.K);
+            },
+            [&](Vec<CT, KU> *to) {
+                rows.put(to);
+                columns.put(to + BR * UNITS);
+            }, acc);
     }
     // the adapters of the tile's rows, one after the other: the rows of others are zero
     for (int e = row_tile(a.g, first, 1).group; e < a.g.groups; ++e) {
@@ -58,26 +48,25 @@ __global__ __launch_bounds__(T::THREADS) void k_adapter(AdapterArgs a, int32_t c
         if (lo >= count) break;
         if (hi <= lo || hi <= 0) continue;
         KMajor<float, CT, BR, T::THREADS> rows;
-        rows.init([&](int r) { return r >= lo && r < hi ? a.low + (int64_t)(first + r) * a.low_stride : nullptr; });
-        NMajor<float, CT, BC, T::THREADS> columns;
-        const float *b = a.b + (int64_t)e * a.rank * a.L + c0;
-        loop(a.rank, [&](int s) { rows.load(s, a.rank); }, rows, [&](int s) { columns.load(s, a.rank, cols, [&](int k) { return b + (int64_t)k * a.L; }); }, columns);
+        rows.init([&](int r) { return a.low + (int64_t)(first + (r < count ? r : 0)) * a.low_stride; });
+        KeyRows<CT, BC, T::THREADS> columns;
+        columns.init(a.b + (int64_t)e * a.rank * a.L + c0, a.L);
+        tile_sum_short<CT, T>(a.rank, lds, wc, wr,
+            [&](int s, auto tail) {
+                rows.template load<decltype(tail)::value>(s, a.rank);
+                columns.template load<decltype(tail)::value>(s, a.rank);
+            },
+            [&](Vec<CT, KU> *to) {
+#pragma unroll
+                for (int i = 0; i < rows.N; ++i) {
+                    const int r = (i * T::THREADS + tid) / UNITS;
+                    if (r < lo || r >= hi) rows.raw[i] = Vec<float, KU>{};
+                }
+                rows.put(to);
+                columns.put(to + BR * UNITS);
+            }, acc);
     }
-    const int l32 = tid & 31, h = (tid & 63) >> 5;
-#pragma unroll
-    for (int j = 0; j < T::MR; ++j) {
-        const int r = wr + 32 * j + l32;
-        if (at[r] < 0) continue;
-        const int64_t to = (int64_t)at[r] * a.out_stride;
-#pragma unroll
-        for (int i = 0; i < T::MC; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = wc + 32 * i + 8 * q + 4 * h;
-                const Vec<float, 4> v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (c < cols) put_typed(a.out, a.out_type, to + c0 + c, v, cols - c);
-            }
-    }
+    put_tile_typed<T>(acc, lds, a.out, a.out_type, c0, a.N, 1.0f, [&](int r) { return at[r] < 0 ? (int64_t)-1 : (int64_t)at[r] * a.out_stride; });
 }
 
 // Few rows, of any adapters: the low-rank part is added to a row's sums number by number.
@@ -111,7 +100,7 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_adap
             for (int i = 0; i < a.rank; ++i) w = w + low[i] * load_some<float, 4>(b + (int64_t)i * a.L, left);
             v = v + w;
         }
-        put_typed(a.out, a.out_type, (int64_t)at[r] * a.out_stride + c0 + c, v, left);
+        put_typed<4>(a.out, a.out_type, (int64_t)at[r] * a.out_stride + c0 + c, v, left);
     }
 }
 
@@ -119,7 +108,10 @@ template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, c
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
     const int64_t grid = ceil_div64(a.g.n, T::ROWS) * col_tiles;
     if (grid >= ((int64_t)1 << 24)) { ps->last_error = "adapters: too large for one launch"; return PS_ELIMIT; }
-    k_adapter<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, 0, st>>>(a, col_tiles, ps->err);
+    static LdsAllowed allowed;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_adapter<CT, XT, TURNED, T>), T::LDS);
+    if (rc) return rc;
+    k_adapter<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
@@ -146,13 +138,78 @@ int product(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     return precise ? product_either<float, f16_t>(ps, a, st) : product_either<f16_t, f16_t>(ps, a, st);
 }
 
-// low_p = s M_a x_p in 32 bits, of the rows at the places of the order
-int low_numbers(dpaps_ps *ps, const RowGroups &g, const void *x, int32_t type, int64_t stride, int32_t K, const float *m, int32_t rank, float scale, bool precise, float *low,
-                int64_t low_stride, int32_t *group_of, hipStream_t st) {
+// low_p = s M_a x_p of the rows at the places of the order, in 32 bits, or, where the second product takes laid matrices, in the rows' type
+struct LowNumbers { float *numbers; int64_t stride; void *rounded; int64_t rounded_stride; int32_t *group_of; };
+int low_numbers(dpaps_ps *ps, const RowGroups &g, const void *x, int32_t type, int64_t stride, int32_t K, const float *m, int32_t rank, float scale, bool precise, const LowNumbers &low,
+                hipStream_t st) {
     ExpertArgs a{};
-    a.g = g; a.x = x; a.x_stride = stride; a.x_type = type; a.w = m; a.L = ps->L; a.each = rank; a.K = K; a.N = rank; a.scale = scale;
-    a.out = low; a.out_stride = low_stride; a.out_type = PS_F32; a.by_place = 1; a.precise = precise; a.group_of = group_of;
+    a.g = g; a.x = x; a.x_stride = stride; a.x_type = type; a.w = m; a.L = ps->L; a.each = rank; a.K = K; a.N = rank; a.scale = scale; a.by_place = 1; a.precise = precise;
+    a.group_of = low.group_of;
+    if (low.rounded) {
+        a.zero_from = rank;
+        a.N = (int32_t)low.rounded_stride;
+    }
+    if (low.numbers) {
+        a.out = low.numbers; a.out_stride = low.stride; a.out_type = PS_F32;
+        a.also = low.rounded; a.also_stride = low.rounded_stride; a.also_type = type;
+    } else { a.out = low.rounded; a.out_stride = low.rounded_stride; a.out_type = type; }
     return dpaps_expert_product(ps, a, st);
+}
+
+// Scratch of a call, and the product with it.  Many rows of 16 bits: the shared matrix and the adapters' second ones are laid (laid.hip).
+constexpr int64_t LAID_ROWS = 1024;
+struct Scratch {
+    bool laid = false;
+    int64_t stride = 0, rounded_stride = 0, w_size = 0, b_size = 0;
+    size_t numbers[2] = {}, rounded = 0, group_of = 0, zeros = 0, w = 0, b = 0, end = 0;
+};
+// both: the numbers in 32 bits of two products, which gradients need
+Scratch scratch_of(const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
+    Scratch s;
+    const int64_t n = g.n;
+    s.laid = !precise && n >= LAID_ROWS && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
+    s.rounded_stride = (rank + 7) / 8 * 8;
+    s.stride = s.rounded_stride;
+    const auto take = [&](int64_t bytes) { const size_t at = s.end; s.end += ((size_t)bytes + 255) / 256 * 256; return at; };
+    if (!s.laid || both) s.numbers[0] = take(n * s.stride * 4);
+    if (both) s.numbers[1] = take(n * s.stride * 4);
+    s.group_of = take(n * 4);
+    if (s.laid) {
+        s.rounded = take(n * s.rounded_stride * 2);
+        s.zeros = take(256);
+        s.w_size = dpaps_laid_size(K, N);
+        s.b_size = dpaps_laid_size(rank, N);
+        s.w = take(s.w_size * 2);
+        s.b = take(s.b_size * 2 * g.groups);
+    }
+    return s;
+}
+LowNumbers low_of(char *ws, const Scratch &s, bool numbers, bool rounded, int which) {
+    LowNumbers l{};
+    l.stride = s.stride; l.rounded_stride = s.rounded_stride;
+    if (numbers || !s.laid) l.numbers = (float *)(ws + s.numbers[which]);
+    if (s.laid && rounded) l.rounded = ws + s.rounded;
+    l.group_of = (int32_t *)(ws + s.group_of);
+    return l;
+}
+int product_with(dpaps_ps *ps, const Scratch &s, const LowNumbers &low, AdapterArgs a, hipStream_t st) {
+    if (!s.laid) {
+        a.low = low.numbers; a.low_stride = low.stride; a.group_of = low.group_of;
+        return product(ps, a, st);
+    }
+    char *ws = (char *)ps->ws;
+    LayArgs l{};
+    l.w = a.w; l.L = a.L; l.K = a.K; l.N = a.N; l.turned = a.turned; l.to = ws + s.w; l.zeros = ws + s.zeros;
+    int rc = dpaps_lay(ps, nullptr, a.x_type, l, st);
+    if (rc) return rc;
+    l = LayArgs{};
+    l.w = a.b; l.L = a.L; l.each = a.rank; l.K = a.rank; l.N = a.N; l.turned = 1; l.to = ws + s.b; l.size = s.b_size;
+    rc = dpaps_lay(ps, &a.g, a.x_type, l, st);
+    if (rc) return rc;
+    LaidArgs p{};
+    p.g = a.g; p.x = a.x; p.x_stride = a.x_stride; p.K = a.K; p.N = a.N; p.w = ws + s.w; p.w_size = s.w_size; p.low = low.rounded; p.low_stride = (int32_t)low.rounded_stride;
+    p.b = ws + s.b; p.b_size = s.b_size; p.rank = a.rank; p.zeros = ws + s.zeros; p.out = a.out; p.out_stride = a.out_stride; p.out_type = a.out_type;
+    return dpaps_laid_product(ps, a.x_type, p, st);
 }
 
 // What both calls check.
@@ -164,7 +221,6 @@ int adapter_call(dpaps_ps *ps, int32_t worker, int64_t first_key, int32_t rows, 
     if (first_key < 0 || rows > ps->K || first_key > ps->K - rows || each > ps->K || first_a < 0 || first_a > ps->K - each || first_b < 0 || first_b > ps->K - each) return PS_EINVAL;
     return dpaps_row_groups(ps, order, offsets, num_adapters, n, g);
 }
-int64_t low_stride(int32_t rank) { return (rank + 3) / 4 * 4; }
 
 }  // namespace
 
@@ -178,17 +234,17 @@ extern "C" int adapter_matmul(ps_handle ps, int32_t worker, int64_t first_key, i
     if (n == 0) return PS_OK;
     if (!x || !out || x_stride < 0 || out_stride < rows) return PS_EINVAL;
     hipStream_t st = (hipStream_t)stream;
-    const int64_t ld = low_stride(rank);
-    rc = dpaps_ws_reserve(ps, (size_t)n * (ld + 1) * sizeof(float));
+    const bool precise = x_type == PS_F32 || out_type == PS_F32;
+    const Scratch s = scratch_of(g, x, x_stride, dim, rows, rank, precise, false);
+    rc = dpaps_ws_reserve(ps, s.end);
     if (rc) return rc;
-    float *low = (float *)ps->ws;
-    int32_t *group_of = (int32_t *)(low + n * ld);
-    rc = low_numbers(ps, g, x, x_type, x_stride, dim, ps->val + first_a * ps->L, rank, scale, x_type == PS_F32 || out_type == PS_F32, low, ld, group_of, st);
+    const LowNumbers low = low_of((char *)ps->ws, s, false, true, 0);
+    rc = low_numbers(ps, g, x, x_type, x_stride, dim, ps->val + first_a * ps->L, rank, scale, precise, low, st);
     if (rc) return rc;
     AdapterArgs a{};
     a.g = g; a.x = x; a.x_stride = x_stride; a.x_type = x_type; a.w = ps->val + first_key * ps->L; a.L = ps->L; a.K = dim; a.N = rows;
-    a.low = low; a.low_stride = ld; a.rank = rank; a.b = ps->val + first_b * ps->L; a.group_of = group_of; a.out = out; a.out_stride = out_stride; a.out_type = out_type;
-    rc = product(ps, a, st);
+    a.rank = rank; a.b = ps->val + first_b * ps->L; a.out = out; a.out_stride = out_stride; a.out_type = out_type;
+    rc = product_with(ps, s, low, a, st);
     if (rc) return rc;
     GroupKeys k;
     k.first = first_key; k.shared = rows; k.first_a = first_a; k.first_b = first_b; k.each = rank;
@@ -204,37 +260,36 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
     if (!is_element_type(type) || !is_element_type(dx_type) || !da || !db) return PS_EINVAL;
     if (n > 0 && (!x || !dout || x_stride < 0 || dout_stride < 0 || (dx && dx_stride < dim))) return PS_EINVAL;
     hipStream_t st = (hipStream_t)stream;
-    const int64_t ld = low_stride(rank);
+    const Scratch s = scratch_of(g, dout, dout_stride, rows, dim, rank, type == PS_F32 || dx_type == PS_F32, true);
     OuterArgs o{};
-    o.g = g; o.left_stride = ld; o.left_type = PS_F32; o.left_by_place = 1; o.rows = rank; o.out_type = PS_F32; o.right_type = type;
-    size_t part_bytes = 0;
+    o.g = g; o.left_stride = s.stride; o.left_type = PS_F32; o.left_by_place = 1; o.rows = rank; o.out_type = PS_F32; o.right_type = type;
+    size_t part = 0;
     for (const int32_t c : {dim, rows}) {
         o.cols = c;
-        part_bytes = std::max(part_bytes, dpaps_outer_bytes(ps, o));
+        part = std::max(part, dpaps_outer_bytes(ps, o));
     }
-    const size_t numbers = (size_t)n * (2 * ld + 1), off_part = (numbers + 63) / 64 * 64;
-    rc = dpaps_ws_reserve(ps, off_part * sizeof(float) + part_bytes);
+    rc = dpaps_ws_reserve(ps, s.end + part);
     if (rc) return rc;
-    float *h = (float *)ps->ws, *t = h + n * ld, *part = h + off_part;
-    int32_t *group_of = (int32_t *)(t + n * ld);
+    char *ws = (char *)ps->ws;
+    const LowNumbers h = low_of(ws, s, true, false, 0), t = low_of(ws, s, true, dx != nullptr, 1);
     const float *pa = ps->val + first_a * ps->L, *pb = ps->val + first_b * ps->L;
     if (n > 0) {
-        rc = low_numbers(ps, g, x, type, x_stride, dim, pa, rank, scale, true, h, ld, group_of, st);
-        if (!rc) rc = low_numbers(ps, g, dout, type, dout_stride, rows, pb, rank, scale, true, t, ld, nullptr, st);
+        rc = low_numbers(ps, g, x, type, x_stride, dim, pa, rank, scale, true, h, st);
+        if (!rc) rc = low_numbers(ps, g, dout, type, dout_stride, rows, pb, rank, scale, true, t, st);
         if (rc) return rc;
         if (dx) {
             AdapterArgs a{};
             a.g = g; a.x = dout; a.x_stride = dout_stride; a.x_type = type; a.w = ps->val + first_key * ps->L; a.L = ps->L; a.K = rows; a.N = dim; a.turned = 1;
-            a.low = t; a.low_stride = ld; a.rank = rank; a.group_of = group_of; a.b = pa; a.out = dx; a.out_stride = dx_stride; a.out_type = dx_type;
-            rc = product(ps, a, st);
+            a.rank = rank; a.b = pa; a.out = dx; a.out_stride = dx_stride; a.out_type = dx_type;
+            rc = product_with(ps, s, t, a, st);
             if (rc) return rc;
         }
     }
-    o.left = t; o.right = x; o.right_stride = x_stride; o.cols = dim; o.out = da;
-    rc = dpaps_outer_sums(ps, o, part, st);
+    o.left = t.numbers; o.right = x; o.right_stride = x_stride; o.cols = dim; o.out = da;
+    rc = dpaps_outer_sums(ps, o, (float *)(ws + s.end), st);
     if (rc) return rc;
-    o.left = h; o.right = dout; o.right_stride = dout_stride; o.cols = rows; o.out = db;
-    rc = dpaps_outer_sums(ps, o, part, st);
+    o.left = h.numbers; o.right = dout; o.right_stride = dout_stride; o.cols = rows; o.out = db;
+    rc = dpaps_outer_sums(ps, o, (float *)(ws + s.end), st);
     if (rc) return rc;
     if (n == 0) return PS_OK;
     GroupKeys k;

@@ -10,65 +10,56 @@
 namespace {
 
 template <class CT, class XT, bool TURNED, class T>
-__global__ __launch_bounds__(T::THREADS) void k_expert(ExpertArgs a, int32_t col_tiles, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertArgs a, int32_t col_tiles, int32_t *err) {
     constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
-    __shared__ Vec<CT, KU> lds[2][(BR + BC) * UNITS];
+    extern __shared__ __align__(16) char shared[];
+    Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
     __shared__ int at[BR];                                           // the rows' numbers; -1: none
     __shared__ int off;
     look_for_all(err, &off);
     const RowTile t = row_tile(a.g, (int)(blockIdx.x / (uint32_t)col_tiles), BR);
     const int c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * BC, tid = threadIdx.x;
-    __syncthreads();
-    if (off || t.rows == 0) return;
+    if (t.rows == 0) return;
     for (int r = tid; r < BR; r += T::THREADS) {
         at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
         if (a.group_of && c0 == 0 && r < t.rows) a.group_of[t.first + r] = t.group;
     }
     __syncthreads();
+    if (off) return;
     floatx16 acc[T::MC][T::MR] = {};
     const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR, cols = a.N - c0;
     if (t.group < a.g.groups) {
         const float *w = a.w + (int64_t)t.group * a.each * a.L;
         KMajor<XT, CT, BR, T::THREADS> rows;
-        rows.init([&](int r) { return at[r] < 0 ? nullptr : reinterpret_cast<const XT *>(a.x) + a.x_shared(at[r]) * a.x_stride; });
-        const int steps = (a.K + step_of<CT>() - 1) / step_of<CT>();
-        auto loop = [&](auto load, auto &columns) {
-            rows.load(0, a.K);
-            load(0);
-            rows.put(lds[0]);
-            columns.put(lds[0] + BR * UNITS);
-            __syncthreads();
-            for (int s = 0; s < steps; ++s) {
-                if (s + 1 < steps) { rows.load(s + 1, a.K); load(s + 1); }
-                step_products<CT, T::MC, T::MR>(lds[s & 1] + BR * UNITS, lds[s & 1], wc, wr, UNITS, acc);
-                if (s + 1 < steps) { rows.put(lds[(s + 1) & 1]); columns.put(lds[(s + 1) & 1] + BR * UNITS); }
-                __syncthreads();
-            }
-        };
-        if constexpr (TURNED) {
-            NMajor<float, CT, BC, T::THREADS> columns;
-            loop([&](int s) { columns.load(s, a.K, cols, [&](int k) { return w + (int64_t)k * a.L + c0; }); }, columns);
-        } else {
-            KMajor<float, CT, BC, T::THREADS> columns;
-            columns.init([&](int c) { return c < cols ? w + (int64_t)(c0 + c) * a.L : nullptr; });
-            loop([&](int s) { columns.load(s, a.K); }, columns);
-        }
+        rows.init([&](int r) { return reinterpret_cast<const XT *>(a.x) + a.x_shared(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
+        std::conditional_t<TURNED, KeyRows<CT, BC, T::THREADS>, KeyColumns<CT, BC, T::THREADS>> columns;
+        if constexpr (TURNED) columns.init(w + c0, a.L);
+        else columns.init(w + c0 * a.L, a.L, cols);
+        tile_sum<CT, T>(a.K, lds, wc, wr,
+            [&](int s, auto tail) {
+                rows.template load<decltype(tail)::value>(s, a.K);
+                columns.template load<decltype(tail)::value>(s, a.K);
+            },
+            [&](Vec<CT, KU> *to) {
+                rows.put(to);
+                columns.put(to + BR * UNITS);
+            }, acc);
     }
-    const int l32 = tid & 31, h = (tid & 63) >> 5;
-#pragma unroll
-    for (int j = 0; j < T::MR; ++j) {
-        const int r = wr + 32 * j + l32;
-        if (at[r] < 0) continue;
-        const int64_t to = (int64_t)(a.by_place ? t.first + r : at[r]) * a.out_stride;
+    if (a.zero_from) {
+        const int h = (tid & 63) >> 5;
 #pragma unroll
         for (int i = 0; i < T::MC; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = wc + 32 * i + 8 * q + 4 * h;
-                const Vec<float, 4> v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (c < cols) put_typed(a.out, a.out_type, to + c0 + c, a.scale * v, cols - c);
-            }
+            for (int e = 0; e < 16; ++e)
+                if (c0 + wc + 32 * i + 8 * (e / 4) + 4 * h + e % 4 >= a.zero_from)
+#pragma unroll
+                    for (int j = 0; j < T::MR; ++j) acc[i][j][e] = 0.0f;
     }
+    put_tile_typed<T>(acc, lds, a.out, a.out_type, c0, a.N, a.scale,
+                      [&](int r) { return at[r] < 0 ? (int64_t)-1 : (int64_t)(a.by_place ? t.first + r : at[r]) * a.out_stride; });
+    if (a.also)
+        put_tile_typed<T>(acc, lds, a.also, a.also_type, c0, a.N, a.scale,
+                          [&](int r) { return at[r] < 0 ? (int64_t)-1 : (int64_t)(a.by_place ? t.first + r : at[r]) * a.also_stride; });
 }
 
 // Groups of few rows.
@@ -98,8 +89,11 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expe
     for (int p = tid; p < F::PIECES; p += F::THREADS) {
         const int r = F::row_of(p), c = F::col_of(p), left = a.N - c0 - c;
         if (at[r] < 0 || left <= 0) continue;
-        const Vec<float, 4> v = t.group < a.g.groups ? a.scale * F::sum(sums, p) : Vec<float, 4>{};
-        put_typed(a.out, a.out_type, (int64_t)(a.by_place ? t.first + r : at[r]) * a.out_stride + c0 + c, v, left);
+        Vec<float, 4> v = t.group < a.g.groups ? a.scale * F::sum(sums, p) : Vec<float, 4>{};
+        if (a.zero_from) v = cut<float, 4>(v, a.zero_from - c0 - c);
+        const int64_t row = a.by_place ? t.first + r : at[r];
+        put_typed<4>(a.out, a.out_type, row * a.out_stride + c0 + c, v, left);
+        if (a.also) put_typed<4>(a.also, a.also_type, row * a.also_stride + c0 + c, v, left);
     }
 }
 
@@ -113,10 +107,11 @@ __device__ __forceinline__ float *outer_slot(const OuterArgs &a, const OuterTile
     return a.out_type == PS_F32 ? reinterpret_cast<float *>(a.out) + group * size : o.part + (o.slots + first / o.chunk) * size;
 }
 template <class CT, class LT, class RT, class T>
-__global__ __launch_bounds__(T::THREADS) void k_outer(OuterArgs a, OuterTiles o, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_outer(OuterArgs a, OuterTiles o, int32_t *err) {
     constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
-    __shared__ Vec<CT, KU> lds[2][(BR + BC) * UNITS];
-    extern __shared__ int at[];                                      // the rows' numbers of the chunk
+    extern __shared__ __align__(16) char shared[];
+    Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
+    int *const at = reinterpret_cast<int *>(lds + 2 * (BR + BC) * UNITS);      // the rows' numbers of the chunk
     __shared__ int off;
     look_for_all(err, &off);
     const int tid = threadIdx.x, tiles = o.rows * o.cols, tile = (int)(blockIdx.x % (uint32_t)tiles);
@@ -135,45 +130,26 @@ __global__ __launch_bounds__(T::THREADS) void k_outer(OuterArgs a, OuterTiles o,
     if (off) return;
     floatx16 acc[T::MC][T::MR] = {};
     const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
-    NMajor<LT, CT, BR, T::THREADS> left;
-    NMajor<RT, CT, BC, T::THREADS> right;
-    const int steps = (t.rows + step_of<CT>() - 1) / step_of<CT>();
-    const auto load = [&](int s) {
-        left.load(s, t.rows, a.rows - r0, [&](int p) {
-            return reinterpret_cast<const LT *>(a.left) + (int64_t)(a.left_by_place ? t.first + p : a.left_shared(at[p])) * a.left_stride + r0;
-        });
-        right.load(s, t.rows, a.cols - c0, [&](int p) { return reinterpret_cast<const RT *>(a.right) + (int64_t)a.right_shared(at[p]) * a.right_stride + c0; });
-    };
-    if (steps > 0) {
-        load(0);
-        left.put(lds[0]);
-        right.put(lds[0] + BR * UNITS);
-        __syncthreads();
-    }
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) load(s + 1);
-        step_products<CT, T::MC, T::MR>(lds[s & 1] + BR * UNITS, lds[s & 1], wc, wr, UNITS, acc);
-        if (s + 1 < steps) { left.put(lds[(s + 1) & 1]); right.put(lds[(s + 1) & 1] + BR * UNITS); }
-        __syncthreads();
-    }
+    ChosenRows<LT, CT, BR, T::THREADS> left;
+    ChosenRows<RT, CT, BC, T::THREADS> right;
+    tile_sum<CT, T>(t.rows, lds, wc, wr,
+        [&](int s, auto tail) {
+            left.template load<decltype(tail)::value>(s, t.rows, a.rows - r0, [&](int p) {
+                return reinterpret_cast<const LT *>(a.left) + (int64_t)(a.left_by_place ? t.first + p : a.left_shared(at[p])) * a.left_stride + r0;
+            });
+            right.template load<decltype(tail)::value>(s, t.rows, a.cols - c0, [&](int p) {
+                return reinterpret_cast<const RT *>(a.right) + (int64_t)a.right_shared(at[p]) * a.right_stride + c0;
+            });
+        },
+        [&](Vec<CT, KU> *to) {
+            left.put(to);
+            right.put(to + BR * UNITS);
+        }, acc);
     const bool whole = end - start <= o.chunk;
     void *out = whole ? a.out : outer_slot(a, o, t.group, start, t.first);
-    const int32_t type = whole ? a.out_type : PS_F32;
     const int64_t base = whole ? (int64_t)t.group * a.rows * a.cols : 0;
-    const int l32 = tid & 31, h = (tid & 63) >> 5;
-#pragma unroll
-    for (int j = 0; j < T::MR; ++j) {
-        const int r = r0 + wr + 32 * j + l32;
-        if (r >= a.rows) continue;
-#pragma unroll
-        for (int i = 0; i < T::MC; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = c0 + wc + 32 * i + 8 * q + 4 * h;
-                const Vec<float, 4> v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (c < a.cols) put_typed(out, type, base + (int64_t)r * a.cols + c, v, a.cols - c);
-            }
-    }
+    put_tile_typed<T>(acc, lds, out, whole ? a.out_type : PS_F32, c0, a.cols, 1.0f,
+                      [&](int r) { return r0 + r < a.rows ? base + (int64_t)(r0 + r) * a.cols : (int64_t)-1; });
 }
 // The chunks of groups of several, added up in their order.  blockIdx.y: the group
 __global__ __launch_bounds__(256) void k_outer_join(OuterArgs a, OuterTiles o, const int32_t *err) {
@@ -186,7 +162,7 @@ __global__ __launch_bounds__(256) void k_outer_join(OuterArgs a, OuterTiles o, c
             const int left = size - i < 4 ? (int)(size - i) : 4;
             Vec<float, 4> v = {};
             for (int first = start; first < end; first += o.chunk) v = v + load_some<float, 4>(outer_slot(a, o, group, start, first) + i, left);
-            put_typed(a.out, a.out_type, group * size + i, v, left);
+            put_typed<4>(a.out, a.out_type, group * size + i, v, left);
         }
     }
 }
@@ -201,7 +177,7 @@ __global__ __launch_bounds__(256) void k_pair_sums(const float *in, int64_t n, i
     const float *p = in + t * b * N + c;
     Vec<float, 4> v = load_some<float, 4>(p, left);
     for (int j = 1; j < b; ++j) v = v + load_some<float, 4>(p + (int64_t)j * N, left);
-    put_typed(out, out_type, t * out_stride + c, v, left);
+    put_typed<4>(out, out_type, t * out_stride + c, v, left);
 }
 
 int too_large(dpaps_ps *ps, const char *what) {
@@ -216,7 +192,10 @@ template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, c
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
     const int64_t grid = row_tiles(a.g.n, a.g.groups, T::ROWS) * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return too_large(ps, "product");
-    k_expert<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, 0, st>>>(a, col_tiles, ps->err);
+    static LdsAllowed allowed;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_expert<CT, XT, TURNED, T>), T::LDS);
+    if (rc) return rc;
+    k_expert<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
@@ -266,9 +245,9 @@ template <class CT, class LT, class RT, class T> int outer_of(dpaps_ps *ps, cons
     const int64_t grid = row_tiles(a.g.n, a.g.groups, o.chunk) * o.rows * o.cols;
     if (grid >= ((int64_t)1 << 24)) return too_large(ps, "expert_grad");
     static LdsAllowed allowed;
-    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer<CT, LT, RT, T>), 2048 * sizeof(int));
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer<CT, LT, RT, T>), T::LDS + 2048 * sizeof(int));
     if (rc) return rc;
-    k_outer<CT, LT, RT, T><<<(unsigned)grid, T::THREADS, o.chunk * sizeof(int), st>>>(a, o, ps->err);
+    k_outer<CT, LT, RT, T><<<(unsigned)grid, T::THREADS, T::LDS + o.chunk * sizeof(int), st>>>(a, o, ps->err);
     PS_HIP(ps, hipGetLastError());
     if (a.g.n <= o.chunk) return PS_OK;
     const int64_t x = ceil_div64((int64_t)a.rows * a.cols, 1024);
@@ -294,6 +273,9 @@ int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t 
     return a.left_type == PS_BF16 ? outer_any<bf16_t, bf16_t, bf16_t>(ps, a, part, st) : outer_any<f16_t, f16_t, f16_t>(ps, a, part, st);
 }
 
+// From so many rows a group on, matrices are laid before the product (laid.hip).
+constexpr int64_t LAID_ROWS = 512;
+
 extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed,
                              const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int32_t x_type, int64_t x_stride, int32_t x_pairs, void *out,
                              int32_t out_type, int64_t out_stride, int32_t out_pairs, void *stream) {
@@ -313,12 +295,23 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     a.w = ps->val + first_key * ps->L; a.L = ps->L; a.each = rows; a.K = K; a.N = N; a.turned = transposed != 0;
     a.scale = 1.0f; a.precise = x_type == PS_F32 || out_type == PS_F32;
     a.out = out; a.out_stride = out_stride; a.out_type = out_type;
-    if (out_pairs > 1) {
-        rc = dpaps_ws_reserve(ps, (size_t)n * N * sizeof(float));
+    const size_t sums = out_pairs > 1 ? ((size_t)n * N * sizeof(float) + 255) / 256 * 256 : 0;
+    const bool lay = !a.precise && n >= LAID_ROWS * num_experts && num_experts < 32768 && dpaps_laid_fits(x, x_stride, K);
+    const int64_t laid = lay ? dpaps_laid_size(K, N) : 0;
+    rc = dpaps_ws_reserve(ps, sums + (size_t)laid * num_experts * 2 + 256);
+    if (rc) return rc;
+    if (out_pairs > 1) { a.out = ps->ws; a.out_stride = N; a.out_type = PS_F32; }
+    if (lay) {
+        char *zeros = (char *)ps->ws + sums;
+        LayArgs l{};
+        l.w = a.w; l.L = a.L; l.each = a.each; l.K = K; l.N = N; l.turned = a.turned; l.to = zeros + 256; l.size = laid; l.zeros = zeros;
+        rc = dpaps_lay(ps, &g, x_type, l, st);
         if (rc) return rc;
-        a.out = ps->ws; a.out_stride = N; a.out_type = PS_F32;
-    }
-    rc = dpaps_expert_product(ps, a, st);
+        LaidArgs p{};
+        p.g = g; p.x = x; p.x_stride = x_stride; p.x_shared = a.x_shared; p.K = K; p.N = N; p.w = l.to; p.w_size = laid; p.zeros = zeros;
+        p.out = a.out; p.out_stride = a.out_stride; p.out_type = a.out_type;
+        rc = dpaps_laid_product(ps, x_type, p, st);
+    } else rc = dpaps_expert_product(ps, a, st);
     if (rc) return rc;
     if (out_pairs > 1) {
         const uint32_t P = (uint32_t)((N + 3) / 4);

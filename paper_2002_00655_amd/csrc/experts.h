@@ -13,6 +13,8 @@ struct ExpertArgs {
     void *out; int64_t out_stride; int32_t out_type, by_place;               // by_place: the row at place p goes to row p of out
     int32_t precise;                                                         // products of numbers of 32 bits
     int32_t *group_of;                                                       // not NULL: the group of the row at place p
+    void *also; int64_t also_stride; int32_t also_type;                      // not NULL: the result once more, in another type
+    int32_t zero_from;                                                       // the columns from here on, up to N, are written as zeros; 0: none
 };
 int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st);
 
@@ -49,6 +51,30 @@ struct AdapterArgs {
     void *out; int64_t out_stride; int32_t out_type;
 };
 
+// Products by way of laid matrices (laid.hip): the server's numbers rounded to 16 bits once, before the product, and put into the order of its loads.
+// sums: x_q' M of group's matrix M (laid: matrix e from e * size on), or, where there is one matrix for all rows, its product plus the low-rank
+// numbers of the rows, low_p (by place, `rank` of them), times their group's laid matrix.
+struct LaidArgs {
+    RowGroups g;
+    const void *x; int64_t x_stride; Quotient x_shared;
+    int32_t K, N;
+    const void *w; int64_t w_size;                                           // elements of a laid matrix
+    const void *low, *b; int64_t b_size; int32_t rank, low_stride;           // low: NULL, a matrix for each group
+    const void *zeros;                                                       // 64 bytes
+    void *out; int64_t out_stride; int32_t out_type;
+};
+// What is laid: M_e's number of column c and place k of the sum is value c of key k (turned) or value k of key c, of keys from w + e * each * L on.
+struct LayArgs {
+    const float *w; int64_t L, each;
+    int32_t K, N, turned;
+    void *to; int64_t size;
+    void *zeros;                                                             // not NULL: 64 bytes that are cleared
+};
+int64_t dpaps_laid_size(int32_t K, int32_t N);
+bool dpaps_laid_fits(const void *x, int64_t x_stride, int32_t K);
+int dpaps_lay(dpaps_ps *ps, const RowGroups *g, int32_t type, const LayArgs &a, hipStream_t st);
+int dpaps_laid_product(dpaps_ps *ps, int32_t type, const LaidArgs &a, hipStream_t st);
+
 // Few rows: MT tiles of 16 rows by the columns of a workgroup, whose wavefronts share the sum over k.  Both operands come straight from memory into the registers
 // that the matrix instruction reads, and nothing but the wavefronts' sums sees LDS: what counts is that all of the matrix is on its way at once.
 //   M as it is:  16 columns; lane l has column l % 16, and of a step's 4 units the one l / 16
@@ -59,6 +85,14 @@ template <class CT, class XT, bool TURNED, int MT> struct FewRows {
     static constexpr int AHEAD = TURNED ? (KU == 8 ? 2 : 4) : (KU == 8 ? 4 : 8);
     static constexpr int SUMS = WAVES * 16 * MT * COLS;
     floatx4 acc[OPS][MT];
+    // The unit that a lane has of 16-bit products with M as it is: four numbers from k on and the four 16 further, on both sides, so that the lanes of a column
+    // read neighbours.
+    template <class ST> __device__ static __forceinline__ Vec<ST, 8> halves(const ST *p, int k, int K) {
+        Vec<ST, 4> lo = {}, hi = {};
+        if (k < K) lo = load_some<ST, 4>(p + k, K - k);
+        if (k + 16 < K) hi = load_some<ST, 4>(p + k + 16, K - k - 16);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
     // w: where the matrix starts; c0: its first column here; x_of(r): where row r < 16 MT of the tile is (any row where there is none)
     template <class F> __device__ __forceinline__ void run(const float *w, int64_t L, int K, int c0, int N, F x_of) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
@@ -89,14 +123,16 @@ template <class CT, class XT, bool TURNED, int MT> struct FewRows {
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
                         for (int i = 0; i < KU; ++i) wv[u][j][i] = rows[i][j];
-                } else {
+                } else if constexpr (KU == 4) {
                     wv[u][0] = Vec<float, KU>{};
                     if (left > 0) wv[u][0] = load_some<float, KU>(mine + k, left);
-                }
+                } else wv[u][0] = halves<float>(mine, (s + u) * STEP + 4 * g, s + u < s1 ? K : 0);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    xv[u][m] = Vec<XT, KU>{};
-                    if (left > 0) xv[u][m] = load_some<XT, KU>(x[m] + k, left);
+                    if constexpr (TURNED || KU == 4) {
+                        xv[u][m] = Vec<XT, KU>{};
+                        if (left > 0) xv[u][m] = load_some<XT, KU>(x[m] + k, left);
+                    } else xv[u][m] = halves<XT>(x[m], (s + u) * STEP + 4 * g, s + u < s1 ? K : 0);
                 }
             }
 #pragma unroll

@@ -1,0 +1,244 @@
+// Products of many rows of 16 bits with matrices of the server: the matrices are laid first, in 16 bits and in the order in which the product loads them, so that the
+// product's operands both go straight from memory into LDS, several stages ahead.
+//
+// A matrix is laid in blocks of 16 columns and 32 numbers of each, 1,024 bytes: a line of 64 bytes for each column, its four units of eight numbers at the
+// places u ^ (column / 4) % 4, where the wavefronts' reads of one unit of 32 columns meet all banks.  Rows come from where they are, 64 bytes each, into
+// LDS in the same order: a lane asks for the unit that belongs to its place.
+#include "experts.h"
+
+namespace {
+
+constexpr int KB = 32;                                       // numbers of a block
+constexpr int STAGES = 4;
+constexpr int64_t BLOCK = 16 * KB;                           // elements
+inline int64_t col_blocks(int32_t N) { return ceil_div64(N, 256) * 16; }      // (whole tiles)
+inline int64_t k_blocks(int32_t K) { return ceil_div64(K, KB); }
+
+// A workgroup lays 16 columns of 256 numbers as they lie, or 64 columns of 64 numbers that it turns in LDS.
+template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(LayArgs a, RowGroups g, int32_t cb_all, int32_t kb_all, const int32_t *err) {
+    if (*(volatile const int32_t *)err) return;
+    const int e = blockIdx.z, tid = threadIdx.x;
+    if (a.zeros && e == 0 && blockIdx.x == 0 && blockIdx.y == 0 && tid < 16) reinterpret_cast<uint32_t *>(a.zeros)[tid] = 0;
+    if (g.offsets && g.start(e) >= g.start(e + 1)) return;
+    const float *w = a.w + (int64_t)e * a.each * a.L;
+    T *to = reinterpret_cast<T *>(a.to) + e * a.size;
+    const auto place = [&](int c, int k) { return ((int64_t)(c >> 4) * kb_all + (k >> 5)) * BLOCK + (c & 15) * KB + (((k >> 3 & 3) ^ (c >> 2 & 3)) * 8); };
+    if constexpr (!TURNED) {
+        const int c = blockIdx.y * 16 + (tid >> 4), k0 = blockIdx.x * 256 + (tid & 15) * 8;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = k0 + u * 128;
+            if (k >= kb_all * KB) return;
+            Vec<float, 8> v = {};
+            if (c < a.N && k < a.K) v = cut<float, 8>(*reinterpret_cast<const Loose<float, 8> *>(w + (int64_t)c * a.L + k), a.K - k);
+            *reinterpret_cast<Vec<T, 8> *>(to + place(c, k)) = as_type<T, float, 8>(v);
+        }
+    } else {
+        __shared__ float turn[64][65];
+        const int c0 = blockIdx.y * 64, k0 = blockIdx.x * 64;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = u * 16 + (tid >> 4), c = (tid & 15) * 4;
+            Vec<float, 4> v = {};
+            if (k0 + k < a.K && c0 + c < a.N) v = load_some<float, 4>(w + (int64_t)(k0 + k) * a.L + c0 + c, a.N - c0 - c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) turn[k][c + i] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int c = tid & 63, k = (tid >> 6) * 16 + u * 8;
+            if (k0 + k >= kb_all * KB || c0 + c >= cb_all * 16) continue;
+            Vec<float, 8> v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = turn[k + i][c];
+            *reinterpret_cast<Vec<T, 8> *>(to + place(c0 + c, k0 + k)) = as_type<T, float, 8>(v);
+        }
+    }
+}
+
+// until at most N of this wavefront's loads are on their way and all it has asked of LDS is there, then until all wavefronts are so far
+template <int N> __device__ __forceinline__ void wait_and_meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+// The order of a turn's instructions: reads of LDS and loads spread over the products.
+template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinline__ void spread() {
+    constexpr int R = (I + 1) * READS / PRODUCTS - I * READS / PRODUCTS, L = (I + 1) * LOADS / PRODUCTS - I * LOADS / PRODUCTS;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (R > 0) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+    if constexpr (L > 0) __builtin_amdgcn_sched_group_barrier(0x020, L, 0);
+    if constexpr (I + 1 < PRODUCTS) spread<PRODUCTS, READS, LOADS, I + 1>();
+}
+
+template <class CT, class T> struct LaidForm {
+    static constexpr int STAGE = (T::ROWS + T::COLS) * KB * 2, LDS = STAGES * STAGE, ROW_LOADS = T::ROWS / 16 / 4, COL_LOADS = T::COLS / 16 / 4, LOADS = ROW_LOADS + COL_LOADS;
+    static_assert(T::THREADS == 256);
+};
+
+template <class CT, class T, bool LOW>
+__global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t col_tiles, int32_t kb_all, int32_t b_kb, int32_t *err) {
+    typedef LaidForm<CT, T> F;
+    constexpr int BR = T::ROWS, BC = T::COLS, H = F::LOADS / 2;
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ int at[BR];
+    __shared__ int off;
+    look_for_all(err, &off);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = (int)(blockIdx.x / (uint32_t)col_tiles), c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * BC;
+    RowTile t;
+    if constexpr (LOW) t = RowTile{0, tile * BR, a.g.n - tile * BR < BR ? a.g.n - tile * BR : BR};
+    else t = row_tile(a.g, tile, BR);
+    if (t.rows == 0) return;
+    for (int r = tid; r < BR; r += 256) at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
+    __syncthreads();
+    if (off) return;
+    floatx16 acc[T::MC][T::MR] = {};
+    const int wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
+    if (LOW || t.group < a.g.groups) {
+        // The loads of a stage: this wavefront's blocks of 16 rows, and of 16 columns.  What they come from changes where an adapter's numbers follow
+        // the shared matrix's, or another adapter's: rows of others are zeros.
+        const int unit = (lane & 3) ^ (lane >> 4 & 3);
+        const CT *row[F::ROW_LOADS];
+        const CT *col = reinterpret_cast<const CT *>(a.w) + (LOW ? 0 : t.group * a.w_size) + (int64_t)(c0 / 16 + wave * F::COL_LOADS) * kb_all * BLOCK + lane * 8;
+        int col_step = kb_all, left = kb_all, K = a.K, adapter = 0, stages = kb_all;
+#pragma unroll
+        for (int i = 0; i < F::ROW_LOADS; ++i) {
+            const int q = at[(wave * F::ROW_LOADS + i) * 16 + (lane >> 2)];
+            row[i] = reinterpret_cast<const CT *>(a.x) + a.x_shared(q < 0 ? 0 : q) * a.x_stride + unit * 8;
+        }
+        if constexpr (LOW) {
+            adapter = row_tile(a.g, t.first, 1).group;
+            for (int e = adapter; e < a.g.groups && a.g.start(e) < t.first + t.rows; ++e)
+                if (a.g.start(e + 1) > a.g.start(e) && a.g.start(e + 1) > t.first) stages += b_kb;
+        }
+        const auto next_adapter = [&]() {
+            while (adapter < a.g.groups && (a.g.start(adapter + 1) <= a.g.start(adapter) || a.g.start(adapter + 1) <= t.first)) ++adapter;
+            const int e = adapter < a.g.groups ? adapter : a.g.groups - 1, lo = a.g.start(e), hi = a.g.start(e + 1);
+#pragma unroll
+            for (int i = 0; i < F::ROW_LOADS; ++i) {
+                const int p = t.first + (wave * F::ROW_LOADS + i) * 16 + (lane >> 2);
+                row[i] = p >= lo && p < hi && p < t.first + t.rows ? reinterpret_cast<const CT *>(a.low) + (int64_t)p * a.low_stride + unit * 8 : nullptr;
+            }
+            col = reinterpret_cast<const CT *>(a.b) + e * a.b_size + (int64_t)(c0 / 16 + wave * F::COL_LOADS) * b_kb * BLOCK + lane * 8;
+            col_step = left = b_kb;
+            K = a.rank;
+            ++adapter;
+        };
+        // half of a stage's loads, the rows' or the columns'; k: where in the sum the stage is
+        const auto fetch = [&](int slot, bool rows, int k) {
+            unsigned char *to = lds + slot * F::STAGE + (rows ? wave * F::ROW_LOADS : BR / 16 + wave * F::COL_LOADS) * 1024;
+            if (rows) {
+                const bool here = k + unit * 8 < K;
+#pragma unroll
+                for (int i = 0; i < F::ROW_LOADS; ++i)
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(here && (!LOW || row[i]) ? row[i] + k : reinterpret_cast<const CT *>(a.zeros)),
+                                                     (__attribute__((address_space(3))) void *)(to + i * 1024), 16, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < F::COL_LOADS; ++i)
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(col + ((int64_t)i * col_step + (k >> 5)) * BLOCK),
+                                                     (__attribute__((address_space(3))) void *)(to + i * 1024), 16, 0, 0);
+            }
+        };
+        int k_next = 0, fetched = 0;
+        // to the stage behind the one that was fetched last; behind the last one that one once more, into a slot that nobody reads, so that all turns are alike
+        const auto advance = [&]() {
+            if (++fetched >= stages) return;
+            if (--left == 0) {
+                if constexpr (LOW) next_adapter();
+                k_next = 0;
+            } else k_next += KB;
+        };
+        const int l32 = lane & 31, h = lane >> 5;
+        typedef Vec<CT, 8> Unit;
+        Unit xa[T::MC], xb[T::MR], ya[T::MC], yb[T::MR];
+        const auto read = [&](Unit (&ra)[T::MC], Unit (&rb)[T::MR], int slot, int pair) {
+            const unsigned char *from = lds + slot * F::STAGE;
+            const auto unit_at = [&](int r) { return *reinterpret_cast<const Unit *>(from + r * 64 + (((2 * pair + h) ^ (r >> 2 & 3)) * 16)); };
+#pragma unroll
+            for (int i = 0; i < T::MC; ++i) ra[i] = unit_at(BR + wc + 32 * i + l32);
+#pragma unroll
+            for (int j = 0; j < T::MR; ++j) rb[j] = unit_at(wr + 32 * j + l32);
+        };
+        const auto multiply = [&](const Unit (&ra)[T::MC], const Unit (&rb)[T::MR]) {
+#pragma unroll
+            for (int i = 0; i < T::MC; ++i)
+#pragma unroll
+                for (int j = 0; j < T::MR; ++j) acc[i][j] = mfma_unit<CT>(ra[i], rb[j], acc[i][j]);
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) {
+            fetch(s, true, k_next);
+            fetch(s, false, k_next);
+            advance();
+        }
+        wait_and_meet<(STAGES - 2) * F::LOADS>();
+        read(xa, xb, 0, 0);
+        int slot = 0, into = STAGES - 1;
+        for (int s = 0; s < stages; ++s) {
+            read(ya, yb, slot, 1);
+            fetch(into, true, k_next);
+            multiply(xa, xb);
+            spread<T::MC * T::MR, T::MC + T::MR, F::ROW_LOADS>();
+            // this stage has been read, and the next one is there
+            wait_and_meet<(STAGES - 3) * F::LOADS + F::ROW_LOADS>();
+            const int next = slot + 1 == STAGES ? 0 : slot + 1;
+            read(xa, xb, next, 0);
+            fetch(into, false, k_next);
+            multiply(ya, yb);
+            spread<T::MC * T::MR, T::MC + T::MR, F::COL_LOADS>();
+            advance();
+            into = slot;
+            slot = next;
+        }
+        wait_and_meet<0>();                                  // nothing is on its way to LDS
+    }
+    put_tile_typed<T>(acc, lds, a.out, a.out_type, c0, a.N, 1.0f, [&](int r) { return at[r] < 0 ? (int64_t)-1 : (int64_t)at[r] * a.out_stride; });
+}
+
+template <class CT, class T, bool LOW> int start(dpaps_ps *ps, const LaidArgs &a, hipStream_t st) {
+    typedef LaidForm<CT, T> F;
+    const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
+    const int64_t grid = (LOW ? ceil_div64(a.g.n, T::ROWS) : row_tiles(a.g.n, a.g.groups, T::ROWS)) * col_tiles;
+    if (grid >= ((int64_t)1 << 24)) { ps->last_error = "product: too large for one launch"; return PS_ELIMIT; }
+    static LdsAllowed allowed;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_laid<CT, T, LOW>), F::LDS);
+    if (rc) return rc;
+    k_laid<CT, T, LOW><<<(unsigned)grid, 256, F::LDS, st>>>(a, col_tiles, (int32_t)k_blocks(a.K), (int32_t)k_blocks(a.rank), ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+template <class CT> int start_any(dpaps_ps *ps, const LaidArgs &a, hipStream_t st) {
+    const bool large = ceil_div64(a.g.n, 256) * ceil_div64(a.N, 256) >= ps->num_cu;
+    if (a.low) return large ? start<CT, Tile256, true>(ps, a, st) : start<CT, Tile128, true>(ps, a, st);
+    return large ? start<CT, Tile256, false>(ps, a, st) : start<CT, Tile128, false>(ps, a, st);
+}
+
+}  // namespace
+
+int64_t dpaps_laid_size(int32_t K, int32_t N) { return col_blocks(N) * k_blocks(K) * BLOCK; }
+bool dpaps_laid_fits(const void *x, int64_t x_stride, int32_t K) { return K % 8 == 0 && (uintptr_t)x % 16 == 0 && x_stride % 8 == 0; }
+
+int dpaps_lay(dpaps_ps *ps, const RowGroups *g, int32_t type, const LayArgs &a, hipStream_t st) {
+    const int32_t cb = (int32_t)col_blocks(a.N), kb = (int32_t)k_blocks(a.K);
+    const RowGroups groups = g ? *g : RowGroups{};
+    const unsigned z = g ? (unsigned)g->groups : 1u;
+    if (a.turned) {
+        const dim3 grid((unsigned)ceil_div64(kb * KB, 64), (unsigned)(cb / 4), z);
+        if (type == PS_BF16) k_lay<bf16_t, true><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
+        else k_lay<f16_t, true><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
+    } else {
+        const dim3 grid((unsigned)ceil_div64(kb * KB, 256), (unsigned)cb, z);
+        if (type == PS_BF16) k_lay<bf16_t, false><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
+        else k_lay<f16_t, false><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
+    }
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+
+int dpaps_laid_product(dpaps_ps *ps, int32_t type, const LaidArgs &a, hipStream_t st) {
+    return type == PS_BF16 ? start_any<bf16_t>(ps, a, st) : start_any<f16_t>(ps, a, st);
+}

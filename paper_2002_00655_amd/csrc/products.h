@@ -2,8 +2,8 @@
 //
 // A tile is sum_k R[k][r] C[k][c]: R, the tile's rows (of a call's tensors), C its columns (of the server's matrices, or of tensors).  Both come into LDS as
 // units of 16 bytes, numbers that follow each other in k, of the type CT that the matrix instruction takes: 8 units of a row or column are a step, and lie in one
-// line of 128 bytes.  What lies in memory in that order is read so (KMajor); what lies the other way - neighbouring columns together - is read as blocks of
-// a unit's numbers in k by four columns and turned in registers (NMajor).  The server's numbers of 32 bits are rounded to CT on the way.
+// line of 128 bytes.  What lies in memory in that order is read so (KMajor, KeyColumns); what lies the other way - neighbouring columns together - is read as blocks of
+// a unit's numbers in k by four columns and turned in registers (KeyRows, ChosenRows).  The server's numbers of 32 bits are rounded to CT on the way.
 #pragma once
 #include "elements.h"
 
@@ -17,7 +17,7 @@ constexpr int UNITS = 8;                                                       /
 template <class CT> constexpr int step_of() { return UNITS * unit_of<CT>(); }  // numbers of a step
 
 // Where unit u of row r lies in a tile in LDS.  Turned within the line by the row, so that neither eight neighbouring rows' same units (the
-// matrix instruction's reads) nor those of every fourth row (what NMajor writes) share banks.
+// matrix instruction's reads) nor those of every fourth row (what Blocks writes) share banks.
 __device__ __forceinline__ int unit_place(int r, int u) { return r * UNITS + (u ^ ((r ^ (r >> 3)) & 7)); }
 
 template <class CT, class ST, int W> __device__ __forceinline__ Vec<CT, W> as_type(Vec<ST, W> v) {
@@ -35,22 +35,34 @@ template <class ST, int W> __device__ __forceinline__ Vec<ST, W> load_some(const
     return v;
 }
 
-// ROWS rows whose numbers follow each other in k.
+// Of a unit that starts at k, the numbers from K on become zero.
+template <class ST, int W> __device__ __forceinline__ Vec<ST, W> cut(Vec<ST, W> v, int left) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = i < left ? v[i] : (ST)0.0f;
+    return v;
+}
+
+// ROWS rows of a call's tensor, whose numbers follow each other in k; `row`s are where they start.  Rows that are not wanted may be any: they
+// change nothing but their own results.
 template <class ST, class CT, int ROWS, int THREADS> struct KMajor {
     static constexpr int KU = unit_of<CT>(), N = ROWS * UNITS / THREADS;
     static_assert(N * THREADS == ROWS * UNITS && THREADS % UNITS == 0);
-    const ST *row[N];                                                          // NULL: a row of zeros
+    const ST *row[N];
     Vec<ST, KU> raw[N];
     template <class F> __device__ __forceinline__ void init(F row_of) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) row[i] = row_of((i * THREADS + (int)threadIdx.x) / UNITS);
+        for (int i = 0; i < N; ++i) row[i] = row_of((i * THREADS + (int)threadIdx.x) / UNITS) + (int)threadIdx.x % UNITS * KU;
     }
-    __device__ __forceinline__ void load(int step, int K) {
-        const int k = step * step_of<CT>() + ((int)threadIdx.x % UNITS) * KU;
+    // TAIL: the step goes past K
+    template <bool TAIL> __device__ __forceinline__ void load(int step, int K) {
+        const int k0 = step * step_of<CT>(), left = K - k0 - (int)threadIdx.x % UNITS * KU;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            raw[i] = Vec<ST, KU>{};
-            if (row[i] && k < K) raw[i] = load_some<ST, KU>(row[i] + k, K - k);
+            if constexpr (!TAIL) raw[i] = *reinterpret_cast<const Loose<ST, KU> *>(row[i] + k0);
+            else {
+                raw[i] = Vec<ST, KU>{};
+                if (left > 0) raw[i] = load_some<ST, KU>(row[i] + k0, left);
+            }
         }
     }
     __device__ __forceinline__ void put(Vec<CT, KU> *lds) const {
@@ -59,35 +71,116 @@ template <class ST, class CT, int ROWS, int THREADS> struct KMajor {
     }
 };
 
-// COLS columns that follow each other, for every k.
-template <class ST, class CT, int COLS, int THREADS> struct NMajor {
+// COLS columns of a matrix in the server that are its keys, so that their numbers follow each other in k, from a key on; `cols` of them exist.  Reads past
+// the last number of a key end in the next one, or in the slack behind the store.
+// (Four numbers a lane, neighbours in neighbouring lanes: with a whole unit of 16-bit numbers a lane, 32 bytes, both of its accesses touched every line, and the
+// die's cache was asked for all of them twice.)
+template <class CT, int COLS, int THREADS> struct KeyColumns {
+    static constexpr int PIECES = step_of<CT>() / 4, N = COLS * PIECES / THREADS;      // of four numbers
+    static_assert(N * THREADS == COLS * PIECES && THREADS % PIECES == 0);
+    const float *base;
+    uint32_t at[N];
+    Vec<float, 4> raw[N];
+    __device__ static __forceinline__ int piece() { return (int)threadIdx.x % PIECES; }
+    __device__ static __forceinline__ int col(int i) { return (i * THREADS + (int)threadIdx.x) / PIECES; }
+    __device__ __forceinline__ void init(const float *w, int64_t L, int cols) {
+        base = w;
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] = (uint32_t)(col(i) < cols ? col(i) : cols - 1) * (uint32_t)L + (uint32_t)(piece() * 4);
+    }
+    template <bool TAIL> __device__ __forceinline__ void load(int step, int K) {
+        const int k0 = step * step_of<CT>(), left = K - k0 - piece() * 4;
+        const float *from = base + k0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            raw[i] = *reinterpret_cast<const Loose<float, 4> *>(from + (!TAIL || left > 0 ? at[i] : at[i] - (uint32_t)(piece() * 4)));
+            if constexpr (TAIL) raw[i] = cut<float, 4>(raw[i], left);
+        }
+    }
+    __device__ __forceinline__ void put(Vec<CT, unit_of<CT>()> *lds) const {
+        constexpr int OF_UNIT = unit_of<CT>() / 4;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            reinterpret_cast<Vec<CT, 4> *>(lds + unit_place(col(i), piece() / OF_UNIT))[piece() % OF_UNIT] = as_type<CT, float, 4>(raw[i]);
+    }
+};
+
+// Blocks of a unit's numbers in k by four columns, turned on their way into LDS.
+template <class ST, class CT, int COLS, int THREADS> struct Blocks {
     static constexpr int KU = unit_of<CT>(), BLOCKS = COLS / 4 * UNITS, N = BLOCKS < THREADS ? 1 : BLOCKS / THREADS;
     static constexpr bool ALL = N * THREADS == BLOCKS;                         // else only the first threads have one
     static_assert(ALL || BLOCKS < THREADS);
     Vec<ST, 4> raw[N][KU];
-    // row_of(k): where the columns are for this k (below K); cols: those that there are
-    template <class F> __device__ __forceinline__ void load(int step, int K, int cols, F row_of) {
-#pragma unroll
-        for (int b = 0; b < N; ++b) {
-            const int at = b * THREADS + (int)threadIdx.x, c = at % (COLS / 4) * 4, k = step * step_of<CT>() + at / (COLS / 4) * KU;
-#pragma unroll
-            for (int i = 0; i < KU; ++i) {
-                raw[b][i] = Vec<ST, 4>{};
-                if (k + i < K && c < cols && (ALL || at < BLOCKS)) raw[b][i] = load_some<ST, 4>(row_of(k + i) + c, cols - c);
-            }
-        }
-    }
+    __device__ static __forceinline__ int block(int b) { return b * THREADS + (int)threadIdx.x; }
+    __device__ static __forceinline__ int col(int b) { return block(b) % (COLS / 4) * 4; }
+    __device__ static __forceinline__ int unit(int b) { return block(b) / (COLS / 4); }
     __device__ __forceinline__ void put(Vec<CT, KU> *lds) const {
 #pragma unroll
         for (int b = 0; b < N; ++b) {
-            const int at = b * THREADS + (int)threadIdx.x, c = at % (COLS / 4) * 4, u = at / (COLS / 4);
-            if (!ALL && at >= BLOCKS) return;
+            if (!ALL && block(b) >= BLOCKS) return;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 Vec<ST, KU> v;
 #pragma unroll
                 for (int i = 0; i < KU; ++i) v[i] = raw[b][i][j];
-                lds[unit_place(c + j, u)] = as_type<CT, ST, KU>(v);
+                lds[unit_place(col(b) + j, unit(b))] = as_type<CT, ST, KU>(v);
+            }
+        }
+    }
+};
+
+// COLS columns of a matrix in the server whose keys follow each other in k; reads past a key's last column end in the next key or in the slack
+// behind the store, which has room for 256.
+template <class CT, int COLS, int THREADS> struct KeyRows : Blocks<float, CT, COLS, THREADS> {
+    typedef Blocks<float, CT, COLS, THREADS> B;
+    static_assert(COLS <= 256);
+    const float *base;
+    int64_t L;
+    __device__ __forceinline__ void init(const float *w, int64_t L_) { base = w; L = L_; }
+    template <bool TAIL> __device__ __forceinline__ void load(int step, int K) {
+        const int k0 = step * step_of<CT>();
+#pragma unroll
+        for (int b = 0; b < B::N; ++b) {
+            const int u = B::ALL || B::block(b) < B::BLOCKS ? B::unit(b) * B::KU : 0;
+            const uint32_t at = (uint32_t)u * (uint32_t)L + (uint32_t)B::col(b);
+#pragma unroll
+            for (int i = 0; i < B::KU; ++i) {
+                if constexpr (!TAIL) this->raw[b][i] = *reinterpret_cast<const Loose<float, 4> *>(base + (int64_t)(k0 + i) * L + at);
+                else {
+                    const int k = k0 + u + i;
+                    this->raw[b][i] = *reinterpret_cast<const Loose<float, 4> *>(base + (int64_t)(k < K ? k : K - 1) * L + B::col(b));
+                    this->raw[b][i] = cut<float, 4>(this->raw[b][i], k < K ? 4 : 0);
+                }
+            }
+        }
+    }
+};
+
+// COLS columns, `cols` of which exist, of rows of a call's tensor that are chosen one by one: row_of(k), where they start.
+template <class ST, class CT, int COLS, int THREADS> struct ChosenRows : Blocks<ST, CT, COLS, THREADS> {
+    typedef Blocks<ST, CT, COLS, THREADS> B;
+    template <bool TAIL, class F> __device__ __forceinline__ void load(int step, int K, int cols, F row_of) {
+        const int k0 = step * step_of<CT>();
+#pragma unroll
+        for (int b = 0; b < B::N; ++b) {
+            const bool here = B::ALL || B::block(b) < B::BLOCKS;
+            const int c = B::col(b), u = here ? B::unit(b) * B::KU : 0, left = here ? cols - c : 0;
+            const ST *p[B::KU];
+#pragma unroll
+            for (int i = 0; i < B::KU; ++i) p[i] = row_of(!TAIL || k0 + u + i < K ? k0 + u + i : K - 1) + c;
+            if (left >= 4) {
+#pragma unroll
+                for (int i = 0; i < B::KU; ++i) this->raw[b][i] = *reinterpret_cast<const Loose<ST, 4> *>(p[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < B::KU; ++i) {
+                    this->raw[b][i] = Vec<ST, 4>{};
+                    if (left > 0) this->raw[b][i] = load_some<ST, 4>(p[i], left);
+                }
+            }
+            if constexpr (TAIL) {
+#pragma unroll
+                for (int i = 0; i < B::KU; ++i) this->raw[b][i] = cut<ST, 4>(this->raw[b][i], k0 + u + i < K ? 4 : 0);
             }
         }
     }
@@ -103,26 +196,6 @@ template <class CT> __device__ __forceinline__ floatx16 mfma_unit(Vec<CT, unit_o
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// A wavefront's part of a tile, 32 MC columns by 32 MR rows from (c0, r0) on: one step's products.  Lane l holds in acc[i][j][4 q + e] the column
-// c0 + 32 i + 8 q + 4 (l / 32) + e of row r0 + 32 j + l % 32.
-template <class CT, int MC, int MR>
-__device__ __forceinline__ void step_products(const Vec<CT, unit_of<CT>()> *cols, const Vec<CT, unit_of<CT>()> *rows, int c0, int r0, int units, floatx16 (&acc)[MC][MR]) {
-    const int l32 = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
-#pragma unroll
-    for (int s = 0; s < UNITS / 2; ++s) {
-        if (2 * s >= units) break;
-        Vec<CT, unit_of<CT>()> a[MC], b[MR];
-#pragma unroll
-        for (int i = 0; i < MC; ++i) a[i] = cols[unit_place(c0 + 32 * i + l32, 2 * s + h)];
-#pragma unroll
-        for (int j = 0; j < MR; ++j) b[j] = rows[unit_place(r0 + 32 * j + l32, 2 * s + h)];
-#pragma unroll
-        for (int i = 0; i < MC; ++i)
-#pragma unroll
-            for (int j = 0; j < MR; ++j) acc[i][j] = mfma_unit<CT>(a[i], b[j], acc[i][j]);
-    }
-}
-
 // The instruction for 16 columns by 16 rows, as many units as there are lanes.
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 template <class CT> __device__ __forceinline__ floatx4 mfma_small(Vec<CT, unit_of<CT>()> a, Vec<CT, unit_of<CT>()> b, floatx4 c) {
@@ -132,6 +205,85 @@ template <class CT> __device__ __forceinline__ floatx4 mfma_small(Vec<CT, unit_o
         return c;
     } else if constexpr (std::is_same<CT, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// What a wavefront multiplies at once: a pair of units of its columns and rows.
+template <class CT, class T> struct Operands {
+    Vec<CT, unit_of<CT>()> a[T::MC], b[T::MR];
+    __device__ __forceinline__ void read(const Vec<CT, unit_of<CT>()> *tile, int c0, int r0, int pair) {
+        const int l32 = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int i = 0; i < T::MC; ++i) a[i] = tile[T::ROWS * UNITS + unit_place(c0 + 32 * i + l32, 2 * pair + h)];
+#pragma unroll
+        for (int j = 0; j < T::MR; ++j) b[j] = tile[unit_place(r0 + 32 * j + l32, 2 * pair + h)];
+    }
+    __device__ __forceinline__ void multiply(floatx16 (&acc)[T::MC][T::MR]) const {
+#pragma unroll
+        for (int i = 0; i < T::MC; ++i)
+#pragma unroll
+            for (int j = 0; j < T::MR; ++j) acc[i][j] = mfma_unit<CT>(a[i], b[j], acc[i][j]);
+    }
+};
+
+// A tile's sum over K.  load(step, tail): asks for a step's numbers; put(where): brings them into LDS, rows and then columns.  Lane l of the wavefront whose part starts
+// at column c0 and row r0 holds in acc[i][j][4 q + e] the column c0 + 32 i + 8 q + 4 (l / 32) + e of row r0 + 32 j + l % 32.
+// Two steps are in LDS and one is on its way to registers.  Every pair of units is read from LDS while the one before is multiplied, the first
+// pair of a step while the last of the step before is.
+template <class CT, class T, class Load, class Put>
+__device__ __forceinline__ void tile_sum(int K, Vec<CT, unit_of<CT>()> *lds, int c0, int r0, Load load, Put put, floatx16 (&acc)[T::MC][T::MR]) {
+    constexpr int SIZE = (T::ROWS + T::COLS) * UNITS;
+    static_assert(UNITS == 8);
+    const int full = K / step_of<CT>(), steps = (K + step_of<CT>() - 1) / step_of<CT>();
+    const auto fetch = [&](int s) {
+        if (s < full) load(s, std::false_type{});
+        else load(s, std::true_type{});
+    };
+    if (steps <= 0) return;
+    Operands<CT, T> x, y;
+    fetch(0);
+    put(lds);
+    if (steps > 1) fetch(1);
+    __syncthreads();
+    x.read(lds, c0, r0, 0);
+    for (int s = 0; s < steps; ++s) {
+        const Vec<CT, unit_of<CT>()> *here = lds + (s & 1) * SIZE;
+        Vec<CT, unit_of<CT>()> *next = lds + ((s + 1) & 1) * SIZE;
+        y.read(here, c0, r0, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        x.multiply(acc);
+        x.read(here, c0, r0, 2);
+        __builtin_amdgcn_sched_barrier(0);
+        y.multiply(acc);
+        y.read(here, c0, r0, 3);
+        __builtin_amdgcn_sched_barrier(0);
+        x.multiply(acc);
+        if (s + 1 < steps) {
+            put(next);
+            if (s + 2 < steps) fetch(s + 2);
+            __syncthreads();
+            x.read(next, c0, r0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        y.multiply(acc);
+    }
+    __syncthreads();                                                 // (LDS is used again)
+}
+// The same, of few numbers: up to one step, of the pairs of units that there are.
+template <class CT, class T, class Load, class Put>
+__device__ __forceinline__ void tile_sum_short(int K, Vec<CT, unit_of<CT>()> *lds, int c0, int r0, Load load, Put put, floatx16 (&acc)[T::MC][T::MR]) {
+    for (int s = 0; s * step_of<CT>() < K; ++s) {
+        const int left = K - s * step_of<CT>();
+        if (left >= step_of<CT>()) load(s, std::false_type{});
+        else load(s, std::true_type{});
+        put(lds);
+        __syncthreads();
+        for (int p = 0; 2 * p * unit_of<CT>() < left && p < UNITS / 2; ++p) {
+            Operands<CT, T> x;
+            x.read(lds, c0, r0, p);
+            x.multiply(acc);
+        }
+        __syncthreads();
+    }
 }
 
 // A quotient by a number that is known before the launch: of q < 2^29.
@@ -147,25 +299,71 @@ struct Quotient {
     __device__ __forceinline__ int operator()(int q) const { return by == 1 ? q : (int)((uint64_t)(uint32_t)q * m >> shift); }
 };
 
-// Four neighbouring numbers of a result, of which `left` exist.
-template <class T> __device__ __forceinline__ void put_some(T *p, Vec<float, 4> v, int left) {
-    if (left >= 4) *reinterpret_cast<Loose<T, 4> *>(p) = as_type<T, float, 4>(v);
-    else
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < left) p[i] = (T)v[i];
-}
-__device__ __forceinline__ void put_typed(void *to, int32_t type, int64_t at, Vec<float, 4> v, int left) {
-    if (type == PS_F32) put_some(reinterpret_cast<float *>(to) + at, v, left);
-    else if (type == PS_BF16) put_some(reinterpret_cast<bf16_t *>(to) + at, v, left);
-    else put_some(reinterpret_cast<f16_t *>(to) + at, v, left);
-}
-
 // A tile's form: WC x WR wavefronts of 32 MC columns by 32 MR rows each.
 template <int MC_, int MR_, int WC_, int WR_> struct Form {
     static constexpr int MC = MC_, MR = MR_, WC = WC_, WR = WR_, COLS = 32 * MC * WC, ROWS = 32 * MR * WR, THREADS = 64 * WC * WR;
+    static constexpr int LDS = 2 * (ROWS + COLS) * UNITS * 16;              // two steps
+    static constexpr int BLOCKS = MC * MR > 4 ? 1 : 2;                  // workgroups a compute unit has to have room for
 };
 typedef Form<1, 1, 2, 2> Tile64;
 typedef Form<2, 2, 2, 2> Tile128;
+typedef Form<4, 4, 2, 2> Tile256;
 typedef Form<1, 1, 1, 4> Narrow;                                     // 32 columns, 128 rows
 typedef Form<1, 1, 4, 1> Low;                                        // 128 columns, 32 rows
+
+// Neighbouring numbers of a result, of which `left` exist.
+template <class T> using Global = __attribute__((address_space(1))) T;
+template <class T, int W> __device__ __forceinline__ void put_some(T *to, Vec<float, W> v, int left) {
+    Global<T> *p = (Global<T> *)to;
+    const Vec<T, W> x = as_type<T, float, W>(v);
+    if (left >= W) *(Global<Loose<T, W>> *)p = x;
+    else
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (i < left) p[i] = x[i];
+}
+template <int W> __device__ __forceinline__ void put_typed(void *to, int32_t type, int64_t at, Vec<float, W> v, int left) {
+    if (type == PS_F32) put_some<float, W>(reinterpret_cast<float *>(to) + at, v, left);
+    else if (type == PS_BF16) put_some<bf16_t, W>(reinterpret_cast<bf16_t *>(to) + at, v, left);
+    else put_some<f16_t, W>(reinterpret_cast<f16_t *>(to) + at, v, left);
+}
+
+// A tile's sums leave by way of LDS, 32 rows of a wavefront at a time, so that rows are written in whole lines: eight numbers a lane.  to_of(r): where
+// row r of the tile starts, counted in elements, or -1: nowhere; c0: the tile's first column of the N.
+constexpr int SUMS_PAD = 4;
+template <class T, class CT> constexpr bool sums_fit() { return T::WC * T::WR * 32 * (32 * T::MC + SUMS_PAD) * 4 <= T::LDS; }
+template <class OT, class T, class F>
+__device__ __forceinline__ void put_tile(const floatx16 (&acc)[T::MC][T::MR], float *lds, OT *out, int c0, int N, float scale, F to_of) {
+    constexpr int LD = 32 * T::MC + SUMS_PAD, LANES = 4 * T::MC, AT_ONCE = 64 / LANES;         // lanes of a row, rows at a time
+    static_assert(sums_fit<T, float>());
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
+    const int wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
+    float *mine = lds + wave * 32 * LD;
+#pragma unroll
+    for (int j = 0; j < T::MR; ++j) {
+#pragma unroll
+        for (int i = 0; i < T::MC; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<Vec<float, 4> *>(mine + l32 * LD + 32 * i + 8 * q + 4 * h) =
+                    Vec<float, 4>{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int c = lane % LANES * 8, left = N - c0 - wc - c;
+#pragma unroll 4
+        for (int r = lane / LANES; r < 32; r += AT_ONCE) {
+            const int64_t to = to_of(wr + 32 * j + r);
+            const Vec<float, 4> lo = *reinterpret_cast<const Vec<float, 4> *>(mine + r * LD + c), hi = *reinterpret_cast<const Vec<float, 4> *>(mine + r * LD + c + 4);
+            if (to < 0 || left <= 0) continue;
+            const Vec<float, 8> v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            put_some<OT, 8>(out + to + c0 + wc + c, scale * v, left);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+template <class T, class F>
+__device__ __forceinline__ void put_tile_typed(const floatx16 (&acc)[T::MC][T::MR], void *lds, void *out, int32_t type, int c0, int N, float scale, F to_of) {
+    float *sums = reinterpret_cast<float *>(lds);
+    if (type == PS_F32) put_tile<float, T>(acc, sums, reinterpret_cast<float *>(out), c0, N, scale, to_of);
+    else if (type == PS_BF16) put_tile<bf16_t, T>(acc, sums, reinterpret_cast<bf16_t *>(out), c0, N, scale, to_of);
+    else put_tile<f16_t, T>(acc, sums, reinterpret_cast<f16_t *>(out), c0, N, scale, to_of);
+}
