@@ -12,15 +12,16 @@
 namespace {
 
 template <class CT, class XT, bool TURNED, class T>
-__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a, int32_t col_tiles, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a, int32_t tiles, int32_t col_tiles, int32_t *err) {
     constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
     extern __shared__ __align__(16) char shared[];
     Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
     __shared__ int at[BR];
     __shared__ int off;
     look_for_all(err, &off);
-    const int first = (int)(blockIdx.x / (uint32_t)col_tiles) * BR, count = a.g.n - first < BR ? a.g.n - first : BR;
-    const int c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * BC, tid = threadIdx.x;
+    const TilePlace place = tile_place(tiles, col_tiles);
+    const int first = place.row * BR, count = a.g.n - first < BR ? a.g.n - first : BR;
+    const int c0 = place.col * BC, tid = threadIdx.x;
     for (int r = tid; r < BR; r += T::THREADS) at[r] = r < count ? row_at(a.g, first + r, err) : -1;
     __syncthreads();
     if (off) return;
@@ -106,12 +107,12 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_adap
 
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
-    const int64_t grid = ceil_div64(a.g.n, T::ROWS) * col_tiles;
+    const int64_t tiles = ceil_div64(a.g.n, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) { ps->last_error = "adapters: too large for one launch"; return PS_ELIMIT; }
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_adapter<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
-    k_adapter<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, col_tiles, ps->err);
+    k_adapter<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, (int32_t)tiles, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }

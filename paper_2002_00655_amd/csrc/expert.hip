@@ -10,15 +10,16 @@
 namespace {
 
 template <class CT, class XT, bool TURNED, class T>
-__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertArgs a, int32_t col_tiles, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertArgs a, int32_t tiles, int32_t col_tiles, int32_t *err) {
     constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
     extern __shared__ __align__(16) char shared[];
     Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
     __shared__ int at[BR];                                           // the rows' numbers; -1: none
     __shared__ int off;
     look_for_all(err, &off);
-    const RowTile t = row_tile(a.g, (int)(blockIdx.x / (uint32_t)col_tiles), BR);
-    const int c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * BC, tid = threadIdx.x;
+    const TilePlace place = tile_place(tiles, col_tiles);
+    const RowTile t = row_tile(a.g, place.row, BR);
+    const int c0 = place.col * BC, tid = threadIdx.x;
     if (t.rows == 0) return;
     for (int r = tid; r < BR; r += T::THREADS) {
         at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
@@ -114,14 +115,15 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_outer(OuterArgs a, Ou
     int *const at = reinterpret_cast<int *>(lds + 2 * (BR + BC) * UNITS);      // the rows' numbers of the chunk
     __shared__ int off;
     look_for_all(err, &off);
-    const int tid = threadIdx.x, tiles = o.rows * o.cols, tile = (int)(blockIdx.x % (uint32_t)tiles);
+    const int tid = threadIdx.x, tiles = o.rows * o.cols;
+    const int tile = (int)(blockIdx.x % (uint32_t)tiles), share = (int)(blockIdx.x / (uint32_t)tiles);
     const int r0 = tile / o.cols * BR, c0 = tile % o.cols * BC;
-    const RowTile t = row_tile(a.g, (int)(blockIdx.x / (uint32_t)tiles), o.chunk);
+    const RowTile t = row_tile(a.g, share, o.chunk);
     if (t.group >= a.g.groups) return;
     const int start = a.g.start(t.group), end = a.g.start(t.group + 1);
     const bool empty = start >= end;
     // (a group without rows has one chunk, of none: its matrix is cleared)
-    if (t.rows == 0 && !(empty && (int)(blockIdx.x / (uint32_t)tiles) == start / o.chunk + t.group)) return;
+    if (t.rows == 0 && !(empty && share == start / o.chunk + t.group)) return;
     for (int p = tid; p < t.rows; p += T::THREADS) {
         const int q = row_at(a.g, t.first + p, err);
         at[p] = q < 0 ? 0 : q;                                       // (row 0 is read in its place; the error is set)
@@ -190,12 +192,12 @@ int too_large(dpaps_ps *ps, const char *what) {
 namespace {
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
-    const int64_t grid = row_tiles(a.g.n, a.g.groups, T::ROWS) * col_tiles;
+    const int64_t tiles = row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return too_large(ps, "product");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_expert<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
-    k_expert<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, col_tiles, ps->err);
+    k_expert<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, (int32_t)tiles, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }

@@ -79,7 +79,7 @@ template <class CT, class T> struct LaidForm {
 };
 
 template <class CT, class T, bool LOW>
-__global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t col_tiles, int32_t kb_all, int32_t b_kb, int32_t *err) {
+__global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t row_tiles, int32_t col_tiles, int32_t kb_all, int32_t b_kb, int32_t *err) {
     typedef LaidForm<CT, T> F;
     constexpr int BR = T::ROWS, BC = T::COLS, H = F::LOADS / 2;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -87,7 +87,8 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t col
     __shared__ int off;
     look_for_all(err, &off);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tile = (int)(blockIdx.x / (uint32_t)col_tiles), c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * BC;
+    const TilePlace place = tile_place(row_tiles, col_tiles);
+    const int tile = place.row, c0 = place.col * BC;
     RowTile t;
     if constexpr (LOW) t = RowTile{0, tile * BR, a.g.n - tile * BR < BR ? a.g.n - tile * BR : BR};
     else t = row_tile(a.g, tile, BR);
@@ -202,12 +203,12 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t col
 template <class CT, class T, bool LOW> int start(dpaps_ps *ps, const LaidArgs &a, hipStream_t st) {
     typedef LaidForm<CT, T> F;
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
-    const int64_t grid = (LOW ? ceil_div64(a.g.n, T::ROWS) : row_tiles(a.g.n, a.g.groups, T::ROWS)) * col_tiles;
+    const int64_t tiles = LOW ? ceil_div64(a.g.n, T::ROWS) : row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) { ps->last_error = "product: too large for one launch"; return PS_ELIMIT; }
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_laid<CT, T, LOW>), F::LDS);
     if (rc) return rc;
-    k_laid<CT, T, LOW><<<(unsigned)grid, 256, F::LDS, st>>>(a, col_tiles, (int32_t)k_blocks(a.K), (int32_t)k_blocks(a.rank), ps->err);
+    k_laid<CT, T, LOW><<<(unsigned)grid, 256, F::LDS, st>>>(a, (int32_t)tiles, col_tiles, (int32_t)k_blocks(a.K), (int32_t)k_blocks(a.rank), ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }

@@ -311,6 +311,21 @@ typedef Form<4, 4, 2, 2> Tile256;
 typedef Form<1, 1, 1, 4> Narrow;                                     // 32 columns, 128 rows
 typedef Form<1, 1, 4, 1> Low;                                        // 128 columns, 32 rows
 
+// Which tile a workgroup has.  Workgroups go to the compute dies in turn: each die gets neighbouring tiles, row by row of tiles in bands of BAND columns of them, so that
+// what its cache holds is read by several: 32 tiles at a time, 4 by 8, instead of 32 by 1.
+constexpr uint32_t DIES = 8;
+constexpr int BAND = 8;
+struct TilePlace { int row, col; };
+__device__ __forceinline__ uint32_t of_die(uint32_t block, uint32_t all) {
+    const uint32_t die = block % DIES;
+    return die * (all / DIES) + (die < all % DIES ? die : all % DIES) + block / DIES;
+}
+__device__ __forceinline__ TilePlace tile_place(int row_tiles, int col_tiles) {
+    const uint32_t at = of_die(blockIdx.x, (uint32_t)row_tiles * col_tiles), of_band = (uint32_t)row_tiles * BAND, band = at / of_band, r = at - band * of_band;
+    const uint32_t cols = (uint32_t)col_tiles - band * BAND < BAND ? (uint32_t)col_tiles - band * BAND : BAND;
+    return TilePlace{(int)(r / cols), (int)(band * BAND + r % cols)};
+}
+
 // Neighbouring numbers of a result, of which `left` exist.
 template <class T> using Global = __attribute__((address_space(1))) T;
 template <class T, int W> __device__ __forceinline__ void put_some(T *to, Vec<float, W> v, int left) {
