@@ -108,7 +108,7 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_adap
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
     const int64_t tiles = ceil_div64(a.g.n, T::ROWS), grid = tiles * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) { ps->last_error = "adapters: too large for one launch"; return PS_ELIMIT; }
+    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "adapters");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_adapter<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
@@ -162,7 +162,7 @@ constexpr int64_t LAID_ROWS = 1024;
 struct Scratch {
     bool laid = false;
     int64_t stride = 0, rounded_stride = 0, w_size = 0, b_size = 0;
-    size_t numbers[2] = {}, rounded = 0, group_of = 0, zeros = 0, w = 0, b = 0, end = 0;
+    size_t numbers[2] = {}, rounded = 0, group_of = 0, w = 0, b = 0, end = 0;
 };
 // both: the numbers in 32 bits of two products, which gradients need
 Scratch scratch_of(const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
@@ -177,7 +177,6 @@ Scratch scratch_of(const RowGroups &g, const void *x, int64_t x_stride, int32_t 
     s.group_of = take(n * 4);
     if (s.laid) {
         s.rounded = take(n * s.rounded_stride * 2);
-        s.zeros = take(256);
         s.w_size = dpaps_laid_size(K, N);
         s.b_size = dpaps_laid_size(rank, N);
         s.w = take(s.w_size * 2);
@@ -200,7 +199,7 @@ int product_with(dpaps_ps *ps, const Scratch &s, const LowNumbers &low, AdapterA
     }
     char *ws = (char *)ps->ws;
     LayArgs l{};
-    l.w = a.w; l.L = a.L; l.K = a.K; l.N = a.N; l.turned = a.turned; l.to = ws + s.w; l.zeros = ws + s.zeros;
+    l.w = a.w; l.L = a.L; l.K = a.K; l.N = a.N; l.turned = a.turned; l.to = ws + s.w;
     int rc = dpaps_lay(ps, nullptr, a.x_type, l, st);
     if (rc) return rc;
     l = LayArgs{};
@@ -209,7 +208,7 @@ int product_with(dpaps_ps *ps, const Scratch &s, const LowNumbers &low, AdapterA
     if (rc) return rc;
     LaidArgs p{};
     p.g = a.g; p.x = a.x; p.x_stride = a.x_stride; p.K = a.K; p.N = a.N; p.w = ws + s.w; p.w_size = s.w_size; p.low = low.rounded; p.low_stride = (int32_t)low.rounded_stride;
-    p.b = ws + s.b; p.b_size = s.b_size; p.rank = a.rank; p.zeros = ws + s.zeros; p.out = a.out; p.out_stride = a.out_stride; p.out_type = a.out_type;
+    p.b = ws + s.b; p.b_size = s.b_size; p.rank = a.rank; p.out = a.out; p.out_stride = a.out_stride; p.out_type = a.out_type;
     return dpaps_laid_product(ps, a.x_type, p, st);
 }
 
@@ -262,14 +261,13 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
     if (n > 0 && (!x || !dout || x_stride < 0 || dout_stride < 0 || (dx && dx_stride < dim))) return PS_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     const Scratch s = scratch_of(g, dout, dout_stride, rows, dim, rank, type == PS_F32 || dx_type == PS_F32, true);
-    OuterArgs o{};
-    o.g = g; o.left_stride = s.stride; o.left_type = PS_F32; o.left_by_place = 1; o.rows = rank; o.out_type = PS_F32; o.right_type = type;
-    size_t part = 0;
-    for (const int32_t c : {dim, rows}) {
-        o.cols = c;
-        part = std::max(part, dpaps_outer_bytes(ps, o));
+    OuterArgs o[2]{};
+    for (int i = 0; i < 2; ++i) {
+        o[i].g = g; o[i].left_stride = s.stride; o[i].left_type = PS_F32; o[i].left_by_place = 1; o[i].rows = rank; o[i].out_type = PS_F32; o[i].right_type = type;
     }
-    rc = dpaps_ws_reserve(ps, s.end + part);
+    o[0].right = x; o[0].right_stride = x_stride; o[0].cols = dim; o[0].out = da;
+    o[1].right = dout; o[1].right_stride = dout_stride; o[1].cols = rows; o[1].out = db;
+    rc = dpaps_ws_reserve(ps, s.end + dpaps_outer_bytes(ps, o, 2));
     if (rc) return rc;
     char *ws = (char *)ps->ws;
     const LowNumbers h = low_of(ws, s, true, false, 0), t = low_of(ws, s, true, dx != nullptr, 1);
@@ -286,11 +284,9 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
             if (rc) return rc;
         }
     }
-    o.left = t.numbers; o.right = x; o.right_stride = x_stride; o.cols = dim; o.out = da;
-    rc = dpaps_outer_sums(ps, o, (float *)(ws + s.end), st);
-    if (rc) return rc;
-    o.left = h.numbers; o.right = dout; o.right_stride = dout_stride; o.cols = rows; o.out = db;
-    rc = dpaps_outer_sums(ps, o, (float *)(ws + s.end), st);
+    o[0].left = t.numbers;
+    o[1].left = h.numbers;
+    rc = dpaps_outer_sums(ps, o, 2, (float *)(ws + s.end), st);
     if (rc) return rc;
     if (n == 0) return PS_OK;
     GroupKeys k;

@@ -98,77 +98,6 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expe
     }
 }
 
-// A group's sum of products, a tile of it, over `chunk` places of its rows: a group of more than that has several workgroups for a tile.  The first of them
-// writes to the result, or, where that is not of 32 bits, to a slot of part; the others to slots that are told apart by their first place, whole chunks:
-// floor(first / chunk) differs between all chunks but the first ones of groups of several, as it does between the first ones.
-struct OuterTiles { int32_t rows, cols, chunk; float *part; int32_t slots; };
-__device__ __forceinline__ float *outer_slot(const OuterArgs &a, const OuterTiles &o, int group, int start, int first) {
-    const int64_t size = (int64_t)a.rows * a.cols;
-    if (first > start) return o.part + first / o.chunk * size;
-    return a.out_type == PS_F32 ? reinterpret_cast<float *>(a.out) + group * size : o.part + (o.slots + first / o.chunk) * size;
-}
-template <class CT, class LT, class RT, class T>
-__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_outer(OuterArgs a, OuterTiles o, int32_t *err) {
-    constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
-    extern __shared__ __align__(16) char shared[];
-    Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
-    int *const at = reinterpret_cast<int *>(lds + 2 * (BR + BC) * UNITS);      // the rows' numbers of the chunk
-    __shared__ int off;
-    look_for_all(err, &off);
-    const int tid = threadIdx.x, tiles = o.rows * o.cols;
-    const int tile = (int)(blockIdx.x % (uint32_t)tiles), share = (int)(blockIdx.x / (uint32_t)tiles);
-    const int r0 = tile / o.cols * BR, c0 = tile % o.cols * BC;
-    const RowTile t = row_tile(a.g, share, o.chunk);
-    if (t.group >= a.g.groups) return;
-    const int start = a.g.start(t.group), end = a.g.start(t.group + 1);
-    const bool empty = start >= end;
-    // (a group without rows has one chunk, of none: its matrix is cleared)
-    if (t.rows == 0 && !(empty && share == start / o.chunk + t.group)) return;
-    for (int p = tid; p < t.rows; p += T::THREADS) {
-        const int q = row_at(a.g, t.first + p, err);
-        at[p] = q < 0 ? 0 : q;                                       // (row 0 is read in its place; the error is set)
-    }
-    __syncthreads();
-    if (off) return;
-    floatx16 acc[T::MC][T::MR] = {};
-    const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
-    ChosenRows<LT, CT, BR, T::THREADS> left;
-    ChosenRows<RT, CT, BC, T::THREADS> right;
-    tile_sum<CT, T>(t.rows, lds, wc, wr,
-        [&](int s, auto tail) {
-            left.template load<decltype(tail)::value>(s, t.rows, a.rows - r0, [&](int p) {
-                return reinterpret_cast<const LT *>(a.left) + (int64_t)(a.left_by_place ? t.first + p : a.left_shared(at[p])) * a.left_stride + r0;
-            });
-            right.template load<decltype(tail)::value>(s, t.rows, a.cols - c0, [&](int p) {
-                return reinterpret_cast<const RT *>(a.right) + (int64_t)a.right_shared(at[p]) * a.right_stride + c0;
-            });
-        },
-        [&](Vec<CT, KU> *to) {
-            left.put(to);
-            right.put(to + BR * UNITS);
-        }, acc);
-    const bool whole = end - start <= o.chunk;
-    void *out = whole ? a.out : outer_slot(a, o, t.group, start, t.first);
-    const int64_t base = whole ? (int64_t)t.group * a.rows * a.cols : 0;
-    put_tile_typed<T>(acc, lds, out, whole ? a.out_type : PS_F32, c0, a.cols, 1.0f,
-                      [&](int r) { return r0 + r < a.rows ? base + (int64_t)(r0 + r) * a.cols : (int64_t)-1; });
-}
-// The chunks of groups of several, added up in their order.  blockIdx.y: the group
-__global__ __launch_bounds__(256) void k_outer_join(OuterArgs a, OuterTiles o, const int32_t *err) {
-    if (*(volatile const int32_t *)err) return;
-    const int64_t size = (int64_t)a.rows * a.cols;
-    for (int group = blockIdx.y; group < a.g.groups; group += gridDim.y) {
-        const int start = a.g.start(group), end = a.g.start(group + 1);
-        if (end - start <= o.chunk) continue;
-        for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
-            const int left = size - i < 4 ? (int)(size - i) : 4;
-            Vec<float, 4> v = {};
-            for (int first = start; first < end; first += o.chunk) v = v + load_some<float, 4>(outer_slot(a, o, group, start, first) + i, left);
-            put_typed<4>(a.out, a.out_type, group * size + i, v, left);
-        }
-    }
-}
-
 // out_t = the sum of the rows t b .. t b + b - 1 of `in`, in that order
 __global__ __launch_bounds__(256) void k_pair_sums(const float *in, int64_t n, int32_t b, int32_t N, void *out, int32_t out_type, int64_t out_stride, uint32_t P, double inv_P,
                                                    const int32_t *err) {
@@ -182,18 +111,13 @@ __global__ __launch_bounds__(256) void k_pair_sums(const float *in, int64_t n, i
     put_typed<4>(out, out_type, t * out_stride + c, v, left);
 }
 
-int too_large(dpaps_ps *ps, const char *what) {
-    ps->last_error = std::string(what) + ": too large for one launch";
-    return PS_ELIMIT;
-}
-
 }  // namespace
 
 namespace {
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
     const int64_t tiles = row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "product");
+    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_expert<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
@@ -205,7 +129,7 @@ template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, cons
     typedef FewRows<CT, XT, TURNED, MT> F;
     const int32_t col_tiles = (a.N + F::COLS - 1) / F::COLS;
     const int64_t grid = row_tiles(a.g.n, a.g.groups, 16 * MT) * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "product");
+    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
     k_expert_few<CT, XT, TURNED, MT><<<(unsigned)grid, F::THREADS, 0, st>>>(a, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
@@ -227,52 +151,6 @@ int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
     if (a.x_type == PS_F32) return product_either<float, float>(ps, a, st);
     if (a.x_type == PS_BF16) return a.precise ? product_either<float, bf16_t>(ps, a, st) : product_either<bf16_t, bf16_t>(ps, a, st);
     return a.precise ? product_either<float, f16_t>(ps, a, st) : product_either<f16_t, f16_t>(ps, a, st);
-}
-
-namespace {
-// The tiles of a sum, and how many of a group's rows a workgroup takes: as few as it needs for two workgroups a compute unit.
-template <class T> OuterTiles outer_tiles(const dpaps_ps *ps, const OuterArgs &a) {
-    OuterTiles o{};
-    o.rows = (a.rows + T::ROWS - 1) / T::ROWS;
-    o.cols = (a.cols + T::COLS - 1) / T::COLS;
-    o.chunk = 2048;
-    while (o.chunk > 256 && (int64_t)o.rows * o.cols * ceil_div64(a.g.n, o.chunk) < 2 * ps->num_cu) o.chunk /= 2;
-    o.slots = a.g.n / o.chunk + 1;
-    return o;
-}
-bool outer_narrow(const OuterArgs &a) { return a.rows <= 64; }
-template <class CT, class LT, class RT, class T> int outer_of(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st) {
-    OuterTiles o = outer_tiles<T>(ps, a);
-    o.part = part;
-    const int64_t grid = row_tiles(a.g.n, a.g.groups, o.chunk) * o.rows * o.cols;
-    if (grid >= ((int64_t)1 << 24)) return too_large(ps, "expert_grad");
-    static LdsAllowed allowed;
-    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer<CT, LT, RT, T>), T::LDS + 2048 * sizeof(int));
-    if (rc) return rc;
-    k_outer<CT, LT, RT, T><<<(unsigned)grid, T::THREADS, T::LDS + o.chunk * sizeof(int), st>>>(a, o, ps->err);
-    PS_HIP(ps, hipGetLastError());
-    if (a.g.n <= o.chunk) return PS_OK;
-    const int64_t x = ceil_div64((int64_t)a.rows * a.cols, 1024);
-    k_outer_join<<<dim3((unsigned)(x < 256 ? x : 256), (unsigned)(a.g.groups < 1024 ? a.g.groups : 1024)), 256, 0, st>>>(a, o, ps->err);
-    PS_HIP(ps, hipGetLastError());
-    return PS_OK;
-}
-template <class CT, class LT, class RT> int outer_any(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st) {
-    return outer_narrow(a) ? outer_of<CT, LT, RT, Low>(ps, a, part, st) : outer_of<CT, LT, RT, Tile128>(ps, a, part, st);
-}
-}  // namespace
-
-size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs &a) {
-    const OuterTiles o = outer_narrow(a) ? outer_tiles<Low>(ps, a) : outer_tiles<Tile128>(ps, a);
-    if (a.g.n <= o.chunk) return 0;
-    return (size_t)o.slots * (a.out_type == PS_F32 ? 1 : 2) * (size_t)a.rows * (size_t)a.cols * sizeof(float);
-}
-int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st) {
-    if (a.left_type == PS_F32) {
-        if (a.right_type == PS_F32) return outer_any<float, float, float>(ps, a, part, st);
-        return a.right_type == PS_BF16 ? outer_any<float, float, bf16_t>(ps, a, part, st) : outer_any<float, float, f16_t>(ps, a, part, st);
-    }
-    return a.left_type == PS_BF16 ? outer_any<bf16_t, bf16_t, bf16_t>(ps, a, part, st) : outer_any<f16_t, f16_t, f16_t>(ps, a, part, st);
 }
 
 // From so many rows a group on, matrices are laid before the product (laid.hip).
@@ -300,17 +178,16 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     const size_t sums = out_pairs > 1 ? ((size_t)n * N * sizeof(float) + 255) / 256 * 256 : 0;
     const bool lay = !a.precise && n >= LAID_ROWS * num_experts && num_experts < 32768 && dpaps_laid_fits(x, x_stride, K);
     const int64_t laid = lay ? dpaps_laid_size(K, N) : 0;
-    rc = dpaps_ws_reserve(ps, sums + (size_t)laid * num_experts * 2 + 256);
+    rc = dpaps_ws_reserve(ps, sums + (size_t)laid * num_experts * 2);
     if (rc) return rc;
     if (out_pairs > 1) { a.out = ps->ws; a.out_stride = N; a.out_type = PS_F32; }
     if (lay) {
-        char *zeros = (char *)ps->ws + sums;
         LayArgs l{};
-        l.w = a.w; l.L = a.L; l.each = a.each; l.K = K; l.N = N; l.turned = a.turned; l.to = zeros + 256; l.size = laid; l.zeros = zeros;
+        l.w = a.w; l.L = a.L; l.each = a.each; l.K = K; l.N = N; l.turned = a.turned; l.to = (char *)ps->ws + sums; l.size = laid;
         rc = dpaps_lay(ps, &g, x_type, l, st);
         if (rc) return rc;
         LaidArgs p{};
-        p.g = g; p.x = x; p.x_stride = x_stride; p.x_shared = a.x_shared; p.K = K; p.N = N; p.w = l.to; p.w_size = laid; p.zeros = zeros;
+        p.g = g; p.x = x; p.x_stride = x_stride; p.x_shared = a.x_shared; p.K = K; p.N = N; p.w = l.to; p.w_size = laid;
         p.out = a.out; p.out_stride = a.out_stride; p.out_type = a.out_type;
         rc = dpaps_laid_product(ps, x_type, p, st);
     } else rc = dpaps_expert_product(ps, a, st);
@@ -318,7 +195,7 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     if (out_pairs > 1) {
         const uint32_t P = (uint32_t)((N + 3) / 4);
         const int64_t blocks = ceil_div64(n / out_pairs * P, 256);
-        if (blocks >= ((int64_t)1 << 24)) return too_large(ps, "expert_matmul");
+        if (blocks >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "expert_matmul");
         k_pair_sums<<<(unsigned)blocks, 256, 0, st>>>((const float *)ps->ws, n / out_pairs, out_pairs, N, out, out_type, out_stride, P, 1.0 / P, ps->err);
         PS_HIP(ps, hipGetLastError());
     }
@@ -339,6 +216,6 @@ extern "C" int expert_grad(ps_handle ps, int32_t num_experts, int32_t rows, int3
     a.g = g; a.left = left; a.left_stride = left_stride; a.left_type = type; a.left_shared = Quotient(left_pairs);
     a.right = right; a.right_stride = right_stride; a.right_type = type; a.right_shared = Quotient(right_pairs);
     a.rows = rows; a.cols = dim; a.out = out; a.out_type = out_type;
-    rc = dpaps_ws_reserve(ps, dpaps_outer_bytes(ps, a));
-    return rc ? rc : dpaps_outer_sums(ps, a, (float *)ps->ws, (hipStream_t)stream);
+    rc = dpaps_ws_reserve(ps, dpaps_outer_bytes(ps, &a, 1));
+    return rc ? rc : dpaps_outer_sums(ps, &a, 1, (float *)ps->ws, (hipStream_t)stream);
 }

@@ -26,9 +26,10 @@ struct OuterArgs {
     int32_t rows, cols;
     void *out; int32_t out_type;
 };
-// part: scratch of dpaps_outer_bytes(...) bytes
-size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs &a);
-int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs &a, float *part, hipStream_t st);
+// count: one, or two of the same groups and types in the same launches.  part: scratch of dpaps_outer_bytes(...) bytes
+size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs *a, int count);
+int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs *a, int count, float *part, hipStream_t st);
+int dpaps_too_large(dpaps_ps *ps, const char *what);
 
 
 // The row number that stands at a place; -1, and the handle's error, where there is no such row.
@@ -60,7 +61,6 @@ struct LaidArgs {
     int32_t K, N;
     const void *w; int64_t w_size;                                           // elements of a laid matrix
     const void *low, *b; int64_t b_size; int32_t rank, low_stride;           // low: NULL, a matrix for each group
-    const void *zeros;                                                       // 64 bytes
     void *out; int64_t out_stride; int32_t out_type;
 };
 // What is laid: M_e's number of column c and place k of the sum is value c of key k (turned) or value k of key c, of keys from w + e * each * L on.
@@ -68,7 +68,6 @@ struct LayArgs {
     const float *w; int64_t L, each;
     int32_t K, N, turned;
     void *to; int64_t size;
-    void *zeros;                                                             // not NULL: 64 bytes that are cleared
 };
 int64_t dpaps_laid_size(int32_t K, int32_t N);
 bool dpaps_laid_fits(const void *x, int64_t x_stride, int32_t K);

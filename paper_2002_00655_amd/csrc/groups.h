@@ -15,7 +15,7 @@ struct RowGroups {
 };
 
 // The rows of one group from place `first` on, `rows` of them.  group == groups: rows of no group.
-struct RowTile { int group, first, rows; };
+struct RowTile { int group, first, rows, start, end; };        // start, end: the group's places
 
 // Tiles of BM places that hold rows of one group only.  Group e's tiles have the numbers from floor(start_e / BM) + e on: as ceil(c / BM) is at most
 // floor((s + c) / BM) + 1 - floor(s / BM), they end before the next group's, and no tile's number has to be looked up in a sum over the groups.
@@ -24,22 +24,29 @@ inline int64_t row_tiles(int64_t n, int32_t groups, int BM) { return n / BM + gr
 __device__ __forceinline__ RowTile row_tile(const RowGroups &g, int tile, int BM) {
     // the last e with floor(start_e / BM) + e <= tile: the wavefront's lanes look at 64 of them at once
     const int lane = threadIdx.x & 63;
-    int lo = 0, hi = g.groups;
-    while (lo < hi) {
-        const int step = (hi - lo) / 64 + 1, e = lo + lane * step;
-        const bool at = e <= hi && g.start(e) / BM + e <= tile;
-        const int c = __popcll(__ballot(at));
-        lo += (c > 1 ? c - 1 : 0) * step;
+    int lo = 0, hi = g.groups, s, end, c, step;
+    do {
+        step = (hi - lo) / 64 + 1;
+        const int e = lo + lane * step;
+        s = e <= g.groups ? g.start(e) : g.n;
+        const bool at = e <= hi && s / BM + e <= tile;
+        c = __popcll(__ballot(at));
+        c = c > 1 ? c - 1 : 0;
+        lo += c * step;
         hi = hi < lo + step - 1 ? hi : lo + step - 1;
-        if (step == 1) break;
-    }
+    } while (step > 1);
+    // (where the group's places start and end, one of the lanes has seen: another trip to memory only where it was the last one)
     RowTile t;
     t.group = __builtin_amdgcn_readfirstlane(lo < g.groups ? lo : g.groups);
-    const int s = g.start(t.group), end = t.group < g.groups ? g.start(t.group + 1) : g.n;
+    c = __builtin_amdgcn_readfirstlane(c);
+    end = c < 63 ? __builtin_amdgcn_readlane(s, c + 1) : t.group < g.groups ? g.start(t.group + 1) : g.n;
+    s = __builtin_amdgcn_readlane(s, c);
     t.first = s + (tile - s / BM - t.group) * BM;
     t.rows = end - t.first;
     if (t.first < s || t.rows < 0) t.rows = 0;
     if (t.rows > BM) t.rows = BM;
+    t.start = s;
+    t.end = end;
     return t;
 }
 

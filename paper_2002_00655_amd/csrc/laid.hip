@@ -18,7 +18,6 @@ inline int64_t k_blocks(int32_t K) { return ceil_div64(K, KB); }
 template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(LayArgs a, RowGroups g, int32_t cb_all, int32_t kb_all, const int32_t *err) {
     if (*(volatile const int32_t *)err) return;
     const int e = blockIdx.z, tid = threadIdx.x;
-    if (a.zeros && e == 0 && blockIdx.x == 0 && blockIdx.y == 0 && tid < 16) reinterpret_cast<uint32_t *>(a.zeros)[tid] = 0;
     if (g.offsets && g.start(e) >= g.start(e + 1)) return;
     const float *w = a.w + (int64_t)e * a.each * a.L;
     T *to = reinterpret_cast<T *>(a.to) + e * a.size;
@@ -57,22 +56,6 @@ template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(Lay
     }
 }
 
-// until at most N of this wavefront's loads are on their way and all it has asked of LDS is there, then until all wavefronts are so far
-template <int N> __device__ __forceinline__ void wait_and_meet() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-// The order of a turn's instructions: reads of LDS and loads spread over the products.
-template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinline__ void spread() {
-    constexpr int R = (I + 1) * READS / PRODUCTS - I * READS / PRODUCTS, L = (I + 1) * LOADS / PRODUCTS - I * LOADS / PRODUCTS;
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if constexpr (R > 0) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-    if constexpr (L > 0) __builtin_amdgcn_sched_group_barrier(0x020, L, 0);
-    if constexpr (I + 1 < PRODUCTS) spread<PRODUCTS, READS, LOADS, I + 1>();
-}
-
 template <class CT, class T> struct LaidForm {
     static constexpr int STAGE = (T::ROWS + T::COLS) * KB * 2, LDS = STAGES * STAGE, ROW_LOADS = T::ROWS / 16 / 4, COL_LOADS = T::COLS / 16 / 4, LOADS = ROW_LOADS + COL_LOADS;
     static_assert(T::THREADS == 256);
@@ -90,7 +73,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t row
     const TilePlace place = tile_place(row_tiles, col_tiles);
     const int tile = place.row, c0 = place.col * BC;
     RowTile t;
-    if constexpr (LOW) t = RowTile{0, tile * BR, a.g.n - tile * BR < BR ? a.g.n - tile * BR : BR};
+    if constexpr (LOW) t = RowTile{0, tile * BR, a.g.n - tile * BR < BR ? a.g.n - tile * BR : BR, 0, 0};
     else t = row_tile(a.g, tile, BR);
     if (t.rows == 0) return;
     for (int r = tid; r < BR; r += 256) at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
@@ -135,7 +118,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t row
                 const bool here = k + unit * 8 < K;
 #pragma unroll
                 for (int i = 0; i < F::ROW_LOADS; ++i)
-                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(here && (!LOW || row[i]) ? row[i] + k : reinterpret_cast<const CT *>(a.zeros)),
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(here && (!LOW || row[i]) ? row[i] + k : reinterpret_cast<const CT *>(zero_bytes)),
                                                      (__attribute__((address_space(3))) void *)(to + i * 1024), 16, 0, 0);
             } else {
 #pragma unroll
@@ -204,7 +187,7 @@ template <class CT, class T, bool LOW> int start(dpaps_ps *ps, const LaidArgs &a
     typedef LaidForm<CT, T> F;
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
     const int64_t tiles = LOW ? ceil_div64(a.g.n, T::ROWS) : row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) { ps->last_error = "product: too large for one launch"; return PS_ELIMIT; }
+    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_laid<CT, T, LOW>), F::LDS);
     if (rc) return rc;

@@ -1,0 +1,314 @@
+// Sums of products of rows by group: the gradients of matrices that rows were multiplied by.
+//
+//   out_e[i][j] = sum over the rows q of group e of left_q[i] right_q[j]
+// Both operands lie the wrong way round for the matrix instruction, which takes numbers that follow each other in the sum, here the rows.  Rows of 16 bits
+// come straight into LDS as they lie, stages ahead, and are turned on their way out of LDS by the instruction that reads four rows of 16 columns and
+// gives each lane one column; other rows are turned in registers on their way in.
+// A group's rows are cut into chunks, so that a group of many rows is the work of several workgroups a tile; their sums are added in the chunks' order.
+#include "experts.h"
+
+#include <algorithm>
+
+namespace {
+
+// The first chunk of a group writes to the result, or, where that is not of 32 bits and the group has several, to a slot of part; the others to slots that
+// are told apart by their first place, in whole chunks: floor(first / chunk) differs between all chunks but the first ones of groups of several, as it does
+// between those.
+struct OuterTiles { int32_t rows, cols, chunk; float *part; int32_t slots; };
+struct OuterCall { OuterArgs a[2]; OuterTiles o[2]; };
+__device__ __forceinline__ float *outer_slot(const OuterArgs &a, const OuterTiles &o, int group, int start, int first) {
+    const int64_t size = (int64_t)a.rows * a.cols;
+    if (first > start) return o.part + first / o.chunk * size;
+    return a.out_type == PS_F32 ? reinterpret_cast<float *>(a.out) + group * size : o.part + (o.slots + first / o.chunk) * size;
+}
+// Which tile, of which chunk; `at`: the numbers of its rows, brought into LDS.  False: nothing to do (for the whole workgroup).
+struct OuterPlace { RowTile t; int r0, c0; };
+template <int BR, int BC>
+__device__ __forceinline__ bool outer_place(const OuterArgs &a, const OuterTiles &o, int *at, int32_t *err, OuterPlace &p) {
+    __shared__ int off;
+    look_for_all(err, &off);
+    const int tiles = o.rows * o.cols, tile = (int)(blockIdx.x % (uint32_t)tiles), share = (int)(blockIdx.x / (uint32_t)tiles);
+    p.r0 = tile / o.cols * BR;
+    p.c0 = tile % o.cols * BC;
+    p.t = row_tile(a.g, share, o.chunk);
+    if (p.t.group >= a.g.groups) return false;
+    // (a group without rows has one chunk, of none: its matrix is cleared)
+    if (p.t.rows == 0 && !(p.t.start >= p.t.end && share == p.t.start / o.chunk + p.t.group)) return false;
+    for (int i0 = threadIdx.x; i0 < p.t.rows; i0 += 8 * blockDim.x) {
+        int q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) q[u] = a.g.order[p.t.first + (i0 + u * (int)blockDim.x < p.t.rows ? i0 + u * (int)blockDim.x : i0)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = i0 + u * (int)blockDim.x;
+            if (q[u] < 0 || q[u] >= a.g.n) {                         // (row 0 is read in its place; the error is set)
+                atomicExch(err, PS_EKEY);
+                q[u] = 0;
+            }
+            if (i < p.t.rows) at[i] = q[u];
+        }
+    }
+    __syncthreads();
+    return off == 0;
+}
+template <class T> __device__ __forceinline__ void outer_put(const OuterArgs &a, const OuterTiles &o, const OuterPlace &p, const floatx16 (&acc)[T::MC][T::MR], void *lds) {
+    const bool whole = p.t.end - p.t.start <= o.chunk;
+    void *out = whole ? a.out : outer_slot(a, o, p.t.group, p.t.start, p.t.first);
+    const int64_t base = whole ? (int64_t)p.t.group * a.rows * a.cols : 0;
+    put_tile_typed<T>(acc, lds, out, whole ? a.out_type : PS_F32, p.c0, a.cols, 1.0f,
+                      [&](int r) { return p.r0 + r < a.rows ? base + (int64_t)(p.r0 + r) * a.cols : (int64_t)-1; });
+}
+
+// Turned in registers.
+template <class CT, class LT, class RT, class T>
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_outer(OuterCall call, int32_t *err) {
+    constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
+    extern __shared__ __align__(16) char shared[];
+    Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
+    int *const at = reinterpret_cast<int *>(lds + 2 * (BR + BC) * UNITS);      // the rows' numbers of the chunk
+    const OuterArgs &a = call.a[blockIdx.y];
+    const OuterTiles &o = call.o[blockIdx.y];
+    OuterPlace p;
+    if (!outer_place<BR, BC>(a, o, at, err, p)) return;
+    floatx16 acc[T::MC][T::MR] = {};
+    const int wave = threadIdx.x >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
+    ChosenRows<LT, CT, BR, T::THREADS> left;
+    ChosenRows<RT, CT, BC, T::THREADS> right;
+    tile_sum<CT, T>(p.t.rows, lds, wc, wr,
+        [&](int s, auto tail) {
+            left.template load<decltype(tail)::value>(s, p.t.rows, a.rows - p.r0, [&](int i) {
+                return reinterpret_cast<const LT *>(a.left) + (int64_t)(a.left_by_place ? p.t.first + i : a.left_shared(at[i])) * a.left_stride + p.r0;
+            });
+            right.template load<decltype(tail)::value>(s, p.t.rows, a.cols - p.c0, [&](int i) {
+                return reinterpret_cast<const RT *>(a.right) + (int64_t)a.right_shared(at[i]) * a.right_stride + p.c0;
+            });
+        },
+        [&](Vec<CT, KU> *to) {
+            left.put(to);
+            right.put(to + BR * UNITS);
+        }, acc);
+    outer_put<T>(a, o, p, acc, lds);
+}
+
+// Turned out of LDS: rows of 16 bits whose numbers lie on 16 bytes.  A step is 64 rows of the sum, two steps are in LDS and two on their way to registers.  A row's
+// columns lie in LDS as in memory, 32 bytes at a time changed over by the row's number, so that the four rows of a read meet all banks.
+// (Straight from memory into LDS, the compiler has every turned read wait for all loads on their way: 78 us instead of 60 turned in registers, for
+// 16,384 rows of 8 groups, 1024 x 512.)
+constexpr int KS = 64;
+template <class T> struct Turned {
+    static constexpr int STEP = KS * (T::ROWS + T::COLS) * 2, LDS = 2 * STEP, N = KS / 16;    // a thread's rows of a step
+    static_assert(T::THREADS == 256 && T::ROWS == 128 && T::COLS == 128);                    // 16 threads a row, on either side
+};
+typedef short Four __attribute__((ext_vector_type(4)));
+typedef short Eight __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ Four turned_four(const unsigned char *part, int k, int chunk, int row, int piece) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four *)(part + (k + row) * 256 + (chunk ^ (2 * row)) * 32 + piece * 8));
+}
+template <class CT, class T>
+__global__ __launch_bounds__(256, T::BLOCKS) void k_outer_turned(OuterCall call, int32_t *err) {
+    typedef Turned<T> F;
+    constexpr int BR = T::ROWS, BC = T::COLS;
+    extern __shared__ __align__(16) unsigned char lds[];
+    int *const at = reinterpret_cast<int *>(lds + F::LDS);
+    const OuterArgs &a = call.a[blockIdx.y];
+    const OuterTiles &o = call.o[blockIdx.y];
+    OuterPlace p;
+    if (!outer_place<BR, BC>(a, o, at, err, p)) return;
+    floatx16 acc[T::MC][T::MR] = {};
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
+    const int steps = (p.t.rows + KS - 1) / KS;
+    if (steps > 0) {
+        struct Numbers { Eight left[F::N], right[F::N]; } x, y;
+        const int k0 = tid >> 4, c = (tid & 15) * 8;
+        const bool in_left = p.r0 + c < a.rows, in_right = p.c0 + c < a.cols;
+        const CT *left = reinterpret_cast<const CT *>(a.left) + (in_left ? p.r0 + c : 0), *right = reinterpret_cast<const CT *>(a.right) + (in_right ? p.c0 + c : 0);
+        const auto fetch = [&](Numbers &to, int s) {
+#pragma unroll
+            for (int i = 0; i < F::N; ++i) {
+                const int k = s * KS + i * 16 + k0, q = at[k < p.t.rows ? k : 0];
+                to.left[i] = *reinterpret_cast<const Eight *>(left + (int64_t)a.left_shared(q) * a.left_stride);
+                to.right[i] = *reinterpret_cast<const Eight *>(right + (int64_t)a.right_shared(q) * a.right_stride);
+            }
+        };
+        // (what does not exist becomes zero on both sides: a number beside it could be an infinity)
+        const auto put = [&](const Numbers &from, int s) {
+            unsigned char *to = lds + (s & 1) * F::STEP;
+#pragma unroll
+            for (int i = 0; i < F::N; ++i) {
+                const int k = i * 16 + k0, place = k * 256 + (((c >> 4) ^ (2 * (k & 3))) * 32) + (c & 8) * 2;
+                const bool row = s * KS + k < p.t.rows;
+                *reinterpret_cast<Eight *>(to + place) = row && in_left ? from.left[i] : Eight{};
+                *reinterpret_cast<Eight *>(to + KS * 256 + place) = row && in_right ? from.right[i] : Eight{};
+            }
+        };
+        typedef Vec<CT, 8> Unit;
+        struct Pair { Unit a[T::MC], b[T::MR]; } u, v;
+        const int row = lane >> 2 & 3, piece = lane & 3, odd = lane >> 4 & 1, k8 = 8 * (lane >> 5);
+        const auto read = [&](Pair &to, int s, int pair) {
+            const unsigned char *from = lds + (s & 1) * F::STEP;
+            const int k = pair * 16 + k8;
+            const auto unit = [&](const unsigned char *part, int first) {
+                const Four lo = turned_four(part, k, first / 16 + odd, row, piece), hi = turned_four(part, k + 4, first / 16 + odd, row, piece);
+                return __builtin_bit_cast(Unit, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+#pragma unroll
+            for (int i = 0; i < T::MC; ++i) to.a[i] = unit(from + KS * 256, wc + 32 * i);
+#pragma unroll
+            for (int j = 0; j < T::MR; ++j) to.b[j] = unit(from, wr + 32 * j);
+        };
+        const auto multiply = [&](const Pair &from) {
+#pragma unroll
+            for (int i = 0; i < T::MC; ++i)
+#pragma unroll
+                for (int j = 0; j < T::MR; ++j) acc[i][j] = mfma_unit<CT>(from.a[i], from.b[j], acc[i][j]);
+        };
+        // step s, whose first pair has been read; `next` holds the numbers of step s + 1
+        const auto step = [&](int s, Numbers &next) {
+            read(v, s, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(u);
+            read(u, s, 2);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(v);
+            read(v, s, 3);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(u);
+            if (s + 1 < steps) {
+                put(next, s + 1);
+                if (s + 3 < steps) fetch(next, s + 3);
+                __syncthreads();
+                read(u, s + 1, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            multiply(v);
+        };
+        fetch(x, 0);
+        if (steps > 1) fetch(y, 1);
+        put(x, 0);
+        if (steps > 2) fetch(x, 2);
+        __syncthreads();
+        read(u, 0, 0);
+        for (int s = 0; s < steps; s += 2) {
+            step(s, y);
+            if (s + 1 < steps) step(s + 1, x);
+        }
+        __syncthreads();
+    }
+    outer_put<T>(a, o, p, acc, lds);
+}
+
+// The chunks of groups of several, added up in their order.  blockIdx.y: the group
+__global__ __launch_bounds__(256) void k_outer_join(OuterCall call, const int32_t *err) {
+    if (*(volatile const int32_t *)err) return;
+    const OuterArgs &a = call.a[blockIdx.z];
+    const OuterTiles &o = call.o[blockIdx.z];
+    const int64_t size = (int64_t)a.rows * a.cols;
+    for (int group = blockIdx.y; group < a.g.groups; group += gridDim.y) {
+        const int start = a.g.start(group), end = a.g.start(group + 1);
+        if (end - start <= o.chunk) continue;
+        for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
+            const int left = size - i < 4 ? (int)(size - i) : 4;
+            Vec<float, 4> v = {};
+#pragma unroll 4
+            for (int first = start; first < end; first += o.chunk) v = v + load_some<float, 4>(outer_slot(a, o, group, start, first) + i, left);
+            put_typed<4>(a.out, a.out_type, group * size + i, v, left);
+        }
+    }
+}
+
+// What a call's sums are worked out by.
+enum { OUTER_LOW, OUTER_64, OUTER_128, OUTER_TURNED };
+int outer_kind(const dpaps_ps *ps, const OuterArgs *a, int count) {
+    if (a->rows <= 64) return OUTER_LOW;
+    const auto fits = [&](const void *p, int64_t stride, int32_t cols) { return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && cols % 8 == 0; };
+    if (count == 1 && a->left_type != PS_F32 && a->right_type != PS_F32 && !a->left_by_place && fits(a->left, a->left_stride, a->rows) && fits(a->right, a->right_stride, a->cols))
+        return OUTER_TURNED;
+    return ceil_div64(a->rows, 128) * ceil_div64(a->cols, 128) * a->g.groups < ps->num_cu ? OUTER_64 : OUTER_128;
+}
+// The tiles of a sum, and how many of a group's rows a workgroup takes.
+template <class T> OuterTiles outer_tiles(const dpaps_ps *ps, const OuterArgs &a, int64_t want) {
+    OuterTiles o{};
+    o.rows = (a.rows + T::ROWS - 1) / T::ROWS;
+    o.cols = (a.cols + T::COLS - 1) / T::COLS;
+    o.chunk = 2048;
+    while (o.chunk > 256 && (int64_t)o.rows * o.cols * ceil_div64(a.g.n, o.chunk) < want * ps->num_cu) o.chunk /= 2;
+    o.slots = a.g.n / o.chunk + 1;
+    return o;
+}
+OuterTiles outer_plan(const dpaps_ps *ps, const OuterArgs &a, int kind) {
+    return kind == OUTER_LOW ? outer_tiles<Low>(ps, a, 2) : kind == OUTER_64 ? outer_tiles<Tile64>(ps, a, 2) : outer_tiles<Tile128>(ps, a, 2);
+}
+size_t outer_part(const OuterArgs &a, const OuterTiles &o) {
+    if (a.g.n <= o.chunk) return 0;
+    return ((size_t)o.slots * (a.out_type == PS_F32 ? 1 : 2) * (size_t)a.rows * (size_t)a.cols * sizeof(float) + 255) / 256 * 256;
+}
+template <class T> int64_t outer_grid(const OuterCall &c, int count) {
+    int64_t most = 0;
+    for (int i = 0; i < count; ++i) most = std::max(most, row_tiles(c.a[i].g.n, c.a[i].g.groups, c.o[i].chunk) * c.o[i].rows * c.o[i].cols);
+    return most;
+}
+template <class CT, class LT, class RT, class T> int outer_of(dpaps_ps *ps, const OuterCall &c, int count, hipStream_t st) {
+    const int64_t grid = outer_grid<T>(c, count);
+    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "expert_grad");
+    static LdsAllowed allowed;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer<CT, LT, RT, T>), T::LDS + 2048 * sizeof(int));
+    if (rc) return rc;
+    k_outer<CT, LT, RT, T><<<dim3((unsigned)grid, (unsigned)count), T::THREADS, T::LDS + std::max(c.o[0].chunk, c.o[1].chunk) * sizeof(int), st>>>(c, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+template <class CT> int outer_turned(dpaps_ps *ps, const OuterCall &c, hipStream_t st) {
+    const int64_t grid = outer_grid<Tile128>(c, 1);
+    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "expert_grad");
+    constexpr int LDS = Turned<Tile128>::LDS;
+    static LdsAllowed allowed;
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer_turned<CT, Tile128>), LDS + 2048 * sizeof(int));
+    if (rc) return rc;
+    k_outer_turned<CT, Tile128><<<(unsigned)grid, 256, LDS + c.o[0].chunk * sizeof(int), st>>>(c, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}
+template <class CT, class LT, class RT> int outer_any(dpaps_ps *ps, const OuterCall &c, int count, int kind, hipStream_t st) {
+    if (kind == OUTER_LOW) return outer_of<CT, LT, RT, Low>(ps, c, count, st);
+    return kind == OUTER_64 ? outer_of<CT, LT, RT, Tile64>(ps, c, count, st) : outer_of<CT, LT, RT, Tile128>(ps, c, count, st);
+}
+
+}  // namespace
+
+int dpaps_too_large(dpaps_ps *ps, const char *what) {
+    ps->last_error = std::string(what) + ": too large for one launch";
+    return PS_ELIMIT;
+}
+
+size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs *a, int count) {
+    const int kind = outer_kind(ps, a, count);
+    size_t bytes = 0;
+    for (int i = 0; i < count; ++i) bytes += outer_part(a[i], outer_plan(ps, a[i], kind));
+    return bytes;
+}
+int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs *a, int count, float *part, hipStream_t st) {
+    const int kind = outer_kind(ps, a, count);
+    char *at = (char *)part;
+    OuterCall c{};
+    bool join = false;
+    int64_t most = 0;
+    for (int i = 0; i < count; ++i) {
+        c.a[i] = a[i];
+        c.o[i] = outer_plan(ps, a[i], kind);
+        c.o[i].part = (float *)at;
+        at += outer_part(a[i], c.o[i]);
+        join |= a[i].g.n > c.o[i].chunk;
+        most = std::max(most, ceil_div64((int64_t)a[i].rows * a[i].cols, 1024));
+    }
+    int rc;
+    if (kind == OUTER_TURNED) rc = a->left_type == PS_BF16 ? outer_turned<bf16_t>(ps, c, st) : outer_turned<f16_t>(ps, c, st);
+    else if (a->left_type == PS_F32) {
+        if (a->right_type == PS_F32) rc = outer_any<float, float, float>(ps, c, count, kind, st);
+        else rc = a->right_type == PS_BF16 ? outer_any<float, float, bf16_t>(ps, c, count, kind, st) : outer_any<float, float, f16_t>(ps, c, count, kind, st);
+    } else rc = a->left_type == PS_BF16 ? outer_any<bf16_t, bf16_t, bf16_t>(ps, c, count, kind, st) : outer_any<f16_t, f16_t, f16_t>(ps, c, count, kind, st);
+    if (rc || !join) return rc;
+    k_outer_join<<<dim3((unsigned)std::min<int64_t>(most, 256), (unsigned)std::min(a->g.groups, 1024), (unsigned)count), 256, 0, st>>>(c, ps->err);
+    PS_HIP(ps, hipGetLastError());
+    return PS_OK;
+}

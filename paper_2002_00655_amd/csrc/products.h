@@ -382,3 +382,22 @@ __device__ __forceinline__ void put_tile_typed(const floatx16 (&acc)[T::MC][T::M
     else if (type == PS_BF16) put_tile<bf16_t, T>(acc, sums, reinterpret_cast<bf16_t *>(out), c0, N, scale, to_of);
     else put_tile<f16_t, T>(acc, sums, reinterpret_cast<f16_t *>(out), c0, N, scale, to_of);
 }
+
+// until at most N of this wavefront's loads are on their way and all it has asked of LDS is there, then until all wavefronts are so far
+template <int N> __device__ __forceinline__ void wait_and_meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+// The order of a turn's instructions: reads of LDS and loads spread over the products.
+template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinline__ void spread() {
+    constexpr int R = (I + 1) * READS / PRODUCTS - I * READS / PRODUCTS, L = (I + 1) * LOADS / PRODUCTS - I * LOADS / PRODUCTS;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (R > 0) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+    if constexpr (L > 0) __builtin_amdgcn_sched_group_barrier(0x020, L, 0);
+    if constexpr (I + 1 < PRODUCTS) spread<PRODUCTS, READS, LOADS, I + 1>();
+}
+
+// What stands in LDS where rows or numbers end comes from here.
+namespace { __device__ __attribute__((aligned(64))) unsigned char zero_bytes[64]; }
