@@ -141,34 +141,31 @@ int product(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
 
 // low_p = s M_a x_p of the rows at the places of the order, in 32 bits, or, where the second product takes laid matrices, in the rows' type
 struct LowNumbers { float *numbers; int64_t stride; void *rounded; int64_t rounded_stride; int32_t *group_of; };
-int low_numbers(dpaps_ps *ps, const RowGroups &g, const void *x, int32_t type, int64_t stride, int32_t K, const float *m, int32_t rank, float scale, bool precise, const LowNumbers &low,
-                hipStream_t st) {
+ExpertArgs low_numbers(const dpaps_ps *ps, const RowGroups &g, const void *x, int32_t type, int64_t stride, int32_t K, const float *m, int32_t rank, float scale, bool precise,
+                       const LowNumbers &low, int32_t columns) {
     ExpertArgs a{};
-    a.g = g; a.x = x; a.x_stride = stride; a.x_type = type; a.w = m; a.L = ps->L; a.each = rank; a.K = K; a.N = rank; a.scale = scale; a.by_place = 1; a.precise = precise;
+    a.g = g; a.x = x; a.x_stride = stride; a.x_type = type; a.w = m; a.L = ps->L; a.each = rank; a.K = K; a.N = columns; a.scale = scale; a.by_place = 1; a.precise = precise;
     a.group_of = low.group_of;
-    if (low.rounded) {
-        a.zero_from = rank;
-        a.N = (int32_t)low.rounded_stride;
-    }
+    a.zero_from = columns > rank ? rank : 0;
     if (low.numbers) {
         a.out = low.numbers; a.out_stride = low.stride; a.out_type = PS_F32;
         a.also = low.rounded; a.also_stride = low.rounded_stride; a.also_type = type;
     } else { a.out = low.rounded; a.out_stride = low.rounded_stride; a.out_type = type; }
-    return dpaps_expert_product(ps, a, st);
+    return a;
 }
 
-// Scratch of a call, and the product with it.  Many rows of 16 bits: the shared matrix and the adapters' second ones are laid (laid.hip).
-constexpr int64_t LAID_ROWS = 1024;
+// Scratch of a call, and the product with it.  Many rows of 16 bits, tiles of 128 x 128 for three rounds of the compute units: the shared matrix and the adapters' second
+// ones are laid (laid.hip).
 struct Scratch {
     bool laid = false;
     int64_t stride = 0, rounded_stride = 0, w_size = 0, b_size = 0;
     size_t numbers[2] = {}, rounded = 0, group_of = 0, w = 0, b = 0, end = 0;
 };
 // both: the numbers in 32 bits of two products, which gradients need
-Scratch scratch_of(const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
+Scratch scratch_of(const dpaps_ps *ps, const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
     Scratch s;
     const int64_t n = g.n;
-    s.laid = !precise && n >= LAID_ROWS && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
+    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 3 * ps->num_cu && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
     s.rounded_stride = (rank + 7) / 8 * 8;
     s.stride = s.rounded_stride;
     const auto take = [&](int64_t bytes) { const size_t at = s.end; s.end += ((size_t)bytes + 255) / 256 * 256; return at; };
@@ -235,11 +232,12 @@ extern "C" int adapter_matmul(ps_handle ps, int32_t worker, int64_t first_key, i
     if (!x || !out || x_stride < 0 || out_stride < rows) return PS_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     const bool precise = x_type == PS_F32 || out_type == PS_F32;
-    const Scratch s = scratch_of(g, x, x_stride, dim, rows, rank, precise, false);
+    const Scratch s = scratch_of(ps, g, x, x_stride, dim, rows, rank, precise, false);
     rc = dpaps_ws_reserve(ps, s.end);
     if (rc) return rc;
     const LowNumbers low = low_of((char *)ps->ws, s, false, true, 0);
-    rc = low_numbers(ps, g, x, x_type, x_stride, dim, ps->val + first_a * ps->L, rank, scale, precise, low, st);
+    const ExpertArgs down = low_numbers(ps, g, x, x_type, x_stride, dim, ps->val + first_a * ps->L, rank, scale, precise, low, (int32_t)(s.laid ? s.rounded_stride : rank));
+    rc = dpaps_expert_product(ps, &down, 1, st);
     if (rc) return rc;
     AdapterArgs a{};
     a.g = g; a.x = x; a.x_stride = x_stride; a.x_type = x_type; a.w = ps->val + first_key * ps->L; a.L = ps->L; a.K = dim; a.N = rows;
@@ -260,7 +258,7 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
     if (!is_element_type(type) || !is_element_type(dx_type) || !da || !db) return PS_EINVAL;
     if (n > 0 && (!x || !dout || x_stride < 0 || dout_stride < 0 || (dx && dx_stride < dim))) return PS_EINVAL;
     hipStream_t st = (hipStream_t)stream;
-    const Scratch s = scratch_of(g, dout, dout_stride, rows, dim, rank, type == PS_F32 || dx_type == PS_F32, true);
+    const Scratch s = scratch_of(ps, g, dout, dout_stride, rows, dim, rank, type == PS_F32 || dx_type == PS_F32, true);
     OuterArgs o[2]{};
     for (int i = 0; i < 2; ++i) {
         o[i].g = g; o[i].left_stride = s.stride; o[i].left_type = PS_F32; o[i].left_by_place = 1; o[i].rows = rank; o[i].out_type = PS_F32; o[i].right_type = type;
@@ -273,8 +271,10 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
     const LowNumbers h = low_of(ws, s, true, false, 0), t = low_of(ws, s, true, dx != nullptr, 1);
     const float *pa = ps->val + first_a * ps->L, *pb = ps->val + first_b * ps->L;
     if (n > 0) {
-        rc = low_numbers(ps, g, x, type, x_stride, dim, pa, rank, scale, true, h, st);
-        if (!rc) rc = low_numbers(ps, g, dout, type, dout_stride, rows, pb, rank, scale, true, t, st);
+        const int32_t columns = (int32_t)(s.laid && dx ? s.rounded_stride : rank);
+        const ExpertArgs both[2] = {low_numbers(ps, g, x, type, x_stride, dim, pa, rank, scale, true, h, columns),
+                                    low_numbers(ps, g, dout, type, dout_stride, rows, pb, rank, scale, true, t, columns)};
+        rc = dpaps_expert_product(ps, both, 2, st);
         if (rc) return rc;
         if (dx) {
             AdapterArgs a{};

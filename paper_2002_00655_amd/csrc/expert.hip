@@ -9,8 +9,11 @@
 
 namespace {
 
+struct ExpertCall { ExpertArgs a[2]; };
+
 template <class CT, class XT, bool TURNED, class T>
-__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertArgs a, int32_t tiles, int32_t col_tiles, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertCall call, int32_t tiles, int32_t col_tiles, int32_t *err) {
+    const ExpertArgs &a = call.a[blockIdx.y];
     constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
     extern __shared__ __align__(16) char shared[];
     Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
@@ -65,7 +68,8 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertArgs a, 
 
 // Groups of few rows.
 template <class CT, class XT, bool TURNED, int MT>
-__global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expert_few(ExpertArgs a, int32_t col_tiles, int32_t *err) {
+__global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expert_few(ExpertCall call, int32_t col_tiles, int32_t *err) {
+    const ExpertArgs &a = call.a[blockIdx.y];
     typedef FewRows<CT, XT, TURNED, MT> F;
     __shared__ float sums[F::SUMS];
     __shared__ int at[16 * MT];
@@ -114,47 +118,53 @@ __global__ __launch_bounds__(256) void k_pair_sums(const float *in, int64_t n, i
 }  // namespace
 
 namespace {
-template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
+template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
+    const ExpertArgs &a = c.a[0];
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
     const int64_t tiles = row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_expert<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
-    k_expert<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, (int32_t)tiles, col_tiles, ps->err);
+    k_expert<CT, XT, TURNED, T><<<dim3((unsigned)grid, (unsigned)count), T::THREADS, T::LDS, st>>>(c, (int32_t)tiles, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
-template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
+template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
+    const ExpertArgs &a = c.a[0];
     typedef FewRows<CT, XT, TURNED, MT> F;
     const int32_t col_tiles = (a.N + F::COLS - 1) / F::COLS;
     const int64_t grid = row_tiles(a.g.n, a.g.groups, 16 * MT) * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
-    k_expert_few<CT, XT, TURNED, MT><<<(unsigned)grid, F::THREADS, 0, st>>>(a, col_tiles, ps->err);
+    k_expert_few<CT, XT, TURNED, MT><<<dim3((unsigned)grid, (unsigned)count), F::THREADS, 0, st>>>(c, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
-template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
-    const int64_t n = a.g.n, groups = a.g.groups;
-    if (n <= 8 * groups || n <= 16) return few_of<CT, XT, TURNED, 1>(ps, a, st);
-    if (n <= 24 * groups || n <= 64) return few_of<CT, XT, TURNED, 2>(ps, a, st);
-    if (a.N <= 32) return tiles_of<CT, XT, TURNED, Narrow>(ps, a, st);
-    if (ceil_div64(n, 128) * ceil_div64(a.N, 128) < 2 * ps->num_cu) return tiles_of<CT, XT, TURNED, Tile64>(ps, a, st);
-    return tiles_of<CT, XT, TURNED, Tile128>(ps, a, st);
+template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
+    const ExpertArgs &a = c.a[0];
+    const int64_t n = a.g.n, groups = a.g.groups, cus = ps->num_cu;
+    // few rows: as long as tiles of 16 rows (a group's last one is half full) make no more workgroups than so many a compute unit
+    const int64_t few = ceil_div64(n + 8 * (groups < n ? groups : n), 16) * ceil_div64(a.N, TURNED ? 64 : 16) * count;
+    if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * cus) return few_of<CT, XT, TURNED, 1>(ps, c, count, st);
+    if (a.N <= 32) return tiles_of<CT, XT, TURNED, Narrow>(ps, c, count, st);
+    if (sizeof(CT) == 4 || ceil_div64(n, 128) * ceil_div64(a.N, 128) < cus) return tiles_of<CT, XT, TURNED, Tile64>(ps, c, count, st);
+    return tiles_of<CT, XT, TURNED, Tile128>(ps, c, count, st);
 }
-template <class CT, class XT> int product_either(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
-    return a.turned ? product_of<CT, XT, true>(ps, a, st) : product_of<CT, XT, false>(ps, a, st);
+template <class CT, class XT> int product_either(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
+    return c.a[0].turned ? product_of<CT, XT, true>(ps, c, count, st) : product_of<CT, XT, false>(ps, c, count, st);
 }
 }  // namespace
 
-int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st) {
-    if (a.x_type == PS_F32) return product_either<float, float>(ps, a, st);
-    if (a.x_type == PS_BF16) return a.precise ? product_either<float, bf16_t>(ps, a, st) : product_either<bf16_t, bf16_t>(ps, a, st);
-    return a.precise ? product_either<float, f16_t>(ps, a, st) : product_either<f16_t, f16_t>(ps, a, st);
+int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs *a, int count, hipStream_t st) {
+    ExpertCall c{};
+    for (int i = 0; i < count; ++i) c.a[i] = a[i];
+    if (a->x_type == PS_F32) return product_either<float, float>(ps, c, count, st);
+    if (a->x_type == PS_BF16) return a->precise ? product_either<float, bf16_t>(ps, c, count, st) : product_either<bf16_t, bf16_t>(ps, c, count, st);
+    return a->precise ? product_either<float, f16_t>(ps, c, count, st) : product_either<f16_t, f16_t>(ps, c, count, st);
 }
 
-// From so many rows a group on, matrices are laid before the product (laid.hip).
-constexpr int64_t LAID_ROWS = 512;
+// From so many rows a group on, and tiles of 256 x 256 for two rounds of the compute units, matrices are laid before the product (laid.hip).
+constexpr int64_t LAID_ROWS = 1024;
 
 extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed,
                              const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int32_t x_type, int64_t x_stride, int32_t x_pairs, void *out,
@@ -176,7 +186,7 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     a.scale = 1.0f; a.precise = x_type == PS_F32 || out_type == PS_F32;
     a.out = out; a.out_stride = out_stride; a.out_type = out_type;
     const size_t sums = out_pairs > 1 ? ((size_t)n * N * sizeof(float) + 255) / 256 * 256 : 0;
-    const bool lay = !a.precise && n >= LAID_ROWS * num_experts && num_experts < 32768 && dpaps_laid_fits(x, x_stride, K);
+    const bool lay = !a.precise && n >= LAID_ROWS * num_experts && ceil_div64(n, 256) * ceil_div64(N, 256) >= 2 * ps->num_cu && num_experts < 32768 && dpaps_laid_fits(x, x_stride, K);
     const int64_t laid = lay ? dpaps_laid_size(K, N) : 0;
     rc = dpaps_ws_reserve(ps, sums + (size_t)laid * num_experts * 2);
     if (rc) return rc;
@@ -190,7 +200,7 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
         p.g = g; p.x = x; p.x_stride = x_stride; p.x_shared = a.x_shared; p.K = K; p.N = N; p.w = l.to; p.w_size = laid;
         p.out = a.out; p.out_stride = a.out_stride; p.out_type = a.out_type;
         rc = dpaps_laid_product(ps, x_type, p, st);
-    } else rc = dpaps_expert_product(ps, a, st);
+    } else rc = dpaps_expert_product(ps, &a, 1, st);
     if (rc) return rc;
     if (out_pairs > 1) {
         const uint32_t P = (uint32_t)((N + 3) / 4);

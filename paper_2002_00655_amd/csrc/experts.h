@@ -16,7 +16,8 @@ struct ExpertArgs {
     void *also; int64_t also_stride; int32_t also_type;                      // not NULL: the result once more, in another type
     int32_t zero_from;                                                       // the columns from here on, up to N, are written as zeros; 0: none
 };
-int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs &a, hipStream_t st);
+// count: one, or two of the same groups, columns and types in one launch
+int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs *a, int count, hipStream_t st);
 
 // out_e[i][j] = sum over group e's rows of left[i] right[j]
 struct OuterArgs {

@@ -57,14 +57,13 @@ template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(Lay
 }
 
 template <class CT, class T> struct LaidForm {
-    static constexpr int STAGE = (T::ROWS + T::COLS) * KB * 2, LDS = STAGES * STAGE, ROW_LOADS = T::ROWS / 16 / 4, COL_LOADS = T::COLS / 16 / 4, LOADS = ROW_LOADS + COL_LOADS;
-    static_assert(T::THREADS == 256);
+    static constexpr int STAGE = (T::ROWS + T::COLS) * KB * 2, LDS = STAGES * STAGE, WAVES = T::WC * T::WR, ROW_LOADS = T::ROWS / 16 / WAVES, COL_LOADS = T::COLS / 16 / WAVES, LOADS = ROW_LOADS + COL_LOADS;
 };
 
 template <class CT, class T, bool LOW>
-__global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t row_tiles, int32_t col_tiles, int32_t kb_all, int32_t b_kb, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_laid(LaidArgs a, int32_t row_tiles, int32_t col_tiles, int32_t kb_all, int32_t b_kb, int32_t *err) {
     typedef LaidForm<CT, T> F;
-    constexpr int BR = T::ROWS, BC = T::COLS, H = F::LOADS / 2;
+    constexpr int BR = T::ROWS, BC = T::COLS;
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ int at[BR];
     __shared__ int off;
@@ -76,7 +75,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_laid(LaidArgs a, int32_t row
     if constexpr (LOW) t = RowTile{0, tile * BR, a.g.n - tile * BR < BR ? a.g.n - tile * BR : BR, 0, 0};
     else t = row_tile(a.g, tile, BR);
     if (t.rows == 0) return;
-    for (int r = tid; r < BR; r += 256) at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
+    for (int r = tid; r < BR; r += T::THREADS) at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
     __syncthreads();
     if (off) return;
     floatx16 acc[T::MC][T::MR] = {};
@@ -191,7 +190,7 @@ template <class CT, class T, bool LOW> int start(dpaps_ps *ps, const LaidArgs &a
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_laid<CT, T, LOW>), F::LDS);
     if (rc) return rc;
-    k_laid<CT, T, LOW><<<(unsigned)grid, 256, F::LDS, st>>>(a, (int32_t)tiles, col_tiles, (int32_t)k_blocks(a.K), (int32_t)k_blocks(a.rank), ps->err);
+    k_laid<CT, T, LOW><<<(unsigned)grid, T::THREADS, F::LDS, st>>>(a, (int32_t)tiles, col_tiles, (int32_t)k_blocks(a.K), (int32_t)k_blocks(a.rank), ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }

@@ -307,7 +307,7 @@ template <int MC_, int MR_, int WC_, int WR_> struct Form {
 };
 typedef Form<1, 1, 2, 2> Tile64;
 typedef Form<2, 2, 2, 2> Tile128;
-typedef Form<4, 4, 2, 2> Tile256;
+typedef Form<2, 4, 4, 2> Tile256;
 typedef Form<1, 1, 1, 4> Narrow;                                     // 32 columns, 128 rows
 typedef Form<1, 1, 4, 1> Low;                                        // 128 columns, 32 rows
 
