@@ -28,19 +28,21 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a
     floatx16 acc[T::MC][T::MR] = {};
     const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR, cols = a.N - c0;
     {
-        KMajor<XT, CT, BR, T::THREADS> rows;
-        rows.init([&](int r) { return reinterpret_cast<const XT *>(a.x) + (int64_t)(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
-        std::conditional_t<TURNED, KeyRows<CT, BC, T::THREADS>, KeyColumns<CT, BC, T::THREADS>> columns;
-        if constexpr (TURNED) columns.init(a.w + c0, a.L);
-        else columns.init(a.w + c0 * a.L, a.L, cols);
+        KMajor<XT, CT, BR, T::THREADS> rows[T::SETS];
+        for (auto &r : rows) r.init([&](int r) { return reinterpret_cast<const XT *>(a.x) + (int64_t)(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
+        std::conditional_t<TURNED, KeyRows<CT, BC, T::THREADS>, KeyColumns<CT, BC, T::THREADS>> columns[T::SETS];
+        for (auto &c : columns) {
+            if constexpr (TURNED) c.init(a.w + c0, a.L);
+            else c.init(a.w + c0 * a.L, a.L, cols);
+        }
         tile_sum<CT, T>(a.K, lds, wc, wr,
-            [&](int s, auto tail) {
-                rows.template load<decltype(tail)::value>(s, a.K);
-                columns.template load<decltype(tail)::value>(s, a.K);
+            [&](auto set, int s, auto tail) {
+                rows[set].template load<decltype(tail)::value>(s, a.K);
+                columns[set].template load<decltype(tail)::value>(s, a.K);
             },
-            [&](Vec<CT, KU> *to) {
-                rows.put(to);
-                columns.put(to + BR * UNITS);
+            [&](auto set, Vec<CT, KU> *to) {
+                rows[set].put(to);
+                columns[set].put(to + BR * UNITS);
             }, acc);
     }
     // the adapters of the tile's rows, one after the other: the rows of others are zero
@@ -53,11 +55,11 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a
         KeyRows<CT, BC, T::THREADS> columns;
         columns.init(a.b + (int64_t)e * a.rank * a.L + c0, a.L);
         tile_sum_short<CT, T>(a.rank, lds, wc, wr,
-            [&](int s, auto tail) {
+            [&](auto set, int s, auto tail) {
                 rows.template load<decltype(tail)::value>(s, a.rank);
                 columns.template load<decltype(tail)::value>(s, a.rank);
             },
-            [&](Vec<CT, KU> *to) {
+            [&](auto set, Vec<CT, KU> *to) {
 #pragma unroll
                 for (int i = 0; i < rows.N; ++i) {
                     const int r = (i * T::THREADS + tid) / UNITS;
@@ -124,9 +126,9 @@ template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, cons
     return PS_OK;
 }
 template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
-    if (a.g.n <= 16) return few_of<CT, XT, TURNED, 1>(ps, a, st);
-    if (a.g.n <= 128) return few_of<CT, XT, TURNED, 2>(ps, a, st);
-    if (ceil_div64(a.g.n, 128) * ceil_div64(a.N, 128) < 2 * ps->num_cu) return tiles_of<CT, XT, TURNED, Tile64>(ps, a, st);
+    const int64_t few = ceil_div64(a.g.n, 16) * ceil_div64(a.N, TURNED ? 64 : 16);
+    if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * ps->num_cu) return few_of<CT, XT, TURNED, 1>(ps, a, st);      // (as products with experts)
+    if (sizeof(CT) == 4 || ceil_div64(a.g.n, 128) * ceil_div64(a.N, 128) < ps->num_cu) return tiles_of<CT, XT, TURNED, Tile64>(ps, a, st);
     return tiles_of<CT, XT, TURNED, Tile128>(ps, a, st);
 }
 template <class CT, class XT> int product_either(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
@@ -230,6 +232,7 @@ extern "C" int adapter_matmul(ps_handle ps, int32_t worker, int64_t first_key, i
     if (!is_element_type(x_type) || !is_element_type(out_type)) return PS_EINVAL;
     if (n == 0) return PS_OK;
     if (!x || !out || x_stride < 0 || out_stride < rows) return PS_EINVAL;
+    if (!dpaps_strides_fit(ps, x_stride, out_stride)) return PS_ELIMIT;
     hipStream_t st = (hipStream_t)stream;
     const bool precise = x_type == PS_F32 || out_type == PS_F32;
     const Scratch s = scratch_of(ps, g, x, x_stride, dim, rows, rank, precise, false);
@@ -257,6 +260,7 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
     if (rc) return rc;
     if (!is_element_type(type) || !is_element_type(dx_type) || !da || !db) return PS_EINVAL;
     if (n > 0 && (!x || !dout || x_stride < 0 || dout_stride < 0 || (dx && dx_stride < dim))) return PS_EINVAL;
+    if (n > 0 && (!dpaps_strides_fit(ps, x_stride, dout_stride) || !dpaps_strides_fit(ps, dx ? dx_stride : 0, 0))) return PS_ELIMIT;
     hipStream_t st = (hipStream_t)stream;
     const Scratch s = scratch_of(ps, g, dout, dout_stride, rows, dim, rank, type == PS_F32 || dx_type == PS_F32, true);
     OuterArgs o[2]{};

@@ -34,19 +34,21 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertCall cal
     const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR, cols = a.N - c0;
     if (t.group < a.g.groups) {
         const float *w = a.w + (int64_t)t.group * a.each * a.L;
-        KMajor<XT, CT, BR, T::THREADS> rows;
-        rows.init([&](int r) { return reinterpret_cast<const XT *>(a.x) + a.x_shared(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
-        std::conditional_t<TURNED, KeyRows<CT, BC, T::THREADS>, KeyColumns<CT, BC, T::THREADS>> columns;
-        if constexpr (TURNED) columns.init(w + c0, a.L);
-        else columns.init(w + c0 * a.L, a.L, cols);
+        KMajor<XT, CT, BR, T::THREADS> rows[T::SETS];
+        for (auto &r : rows) r.init([&](int r) { return reinterpret_cast<const XT *>(a.x) + a.x_shared(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
+        std::conditional_t<TURNED, KeyRows<CT, BC, T::THREADS>, KeyColumns<CT, BC, T::THREADS>> columns[T::SETS];
+        for (auto &c : columns) {
+            if constexpr (TURNED) c.init(w + c0, a.L);
+            else c.init(w + c0 * a.L, a.L, cols);
+        }
         tile_sum<CT, T>(a.K, lds, wc, wr,
-            [&](int s, auto tail) {
-                rows.template load<decltype(tail)::value>(s, a.K);
-                columns.template load<decltype(tail)::value>(s, a.K);
+            [&](auto set, int s, auto tail) {
+                rows[set].template load<decltype(tail)::value>(s, a.K);
+                columns[set].template load<decltype(tail)::value>(s, a.K);
             },
-            [&](Vec<CT, KU> *to) {
-                rows.put(to);
-                columns.put(to + BR * UNITS);
+            [&](auto set, Vec<CT, KU> *to) {
+                rows[set].put(to);
+                columns[set].put(to + BR * UNITS);
             }, acc);
     }
     if (a.zero_from) {
@@ -146,7 +148,7 @@ template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const Ex
     // few rows: as long as tiles of 16 rows (a group's last one is half full) make no more workgroups than so many a compute unit
     const int64_t few = ceil_div64(n + 8 * (groups < n ? groups : n), 16) * ceil_div64(a.N, TURNED ? 64 : 16) * count;
     if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * cus) return few_of<CT, XT, TURNED, 1>(ps, c, count, st);
-    if (a.N <= 32) return tiles_of<CT, XT, TURNED, Narrow>(ps, c, count, st);
+    if (a.N <= 32) return sizeof(CT) != sizeof(XT) ? few_of<CT, XT, TURNED, 2>(ps, c, count, st) : tiles_of<CT, XT, TURNED, Narrow>(ps, c, count, st);
     if (sizeof(CT) == 4 || ceil_div64(n, 128) * ceil_div64(a.N, 128) < cus) return tiles_of<CT, XT, TURNED, Tile64>(ps, c, count, st);
     return tiles_of<CT, XT, TURNED, Tile128>(ps, c, count, st);
 }
@@ -179,6 +181,7 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     if (n == 0) return PS_OK;
     const int32_t K = transposed ? rows : dim, N = transposed ? dim : rows;
     if (x_pairs < 1 || out_pairs < 1 || n % x_pairs || n % out_pairs || !x || !out || x_stride < 0 || out_stride < N) return PS_EINVAL;
+    if (!dpaps_strides_fit(ps, x_stride, out_stride)) return PS_ELIMIT;
     hipStream_t st = (hipStream_t)stream;
     ExpertArgs a{};
     a.g = g; a.x = x; a.x_stride = x_stride; a.x_type = x_type; a.x_shared = Quotient(x_pairs);
@@ -222,6 +225,8 @@ extern "C" int expert_grad(ps_handle ps, int32_t num_experts, int32_t rows, int3
     int rc = dpaps_row_groups(ps, order, offsets, num_experts, n, &g);
     if (rc) return rc;
     if (left_pairs < 1 || right_pairs < 1 || n % left_pairs || n % right_pairs || (n > 0 && (!left || !right || left_stride < 0 || right_stride < 0))) return PS_EINVAL;
+    if (rows > PS_EMB_MAX_DIM || dim > PS_EMB_MAX_DIM) { ps->last_error = "expert_grad: sides of at most 65536"; return PS_ELIMIT; }
+    if (n > 0 && !dpaps_strides_fit(ps, left_stride, right_stride)) return PS_ELIMIT;
     OuterArgs a{};
     a.g = g; a.left = left; a.left_stride = left_stride; a.left_type = type; a.left_shared = Quotient(left_pairs);
     a.right = right; a.right_stride = right_stride; a.right_type = type; a.right_shared = Quotient(right_pairs);

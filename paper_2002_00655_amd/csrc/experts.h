@@ -81,7 +81,7 @@ int dpaps_laid_product(dpaps_ps *ps, int32_t type, const LaidArgs &a, hipStream_
 //   turned:      64 columns; lane l has the four columns from 4 (l % 16) on, for the numbers of unit l / 16: operand j is column 4 i + j of lane i
 // out[row][column] of wavefront w in sums, [w][16 MT][columns].
 template <class CT, class XT, bool TURNED, int MT> struct FewRows {
-    static constexpr int KU = unit_of<CT>(), COLS = TURNED ? 64 : 16, OPS = TURNED ? 4 : 1, WAVES = TURNED && MT == 4 ? 4 : 8, THREADS = 64 * WAVES, STEP = 4 * KU;
+    static constexpr int KU = unit_of<XT>(), COLS = TURNED ? 64 : 16, OPS = TURNED ? 4 : 1, WAVES = TURNED && MT == 4 ? 4 : 8, THREADS = 64 * WAVES, STEP = 4 * KU;
     static constexpr int AHEAD = TURNED ? (KU == 8 ? 2 : 4) : (KU == 8 ? 4 : 8);
     static constexpr int SUMS = WAVES * 16 * MT * COLS;
     floatx4 acc[OPS][MT];
@@ -123,13 +123,13 @@ template <class CT, class XT, bool TURNED, int MT> struct FewRows {
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
                         for (int i = 0; i < KU; ++i) wv[u][j][i] = rows[i][j];
-                } else if constexpr (KU == 4) {
+                } else if constexpr (sizeof(CT) == 4) {
                     wv[u][0] = Vec<float, KU>{};
                     if (left > 0) wv[u][0] = load_some<float, KU>(mine + k, left);
                 } else wv[u][0] = halves<float>(mine, (s + u) * STEP + 4 * g, s + u < s1 ? K : 0);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    if constexpr (TURNED || KU == 4) {
+                    if constexpr (TURNED || sizeof(CT) == 4) {
                         xv[u][m] = Vec<XT, KU>{};
                         if (left > 0) xv[u][m] = load_some<XT, KU>(x[m] + k, left);
                     } else xv[u][m] = halves<XT>(x[m], (s + u) * STEP + 4 * g, s + u < s1 ? K : 0);
@@ -140,7 +140,7 @@ template <class CT, class XT, bool TURNED, int MT> struct FewRows {
 #pragma unroll
                 for (int j = 0; j < OPS; ++j)
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[j][m] = mfma_small<CT>(as_type<CT, float, KU>(wv[u][j]), as_type<CT, XT, KU>(xv[u][m]), acc[j][m]);
+                    for (int m = 0; m < MT; ++m) acc[j][m] = mfma_small<CT, KU>(as_type<CT, float, KU>(wv[u][j]), as_type<CT, XT, KU>(xv[u][m]), acc[j][m]);
         }
     }
     __device__ __forceinline__ void put(float *sums) const {

@@ -221,6 +221,12 @@ int dpaps_row_groups(dpaps_ps *ps, const int32_t *order, const int32_t *offsets,
     return PS_OK;
 }
 
+bool dpaps_strides_fit(dpaps_ps *ps, int64_t a, int64_t b) {
+    if (a < ((int64_t)1 << 31) && b < ((int64_t)1 << 31)) return true;
+    ps->last_error = "rows at most 2^31 - 1 elements apart";
+    return false;
+}
+
 int dpaps_route_groups(dpaps_ps *ps, int32_t worker, const RowGroups &g, const GroupKeys &k, hipStream_t st) {
     if (worker < 0) return PS_OK;
     const int64_t n = k.shared + (int64_t)g.groups * k.each * (k.first_b >= 0 ? 2 : 1);

@@ -56,3 +56,4 @@ struct GroupKeys { int64_t first = 0, shared = 0, first_a = 0, first_b = -1; int
 int dpaps_route_groups(dpaps_ps *ps, int32_t worker, const RowGroups &g, const GroupKeys &k, hipStream_t st);
 // group_rows.hip: what all calls check of the groups that they are given
 int dpaps_row_groups(dpaps_ps *ps, const int32_t *order, const int32_t *offsets, int32_t groups, int64_t n, RowGroups *g);
+bool dpaps_strides_fit(dpaps_ps *ps, int64_t a, int64_t b);      // below 2^31

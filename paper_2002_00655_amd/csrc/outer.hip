@@ -59,6 +59,9 @@ template <class T> __device__ __forceinline__ void outer_put(const OuterArgs &a,
                       [&](int r) { return p.r0 + r < a.rows ? base + (int64_t)(p.r0 + r) * a.cols : (int64_t)-1; });
 }
 
+// (one multiplication: strides are below 2^31, and rows' numbers are not negative)
+template <class T> __device__ __forceinline__ const T *row_of(const T *base, int row, int64_t stride) { return base + (uint64_t)(uint32_t)row * (uint32_t)stride; }
+
 // Turned in registers.
 template <class CT, class LT, class RT, class T>
 __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_outer(OuterCall call, int32_t *err) {
@@ -72,20 +75,20 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_outer(OuterCall call,
     if (!outer_place<BR, BC>(a, o, at, err, p)) return;
     floatx16 acc[T::MC][T::MR] = {};
     const int wave = threadIdx.x >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
-    ChosenRows<LT, CT, BR, T::THREADS> left;
-    ChosenRows<RT, CT, BC, T::THREADS> right;
+    ChosenRows<LT, CT, BR, T::THREADS> left[T::SETS];
+    ChosenRows<RT, CT, BC, T::THREADS> right[T::SETS];
     tile_sum<CT, T>(p.t.rows, lds, wc, wr,
-        [&](int s, auto tail) {
-            left.template load<decltype(tail)::value>(s, p.t.rows, a.rows - p.r0, [&](int i) {
-                return reinterpret_cast<const LT *>(a.left) + (int64_t)(a.left_by_place ? p.t.first + i : a.left_shared(at[i])) * a.left_stride + p.r0;
+        [&](auto set, int s, auto tail) {
+            left[set].template load<decltype(tail)::value>(s, p.t.rows, a.rows - p.r0, [&](int i) {
+                return row_of(reinterpret_cast<const LT *>(a.left) + p.r0, a.left_by_place ? p.t.first + i : a.left_shared(at[i]), a.left_stride);
             });
-            right.template load<decltype(tail)::value>(s, p.t.rows, a.cols - p.c0, [&](int i) {
-                return reinterpret_cast<const RT *>(a.right) + (int64_t)a.right_shared(at[i]) * a.right_stride + p.c0;
+            right[set].template load<decltype(tail)::value>(s, p.t.rows, a.cols - p.c0, [&](int i) {
+                return row_of(reinterpret_cast<const RT *>(a.right) + p.c0, a.right_shared(at[i]), a.right_stride);
             });
         },
-        [&](Vec<CT, KU> *to) {
-            left.put(to);
-            right.put(to + BR * UNITS);
+        [&](auto set, Vec<CT, KU> *to) {
+            left[set].put(to);
+            right[set].put(to + BR * UNITS);
         }, acc);
     outer_put<T>(a, o, p, acc, lds);
 }
@@ -127,8 +130,8 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_outer_turned(OuterCall call,
 #pragma unroll
             for (int i = 0; i < F::N; ++i) {
                 const int k = s * KS + i * 16 + k0, q = at[k < p.t.rows ? k : 0];
-                to.left[i] = *reinterpret_cast<const Eight *>(left + (int64_t)a.left_shared(q) * a.left_stride);
-                to.right[i] = *reinterpret_cast<const Eight *>(right + (int64_t)a.right_shared(q) * a.right_stride);
+                to.left[i] = *reinterpret_cast<const Eight *>(row_of(left, a.left_shared(q), a.left_stride));
+                to.right[i] = *reinterpret_cast<const Eight *>(row_of(right, a.right_shared(q), a.right_stride));
             }
         };
         // (what does not exist becomes zero on both sides: a number beside it could be an infinity)
@@ -232,7 +235,7 @@ template <class T> OuterTiles outer_tiles(const dpaps_ps *ps, const OuterArgs &a
     o.rows = (a.rows + T::ROWS - 1) / T::ROWS;
     o.cols = (a.cols + T::COLS - 1) / T::COLS;
     o.chunk = 2048;
-    while (o.chunk > 256 && (int64_t)o.rows * o.cols * ceil_div64(a.g.n, o.chunk) < want * ps->num_cu) o.chunk /= 2;
+    while (o.chunk > (a.g.n <= 512 ? 512 : 256) && (int64_t)o.rows * o.cols * ceil_div64(a.g.n, o.chunk) < want * ps->num_cu) o.chunk /= 2;
     o.slots = a.g.n / o.chunk + 1;
     return o;
 }

@@ -25,21 +25,20 @@ template <class CT, class ST, int W> __device__ __forceinline__ Vec<CT, W> as_ty
     else return __builtin_convertvector(v, Vec<CT, W>);
 }
 
-// The W elements at p of which `left` exist, the others zero.
-template <class ST, int W> __device__ __forceinline__ Vec<ST, W> load_some(const ST *p, int left) {
-    if (left >= W) return *reinterpret_cast<const Loose<ST, W> *>(p);
-    Vec<ST, W> v = {};
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-        if (i < left) v[i] = p[i];
-    return v;
-}
-
 // Of a unit that starts at k, the numbers from K on become zero.
 template <class ST, int W> __device__ __forceinline__ Vec<ST, W> cut(Vec<ST, W> v, int left) {
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = i < left ? v[i] : (ST)0.0f;
     return v;
+}
+
+// The W elements at p of which `left` exist (one at least), the others zero.  (Without a branch for each: their loads are on their way together.)
+template <class ST, int W> __device__ __forceinline__ Vec<ST, W> load_some(const ST *p, int left) {
+    if (left >= W) return *reinterpret_cast<const Loose<ST, W> *>(p);
+    Vec<ST, W> v;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = p[i < left ? i : 0];
+    return cut<ST, W>(v, left);
 }
 
 // ROWS rows of a call's tensor, whose numbers follow each other in k; `row`s are where they start.  Rows that are not wanted may be any: they
@@ -198,10 +197,10 @@ template <class CT> __device__ __forceinline__ floatx16 mfma_unit(Vec<CT, unit_o
 
 // The instruction for 16 columns by 16 rows, as many units as there are lanes.
 typedef float floatx4 __attribute__((ext_vector_type(4)));
-template <class CT> __device__ __forceinline__ floatx4 mfma_small(Vec<CT, unit_of<CT>()> a, Vec<CT, unit_of<CT>()> b, floatx4 c) {
+template <class CT, int KU> __device__ __forceinline__ floatx4 mfma_small(Vec<CT, KU> a, Vec<CT, KU> b, floatx4 c) {
     if constexpr (sizeof(CT) == 4) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        for (int j = 0; j < KU; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
         return c;
     } else if constexpr (std::is_same<CT, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -225,27 +224,32 @@ template <class CT, class T> struct Operands {
     }
 };
 
-// A tile's sum over K.  load(step, tail): asks for a step's numbers; put(where): brings them into LDS, rows and then columns.  Lane l of the wavefront whose part starts
-// at column c0 and row r0 holds in acc[i][j][4 q + e] the column c0 + 32 i + 8 q + 4 (l / 32) + e of row r0 + 32 j + l % 32.
-// Two steps are in LDS and one is on its way to registers.  Every pair of units is read from LDS while the one before is multiplied, the first
+// A tile's sum over K.  load(set, step, tail): asks for a step's numbers, put(set, where): brings them into LDS, rows and then columns; a set is what a thread holds of a
+// step.  Lane l of the wavefront whose part starts at column c0 and row r0 holds in acc[i][j][4 q + e] the column c0 + 32 i + 8 q + 4 (l / 32) + e of row
+// r0 + 32 j + l % 32.
+// Two steps are in LDS, and T::SETS more are on their way to registers.  Every pair of units is read from LDS while the one before is multiplied, the first
 // pair of a step while the last of the step before is.
 template <class CT, class T, class Load, class Put>
 __device__ __forceinline__ void tile_sum(int K, Vec<CT, unit_of<CT>()> *lds, int c0, int r0, Load load, Put put, floatx16 (&acc)[T::MC][T::MR]) {
     constexpr int SIZE = (T::ROWS + T::COLS) * UNITS;
-    static_assert(UNITS == 8);
+    static_assert(UNITS == 8 && (T::SETS == 1 || T::SETS == 2));
+    typedef std::integral_constant<int, 0> First;
+    typedef std::integral_constant<int, T::SETS - 1> Second;
     const int full = K / step_of<CT>(), steps = (K + step_of<CT>() - 1) / step_of<CT>();
-    const auto fetch = [&](int s) {
-        if (s < full) load(s, std::false_type{});
-        else load(s, std::true_type{});
+    const auto fetch = [&](auto set, int s) {
+        if (s < full) load(set, s, std::false_type{});
+        else load(set, s, std::true_type{});
     };
     if (steps <= 0) return;
     Operands<CT, T> x, y;
-    fetch(0);
-    put(lds);
-    if (steps > 1) fetch(1);
+    fetch(First{}, 0);
+    if (T::SETS == 2 && steps > 1) fetch(Second{}, 1);
+    put(First{}, lds);
+    if (steps > T::SETS) fetch(First{}, T::SETS);
     __syncthreads();
     x.read(lds, c0, r0, 0);
-    for (int s = 0; s < steps; ++s) {
+    // step s; `set` holds the next one
+    const auto step = [&](int s, auto set) {
         const Vec<CT, unit_of<CT>()> *here = lds + (s & 1) * SIZE;
         Vec<CT, unit_of<CT>()> *next = lds + ((s + 1) & 1) * SIZE;
         y.read(here, c0, r0, 1);
@@ -258,13 +262,17 @@ __device__ __forceinline__ void tile_sum(int K, Vec<CT, unit_of<CT>()> *lds, int
         __builtin_amdgcn_sched_barrier(0);
         x.multiply(acc);
         if (s + 1 < steps) {
-            put(next);
-            if (s + 2 < steps) fetch(s + 2);
+            put(set, next);
+            if (s + 1 + T::SETS < steps) fetch(set, s + 1 + T::SETS);
             __syncthreads();
             x.read(next, c0, r0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
         y.multiply(acc);
+    };
+    for (int s = 0; s < steps; s += T::SETS) {
+        step(s, Second{});
+        if (T::SETS == 2 && s + 1 < steps) step(s + 1, First{});
     }
     __syncthreads();                                                 // (LDS is used again)
 }
@@ -273,9 +281,9 @@ template <class CT, class T, class Load, class Put>
 __device__ __forceinline__ void tile_sum_short(int K, Vec<CT, unit_of<CT>()> *lds, int c0, int r0, Load load, Put put, floatx16 (&acc)[T::MC][T::MR]) {
     for (int s = 0; s * step_of<CT>() < K; ++s) {
         const int left = K - s * step_of<CT>();
-        if (left >= step_of<CT>()) load(s, std::false_type{});
-        else load(s, std::true_type{});
-        put(lds);
+        if (left >= step_of<CT>()) load(std::integral_constant<int, 0>{}, s, std::false_type{});
+        else load(std::integral_constant<int, 0>{}, s, std::true_type{});
+        put(std::integral_constant<int, 0>{}, lds);
         __syncthreads();
         for (int p = 0; 2 * p * unit_of<CT>() < left && p < UNITS / 2; ++p) {
             Operands<CT, T> x;
@@ -304,6 +312,7 @@ template <int MC_, int MR_, int WC_, int WR_> struct Form {
     static constexpr int MC = MC_, MR = MR_, WC = WC_, WR = WR_, COLS = 32 * MC * WC, ROWS = 32 * MR * WR, THREADS = 64 * WC * WR;
     static constexpr int LDS = 2 * (ROWS + COLS) * UNITS * 16;              // two steps
     static constexpr int BLOCKS = MC * MR > 4 ? 1 : 2;                  // workgroups a compute unit has to have room for
+    static constexpr int SETS = MC * MR == 1 ? 2 : 1;                   // steps on their way to registers
 };
 typedef Form<1, 1, 2, 2> Tile64;
 typedef Form<2, 2, 2, 2> Tile128;
