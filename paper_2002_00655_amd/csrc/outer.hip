@@ -69,8 +69,8 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_outer(OuterCall call,
     extern __shared__ __align__(16) char shared[];
     Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
     int *const at = reinterpret_cast<int *>(lds + 2 * (BR + BC) * UNITS);      // the rows' numbers of the chunk
-    const OuterArgs &a = call.a[blockIdx.y];
-    const OuterTiles &o = call.o[blockIdx.y];
+    const OuterArgs a = call.a[blockIdx.y];
+    const OuterTiles o = call.o[blockIdx.y];
     OuterPlace p;
     if (!outer_place<BR, BC>(a, o, at, err, p)) return;
     floatx16 acc[T::MC][T::MR] = {};
@@ -104,8 +104,8 @@ template <class T> struct Turned {
 };
 typedef short Four __attribute__((ext_vector_type(4)));
 typedef short Eight __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ Four turned_four(const unsigned char *part, int k, int chunk, int row, int piece) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four *)(part + (k + row) * 256 + (chunk ^ (2 * row)) * 32 + piece * 8));
+__device__ __forceinline__ Four turned_four(const unsigned char *from) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four *)from);
 }
 template <class CT, class T>
 __global__ __launch_bounds__(256, T::BLOCKS) void k_outer_turned(OuterCall call, int32_t *err) {
@@ -113,8 +113,8 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_outer_turned(OuterCall call,
     constexpr int BR = T::ROWS, BC = T::COLS;
     extern __shared__ __align__(16) unsigned char lds[];
     int *const at = reinterpret_cast<int *>(lds + F::LDS);
-    const OuterArgs &a = call.a[blockIdx.y];
-    const OuterTiles &o = call.o[blockIdx.y];
+    const OuterArgs a = call.a[blockIdx.y];
+    const OuterTiles o = call.o[blockIdx.y];
     OuterPlace p;
     if (!outer_place<BR, BC>(a, o, at, err, p)) return;
     floatx16 acc[T::MC][T::MR] = {};
@@ -134,31 +134,42 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_outer_turned(OuterCall call,
                 to.right[i] = *reinterpret_cast<const Eight *>(row_of(right, a.right_shared(q), a.right_stride));
             }
         };
-        // (what does not exist becomes zero on both sides: a number beside it could be an infinity)
-        const auto put = [&](const Numbers &from, int s) {
-            unsigned char *to = lds + (s & 1) * F::STEP;
+        // (rows that do not exist become zero on both sides: a number in their place could be an infinity; columns that do not are nobody's)
+        const auto put = [&](const Numbers &from, int s, auto half) {
+            unsigned char *to = lds + decltype(half)::value * F::STEP + k0 * 256 + (((c >> 4) ^ (2 * (k0 & 3))) * 32) + (c & 8) * 2;
+            if ((s + 1) * KS <= p.t.rows) {
 #pragma unroll
-            for (int i = 0; i < F::N; ++i) {
-                const int k = i * 16 + k0, place = k * 256 + (((c >> 4) ^ (2 * (k & 3))) * 32) + (c & 8) * 2;
-                const bool row = s * KS + k < p.t.rows;
-                *reinterpret_cast<Eight *>(to + place) = row && in_left ? from.left[i] : Eight{};
-                *reinterpret_cast<Eight *>(to + KS * 256 + place) = row && in_right ? from.right[i] : Eight{};
+                for (int i = 0; i < F::N; ++i) {
+                    *reinterpret_cast<Eight *>(to + i * 4096) = from.left[i];
+                    *reinterpret_cast<Eight *>(to + i * 4096 + KS * 256) = from.right[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < F::N; ++i) {
+                    const bool row = s * KS + i * 16 + k0 < p.t.rows;
+                    *reinterpret_cast<Eight *>(to + i * 4096) = row ? from.left[i] : Eight{};
+                    *reinterpret_cast<Eight *>(to + i * 4096 + KS * 256) = row ? from.right[i] : Eight{};
+                }
             }
         };
         typedef Vec<CT, 8> Unit;
         struct Pair { Unit a[T::MC], b[T::MR]; } u, v;
         const int row = lane >> 2 & 3, piece = lane & 3, odd = lane >> 4 & 1, k8 = 8 * (lane >> 5);
-        const auto read = [&](Pair &to, int s, int pair) {
-            const unsigned char *from = lds + (s & 1) * F::STEP;
-            const int k = pair * 16 + k8;
-            const auto unit = [&](const unsigned char *part, int first) {
-                const Four lo = turned_four(part, k, first / 16 + odd, row, piece), hi = turned_four(part, k + 4, first / 16 + odd, row, piece);
-                return __builtin_bit_cast(Unit, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        // where this lane reads for a column block of 32: the rest of an address is known before
+        const unsigned char *left_at[T::MR], *right_at[T::MC];
+#pragma unroll
+        for (int j = 0; j < T::MR; ++j) left_at[j] = lds + (k8 + row) * 256 + (((wr + 32 * j) / 16 + odd) ^ (2 * row)) * 32 + piece * 8;
+#pragma unroll
+        for (int i = 0; i < T::MC; ++i) right_at[i] = lds + KS * 256 + (k8 + row) * 256 + (((wc + 32 * i) / 16 + odd) ^ (2 * row)) * 32 + piece * 8;
+        const auto read = [&](Pair &to, auto half, auto pair) {
+            constexpr int at = decltype(half)::value * F::STEP + decltype(pair)::value * 16 * 256;
+            const auto unit = [&](const unsigned char *from) {
+                return __builtin_bit_cast(Unit, __builtin_shufflevector(turned_four(from + at), turned_four(from + at + 4 * 256), 0, 1, 2, 3, 4, 5, 6, 7));
             };
 #pragma unroll
-            for (int i = 0; i < T::MC; ++i) to.a[i] = unit(from + KS * 256, wc + 32 * i);
+            for (int i = 0; i < T::MC; ++i) to.a[i] = unit(right_at[i]);
 #pragma unroll
-            for (int j = 0; j < T::MR; ++j) to.b[j] = unit(from, wr + 32 * j);
+            for (int j = 0; j < T::MR; ++j) to.b[j] = unit(left_at[j]);
         };
         const auto multiply = [&](const Pair &from) {
 #pragma unroll
@@ -166,35 +177,39 @@ __global__ __launch_bounds__(256, T::BLOCKS) void k_outer_turned(OuterCall call,
 #pragma unroll
                 for (int j = 0; j < T::MR; ++j) acc[i][j] = mfma_unit<CT>(from.a[i], from.b[j], acc[i][j]);
         };
-        // step s, whose first pair has been read; `next` holds the numbers of step s + 1
-        const auto step = [&](int s, Numbers &next) {
-            read(v, s, 1);
+        typedef std::integral_constant<int, 0> Zero;
+        typedef std::integral_constant<int, 1> One;
+        typedef std::integral_constant<int, 2> Two;
+        typedef std::integral_constant<int, 3> Three;
+        // step s, in that half of LDS, whose first pair has been read; `next` holds the numbers of step s + 1
+        const auto step = [&](int s, Numbers &next, auto half, auto other) {
+            read(v, half, One{});
             __builtin_amdgcn_sched_barrier(0);
             multiply(u);
-            read(u, s, 2);
+            read(u, half, Two{});
             __builtin_amdgcn_sched_barrier(0);
             multiply(v);
-            read(v, s, 3);
+            read(v, half, Three{});
             __builtin_amdgcn_sched_barrier(0);
             multiply(u);
             if (s + 1 < steps) {
-                put(next, s + 1);
+                put(next, s + 1, other);
                 if (s + 3 < steps) fetch(next, s + 3);
                 __syncthreads();
-                read(u, s + 1, 0);
+                read(u, other, Zero{});
                 __builtin_amdgcn_sched_barrier(0);
             }
             multiply(v);
         };
         fetch(x, 0);
         if (steps > 1) fetch(y, 1);
-        put(x, 0);
+        put(x, 0, Zero{});
         if (steps > 2) fetch(x, 2);
         __syncthreads();
-        read(u, 0, 0);
+        read(u, Zero{}, Zero{});
         for (int s = 0; s < steps; s += 2) {
-            step(s, y);
-            if (s + 1 < steps) step(s + 1, x);
+            step(s, y, Zero{}, One{});
+            if (s + 1 < steps) step(s + 1, x, One{}, Zero{});
         }
         __syncthreads();
     }
@@ -230,17 +245,20 @@ int outer_kind(const dpaps_ps *ps, const OuterArgs *a, int count) {
     return ceil_div64(a->rows, 128) * ceil_div64(a->cols, 128) * a->g.groups < ps->num_cu ? OUTER_64 : OUTER_128;
 }
 // The tiles of a sum, and how many of a group's rows a workgroup takes.
+constexpr int CHUNK_MOST = 2048;
 template <class T> OuterTiles outer_tiles(const dpaps_ps *ps, const OuterArgs &a, int64_t want) {
     OuterTiles o{};
     o.rows = (a.rows + T::ROWS - 1) / T::ROWS;
     o.cols = (a.cols + T::COLS - 1) / T::COLS;
-    o.chunk = 2048;
-    while (o.chunk > (a.g.n <= 512 ? 512 : 256) && (int64_t)o.rows * o.cols * ceil_div64(a.g.n, o.chunk) < want * ps->num_cu) o.chunk /= 2;
+    // chunks that make, with the rests of the groups (half a chunk each), one round of `want` workgroups a compute unit: the longest one is what a call takes
+    const int64_t shares = want * ps->num_cu / ((int64_t)o.rows * o.cols) - a.g.groups / 2;
+    const int64_t rows = shares > 0 ? ceil_div64(ceil_div64(a.g.n, shares), 64) * 64 : CHUNK_MOST, least = a.g.n <= 512 ? 512 : 192;
+    o.chunk = (int32_t)(rows < least ? least : rows > CHUNK_MOST ? CHUNK_MOST : rows);
     o.slots = a.g.n / o.chunk + 1;
     return o;
 }
-OuterTiles outer_plan(const dpaps_ps *ps, const OuterArgs &a, int kind) {
-    return kind == OUTER_LOW ? outer_tiles<Low>(ps, a, 2) : kind == OUTER_64 ? outer_tiles<Tile64>(ps, a, 2) : outer_tiles<Tile128>(ps, a, 2);
+OuterTiles outer_plan(const dpaps_ps *ps, const OuterArgs &a, int kind, int count) {
+    return kind == OUTER_LOW ? outer_tiles<Low>(ps, a, count == 2 ? 2 : 3) : kind == OUTER_64 ? outer_tiles<Tile64>(ps, a, 2) : outer_tiles<Tile128>(ps, a, 2);
 }
 size_t outer_part(const OuterArgs &a, const OuterTiles &o) {
     if (a.g.n <= o.chunk) return 0;
@@ -255,7 +273,7 @@ template <class CT, class LT, class RT, class T> int outer_of(dpaps_ps *ps, cons
     const int64_t grid = outer_grid<T>(c, count);
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "expert_grad");
     static LdsAllowed allowed;
-    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer<CT, LT, RT, T>), T::LDS + 2048 * sizeof(int));
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer<CT, LT, RT, T>), T::LDS + CHUNK_MOST * sizeof(int));
     if (rc) return rc;
     k_outer<CT, LT, RT, T><<<dim3((unsigned)grid, (unsigned)count), T::THREADS, T::LDS + std::max(c.o[0].chunk, c.o[1].chunk) * sizeof(int), st>>>(c, ps->err);
     PS_HIP(ps, hipGetLastError());
@@ -266,7 +284,7 @@ template <class CT> int outer_turned(dpaps_ps *ps, const OuterCall &c, hipStream
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "expert_grad");
     constexpr int LDS = Turned<Tile128>::LDS;
     static LdsAllowed allowed;
-    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer_turned<CT, Tile128>), LDS + 2048 * sizeof(int));
+    const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_outer_turned<CT, Tile128>), LDS + CHUNK_MOST * sizeof(int));
     if (rc) return rc;
     k_outer_turned<CT, Tile128><<<(unsigned)grid, 256, LDS + c.o[0].chunk * sizeof(int), st>>>(c, ps->err);
     PS_HIP(ps, hipGetLastError());
@@ -287,7 +305,7 @@ int dpaps_too_large(dpaps_ps *ps, const char *what) {
 size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs *a, int count) {
     const int kind = outer_kind(ps, a, count);
     size_t bytes = 0;
-    for (int i = 0; i < count; ++i) bytes += outer_part(a[i], outer_plan(ps, a[i], kind));
+    for (int i = 0; i < count; ++i) bytes += outer_part(a[i], outer_plan(ps, a[i], kind, count));
     return bytes;
 }
 int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs *a, int count, float *part, hipStream_t st) {
@@ -298,7 +316,7 @@ int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs *a, int count, float *part, h
     int64_t most = 0;
     for (int i = 0; i < count; ++i) {
         c.a[i] = a[i];
-        c.o[i] = outer_plan(ps, a[i], kind);
+        c.o[i] = outer_plan(ps, a[i], kind, count);
         c.o[i].part = (float *)at;
         at += outer_part(a[i], c.o[i]);
         join |= a[i].g.n > c.o[i].chunk;

@@ -248,10 +248,10 @@ __device__ __forceinline__ void tile_sum(int K, Vec<CT, unit_of<CT>()> *lds, int
     if (steps > T::SETS) fetch(First{}, T::SETS);
     __syncthreads();
     x.read(lds, c0, r0, 0);
-    // step s; `set` holds the next one
-    const auto step = [&](int s, auto set) {
-        const Vec<CT, unit_of<CT>()> *here = lds + (s & 1) * SIZE;
-        Vec<CT, unit_of<CT>()> *next = lds + ((s + 1) & 1) * SIZE;
+    // step s, which is in that half of LDS; `set` holds the next one
+    const auto step = [&](int s, auto set, auto half) {
+        const Vec<CT, unit_of<CT>()> *here = lds + decltype(half)::value * SIZE;
+        Vec<CT, unit_of<CT>()> *next = lds + (1 - decltype(half)::value) * SIZE;
         y.read(here, c0, r0, 1);
         __builtin_amdgcn_sched_barrier(0);
         x.multiply(acc);
@@ -270,9 +270,9 @@ __device__ __forceinline__ void tile_sum(int K, Vec<CT, unit_of<CT>()> *lds, int
         }
         y.multiply(acc);
     };
-    for (int s = 0; s < steps; s += T::SETS) {
-        step(s, Second{});
-        if (T::SETS == 2 && s + 1 < steps) step(s + 1, First{});
+    for (int s = 0; s < steps; s += 2) {
+        step(s, Second{}, std::integral_constant<int, 0>{});
+        if (s + 1 < steps) step(s + 1, First{}, std::integral_constant<int, 1>{});
     }
     __syncthreads();                                                 // (LDS is used again)
 }

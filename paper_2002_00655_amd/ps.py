@@ -8,6 +8,7 @@ fallback: if the library has not been built, importing fails loudly.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -154,10 +155,17 @@ def _groups(groups) -> tuple[int, int, int, int]:
 
 
 def _count_of(t: torch.Tensor) -> int:
-    n = 1
-    for d in t.shape[:-1]:
-        n *= d
-    return n
+    """The rows of a tensor, its last dimension being a row."""
+    return t.shape[0] if t.dim() == 2 else math.prod(t.shape[:-1])
+
+
+def _result(shape, like: torch.Tensor, dtype: torch.dtype | None) -> tuple[torch.Tensor, int, int, int]:
+    """A new tensor of rows, in `dtype` or the type of `like`: itself, where it is, its type, the rows' distance."""
+    dtype = like.dtype if dtype is None else dtype
+    if dtype not in _TYPES:
+        raise TypeError(f"the result is float32, bfloat16 or float16, not {dtype}")
+    out = torch.empty(shape, dtype=dtype, device=like.device)
+    return out, out.data_ptr(), _TYPES[dtype], shape[-1]
 
 
 def _pairs_of(t: torch.Tensor, n: int, what: str) -> tuple[int, int]:
@@ -408,13 +416,14 @@ class ParameterServer:
         x_rows, x_pairs = _pairs_of(x, n, "x")
         if sum_pairs < 1 or n % sum_pairs:
             raise ValueError(f"sums of {sum_pairs} of {n} rows")
-        shape = (n // sum_pairs, columns)
-        if out is None:
-            out = torch.empty(shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
-        elif out.shape[-1:] != shape[1:] or _count_of(out) != shape[0]:
-            raise ValueError(f"out must have the shape {shape}")
         kept, frm, kind, stride = _rows(x, x_rows)
-        _, to, out_kind, out_stride = _rows(out, shape[0], copy=False)
+        out_rows = n // sum_pairs
+        if out is None:
+            out, to, out_kind, out_stride = _result((out_rows, columns), x, dtype)
+        elif out.dim() == 0 or out.shape[-1] != columns or _count_of(out) != out_rows:
+            raise ValueError(f"out must have the shape {(out_rows, columns)}")
+        else:
+            _, to, out_kind, out_stride = _rows(out, out_rows, copy=False)
         self._check(_lib.expert_matmul(self._h, worker, first_key, experts, rows, dim, int(transposed), order, offsets, n, frm, kind, stride, x_pairs, to, out_kind,
                                        out_stride, sum_pairs, _stream()), "expert_matmul")
         return out
@@ -445,12 +454,13 @@ class ParameterServer:
         dim = self.L if dim is None else dim
         if x.dim() == 0 or x.shape[-1] != dim or _count_of(x) != n:
             raise ValueError(f"expected {n} rows of {dim} numbers, got shape {tuple(x.shape)}")
+        kept, frm, kind, stride = _rows(x, n)
         if out is None:
-            out = torch.empty((*x.shape[:-1], rows), dtype=x.dtype if dtype is None else dtype, device=x.device)
+            out, to, out_kind, out_stride = _result((*x.shape[:-1], rows), x, dtype)
         elif out.shape != (*x.shape[:-1], rows):
             raise ValueError(f"out must have the shape {(*x.shape[:-1], rows)}")
-        kept, frm, kind, stride = _rows(x, n)
-        _, to, out_kind, out_stride = _rows(out, n, copy=False)
+        else:
+            _, to, out_kind, out_stride = _rows(out, n, copy=False)
         self._check(_lib.adapter_matmul(self._h, worker, first_key, rows, dim, first_a, first_b, adapters, rank, scale, order, offsets, n, frm, kind, stride, to, out_kind,
                                         out_stride, _stream()), "adapter_matmul")
         return out
@@ -465,11 +475,10 @@ class ParameterServer:
         if x.dim() == 0 or dout.shape[:-1] != x.shape[:-1] or _count_of(x) != n:
             raise ValueError(f"expected {n} rows, got shapes {tuple(x.shape)} and {tuple(dout.shape)}")
         dim, rows = x.shape[-1], dout.shape[-1]
-        dx = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device) if want_dx else None
+        dx, to, to_kind, to_stride = _result(x.shape, x, dtype) if want_dx else (None, None, _TYPES.get(x.dtype, 0), dim)
         da, db = (torch.empty((adapters, rank, c), dtype=torch.float32, device=x.device) for c in (dim, rows))
         kept_x, frm, kind, stride = _rows(x, n)
         kept_d, d, _, d_stride = _rows(dout, n)
-        to, to_kind, to_stride = (_rows(dx, n, copy=False)[1:]) if want_dx else (None, kind, dim)
         self._check(_lib.adapter_grad(self._h, worker, first_key, rows, dim, first_a, first_b, adapters, rank, scale, order, offsets, n, frm, stride, d, d_stride, kind, to,
                                       to_kind, to_stride, da.data_ptr(), db.data_ptr(), _stream()), "adapter_grad")
         return dx, da, db
