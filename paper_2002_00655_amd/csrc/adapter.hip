@@ -11,8 +11,17 @@
 
 namespace {
 
+// v += the low-rank numbers of the row at a place times W columns of its adapter's second matrix
+template <int W> __device__ __forceinline__ void add_low(const AdapterArgs &a, int place, int group, int c, int left, Vec<float, W> &v) {
+    const float *low = a.low + (int64_t)place * a.low_stride, *b = a.b + (int64_t)group * a.rank * a.L + c;
+    Vec<float, W> w = {};
+#pragma unroll 4
+    for (int i = 0; i < a.rank; ++i) w = w + low[i] * load_some<float, W>(b + (int64_t)i * a.L, left);
+    v = v + w;
+}
+
 template <class CT, class XT, bool TURNED, class T>
-__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a, int32_t tiles, int32_t col_tiles, int32_t *err) {
+__global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a, int32_t tiles, int32_t col_tiles, int32_t by_group, int32_t *err) {
     constexpr int KU = unit_of<CT>(), BR = T::ROWS, BC = T::COLS;
     extern __shared__ __align__(16) char shared[];
     Vec<CT, KU> *const lds = reinterpret_cast<Vec<CT, KU> *>(shared);
@@ -20,8 +29,12 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a
     __shared__ int off;
     look_for_all(err, &off);
     const TilePlace place = tile_place(tiles, col_tiles);
-    const int first = place.row * BR, count = a.g.n - first < BR ? a.g.n - first : BR;
+    if (place.row < 0) return;
     const int c0 = place.col * BC, tid = threadIdx.x;
+    // rows of one adapter, or as they follow each other in the order
+    const RowTile own = by_group ? row_tile(a.g, place.row, BR) : row_tile(a.g, place.row * BR, 1);
+    const int first = by_group ? own.first : place.row * BR, count = by_group ? own.rows : a.g.n - first < BR ? a.g.n - first : BR;
+    if (count <= 0) return;
     for (int r = tid; r < BR; r += T::THREADS) at[r] = r < count ? row_at(a.g, first + r, err) : -1;
     __syncthreads();
     if (off) return;
@@ -45,31 +58,30 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a
                 columns[set].put(to + BR * UNITS);
             }, acc);
     }
-    // the adapters of the tile's rows, one after the other: the rows of others are zero
-    for (int e = row_tile(a.g, first, 1).group; e < a.g.groups; ++e) {
-        const int lo = a.g.start(e) - first, hi = a.g.start(e + 1) - first;
-        if (lo >= count) break;
-        if (hi <= lo || hi <= 0) continue;
+    // Rows of one adapter: its product goes on where W's has ended.  Rows of several: a row's part is worked out number by number as the sums leave, so that
+    // nothing of one adapter comes near the rows of another (a zero times its infinity would be no number).
+    const bool alone = by_group || own.end >= first + count;
+    if (alone && own.group < a.g.groups) {
         KMajor<float, CT, BR, T::THREADS> rows;
         rows.init([&](int r) { return a.low + (int64_t)(first + (r < count ? r : 0)) * a.low_stride; });
         KeyRows<CT, BC, T::THREADS> columns;
-        columns.init(a.b + (int64_t)e * a.rank * a.L + c0, a.L);
+        columns.init(a.b + (int64_t)own.group * a.rank * a.L + c0, a.L);
         tile_sum_short<CT, T>(a.rank, lds, wc, wr,
-            [&](auto set, int s, auto tail) {
+            [&](auto, int s, auto tail) {
                 rows.template load<decltype(tail)::value>(s, a.rank);
                 columns.template load<decltype(tail)::value>(s, a.rank);
             },
-            [&](auto set, Vec<CT, KU> *to) {
-#pragma unroll
-                for (int i = 0; i < rows.N; ++i) {
-                    const int r = (i * T::THREADS + tid) / UNITS;
-                    if (r < lo || r >= hi) rows.raw[i] = Vec<float, KU>{};
-                }
+            [&](auto, Vec<CT, KU> *to) {
                 rows.put(to);
                 columns.put(to + BR * UNITS);
             }, acc);
     }
-    put_tile_typed<T>(acc, lds, a.out, a.out_type, c0, a.N, 1.0f, [&](int r) { return at[r] < 0 ? (int64_t)-1 : (int64_t)at[r] * a.out_stride; });
+    put_tile_typed<T>(acc, lds, a.out, a.out_type, c0, a.N, 1.0f, [&](int r) { return at[r] < 0 ? (int64_t)-1 : (int64_t)at[r] * a.out_stride; },
+                      [&](int r, int c, int left, Vec<float, 8> &v) {
+                          if (alone) return;
+                          const uint32_t e = (uint32_t)a.group_of[first + r];
+                          if (e < (uint32_t)a.g.groups) add_low<8>(a, first + r, (int)e, c0 + c, left, v);
+                      });
 }
 
 // Few rows, of any adapters: the low-rank part is added to a row's sums number by number.
@@ -96,25 +108,21 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_adap
         const int r = F::row_of(p), c = F::col_of(p), left = a.N - c0 - c;
         if (at[r] < 0 || left <= 0) continue;
         Vec<float, 4> v = F::sum(sums, p);
-        if ((uint32_t)group[r] < (uint32_t)a.g.groups) {              // (whatever the offsets are)
-            const float *low = a.low + (int64_t)(first + r) * a.low_stride, *b = a.b + (int64_t)group[r] * a.rank * a.L + c0 + c;
-            Vec<float, 4> w = {};
-#pragma unroll 8
-            for (int i = 0; i < a.rank; ++i) w = w + low[i] * load_some<float, 4>(b + (int64_t)i * a.L, left);
-            v = v + w;
-        }
+        if ((uint32_t)group[r] < (uint32_t)a.g.groups) add_low<4>(a, first + r, group[r], c0 + c, left, v);       // (whatever the offsets are)
         put_typed<4>(a.out, a.out_type, (int64_t)at[r] * a.out_stride + c0 + c, v, left);
     }
 }
 
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
-    const int64_t tiles = ceil_div64(a.g.n, T::ROWS), grid = tiles * col_tiles;
+    // (tiles of one adapter where most of them are full: rows of several in one take longer, 128 x 128 of 16 numbers 12 us)
+    const bool by_group = a.g.n >= (int64_t)T::ROWS * a.g.groups;
+    const int64_t tiles = by_group ? row_tiles(a.g.n, a.g.groups, T::ROWS) : ceil_div64(a.g.n, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "adapters");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_adapter<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
-    k_adapter<CT, XT, TURNED, T><<<(unsigned)grid, T::THREADS, T::LDS, st>>>(a, (int32_t)tiles, col_tiles, ps->err);
+    k_adapter<CT, XT, TURNED, T><<<die_grid(grid), T::THREADS, T::LDS, st>>>(a, (int32_t)tiles, col_tiles, by_group, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
@@ -167,7 +175,7 @@ struct Scratch {
 Scratch scratch_of(const dpaps_ps *ps, const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
     Scratch s;
     const int64_t n = g.n;
-    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 3 * ps->num_cu && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
+    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 3 * ps->num_cu && n >= 128 * (int64_t)g.groups && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
     s.rounded_stride = (rank + 7) / 8 * 8;
     s.stride = s.rounded_stride;
     const auto take = [&](int64_t bytes) { const size_t at = s.end; s.end += ((size_t)bytes + 255) / 256 * 256; return at; };

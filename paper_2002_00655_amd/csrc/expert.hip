@@ -21,6 +21,7 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertCall cal
     __shared__ int off;
     look_for_all(err, &off);
     const TilePlace place = tile_place(tiles, col_tiles);
+    if (place.row < 0) return;
     const RowTile t = row_tile(a.g, place.row, BR);
     const int c0 = place.col * BC, tid = threadIdx.x;
     if (t.rows == 0) return;
@@ -128,7 +129,7 @@ template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, c
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_expert<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
-    k_expert<CT, XT, TURNED, T><<<dim3((unsigned)grid, (unsigned)count), T::THREADS, T::LDS, st>>>(c, (int32_t)tiles, col_tiles, ps->err);
+    k_expert<CT, XT, TURNED, T><<<dim3(die_grid(grid), (unsigned)count), T::THREADS, T::LDS, st>>>(c, (int32_t)tiles, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }

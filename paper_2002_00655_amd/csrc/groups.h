@@ -22,25 +22,31 @@ struct RowTile { int group, first, rows, start, end; };        // start, end: th
 // Numbers that belong to no tile have no rows.
 inline int64_t row_tiles(int64_t n, int32_t groups, int BM) { return n / BM + groups + 1; }
 __device__ __forceinline__ RowTile row_tile(const RowGroups &g, int tile, int BM) {
-    // the last e with floor(start_e / BM) + e <= tile: the wavefront's lanes look at 64 of them at once
-    const int lane = threadIdx.x & 63;
-    int lo = 0, hi = g.groups, s, end, c, step;
+    // the last e with floor(start_e / BM) + e <= tile: the rows of no group, or what the wavefront's lanes find, 64 groups at once
+    const int lane = threadIdx.x & 63, none = g.start(g.groups);
+    int lo = 0, hi = g.groups - 1, s, end, c, step;
     do {
         step = (hi - lo) / 64 + 1;
         const int e = lo + lane * step;
-        s = e <= g.groups ? g.start(e) : g.n;
+        s = e < g.groups ? g.start(e) : none;
         const bool at = e <= hi && s / BM + e <= tile;
         c = __popcll(__ballot(at));
         c = c > 1 ? c - 1 : 0;
         lo += c * step;
         hi = hi < lo + step - 1 ? hi : lo + step - 1;
     } while (step > 1);
-    // (where the group's places start and end, one of the lanes has seen: another trip to memory only where it was the last one)
     RowTile t;
-    t.group = __builtin_amdgcn_readfirstlane(lo < g.groups ? lo : g.groups);
-    c = __builtin_amdgcn_readfirstlane(c);
-    end = c < 63 ? __builtin_amdgcn_readlane(s, c + 1) : t.group < g.groups ? g.start(t.group + 1) : g.n;
-    s = __builtin_amdgcn_readlane(s, c);
+    if (none / BM + g.groups <= tile) {
+        t.group = g.groups;
+        s = none;
+        end = g.n;
+    } else {
+        // (where the group's places start and end, the lanes have seen: another trip to memory only where it was the last one)
+        t.group = __builtin_amdgcn_readfirstlane(lo);
+        c = __builtin_amdgcn_readfirstlane(c);
+        end = t.group + 1 == g.groups ? none : c < 63 ? __builtin_amdgcn_readlane(s, c + 1) : g.start(t.group + 1);
+        s = __builtin_amdgcn_readlane(s, c);
+    }
     t.first = s + (tile - s / BM - t.group) * BM;
     t.rows = end - t.first;
     if (t.first < s || t.rows < 0) t.rows = 0;

@@ -9,7 +9,6 @@
 namespace {
 
 constexpr int KB = 32;                                       // numbers of a block
-constexpr int STAGES = 4;
 constexpr int64_t BLOCK = 16 * KB;                           // elements
 inline int64_t col_blocks(int32_t N) { return ceil_div64(N, 256) * 16; }      // (whole tiles)
 inline int64_t k_blocks(int32_t K) { return ceil_div64(K, KB); }
@@ -57,23 +56,23 @@ template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(Lay
 }
 
 template <class CT, class T> struct LaidForm {
-    static constexpr int STAGE = (T::ROWS + T::COLS) * KB * 2, LDS = STAGES * STAGE, WAVES = T::WC * T::WR, ROW_LOADS = T::ROWS / 16 / WAVES, COL_LOADS = T::COLS / 16 / WAVES, LOADS = ROW_LOADS + COL_LOADS;
+    // (four stages of 32 KB, or three of 16, of which three workgroups share a compute unit)
+    static constexpr int STAGES = T::ROWS == 256 ? 4 : 3, STAGE = (T::ROWS + T::COLS) * KB * 2, LDS = STAGES * STAGE, WAVES = T::WC * T::WR, ROW_LOADS = T::ROWS / 16 / WAVES, COL_LOADS = T::COLS / 16 / WAVES, LOADS = ROW_LOADS + COL_LOADS;
 };
 
 template <class CT, class T, bool LOW>
 __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_laid(LaidArgs a, int32_t row_tiles, int32_t col_tiles, int32_t kb_all, int32_t b_kb, int32_t *err) {
     typedef LaidForm<CT, T> F;
-    constexpr int BR = T::ROWS, BC = T::COLS;
+    constexpr int BR = T::ROWS, BC = T::COLS, STAGES = F::STAGES;
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ int at[BR];
     __shared__ int off;
     look_for_all(err, &off);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const TilePlace place = tile_place(row_tiles, col_tiles);
+    if (place.row < 0) return;
     const int tile = place.row, c0 = place.col * BC;
-    RowTile t;
-    if constexpr (LOW) t = RowTile{0, tile * BR, a.g.n - tile * BR < BR ? a.g.n - tile * BR : BR, 0, 0};
-    else t = row_tile(a.g, tile, BR);
+    const RowTile t = row_tile(a.g, tile, BR);
     if (t.rows == 0) return;
     for (int r = tid; r < BR; r += T::THREADS) at[r] = r < t.rows ? row_at(a.g, t.first + r, err) : -1;
     __syncthreads();
@@ -82,33 +81,27 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_laid(LaidArgs a, int3
     const int wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR;
     if (LOW || t.group < a.g.groups) {
         // The loads of a stage: this wavefront's blocks of 16 rows, and of 16 columns.  What they come from changes where an adapter's numbers follow
-        // the shared matrix's, or another adapter's: rows of others are zeros.
+        // the shared matrix's.
         const int unit = (lane & 3) ^ (lane >> 4 & 3);
+        const bool low = LOW && t.group < a.g.groups;
         const CT *row[F::ROW_LOADS];
         const CT *col = reinterpret_cast<const CT *>(a.w) + (LOW ? 0 : t.group * a.w_size) + (int64_t)(c0 / 16 + wave * F::COL_LOADS) * kb_all * BLOCK + lane * 8;
-        int col_step = kb_all, left = kb_all, K = a.K, adapter = 0, stages = kb_all;
+        const int stages = kb_all + (low ? b_kb : 0);
+        int col_step = kb_all, left = kb_all, K = a.K;
 #pragma unroll
         for (int i = 0; i < F::ROW_LOADS; ++i) {
             const int q = at[(wave * F::ROW_LOADS + i) * 16 + (lane >> 2)];
             row[i] = reinterpret_cast<const CT *>(a.x) + a.x_shared(q < 0 ? 0 : q) * a.x_stride + unit * 8;
         }
-        if constexpr (LOW) {
-            adapter = row_tile(a.g, t.first, 1).group;
-            for (int e = adapter; e < a.g.groups && a.g.start(e) < t.first + t.rows; ++e)
-                if (a.g.start(e + 1) > a.g.start(e) && a.g.start(e + 1) > t.first) stages += b_kb;
-        }
-        const auto next_adapter = [&]() {
-            while (adapter < a.g.groups && (a.g.start(adapter + 1) <= a.g.start(adapter) || a.g.start(adapter + 1) <= t.first)) ++adapter;
-            const int e = adapter < a.g.groups ? adapter : a.g.groups - 1, lo = a.g.start(e), hi = a.g.start(e + 1);
+        const auto to_adapter = [&]() {
 #pragma unroll
             for (int i = 0; i < F::ROW_LOADS; ++i) {
-                const int p = t.first + (wave * F::ROW_LOADS + i) * 16 + (lane >> 2);
-                row[i] = p >= lo && p < hi && p < t.first + t.rows ? reinterpret_cast<const CT *>(a.low) + (int64_t)p * a.low_stride + unit * 8 : nullptr;
+                const int r = (wave * F::ROW_LOADS + i) * 16 + (lane >> 2);
+                row[i] = reinterpret_cast<const CT *>(a.low) + (int64_t)(t.first + (r < t.rows ? r : 0)) * a.low_stride + unit * 8;
             }
-            col = reinterpret_cast<const CT *>(a.b) + e * a.b_size + (int64_t)(c0 / 16 + wave * F::COL_LOADS) * b_kb * BLOCK + lane * 8;
+            col = reinterpret_cast<const CT *>(a.b) + t.group * a.b_size + (int64_t)(c0 / 16 + wave * F::COL_LOADS) * b_kb * BLOCK + lane * 8;
             col_step = left = b_kb;
             K = a.rank;
-            ++adapter;
         };
         // half of a stage's loads, the rows' or the columns'; k: where in the sum the stage is
         const auto fetch = [&](int slot, bool rows, int k) {
@@ -117,7 +110,7 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_laid(LaidArgs a, int3
                 const bool here = k + unit * 8 < K;
 #pragma unroll
                 for (int i = 0; i < F::ROW_LOADS; ++i)
-                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(here && (!LOW || row[i]) ? row[i] + k : reinterpret_cast<const CT *>(zero_bytes)),
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(here ? row[i] + k : reinterpret_cast<const CT *>(zero_bytes)),
                                                      (__attribute__((address_space(3))) void *)(to + i * 1024), 16, 0, 0);
             } else {
 #pragma unroll
@@ -131,7 +124,7 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_laid(LaidArgs a, int3
         const auto advance = [&]() {
             if (++fetched >= stages) return;
             if (--left == 0) {
-                if constexpr (LOW) next_adapter();
+                if constexpr (LOW) to_adapter();
                 k_next = 0;
             } else k_next += KB;
         };
@@ -185,17 +178,18 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_laid(LaidArgs a, int3
 template <class CT, class T, bool LOW> int start(dpaps_ps *ps, const LaidArgs &a, hipStream_t st) {
     typedef LaidForm<CT, T> F;
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
-    const int64_t tiles = LOW ? ceil_div64(a.g.n, T::ROWS) : row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
+    const int64_t tiles = row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_laid<CT, T, LOW>), F::LDS);
     if (rc) return rc;
-    k_laid<CT, T, LOW><<<(unsigned)grid, T::THREADS, F::LDS, st>>>(a, (int32_t)tiles, col_tiles, (int32_t)k_blocks(a.K), (int32_t)k_blocks(a.rank), ps->err);
+    k_laid<CT, T, LOW><<<die_grid(grid), T::THREADS, F::LDS, st>>>(a, (int32_t)tiles, col_tiles, (int32_t)k_blocks(a.K), (int32_t)k_blocks(a.rank), ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
 template <class CT> int start_any(dpaps_ps *ps, const LaidArgs &a, hipStream_t st) {
-    const bool large = ceil_div64(a.g.n, 256) * ceil_div64(a.N, 256) >= ps->num_cu;
+    // (with adapters the rests of their rows fill tiles of 128 better)
+    const bool large = ceil_div64(a.g.n, 256) * ceil_div64(a.N, 256) >= (a.low ? 4 : 1) * ps->num_cu;
     if (a.low) return large ? start<CT, Tile256, true>(ps, a, st) : start<CT, Tile128, true>(ps, a, st);
     return large ? start<CT, Tile256, false>(ps, a, st) : start<CT, Tile128, false>(ps, a, st);
 }
