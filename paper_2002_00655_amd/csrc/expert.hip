@@ -167,7 +167,7 @@ int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs *a, int count, hipStream
 }
 
 // From so many rows a group on, and tiles of 256 x 256 for two rounds of the compute units, matrices are laid before the product (laid.hip).
-constexpr int64_t LAID_ROWS = 1024;
+constexpr int64_t LAID_ROWS = 1024, LAID_MOST = (int64_t)1 << 29;   // ... of at most a GiB
 
 extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed,
                              const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int32_t x_type, int64_t x_stride, int32_t x_pairs, void *out,
@@ -190,9 +190,10 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     a.scale = 1.0f; a.precise = x_type == PS_F32 || out_type == PS_F32;
     a.out = out; a.out_stride = out_stride; a.out_type = out_type;
     const size_t sums = out_pairs > 1 ? ((size_t)n * N * sizeof(float) + 255) / 256 * 256 : 0;
-    const bool lay = !a.precise && n >= LAID_ROWS * num_experts && ceil_div64(n, 256) * ceil_div64(N, 256) >= 2 * ps->num_cu && num_experts < 32768 && dpaps_laid_fits(x, x_stride, K);
-    const int64_t laid = lay ? dpaps_laid_size(K, N) : 0;
-    rc = dpaps_ws_reserve(ps, sums + (size_t)laid * num_experts * 2);
+    const int64_t laid = dpaps_laid_size(K, N);
+    const bool lay = !a.precise && n >= LAID_ROWS * num_experts && ceil_div64(n, 256) * ceil_div64(N, 256) >= 2 * ps->num_cu && dpaps_laid_fits(x, x_stride, K) &&
+                     num_experts < 32768 && N < (1 << 19) && laid * num_experts <= LAID_MOST;
+    rc = dpaps_ws_reserve(ps, sums + (lay ? (size_t)laid * num_experts * 2 : 0));
     if (rc) return rc;
     if (out_pairs > 1) { a.out = ps->ws; a.out_stride = N; a.out_type = PS_F32; }
     if (lay) {
