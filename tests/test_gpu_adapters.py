@@ -22,6 +22,8 @@ CASES = [
     (3000, 2, 33, 200, 136, 272),
     (5000, 7, 64, 512, 96, 512),
     (9000, 3, 4, 1000, 264, 1000),
+    (13000, 20, 20, 1000, 72, 1000),                 # (W and B laid)
+    (13000, 5, 33, 72, 1000, 1000),                  # (the same of the gradient)
 ]
 
 
@@ -113,7 +115,7 @@ def test_adapter_grad(case, kind):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("n", [40, 300, 2000, 9000])
+@pytest.mark.parametrize("n", [40, 300, 2000, 9000, 26000])
 def test_an_adapter_that_is_no_number_spoils_no_other(kind, n):
     """Infinities of one adapter's matrices, and rows that are no numbers: others in the same tile stay."""
     import torch

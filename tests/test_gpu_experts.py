@@ -138,6 +138,8 @@ CASES = [
     (2500, 5, 200, 1024, 1024, 11),
     (4100, 1, 1030, 72, 73, 0),
     (9000, 2, 515, 264, 264, 0),
+    (16400, 3, 2050, 40, 41, 0),                     # (laid)
+    (33000, 2, 48, 1000, 1000, 0),                   # (laid, transposed)
 ]
 
 
@@ -170,7 +172,7 @@ def test_expert_matmul(case, kind, transposed):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("n,rows,dim", [(40, 48, 72), (900, 130, 200), (5200, 512, 520)])
+@pytest.mark.parametrize("n,rows,dim", [(40, 48, 72), (900, 130, 200), (5200, 512, 520), (16500, 2056, 40)])
 def test_expert_matmul_strides_and_numbers_that_are_none(kind, n, rows, dim):
     """Rows of x with gaps and at odd places, rows of the result with gaps; no number beside what belongs to a row, in the server or in x, has a part in it, and
     what lies between the rows of the result stays."""
