@@ -164,7 +164,7 @@ ExpertArgs low_numbers(const dpaps_ps *ps, const RowGroups &g, const void *x, in
     return a;
 }
 
-// Scratch of a call, and the product with it.  Many rows of 16 bits, tiles of 128 x 128 for three rounds of the compute units: the shared matrix and the adapters' second
+// Scratch of a call, and the product with it.  Many rows of 16 bits, tiles of 128 x 128 for two workgroups a compute unit: the shared matrix and the adapters' second
 // ones are laid (laid.hip).
 struct Scratch {
     bool laid = false;
@@ -175,7 +175,7 @@ struct Scratch {
 Scratch scratch_of(const dpaps_ps *ps, const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
     Scratch s;
     const int64_t n = g.n;
-    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 3 * ps->num_cu && n >= 128 * (int64_t)g.groups && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
+    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 2 * ps->num_cu && n >= 128 * (int64_t)g.groups && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
     s.rounded_stride = (rank + 7) / 8 * 8;
     s.stride = s.rounded_stride;
     const auto take = [&](int64_t bytes) { const size_t at = s.end; s.end += ((size_t)bytes + 255) / 256 * 256; return at; };
@@ -205,13 +205,10 @@ int product_with(dpaps_ps *ps, const Scratch &s, const LowNumbers &low, AdapterA
         return product(ps, a, st);
     }
     char *ws = (char *)ps->ws;
-    LayArgs l{};
-    l.w = a.w; l.L = a.L; l.K = a.K; l.N = a.N; l.turned = a.turned; l.to = ws + s.w;
-    int rc = dpaps_lay(ps, nullptr, a.x_type, l, st);
-    if (rc) return rc;
-    l = LayArgs{};
-    l.w = a.b; l.L = a.L; l.each = a.rank; l.K = a.rank; l.N = a.N; l.turned = 1; l.to = ws + s.b; l.size = s.b_size;
-    rc = dpaps_lay(ps, &a.g, a.x_type, l, st);
+    LayArgs shared{}, second{};
+    shared.w = a.w; shared.L = a.L; shared.K = a.K; shared.N = a.N; shared.turned = a.turned; shared.to = ws + s.w;
+    second.w = a.b; second.L = a.L; second.each = a.rank; second.K = a.rank; second.N = a.N; second.turned = 1; second.to = ws + s.b; second.size = s.b_size;
+    const int rc = dpaps_lay(ps, a.g, a.x_type, second, &shared, st);
     if (rc) return rc;
     LaidArgs p{};
     p.g = a.g; p.x = a.x; p.x_stride = a.x_stride; p.K = a.K; p.N = a.N; p.w = ws + s.w; p.w_size = s.w_size; p.low = low.rounded; p.low_stride = (int32_t)low.rounded_stride;

@@ -166,7 +166,8 @@ int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs *a, int count, hipStream
     return a->precise ? product_either<float, f16_t>(ps, c, count, st) : product_either<f16_t, f16_t>(ps, c, count, st);
 }
 
-// From so many rows a group on, and tiles of 256 x 256 for two rounds of the compute units, matrices are laid before the product (laid.hip).
+// From so many rows a group on, and tiles of 128 x 128 for two workgroups a compute unit, matrices are laid before the product (laid.hip): 16,384 rows of 8 groups,
+// bf16, 2048 x 1024, 108 us with the laying and 113 by tiles, 1024 x 1024 60 and 68; of 16 groups, 1,024 rows each, 69 and 74, 2048 x 1024 124 and 114; 8,192 rows of 16, 52 and 62.
 constexpr int64_t LAID_ROWS = 1024, LAID_MOST = (int64_t)1 << 29;   // ... of at most a GiB
 
 extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed,
@@ -191,7 +192,7 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     a.out = out; a.out_stride = out_stride; a.out_type = out_type;
     const size_t sums = out_pairs > 1 ? ((size_t)n * N * sizeof(float) + 255) / 256 * 256 : 0;
     const int64_t laid = dpaps_laid_size(K, N);
-    const bool lay = !a.precise && n >= LAID_ROWS * num_experts && ceil_div64(n, 256) * ceil_div64(N, 256) >= 2 * ps->num_cu && dpaps_laid_fits(x, x_stride, K) &&
+    const bool lay = !a.precise && n >= LAID_ROWS * num_experts && ceil_div64(n, 128) * ceil_div64(N, 128) >= 2 * ps->num_cu && dpaps_laid_fits(x, x_stride, K) &&
                      num_experts < 32768 && N < (1 << 19) && laid * num_experts <= LAID_MOST;
     rc = dpaps_ws_reserve(ps, sums + (lay ? (size_t)laid * num_experts * 2 : 0));
     if (rc) return rc;
@@ -199,7 +200,7 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     if (lay) {
         LayArgs l{};
         l.w = a.w; l.L = a.L; l.each = a.each; l.K = K; l.N = N; l.turned = a.turned; l.to = (char *)ps->ws + sums; l.size = laid;
-        rc = dpaps_lay(ps, &g, x_type, l, st);
+        rc = dpaps_lay(ps, g, x_type, l, nullptr, st);
         if (rc) return rc;
         LaidArgs p{};
         p.g = g; p.x = x; p.x_stride = x_stride; p.x_shared = a.x_shared; p.K = K; p.N = N; p.w = l.to; p.w_size = laid;

@@ -72,7 +72,8 @@ struct LayArgs {
 };
 int64_t dpaps_laid_size(int32_t K, int32_t N);
 bool dpaps_laid_fits(const void *x, int64_t x_stride, int32_t K);
-int dpaps_lay(dpaps_ps *ps, const RowGroups *g, int32_t type, const LayArgs &a, hipStream_t st);
+// `each`: of the matrices of all groups that have rows (each.each: how many keys one has), and, if `one` is there, of a single one, in the same launch
+int dpaps_lay(dpaps_ps *ps, const RowGroups &g, int32_t type, const LayArgs &each, const LayArgs *one, hipStream_t st);
 int dpaps_laid_product(dpaps_ps *ps, int32_t type, const LaidArgs &a, hipStream_t st);
 
 // Few rows: MT tiles of 16 rows by the columns of a workgroup, whose wavefronts share the sum over k.  Both operands come straight from memory into the registers

@@ -32,30 +32,46 @@ __device__ __forceinline__ uint64_t same_key(bool in, uint32_t key, int bits) {
     }
     return m;
 }
-// f(row, key, lanes with that key) for the wavefront's rows, 64 at a time; returns whether a row names no group that there is
-template <class F> __device__ __forceinline__ bool each_64(const GroupArgs &a, int64_t first, F f) {
+// A wavefront's rows, HELD times 64 of them at once (so that their ids are asked for together): f(row, is there one, key, lanes with that key).  Up to that many, what has
+// been read for the count is kept for the places.  Returns whether a row names no group that there is.
+constexpr int HELD = 4;
+struct Held { uint32_t key[HELD]; uint64_t same[HELD]; };
+template <bool AGAIN, class F> __device__ __forceinline__ bool each_64(const GroupArgs &a, int64_t first, Held &held, F f) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t end = first + a.chunk < a.t.n ? first + a.chunk : a.t.n, share = (a.chunk + 64 * WAVES - 1) / (64 * WAVES) * 64;
     int64_t stop = first + (wave + 1) * share;
     if (stop > end) stop = end;
+    const bool keep = share <= 64 * HELD;
     bool bad = false;
-    for (int64_t p0 = first + wave * share; p0 < stop; p0 += 64) {
-        const int64_t p = p0 + lane;
-        const bool in = p < stop;
-        const int64_t id = in ? a.t.at(p) : 0;
-        bad |= in && a.t.bad(id);
-        const uint32_t key = a.t.padding(id) || a.t.bad(id) ? (uint32_t)a.groups : (uint32_t)id;
-        f(p, in, key, same_key(in, key, a.bits));
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // what one lane has counted, another reads next
+    for (int64_t p0 = first + wave * share; p0 < stop; p0 += 64 * HELD) {
+        if (!(AGAIN && keep)) {
+            int64_t id[HELD];
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) id[i] = p0 + 64 * i + lane < stop ? a.t.at(p0 + 64 * i + lane) : 0;
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                if (p0 + 64 * i >= stop) break;
+                const bool in = p0 + 64 * i + lane < stop;
+                bad |= in && a.t.bad(id[i]);
+                held.key[i] = a.t.padding(id[i]) || a.t.bad(id[i]) ? (uint32_t)a.groups : (uint32_t)id[i];
+                held.same[i] = same_key(in, held.key[i], a.bits);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            if (p0 + 64 * i >= stop) break;
+            f(p0 + 64 * i + lane, p0 + 64 * i + lane < stop, held.key[i], held.same[i]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // what one lane has counted, another reads next
+        }
     }
     return bad;
 }
 // count[key * WAVES + wave]: a wavefront's rows of a key.  Returns whether a row of the workgroup is bad, in all threads.
-__device__ __forceinline__ bool count_keys(const GroupArgs &a, int64_t first, uint32_t *count) {
+__device__ __forceinline__ bool count_keys(const GroupArgs &a, int64_t first, uint32_t *count, Held &held) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int i = threadIdx.x; i < (a.groups + 1) * WAVES; i += THREADS) count[i] = 0;
     __syncthreads();
-    const bool bad = each_64(a, first, [&](int64_t, bool in, uint32_t key, uint64_t same) {
+    const bool bad = each_64<false>(a, first, held, [&](int64_t, bool in, uint32_t key, uint64_t same) {
         if (in && __ffsll((unsigned long long)same) - 1 == lane) count[key * WAVES + wave] += (uint32_t)__popcll(same);
     });
     return __syncthreads_or(bad ? 1 : 0) != 0;
@@ -80,9 +96,9 @@ __device__ __forceinline__ void sums_before(uint32_t *x, int n) {
         if (at + i < n) { const uint32_t y = x[at + i]; x[at + i] = before; before += y; }
     __syncthreads();
 }
-__device__ __forceinline__ void put_rows(const GroupArgs &a, int64_t first, uint32_t *next) {
+__device__ __forceinline__ void put_rows(const GroupArgs &a, int64_t first, uint32_t *next, Held &held) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    each_64(a, first, [&](int64_t p, bool in, uint32_t key, uint64_t same) {
+    each_64<true>(a, first, held, [&](int64_t p, bool in, uint32_t key, uint64_t same) {
         if (in) a.order[next[key * WAVES + wave] + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (int32_t)p;
         if (in && __ffsll((unsigned long long)same) - 1 == lane) next[key * WAVES + wave] += (uint32_t)__popcll(same);
     });
@@ -93,7 +109,8 @@ __global__ __launch_bounds__(THREADS) void k_group_one(GroupArgs a, int32_t *err
     extern __shared__ uint32_t count[];
     __shared__ int off;
     look_for_all(err, &off);
-    const bool bad = count_keys(a, 0, count);
+    Held held;
+    const bool bad = count_keys(a, 0, count, held);
     if (off) return;
     if (bad) {
         if (threadIdx.x == 0) atomicExch(err, PS_EKEY);
@@ -102,13 +119,14 @@ __global__ __launch_bounds__(THREADS) void k_group_one(GroupArgs a, int32_t *err
     sums_before(count, (a.groups + 1) * WAVES);
     for (int e = threadIdx.x; e <= a.groups; e += THREADS) a.offsets[e] = (int32_t)count[e * WAVES];
     __syncthreads();
-    put_rows(a, 0, count);
+    put_rows(a, 0, count, held);
 }
 
 // More of them: what every workgroup counts, and then the places - each workgroup adds up the counts of those before it, which are few.
 __global__ __launch_bounds__(THREADS) void k_group_count(GroupArgs a, int32_t *err) {
     extern __shared__ uint32_t count[];
-    const bool bad = count_keys(a, (int64_t)blockIdx.x * a.chunk, count);
+    Held held;
+    const bool bad = count_keys(a, (int64_t)blockIdx.x * a.chunk, count, held);
     if (bad && threadIdx.x == 0) atomicExch(err, PS_EKEY);
     for (int e = threadIdx.x; e <= a.groups; e += THREADS) {
         uint32_t s = 0;
@@ -122,7 +140,8 @@ __global__ __launch_bounds__(THREADS) void k_group_place(GroupArgs a, const int3
     const int keys = a.groups + 1;
     uint32_t *total = count + keys * WAVES, *before = total + keys;
     look_for_all(err, &off);
-    count_keys(a, (int64_t)blockIdx.x * a.chunk, count);
+    Held held;
+    count_keys(a, (int64_t)blockIdx.x * a.chunk, count, held);
     if (off) return;
     for (int i = threadIdx.x; i < 2 * keys; i += THREADS) total[i] = 0;
     __syncthreads();
@@ -148,7 +167,7 @@ __global__ __launch_bounds__(THREADS) void k_group_place(GroupArgs a, const int3
         for (int w = 0; w < WAVES; ++w) { const uint32_t c = count[e * WAVES + w]; count[e * WAVES + w] = at; at += c; }
     }
     __syncthreads();
-    put_rows(a, (int64_t)blockIdx.x * a.chunk, count);
+    put_rows(a, (int64_t)blockIdx.x * a.chunk, count, held);
 }
 
 // From rows sorted as keys.

@@ -13,16 +13,19 @@ constexpr int64_t BLOCK = 16 * KB;                           // elements
 inline int64_t col_blocks(int32_t N) { return ceil_div64(N, 256) * 16; }      // (whole tiles)
 inline int64_t k_blocks(int32_t K) { return ceil_div64(K, KB); }
 
-// A workgroup lays 16 columns of 256 numbers as they lie, or 64 columns of 64 numbers that it turns in LDS.
-template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(LayArgs a, RowGroups g, int32_t cb_all, int32_t kb_all, const int32_t *err) {
-    if (*(volatile const int32_t *)err) return;
-    const int e = blockIdx.z, tid = threadIdx.x;
-    if (g.offsets && g.start(e) >= g.start(e + 1)) return;
+// A workgroup lays 16 columns of 256 numbers as they lie, or 64 columns of 64 numbers that it turns in LDS; each[0]: of group blockIdx.z's matrix, each[1]: of the
+// one behind them.
+struct LayCall {
+    LayArgs a[2];
+    int32_t cb[2], kb[2], tiles[2];                          // columns and numbers in blocks, workgroups of a matrix
+};
+template <class T, bool TURNED> __device__ __forceinline__ void lay(const LayArgs &a, int e, int tile, int cb_all, int kb_all) {
+    const int tid = threadIdx.x;
     const float *w = a.w + (int64_t)e * a.each * a.L;
     T *to = reinterpret_cast<T *>(a.to) + e * a.size;
     const auto place = [&](int c, int k) { return ((int64_t)(c >> 4) * kb_all + (k >> 5)) * BLOCK + (c & 15) * KB + (((k >> 3 & 3) ^ (c >> 2 & 3)) * 8); };
     if constexpr (!TURNED) {
-        const int c = blockIdx.y * 16 + (tid >> 4), k0 = blockIdx.x * 256 + (tid & 15) * 8;
+        const int across = (kb_all * KB + 255) / 256, c = tile / across * 16 + (tid >> 4), k0 = tile % across * 256 + (tid & 15) * 8;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int k = k0 + u * 128;
@@ -33,7 +36,7 @@ template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(Lay
         }
     } else {
         __shared__ float turn[64][65];
-        const int c0 = blockIdx.y * 64, k0 = blockIdx.x * 64;
+        const int across = (kb_all * KB + 63) / 64, c0 = tile / across * 64, k0 = tile % across * 64;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int k = u * 16 + (tid >> 4), c = (tid & 15) * 4;
@@ -53,6 +56,15 @@ template <class T, bool TURNED> __global__ __launch_bounds__(256) void k_lay(Lay
             *reinterpret_cast<Vec<T, 8> *>(to + place(c0 + c, k0 + k)) = as_type<T, float, 8>(v);
         }
     }
+}
+template <class T> __global__ __launch_bounds__(256) void k_lay(LayCall call, RowGroups g, const int32_t *err) {
+    if (*(volatile const int32_t *)err) return;
+    const int e = blockIdx.z, which = e == g.groups ? 1 : 0, tile = blockIdx.x;
+    if (tile >= call.tiles[which]) return;
+    if (which == 0 && g.start(e) >= g.start(e + 1)) return;
+    const LayArgs &a = call.a[which];
+    if (a.turned) lay<T, true>(a, which ? 0 : e, tile, call.cb[which], call.kb[which]);
+    else lay<T, false>(a, which ? 0 : e, tile, call.cb[which], call.kb[which]);
 }
 
 template <class CT, class T> struct LaidForm {
@@ -188,8 +200,9 @@ template <class CT, class T, bool LOW> int start(dpaps_ps *ps, const LaidArgs &a
     return PS_OK;
 }
 template <class CT> int start_any(dpaps_ps *ps, const LaidArgs &a, hipStream_t st) {
-    // (with adapters the rests of their rows fill tiles of 128 better)
-    const bool large = ceil_div64(a.g.n, 256) * ceil_div64(a.N, 256) >= (a.low ? 4 : 1) * ps->num_cu;
+    // tiles of 256 where nearly all of them are full, and there is one for every compute unit: 16,384 rows of one group, 1024 x 1024, 44 us and 53 by tiles of 128; of
+    // four groups 69 and 57, because the rests of the groups leave the last round of the compute units half empty
+    const bool large = a.g.n >= 16384 * (int64_t)a.g.groups && ceil_div64(a.g.n, 256) * ceil_div64(a.N, 256) >= ps->num_cu;
     if (a.low) return large ? start<CT, Tile256, true>(ps, a, st) : start<CT, Tile128, true>(ps, a, st);
     return large ? start<CT, Tile256, false>(ps, a, st) : start<CT, Tile128, false>(ps, a, st);
 }
@@ -199,19 +212,20 @@ template <class CT> int start_any(dpaps_ps *ps, const LaidArgs &a, hipStream_t s
 int64_t dpaps_laid_size(int32_t K, int32_t N) { return col_blocks(N) * k_blocks(K) * BLOCK; }
 bool dpaps_laid_fits(const void *x, int64_t x_stride, int32_t K) { return K % 8 == 0 && (uintptr_t)x % 16 == 0 && x_stride % 8 == 0; }
 
-int dpaps_lay(dpaps_ps *ps, const RowGroups *g, int32_t type, const LayArgs &a, hipStream_t st) {
-    const int32_t cb = (int32_t)col_blocks(a.N), kb = (int32_t)k_blocks(a.K);
-    const RowGroups groups = g ? *g : RowGroups{};
-    const unsigned z = g ? (unsigned)g->groups : 1u;
-    if (a.turned) {
-        const dim3 grid((unsigned)ceil_div64(kb * KB, 64), (unsigned)(cb / 4), z);
-        if (type == PS_BF16) k_lay<bf16_t, true><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
-        else k_lay<f16_t, true><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
-    } else {
-        const dim3 grid((unsigned)ceil_div64(kb * KB, 256), (unsigned)cb, z);
-        if (type == PS_BF16) k_lay<bf16_t, false><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
-        else k_lay<f16_t, false><<<grid, 256, 0, st>>>(a, groups, cb, kb, ps->err);
+int dpaps_lay(dpaps_ps *ps, const RowGroups &g, int32_t type, const LayArgs &each, const LayArgs *one, hipStream_t st) {
+    LayCall c{};
+    int32_t most = 0;
+    for (int i = 0; i < (one ? 2 : 1); ++i) {
+        c.a[i] = i ? *one : each;
+        const LayArgs &a = c.a[i];
+        c.cb[i] = (int32_t)col_blocks(a.N);
+        c.kb[i] = (int32_t)k_blocks(a.K);
+        c.tiles[i] = (int32_t)(a.turned ? c.cb[i] / 4 * ceil_div64(c.kb[i] * KB, 64) : c.cb[i] * ceil_div64(c.kb[i] * KB, 256));
+        most = c.tiles[i] > most ? c.tiles[i] : most;
     }
+    const dim3 grid((unsigned)most, 1, (unsigned)(g.groups + (one ? 1 : 0)));
+    if (type == PS_BF16) k_lay<bf16_t><<<grid, 256, 0, st>>>(c, g, ps->err);
+    else k_lay<f16_t><<<grid, 256, 0, st>>>(c, g, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
