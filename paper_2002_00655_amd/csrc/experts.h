@@ -82,7 +82,7 @@ int dpaps_laid_product(dpaps_ps *ps, int32_t type, const LaidArgs &a, hipStream_
 //   turned:      64 columns; lane l has the four columns from 4 (l % 16) on, for the numbers of unit l / 16: operand j is column 4 i + j of lane i
 // out[row][column] of wavefront w in sums, [w][16 MT][columns].
 template <class CT, class XT, bool TURNED, int MT> struct FewRows {
-    static constexpr int KU = unit_of<XT>(), COLS = TURNED ? 64 : 16, OPS = TURNED ? 4 : 1, WAVES = TURNED && MT == 4 ? 4 : 8, THREADS = 64 * WAVES, STEP = 4 * KU;
+    static constexpr int KU = unit_of<XT>(), COLS = TURNED ? 64 : 16, OPS = TURNED ? 4 : 1, WAVES = TURNED ? 8 : 4, THREADS = 64 * WAVES, STEP = 4 * KU;
     static constexpr int AHEAD = TURNED ? (KU == 8 ? 2 : 4) : (KU == 8 ? 4 : 8);
     static constexpr int SUMS = WAVES * 16 * MT * COLS;
     floatx4 acc[OPS][MT];

@@ -149,7 +149,7 @@ __global__ __launch_bounds__(THREADS) void k_group_place(GroupArgs a, const int3
     for (int i = threadIdx.x; i < parts * keys; i += THREADS) {
         const int key = i % keys, part = i / keys, lo = a.blocks * part / parts, hi = a.blocks * (part + 1) / parts;
         uint32_t all = 0, first = 0;
-#pragma unroll 16
+#pragma unroll 8
         for (int b = lo; b < hi; ++b) {
             const uint32_t c = a.count[(int64_t)b * keys + key];
             all += c;
