@@ -250,8 +250,9 @@ template <class T> OuterTiles outer_tiles(const dpaps_ps *ps, const OuterArgs &a
     OuterTiles o{};
     o.rows = (a.rows + T::ROWS - 1) / T::ROWS;
     o.cols = (a.cols + T::COLS - 1) / T::COLS;
-    // chunks that make, with the rests of the groups (half a chunk each), one round of `want` workgroups a compute unit: the longest one is what a call takes
-    const int64_t shares = want * ps->num_cu / ((int64_t)o.rows * o.cols) - a.g.groups / 2;
+    // chunks that make, with the rests of the groups (half a chunk each, if all have rows), one round of `want` workgroups a compute unit: the longest one is
+    // what a call takes
+    const int64_t round = want * ps->num_cu / ((int64_t)o.rows * o.cols), shares = std::max(round - a.g.groups / 2, round / 2);
     const int64_t rows = shares > 0 ? ceil_div64(ceil_div64(a.g.n, shares), 64) * 64 : CHUNK_MOST, least = a.g.n <= 512 ? 512 : 192;
     o.chunk = (int32_t)(rows < least ? least : rows > CHUNK_MOST ? CHUNK_MOST : rows);
     o.slots = a.g.n / o.chunk + 1;
