@@ -32,8 +32,17 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a
     if (place.row < 0) return;
     const int c0 = place.col * BC, tid = threadIdx.x;
     // rows of one adapter, or as they follow each other in the order
-    const RowTile own = by_group ? row_tile(a.g, place.row, BR) : row_tile(a.g, place.row * BR, 1);
-    const int first = by_group ? own.first : place.row * BR, count = by_group ? own.rows : a.g.n - first < BR ? a.g.n - first : BR;
+    int first, count, group;
+    bool alone = true;
+    if (by_group) {
+        const RowTile t = row_tile(a.g, place.row, BR);
+        first = t.first; count = t.rows; group = t.group;
+    } else {
+        first = place.row * BR;
+        count = a.g.n - first < BR ? a.g.n - first : BR;
+        group = a.group_of[first];
+        alone = group == a.group_of[first + count - 1];
+    }
     if (count <= 0) return;
     for (int r = tid; r < BR; r += T::THREADS) at[r] = r < count ? row_at(a.g, first + r, err) : -1;
     __syncthreads();
@@ -60,12 +69,11 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a
     }
     // Rows of one adapter: its product goes on where W's has ended.  Rows of several: a row's part is worked out number by number as the sums leave, so that
     // nothing of one adapter comes near the rows of another (a zero times its infinity would be no number).
-    const bool alone = by_group || own.end >= first + count;
-    if (alone && own.group < a.g.groups) {
+    if (alone && (uint32_t)group < (uint32_t)a.g.groups) {
         KMajor<float, CT, BR, T::THREADS> rows;
         rows.init([&](int r) { return a.low + (int64_t)(first + (r < count ? r : 0)) * a.low_stride; });
         KeyRows<CT, BC, T::THREADS> columns;
-        columns.init(a.b + (int64_t)own.group * a.rank * a.L + c0, a.L);
+        columns.init(a.b + (int64_t)group * a.rank * a.L + c0, a.L);
         tile_sum_short<CT, T>(a.rank, lds, wc, wr,
             [&](auto, int s, auto tail) {
                 rows.template load<decltype(tail)::value>(s, a.rank);
