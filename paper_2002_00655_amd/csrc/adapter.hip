@@ -123,8 +123,10 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_adap
 
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
-    // (tiles of one adapter where most of them are full: rows of several in one take longer, 128 x 128 of 16 numbers 12 us)
-    const bool by_group = a.g.n >= (int64_t)T::ROWS * a.g.groups;
+    // Tiles of one adapter leave the last tile of each half empty; mixed ones add up to `rank` terms number by number.  1024 x 1024, rank 32, rows of all adapters,
+    // 16 bits: 5,000 rows of 64 45 us by adapter and 66 mixed, 10,000 of 200 85 and 111, 2,000 of 64 34 and 27;   32 bits, where products take longer: 5,000 of 20
+    // 128 and 133, of 64 162 and 139
+    const bool by_group = sizeof(CT) == 4 ? a.g.n >= 4 * (int64_t)T::ROWS * a.g.groups : 3 * (int64_t)a.g.n >= (int64_t)T::ROWS * a.g.groups;
     const int64_t tiles = by_group ? row_tiles(a.g.n, a.g.groups, T::ROWS) : ceil_div64(a.g.n, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "adapters");
     static LdsAllowed allowed;
@@ -144,7 +146,7 @@ template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, cons
 template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     const int64_t few = ceil_div64(a.g.n, 16) * ceil_div64(a.N, TURNED ? 64 : 16);
     if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * ps->num_cu) return few_of<CT, XT, TURNED, 1>(ps, a, st);      // (as products with experts)
-    if (sizeof(CT) == 4 || ceil_div64(a.g.n, 128) * ceil_div64(a.N, 128) < ps->num_cu) return tiles_of<CT, XT, TURNED, Tile64>(ps, a, st);
+    if (sizeof(CT) == 4 || 2 * ceil_div64(a.g.n, 128) * ceil_div64(a.N, 128) < ps->num_cu) return tiles_of<CT, XT, TURNED, Tile64>(ps, a, st);
     return tiles_of<CT, XT, TURNED, Tile128>(ps, a, st);
 }
 template <class CT, class XT> int product_either(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
@@ -172,8 +174,9 @@ ExpertArgs low_numbers(const dpaps_ps *ps, const RowGroups &g, const void *x, in
     return a;
 }
 
-// Scratch of a call, and the product with it.  Many rows of 16 bits, tiles of 128 x 128 for two workgroups a compute unit: the shared matrix and the adapters' second
-// ones are laid (laid.hip).
+// Scratch of a call, and the product with it.  Many rows of 16 bits, tiles of 128 x 128 for one and a half workgroups a compute unit: the shared matrix and the adapters'
+// second ones are laid (laid.hip).  1024 x 1024, rank 32, with the laying: 5,000 rows of 20 adapters 31 us and 31 without, 8,000 of 100 55 and 71, 16,384 of 200 99 and
+// 131, 16,001 of 64 (24 of them asked for) 71 and 92.
 struct Scratch {
     bool laid = false;
     int64_t stride = 0, rounded_stride = 0, w_size = 0, b_size = 0;
@@ -183,7 +186,7 @@ struct Scratch {
 Scratch scratch_of(const dpaps_ps *ps, const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
     Scratch s;
     const int64_t n = g.n;
-    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 2 * ps->num_cu && n >= 128 * (int64_t)g.groups && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
+    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 3 * ps->num_cu / 2 && n >= 64 * (int64_t)g.groups && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
     s.rounded_stride = (rank + 7) / 8 * 8;
     s.stride = s.rounded_stride;
     const auto take = [&](int64_t bytes) { const size_t at = s.end; s.end += ((size_t)bytes + 255) / 256 * 256; return at; };

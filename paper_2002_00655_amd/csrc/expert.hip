@@ -146,11 +146,17 @@ template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, cons
 template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
     const ExpertArgs &a = c.a[0];
     const int64_t n = a.g.n, groups = a.g.groups, cus = ps->num_cu;
-    // few rows: as long as tiles of 16 rows (a group's last one is half full) make no more workgroups than so many a compute unit
+    // Few rows, as long as tiles of 16 rows (a group's last one is half full) make no more workgroups than so many a compute unit.  At the borders, K 1024 but for the last:
+    //   16 bits, 128 rows of 16 groups x 256 columns 8.0 us and by tiles of 64 8.0, x 512 9.7 and 8.0;   turned, 500 rows of 8 groups x 512 8.4 and 9.2, x 1024 12.3 and 9.5;
+    //   32 bits, 333 rows of 5 groups x 400, K 100, 6.6 and 8.0, 1,000 rows 10.5 and 8.1
     const int64_t few = ceil_div64(n + 8 * (groups < n ? groups : n), 16) * ceil_div64(a.N, TURNED ? 64 : 16) * count;
     if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * cus) return few_of<CT, XT, TURNED, 1>(ps, c, count, st);
+    // 32 columns: tiles of 128 rows (16,384 rows of 8 groups, 16 bits, 13.0 us, and 21.2 by the kernel for few rows; 100,000 of 16 groups, 32 bits, 131 and 213), but where the
+    // rows' numbers are made longer on their way (two of 16,384 rows of 16 groups, K 512, 26 and 16.5)
     if (a.N <= 32) return sizeof(CT) != sizeof(XT) ? few_of<CT, XT, TURNED, 2>(ps, c, count, st) : tiles_of<CT, XT, TURNED, Narrow>(ps, c, count, st);
-    if (sizeof(CT) == 4 || ceil_div64(n, 128) * ceil_div64(a.N, 128) < cus) return tiles_of<CT, XT, TURNED, Tile64>(ps, c, count, st);
+    // 32 bits: tiles of 64, whose workgroups cover for each other's meetings (16,384 rows x 1024, K 1024, 345 us, by tiles of 128 371).  16 bits, rows of 8 groups x 1024,
+    // K 1024: 1,000 rows 17.0 us by tiles of 64 and 20.4 by tiles of 128, 2,000 rows 28 and 22, 3,000 rows 38 and 24
+    if (sizeof(CT) == 4 || 2 * ceil_div64(n, 128) * ceil_div64(a.N, 128) < cus) return tiles_of<CT, XT, TURNED, Tile64>(ps, c, count, st);
     return tiles_of<CT, XT, TURNED, Tile128>(ps, c, count, st);
 }
 template <class CT, class XT> int product_either(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
