@@ -1,4 +1,5 @@
-// Products of grouped rows: what their kernels are given (expert.hip), for the calls made of them.
+// Products of grouped rows: what their kernels are given, for the calls made of them.  Products in tiles: expert.hip; by way of laid matrices: laid.hip; with adapters:
+// adapter.hip; sums over a group's rows: outer.hip.
 #pragma once
 #include "groups.h"
 #include "products.h"
@@ -32,7 +33,6 @@ size_t dpaps_outer_bytes(const dpaps_ps *ps, const OuterArgs *a, int count);
 int dpaps_outer_sums(dpaps_ps *ps, const OuterArgs *a, int count, float *part, hipStream_t st);
 int dpaps_too_large(dpaps_ps *ps, const char *what);
 
-
 // The row number that stands at a place; -1, and the handle's error, where there is no such row.
 __device__ __forceinline__ int row_at(const RowGroups &g, int place, int32_t *err) {
     const int q = g.order[place];
@@ -54,8 +54,8 @@ struct AdapterArgs {
 };
 
 // Products by way of laid matrices (laid.hip): the server's numbers rounded to 16 bits once, before the product, and put into the order of its loads.
-// sums: x_q' M of group's matrix M (laid: matrix e from e * size on), or, where there is one matrix for all rows, its product plus the low-rank
-// numbers of the rows, low_p (by place, `rank` of them), times their group's laid matrix.
+// out_q = M x_q, M the group's matrix (laid: matrix e from e * w_size on; zero for rows of no group), or, with `low`, M x_q + B_e' low_p of one matrix M for all rows,
+// low_p: the low-rank numbers of the row at place p, `rank` of them and zeros up to a multiple of eight, B_e: the laid matrix of its group.
 struct LaidArgs {
     RowGroups g;
     const void *x; int64_t x_stride; Quotient x_shared;
@@ -80,6 +80,8 @@ int dpaps_laid_product(dpaps_ps *ps, int32_t type, const LaidArgs &a, hipStream_
 // that the matrix instruction reads, and nothing but the wavefronts' sums sees LDS: what counts is that all of the matrix is on its way at once.
 //   M as it is:  16 columns; lane l has column l % 16, and of a step's 4 units the one l / 16
 //   turned:      64 columns; lane l has the four columns from 4 (l % 16) on, for the numbers of unit l / 16: operand j is column 4 i + j of lane i
+// Of M as it is four wavefronts share the sum (the low-rank numbers of 16,384 rows of 16 adapters, K 512: 16.6 us, by eight 22.5; 128 rows of 16 experts x 256: 7.8 and 7.9), of turned
+// ones, of which there are a quarter as many workgroups, eight (333 rows of 5 experts, 400 x 100, 32 bits: 7.5 us, by four 8.6).
 // out[row][column] of wavefront w in sums, [w][16 MT][columns].
 template <class CT, class XT, bool TURNED, int MT> struct FewRows {
     static constexpr int KU = unit_of<XT>(), COLS = TURNED ? 64 : 16, OPS = TURNED ? 4 : 1, WAVES = TURNED ? 8 : 4, THREADS = 64 * WAVES, STEP = 4 * KU;

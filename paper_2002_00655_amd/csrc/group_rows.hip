@@ -3,6 +3,8 @@
 // place of row p = #{q: g_q < g_p} + #{q < p: g_q = g_p};  rows of no group (padding) stand behind all others, as group `groups`.
 // A wavefront takes 64 neighbouring rows at a time: the lanes that name one group are found by a vote per bit of the group's number, so that a
 // row's place within the 64 is a count of bits, and a wavefront's counts of a group are its own word in LDS.  No atomics on places: the order is stable.
+//
+// Few bytes move (131,072 int32 ids in, their order out: 1 MB); what a call takes are launches and the chain of trips to memory and of votes in each.
 #include "groups.h"
 
 #include <algorithm>
@@ -104,7 +106,7 @@ __device__ __forceinline__ void put_rows(const GroupArgs &a, int64_t first, uint
     });
 }
 
-// Few rows, by one workgroup.
+// Few rows, by one workgroup: 128 rows 3.4 us, 3,998 rows 7.0.
 __global__ __launch_bounds__(THREADS) void k_group_one(GroupArgs a, int32_t *err) {
     extern __shared__ uint32_t count[];
     __shared__ int off;
@@ -122,7 +124,8 @@ __global__ __launch_bounds__(THREADS) void k_group_one(GroupArgs a, int32_t *err
     put_rows(a, 0, count, held);
 }
 
-// More of them: what every workgroup counts, and then the places - each workgroup adds up the counts of those before it, which are few.
+// More of them: what every workgroup counts, and then the places - each workgroup counts its own rows again and adds up the counts of those before it, which are at
+// most 128.  131,072 rows of 64 groups: 4.2 and 7.8 us; in one launch, workgroups would have to wait for each other.
 __global__ __launch_bounds__(THREADS) void k_group_count(GroupArgs a, int32_t *err) {
     extern __shared__ uint32_t count[];
     Held held;
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(THREADS) void k_group_place(GroupArgs a, const int3
     put_rows(a, (int64_t)blockIdx.x * a.chunk, count, held);
 }
 
-// From rows sorted as keys.
+// From rows sorted as keys: more groups than counts have room for in LDS, or more rows than 128 workgroups of 16,384.
 __global__ __launch_bounds__(256) void k_group_sorted(const uint64_t *skeys, const uint32_t *spos, int64_t n, int32_t groups, int32_t *order, int32_t *offsets,
                                                       const int32_t *err) {
     if (*(volatile const int32_t *)err) return;

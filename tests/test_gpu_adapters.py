@@ -173,6 +173,25 @@ def test_strides_and_shapes(kind):
             assert torch.equal(got, known)
 
 
+def test_gradients_of_millions_of_rows():
+    """Chunks of more rows than a workgroup holds the numbers of; sums of numbers of 0 and 1, which are exact in 32 bits (below 8 x 2^21), in whatever order."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    n, rank, rows, dim = 2_300_000, 64, 8, 1024
+    g = torch.Generator(device="cuda").manual_seed(5)
+    values = torch.randint(0, 2, (rows + 4 * rank, dim), device="cuda", generator=g).float()
+    srv = P.ParameterServer(values.shape[0], dim, 1)
+    srv.push(torch.arange(values.shape[0], device="cuda"), values)
+    x, dout = (torch.randint(0, 2, (n, c), device="cuda", generator=g, dtype=torch.int8).bfloat16() for c in (dim, rows))
+    ids = torch.where(torch.rand(n, device="cuda", generator=g) < 0.6, 1, 0)
+    _, da, db = srv.adapter_grad(x, dout, srv.group_rows(ids, 2), 0, rows, rows + 2 * rank, rank, want_dx=False)
+    for e in range(2):
+        low = dout.double() @ values[rows + (2 + e) * rank:rows + (3 + e) * rank, :rows].double().t() * (ids == e)[:, None]
+        want = sum(low[i:i + 100_000].t() @ x[i:i + 100_000].double() for i in range(0, n, 100_000))
+        assert want.max() < 2 ** 24 and torch.equal(da[e].double(), want), e
+    srv.status()
+
+
 def test_gradients_against_differences():
     import torch
     case = (9, 3, 4, 20, 24, 24)

@@ -298,6 +298,24 @@ def test_expert_grad(kind, n, experts, rows, dim):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("n,side", [(9000, 4096), (20001, 2056)])
+def test_expert_grad_of_large_matrices(kind, n, side):
+    """Chunks of more rows than a workgroup holds the numbers of; sums of numbers of -1, 0 and 1, which are exact in 32 bits, in whatever order."""
+    import torch
+    print("case", kind, n, side, flush=True)
+    srv, _ = _server(1, 1)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    left, right = (torch.randint(-1, 2, (n, side), device="cuda", generator=g).to(_type(kind)) for _ in range(2))
+    ids = torch.where(torch.rand(n, device="cuda", generator=g) < 0.9, 2, 0)
+    ids[::17] = -1
+    out = srv.expert_grad(left, right, srv.group_rows(ids, 3, pad=-1))
+    for e in range(3):
+        q = (ids == e).nonzero()[:, 0]
+        assert torch.equal(out[e].double(), left[q].double().t() @ right[q].double()), e
+    srv.status()
+
+
+@pytest.mark.parametrize("kind", TYPES)
 def test_expert_grad_strides_and_numbers_that_are_none(kind):
     import torch
     srv, _ = _server(1, 1)
