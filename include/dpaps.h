@@ -40,6 +40,7 @@
  *   mf_sgd_epoch_handoff   allocates its state on first use, and always waits for `stream` at its end: it
  *       returns the order of the epoch to the host;
  *   ps_set_option(PS_OPT_LOCATION_CACHES)   waits for the device, frees and allocates the caches.
+ *   the calls of token models and of models of many matrices   scratch, as for ps_push (below);
  * ps_pull, ps_localize, ps_owner and ps_push_noalloc neither wait nor allocate.
  *
  * Errors.  Host-visible mistakes (null pointers, sizes, worker ids, a bad
@@ -384,11 +385,14 @@ int muon_step(ps_handle ps, int32_t worker, int64_t first_key, int32_t batch, in
 /* Rows are grouped by the matrix that they use (an expert, an adapter), and products, and the matrices' gradients, are taken by group.  Matrices lie in the
  * server: row r of a matrix of `rows` x `dim` is the first dim <= value_len values of one key, as in muon_step, so that an optimiser's numbers can lie next to
  * them.  Types, strides, n = 0, waiting, capture and `worker` are as for token models, above; a product counts as a pull of the keys that it uses: those of
- * groups that have rows, once each (and of the shared matrix).  Limits (PS_ELIMIT): PS_MAX_GROUPS groups, PS_EMB_MAX_TOKENS rows, and results of less than 2^24
- * tiles of 128 x 128.
- * Precision.  Where rows and result both have 16 bits, products are of numbers of the rows' type, to which the server's 32-bit numbers are rounded on the
- * way (beyond 65504 they become infinite in PS_F16); else of numbers of 32 bits.  Sums are in 32 bits; a result is rounded to its type once.  The
- * order of additions depends on the arguments only. */
+ * groups that have rows, once each (and of the shared matrix).  Limits (PS_ELIMIT): PS_MAX_GROUPS groups, PS_EMB_MAX_TOKENS rows, strides below 2^31, and
+ * fewer than 2^24 workgroups, each of which takes 64 x 64 numbers of a result at least (32 rows x 16 columns where there are 32 columns at most) and every
+ * group one more row of them.
+ * Precision.  Where rows and result both have 16 bits, products are of numbers of the rows' type, to which the server's 32-bit numbers, and an adapter's low-rank
+ * numbers between its two matrices, are rounded on the way (beyond 65504 they become infinite in PS_F16); else of numbers of 32 bits.  Sums are in 32 bits; a
+ * result is rounded to its type once.  The order of additions depends on the arguments only.
+ * Scratch, grown as needed (see above; a call that grows it cannot be captured): group_rows 512 bytes a group (of up to 2,046 groups and 2^21 rows), else 12 a row
+ * and the sort's; the others as they say. */
 #define PS_MAX_GROUPS 65536
 
 /* order, offsets: the rows 0 .. n - 1 by group, those of a group in increasing order (group e's are order[offsets[e]] .. order[offsets[e + 1] - 1]; offsets has
@@ -401,26 +405,30 @@ int group_rows(ps_handle ps, int32_t num_groups, const void *ids, int32_t id_typ
 /* out_q = W_e x_q for the n rows q of the order, e: the row's group, W_e: rows x dim, its row r under key first_key + e * rows + r; transposed != 0: out_q = W_e' x_q.
  * Zero for rows of no group.  A row of x may stand for several: row q is row q / x_pairs of x, which has n / x_pairs rows (the choices of one
  * token, next to each other).  With out_pairs > 1 the products of as many neighbouring rows are added up, in that order, in 32 bits: out has n / out_pairs rows
- * (this needs 4 n bytes of scratch per column).  So W_e' with x_pairs and out_pairs exchanged is the gradient with respect to x.  x_stride may be 0. */
+ * (this needs 4 n bytes of scratch per column).  Many rows of 16 bits: 2 bytes of scratch per number of the experts' matrices besides (sides count as multiples of 256 and
+ * of 32), up to 1 GiB.  So W_e' with x_pairs and out_pairs exchanged is the gradient with respect to x.  x_stride may be 0. */
 int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed, const int32_t *order,
                   const int32_t *offsets, int64_t n, const void *x, int32_t x_type, int64_t x_stride, int32_t x_pairs, void *out, int32_t out_type, int64_t out_stride,
                   int32_t out_pairs, void *stream);
 
 /* out[e][i][j] = sum over the rows q of group e of left[q / left_pairs][i] * right[q / right_pairs][j]: the matrices' gradients, num_experts contiguous
  * matrices of rows x dim, zero where a group has no rows - as muon_step takes them.  left and right have one type; rows of no group count for nothing.  (Of out = W x:
- * left the gradient of out, right x; of out = W' x the other way.)  rows, dim <= PS_EMB_MAX_DIM.  The server's values have no part in it. */
+ * left the gradient of out, right x; of out = W' x the other way.)  rows, dim <= PS_EMB_MAX_DIM.  The server's values have no part in it.  Scratch: up to 256 MiB, 512
+ * where the result has 16 bits. */
 int expert_grad(ps_handle ps, int32_t num_experts, int32_t rows, int32_t dim, const int32_t *order, const int32_t *offsets, int64_t n, const void *left, int64_t left_stride,
                 int32_t left_pairs, const void *right, int64_t right_stride, int32_t right_pairs, int32_t type, void *out, int32_t out_type, void *stream);
 
 /* out_p = W x_p + scale B_a (A_a x_p) for the n rows p of the order, a: the row's adapter; W x_p for rows of none.  W: rows x dim, keys first_key + r; A_a: rank x dim, keys
- * first_a + a * rank + i; B_a transposed: rank x rows, keys first_b + a * rank + i (rows <= value_len, too).  Scratch: 4 (rank + 3) bytes a row. */
+ * first_a + a * rank + i; B_a transposed: rank x rows, keys first_b + a * rank + i (rows <= value_len, too).  Scratch: 4 (rank + 1) bytes a row, rank as a multiple of eight, and for many
+ * rows of 16 bits 2 bytes per number of W and of all B. */
 int adapter_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t rows, int32_t dim, int64_t first_a, int64_t first_b, int32_t num_adapters, int32_t rank,
                    float scale, const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int32_t x_type, int64_t x_stride, void *out, int32_t out_type,
                    int64_t out_stride, void *stream);
 
 /* Its gradients, from that of out: dx_p = W' dout_p + scale A_a' (B_a' dout_p) (may be NULL: not wanted); da: of all A, num_adapters * rank x dim, and db: of all
  * B transposed, num_adapters * rank x rows, contiguous and fp32, in the order of their keys, zero for adapters without rows - as
- * emb_adagrad_step takes them with the keys as tokens.  x and dout have one type.  da and db are sums of products of numbers of 32 bits whatever the types. */
+ * emb_adagrad_step takes them with the keys as tokens.  x and dout have one type.  da and db are sums of products of numbers of 32 bits whatever the types.
+ * Scratch: 10 rank + 4 bytes a row, and as for adapter_matmul (of W and all A); up to 512 MiB for da and db. */
 int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int32_t rows, int32_t dim, int64_t first_a, int64_t first_b, int32_t num_adapters, int32_t rank,
                  float scale, const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int64_t x_stride, const void *dout, int64_t dout_stride, int32_t type,
                  void *dx, int32_t dx_type, int64_t dx_stride, float *da, float *db, void *stream);
