@@ -47,9 +47,10 @@ __device__ __forceinline__ RowTile row_tile(const RowGroups &g, int tile, int BM
         end = t.group + 1 == g.groups ? none : c < 63 ? __builtin_amdgcn_readlane(s, c + 1) : g.start(t.group + 1);
         s = __builtin_amdgcn_readlane(s, c);
     }
-    t.first = s + (tile - s / BM - t.group) * BM;
-    t.rows = end - t.first;
-    if (t.first < s || t.rows < 0) t.rows = 0;
+    // (a number that is none of the group's, where offsets do not rise, is not multiplied: it could pass 32 bits)
+    const int turn = tile - s / BM - t.group, last = (end - s) / BM;
+    t.first = s + (turn < 0 || turn > last ? 0 : turn) * BM;
+    t.rows = turn < 0 || turn > last || end < t.first ? 0 : end - t.first;
     if (t.rows > BM) t.rows = BM;
     t.start = s;
     t.end = end;

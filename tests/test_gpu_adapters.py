@@ -173,6 +173,39 @@ def test_strides_and_shapes(kind):
             assert torch.equal(got, known)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("n", [40, 700, 9000])
+def test_orders_that_are_none_do_no_harm(kind, n):
+    """As products with experts: numbers out of range are found where they are read, offsets that do not rise are nobody's rows."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    adapters, rank, rows, dim = 3, 8, 1024, 64
+    first_a, first_b = rows, rows + adapters * rank
+    srv, _ = _server(first_b + adapters * rank, 1024, seed=n, scale=0.1)
+    x, dout = _randn(1, n, dim, kind=kind).cuda(), _randn(2, n, rows, kind=kind).cuda()
+    calls = (lambda g: srv.adapter_matmul(x, g, 0, rows, first_a, first_b, rank, dim=dim), lambda g: srv.adapter_grad(x, dout, g, 0, first_a, first_b, rank),
+             lambda g: srv.expert_matmul(x, g, 0, rows // 4, dim=dim), lambda g: srv.expert_matmul(dout, g, 0, 64, dim=1024, transposed=False),
+             lambda g: srv.expert_grad(dout, x, g))
+    order = torch.arange(n, dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, n // 3, n // 2, n], dtype=torch.int32, device="cuda")
+    good = [call((order, offsets)) for call in calls]
+    for wrong in (-1, n, 1 << 30, -(1 << 31)):
+        bad = order.clone()
+        bad[n // 2] = wrong
+        for call in calls:
+            call((bad, offsets))
+            with pytest.raises(P.PSError) as e:
+                srv.status()
+            assert e.value.code == P.PS_EKEY
+    for wrong in ([0, -5, n, 2 * n], [n, n, n, n], [5, 3, 2, 1], [0, 1 << 30, -(1 << 31), 7]):
+        for call in calls:
+            call((order, torch.tensor(wrong, dtype=torch.int32, device="cuda")))
+            srv.status()
+    for call, was in zip(calls, good):                                  # and nothing of it stays
+        for got, want in zip(*((r if isinstance(r, tuple) else (r,)) for r in (call((order, offsets)), was))):
+            assert torch.equal(got, want)
+
+
 def test_gradients_of_millions_of_rows():
     """Chunks of more rows than a workgroup holds the numbers of; sums of numbers of 0 and 1, which are exact in 32 bits (below 8 x 2^21), in whatever order."""
     import torch
