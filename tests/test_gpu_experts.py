@@ -266,6 +266,35 @@ def test_pairs(kind, tokens, k):
     _close(srv.expert_matmul(one, groups, 0, rows, dim=dim), want, mag, _terms_off(kind, kind == "float32", dim), kind, small)
 
 
+@pytest.mark.parametrize("dim", [7, 8])
+def test_beyond_32_bits(dim):
+    """Matrices at the end of a server of more than 2^31 numbers, rows and results of as many; numbers of 0 and 1, whose sums are exact."""
+    import torch
+    from paper_2002_00655_amd import ps as P
+    n, rows, experts, L = 2_200_002, 1024, 2, 1024
+    first = 2_200_000
+    srv = P.ParameterServer(first + experts * rows, L, 1)
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    w = torch.randint(0, 2, (experts * rows, L), device="cuda", generator=g).float()
+    srv.push(torch.arange(first, first + experts * rows, device="cuda"), w)
+    ids = torch.where(torch.rand(n, device="cuda", generator=g) < 0.6, 1, 0)
+    ids[::19] = -1
+    groups = srv.group_rows(ids, experts, pad=-1)
+    x = torch.zeros(n, 1024, dtype=torch.bfloat16, device="cuda")[:, :dim]
+    x.copy_(torch.randint(0, 2, (n, dim), device="cuda", generator=g))
+    out = srv.expert_matmul(x, groups, first, rows, dim=dim)
+    back = srv.expert_matmul(out, groups, first, rows, dim=dim, transposed=True, sum_pairs=2, dtype=torch.float32)
+    m = w.view(experts, rows, L)[:, :, :dim]
+    for i in range(0, n, 200_000):
+        j = min(n, i + 200_000)
+        one = torch.stack([(ids[i:j] == e).float() for e in range(experts)])
+        want = sum((x[i:j].float() * one[e][:, None]) @ m[e].t() for e in range(experts))
+        assert torch.equal(out[i:j].float(), want), i
+        want = sum((want * one[e][:, None]) @ m[e] for e in range(experts))
+        assert torch.equal(back[i // 2:j // 2], want.view(-1, 2, dim).sum(1)), i
+    srv.status()
+
+
 # ---- expert_grad ----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("n,experts,rows,dim", [(0, 3, 5, 7), (1, 2, 1, 1), (5, 9, 16, 24), (200, 3, 64, 65), (333, 5, 100, 127), (700, 4, 72, 136), (3000, 2, 136, 264),
