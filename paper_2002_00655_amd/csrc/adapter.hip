@@ -149,7 +149,7 @@ template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, cons
 }
 template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     const int64_t few = ceil_div64(a.g.n, 16) * ceil_div64(a.N, TURNED ? 64 : 16);
-    if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * ps->num_cu) return few_of<CT, XT, TURNED, 1>(ps, a, st);      // (as products with experts)
+    if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * ps->num_cu) return few_of<CT, XT, TURNED, 1>(ps, a, st);      // (as products with few experts)
     if (sizeof(CT) == 4 || 2 * ceil_div64(a.g.n, 128) * ceil_div64(a.N, 128) < ps->num_cu) return tiles_of<CT, XT, TURNED, Tile64>(ps, a, st);
     return tiles_of<CT, XT, TURNED, Tile128>(ps, a, st);
 }

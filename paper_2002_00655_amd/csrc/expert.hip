@@ -7,6 +7,8 @@
 // puts as much error on a result as its own rounding does (2^-9 or 2^-12 of each term at most, on average over the terms).  Else of numbers of 32 bits.
 #include "experts.h"
 
+#include <algorithm>
+
 namespace {
 
 struct ExpertCall { ExpertArgs a[2]; };
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertCall cal
 }
 
 // Groups of few rows: 16 rows a workgroup, whose wavefronts share the sum, so that a chain is short and all of a matrix is asked for at once.  One token of two experts of
-// 512 x 512: 5.5 us; 3,998 rows of 7 experts, 32 bits, 400 x 127 turned: 16.0.
+// 512 x 512: 5.5 us; 333 rows of 5, 400 x 100 turned, 32 bits: 7.5.
 template <class CT, class XT, bool TURNED, int MT>
 __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expert_few(ExpertCall call, int32_t col_tiles, int32_t *err) {
     const ExpertArgs &a = call.a[blockIdx.y];
@@ -155,7 +157,10 @@ template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const Ex
     //   16 bits, 128 rows of 16 groups x 256 columns 8.0 us and by tiles of 64 8.0, x 512 9.7 and 8.0;   turned, 500 rows of 8 groups x 512 8.4 and 9.2, x 1024 12.3 and 9.5;
     //   32 bits, 333 rows of 5 groups x 400, K 100, 6.6 and 8.0, 1,000 rows 10.5 and 8.1
     const int64_t few = ceil_div64(n + 8 * (groups < n ? groups : n), 16) * ceil_div64(a.N, TURNED ? 64 : 16) * count;
-    if (4 * few <= (sizeof(CT) == 4 ? 16 : TURNED ? 8 : 5) * cus) return few_of<CT, XT, TURNED, 1>(ps, c, count, st);
+    // Turned in 32 bits, the longer the sum the more of them, as it is a tile's chain and shared by wavefronts here: 400 x 127, K 400, 3,998 rows of 64 experts 31.3 us and
+    // 16.5 by tiles of 64, 1,000 rows 12.8 and 15.5;   1024 x 512, K 1024, 1,000 rows of 64 41 and 64
+    const int64_t limit = sizeof(CT) == 4 ? (TURNED ? std::min(std::max(a.K / 64, 4), 16) : 16) : TURNED ? 8 : 5;
+    if (4 * few <= limit * cus) return few_of<CT, XT, TURNED, 1>(ps, c, count, st);
     // 32 columns: tiles of 128 rows (16,384 rows of 8 groups, 16 bits, 13.0 us, and 21.2 by the kernel for few rows; 100,000 of 16 groups, 32 bits, 131 and 213), but where the
     // rows' numbers are made longer on their way (two of 16,384 rows of 16 groups, K 512, 26 and 16.5)
     if (a.N <= 32) return sizeof(CT) != sizeof(XT) ? few_of<CT, XT, TURNED, 2>(ps, c, count, st) : tiles_of<CT, XT, TURNED, Narrow>(ps, c, count, st);
