@@ -37,7 +37,7 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_expert(ExpertCall cal
     __syncthreads();
     if (off) return;
     floatx16 acc[T::MC][T::MR] = {};
-    const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR, cols = a.N - c0;
+    const int wave = tid >> 6, wc = wave % T::WC * 32 * T::MC, wr = wave / T::WC * 32 * T::MR, cols = a.columns() - c0;
     if (t.group < a.g.groups) {
         const float *w = a.w + (int64_t)t.group * a.each * a.L;
         KMajor<XT, CT, BR, T::THREADS> rows[T::SETS];
@@ -95,7 +95,7 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expe
     __syncthreads();
     if (t.group < a.g.groups) {
         F f;
-        f.run(a.w + (int64_t)t.group * a.each * a.L, a.L, a.K, c0, a.N,
+        f.run(a.w + (int64_t)t.group * a.each * a.L, a.L, a.K, c0, a.columns(),
               [&](int r) { return reinterpret_cast<const XT *>(a.x) + a.x_shared(at[r] < 0 ? 0 : at[r]) * a.x_stride; });
         f.put(sums);
     }

@@ -15,7 +15,8 @@ struct ExpertArgs {
     int32_t precise;                                                         // products of numbers of 32 bits
     int32_t *group_of;                                                       // not NULL: the group of the row at place p
     void *also; int64_t also_stride; int32_t also_type;                      // not NULL: the result once more, in another type
-    int32_t zero_from;                                                       // the columns from here on, up to N, are written as zeros; 0: none
+    int32_t zero_from;                                                       // the columns from here on, up to N, have no key: they are written as zeros; 0: none
+    __host__ __device__ int32_t columns() const { return zero_from ? zero_from : N; }      // that may be read; one at least in every workgroup's columns
 };
 // count: one, or two of the same groups, columns and types in one launch
 int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs *a, int count, hipStream_t st);
@@ -96,7 +97,7 @@ template <class CT, class XT, bool TURNED, int MT> struct FewRows {
         if (k + 16 < K) hi = load_some<ST, 4>(p + k + 16, K - k - 16);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    // w: where the matrix starts; c0: its first column here; x_of(r): where row r < 16 MT of the tile is (any row where there is none)
+    // w: where the matrix starts; c0: its first column here; N: the columns that it has; x_of(r): where row r < 16 MT of the tile is (any row where there is none)
     template <class F> __device__ __forceinline__ void run(const float *w, int64_t L, int K, int c0, int N, F x_of) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
         const int steps = (K + STEP - 1) / STEP, s0 = steps * wave / WAVES, s1 = steps * (wave + 1) / WAVES;

@@ -1,0 +1,84 @@
+"""CPU: what the calls of models of many matrices launch, with a stand-in for the HIP runtime (tests/_hip_launches.hip): the numbers of the server that
+low-rank products read."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PACKAGE = os.path.join(ROOT, "paper_2002_00655_amd")
+
+PROGRAM = r"""
+import ctypes as C, sys
+stub, lib = C.CDLL(sys.argv[1], C.RTLD_GLOBAL), C.CDLL(sys.argv[2])
+i32, i64, f, vp = C.c_int32, C.c_int64, C.c_float, C.c_void_p
+for name in ("launch_groups", "launch_reads_from", "launch_reads_to", "allocated", "largest_allocation"):
+    getattr(stub, name).restype = i64
+stub.launch_name.restype = C.c_char_p
+lib.ps_last_error.restype = C.c_char_p
+at = lambda x: vp(x << 32)                           # tensors: addresses, on 16 bytes
+F32, BF16, F16 = 0, 1, 2
+def server(keys, values):
+    h = vp()
+    assert lib.ps_create(i64(keys), i32(values), i32(1), C.byref(h)) == 0
+    stub.launch_clear()
+    return h
+def launches():
+    n = stub.launch_count()
+    got = [(stub.launch_name(i).decode(), stub.launch_groups(i), stub.launch_reads_from(i), stub.launch_reads_to(i)) for i in range(n)]
+    stub.launch_clear()
+    return got
+def adapter_matmul(h, n, rows, dim, first_a, first_b, adapters, rank, kind, out_kind=None):
+    return lib.adapter_matmul(h, i32(-1), i64(0), i32(rows), i32(dim), i64(first_a), i64(first_b), i32(adapters), i32(rank), f(1), at(1), at(2), i64(n), at(3), i32(kind),
+                              i64(dim), at(4), i32(kind if out_kind is None else out_kind), i64(rows), None)
+def adapter_grad(h, n, rows, dim, first_a, first_b, adapters, rank, kind, dx=True):
+    return lib.adapter_grad(h, i32(-1), i64(0), i32(rows), i32(dim), i64(first_a), i64(first_b), i32(adapters), i32(rank), f(1), at(1), at(2), i64(n), at(3), i64(dim),
+                            at(4), i64(rows), i32(kind), at(5) if dx else None, i32(kind), i64(dim), at(6), at(7), None)
+def expert_matmul(h, n, experts, rows, dim, kind, turned=0, x_pairs=1, out_pairs=1):
+    return lib.expert_matmul(h, i32(-1), i64(0), i32(experts), i32(rows), i32(dim), i32(turned), at(1), at(2), i64(n), at(3), i32(kind), i64(rows if turned else dim),
+                             i32(x_pairs), at(4), i32(kind), i64(dim if turned else rows), i32(out_pairs), None)
+exec(sys.argv[3])
+"""
+
+
+@pytest.fixture(scope="module")
+def run(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("launches") / "launches.so")
+    subprocess.check_call(["hipcc", "--offload-arch=gfx950", "--offload-host-only", "-O1", "-std=c++17", "-shared", "-fPIC", "-Wno-unused-command-line-argument",
+                           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(PACKAGE, "csrc"), os.path.join(ROOT, "tests", "_hip_launches.hip"), "-o", so])
+    lib = os.path.join(PACKAGE, "libdpaps.so")
+    if not os.path.exists(lib):
+        from paper_2002_00655_amd import build
+        build.build(verbose=False)
+
+    def program(steps):
+        r = subprocess.run([sys.executable, "-c", PROGRAM, so, lib, steps], capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0, r.stderr[-2000:]
+    return program
+
+
+def test_products_with_adapters_read_their_keys_only(run):
+    """Nothing behind the last adapter's matrices, whatever the rank: the last key of the server may be theirs."""
+    run("""
+laid = 0
+for rank in range(1, 65):
+    for rows, dim, n, adapters in ((1024, 1024, 8192, 16), (72, 1000, 13000, 5), (1000, 72, 13000, 20), (512, 512, 300, 7), (96, 128, 5, 3), (1024, 1024, 2000, 200)):
+        for kind in (F32, BF16, F16):
+            for b_last in (True, False):
+                L, W = max(rows, dim), adapters * rank
+                keys = rows + 2 * W
+                h = server(keys, L)
+                first_a, first_b = (rows, rows + W) if b_last else (rows + W, rows)
+                assert adapter_matmul(h, n, rows, dim, first_a, first_b, adapters, rank, kind) == 0
+                for dx in (True, False):
+                    assert adapter_grad(h, n, rows, dim, first_a, first_b, adapters, rank, kind, dx) == 0
+                got = launches()
+                laid += sum("k_laid" in name for name, *_ in got) if rank % 8 else 0
+                products = [l for l in got if "k_expert" in l[0] or "k_adapter" in l[0]]
+                assert products
+                for name, _, first, end in products:
+                    assert 0 <= first < end <= keys * L, (rank, rows, dim, n, kind, name, end, keys * L)
+                lib.ps_destroy(h)
+assert laid > 0
+""")
