@@ -420,7 +420,7 @@ int expert_grad(ps_handle ps, int32_t num_experts, int32_t rows, int32_t dim, co
 
 /* out_p = W x_p + scale B_a (A_a x_p) for the n rows p of the order, a: the row's adapter; W x_p for rows of none.  W: rows x dim, keys first_key + r; A_a: rank x dim, keys
  * first_a + a * rank + i; B_a transposed: rank x rows, keys first_b + a * rank + i (rows <= value_len, too).  Scratch: 4 (rank + 1) bytes a row, rank as a multiple of eight, and for many
- * rows of 16 bits 2 bytes per number of W and of all B. */
+ * rows of 16 bits 2 bytes per number of W and of all B (rows count as a multiple of 256, dim and rank of 32), up to 1 GiB. */
 int adapter_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t rows, int32_t dim, int64_t first_a, int64_t first_b, int32_t num_adapters, int32_t rank,
                    float scale, const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int32_t x_type, int64_t x_stride, void *out, int32_t out_type,
                    int64_t out_stride, void *stream);
@@ -428,7 +428,8 @@ int adapter_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t rows
 /* Its gradients, from that of out: dx_p = W' dout_p + scale A_a' (B_a' dout_p) (may be NULL: not wanted); da: of all A, num_adapters * rank x dim, and db: of all
  * B transposed, num_adapters * rank x rows, contiguous and fp32, in the order of their keys, zero for adapters without rows - as
  * emb_adagrad_step takes them with the keys as tokens.  x and dout have one type.  da and db are sums of products of numbers of 32 bits whatever the types.
- * Scratch: 10 rank + 4 bytes a row, and as for adapter_matmul (of W and all A); up to 512 MiB for da and db. */
+ * Scratch: 10 rank + 4 bytes a row, rank as a multiple of eight, and, if dx is wanted, as for adapter_matmul (of W and all A, dim a multiple of 256, rows and rank of 32); up to
+ * 512 MiB for da and db. */
 int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int32_t rows, int32_t dim, int64_t first_a, int64_t first_b, int32_t num_adapters, int32_t rank,
                  float scale, const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int64_t x_stride, const void *dout, int64_t dout_stride, int32_t type,
                  void *dx, int32_t dx_type, int64_t dx_stride, float *da, float *db, void *stream);

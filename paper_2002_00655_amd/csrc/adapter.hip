@@ -186,11 +186,14 @@ struct Scratch {
     int64_t stride = 0, rounded_stride = 0, w_size = 0, b_size = 0;
     size_t numbers[2] = {}, rounded = 0, group_of = 0, w = 0, b = 0, end = 0;
 };
-// both: the numbers in 32 bits of two products, which gradients need
-Scratch scratch_of(const dpaps_ps *ps, const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both) {
+// both: the numbers in 32 bits of two products, which gradients need; product: whether there is one with the shared matrix
+Scratch scratch_of(const dpaps_ps *ps, const RowGroups &g, const void *x, int64_t x_stride, int32_t K, int32_t N, int32_t rank, bool precise, bool both, bool product) {
     Scratch s;
     const int64_t n = g.n;
-    s.laid = !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 3 * ps->num_cu / 2 && n >= 64 * (int64_t)g.groups && g.groups < 32768 && dpaps_laid_fits(x, x_stride, K);
+    s.w_size = dpaps_laid_size(K, N);
+    s.b_size = dpaps_laid_size(rank, N);
+    s.laid = product && !precise && ceil_div64(n, 128) * ceil_div64(N, 128) >= 3 * ps->num_cu / 2 && n >= 64 * (int64_t)g.groups && g.groups < 32768 &&
+             dpaps_laid_fits(x, x_stride, K) && s.w_size + s.b_size * g.groups <= LAID_MOST;
     s.rounded_stride = (rank + 7) / 8 * 8;
     s.stride = s.rounded_stride;
     const auto take = [&](int64_t bytes) { const size_t at = s.end; s.end += ((size_t)bytes + 255) / 256 * 256; return at; };
@@ -199,8 +202,6 @@ Scratch scratch_of(const dpaps_ps *ps, const RowGroups &g, const void *x, int64_
     s.group_of = take(n * 4);
     if (s.laid) {
         s.rounded = take(n * s.rounded_stride * 2);
-        s.w_size = dpaps_laid_size(K, N);
-        s.b_size = dpaps_laid_size(rank, N);
         s.w = take(s.w_size * 2);
         s.b = take(s.b_size * 2 * g.groups);
     }
@@ -255,7 +256,7 @@ extern "C" int adapter_matmul(ps_handle ps, int32_t worker, int64_t first_key, i
     if (!dpaps_strides_fit(ps, x_stride, out_stride)) return PS_ELIMIT;
     hipStream_t st = (hipStream_t)stream;
     const bool precise = x_type == PS_F32 || out_type == PS_F32;
-    const Scratch s = scratch_of(ps, g, x, x_stride, dim, rows, rank, precise, false);
+    const Scratch s = scratch_of(ps, g, x, x_stride, dim, rows, rank, precise, false, true);
     rc = dpaps_ws_reserve(ps, s.end);
     if (rc) return rc;
     const LowNumbers low = low_of((char *)ps->ws, s, false, true, 0);
@@ -282,7 +283,7 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
     if (n > 0 && (!x || !dout || x_stride < 0 || dout_stride < 0 || (dx && dx_stride < dim))) return PS_EINVAL;
     if (n > 0 && (!dpaps_strides_fit(ps, x_stride, dout_stride) || !dpaps_strides_fit(ps, dx ? dx_stride : 0, 0))) return PS_ELIMIT;
     hipStream_t st = (hipStream_t)stream;
-    const Scratch s = scratch_of(ps, g, dout, dout_stride, rows, dim, rank, type == PS_F32 || dx_type == PS_F32, true);
+    const Scratch s = scratch_of(ps, g, dout, dout_stride, rows, dim, rank, type == PS_F32 || dx_type == PS_F32, true, dx != nullptr);
     OuterArgs o[2]{};
     for (int i = 0; i < 2; ++i) {
         o[i].g = g; o[i].left_stride = s.stride; o[i].left_type = PS_F32; o[i].left_by_place = 1; o[i].rows = rank; o[i].out_type = PS_F32; o[i].right_type = type;
@@ -292,10 +293,10 @@ extern "C" int adapter_grad(ps_handle ps, int32_t worker, int64_t first_key, int
     rc = dpaps_ws_reserve(ps, s.end + dpaps_outer_bytes(ps, o, 2));
     if (rc) return rc;
     char *ws = (char *)ps->ws;
-    const LowNumbers h = low_of(ws, s, true, false, 0), t = low_of(ws, s, true, dx != nullptr, 1);
+    const LowNumbers h = low_of(ws, s, true, false, 0), t = low_of(ws, s, true, true, 1);
     const float *pa = ps->val + first_a * ps->L, *pb = ps->val + first_b * ps->L;
     if (n > 0) {
-        const int32_t columns = (int32_t)(s.laid && dx ? s.rounded_stride : rank);
+        const int32_t columns = (int32_t)(s.laid ? s.rounded_stride : rank);
         const ExpertArgs both[2] = {low_numbers(ps, g, x, type, x_stride, dim, pa, rank, scale, true, h, columns),
                                     low_numbers(ps, g, dout, type, dout_stride, rows, pb, rank, scale, true, t, columns)};
         rc = dpaps_expert_product(ps, both, 2, st);

@@ -184,7 +184,7 @@ int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs *a, int count, hipStream
 
 // From so many rows a group on, and tiles of 128 x 128 for two workgroups a compute unit, matrices are laid before the product (laid.hip): 16,384 rows of 8 groups,
 // bf16, 2048 x 1024, 108 us with the laying and 113 by tiles, 1024 x 1024 60 and 68; of 16 groups, 1,024 rows each, 69 and 74, 2048 x 1024 124 and 114; 8,192 rows of 16, 52 and 62.
-constexpr int64_t LAID_ROWS = 1024, LAID_MOST = (int64_t)1 << 29;   // ... of at most a GiB
+constexpr int64_t LAID_ROWS = 1024;
 
 extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed,
                              const int32_t *order, const int32_t *offsets, int64_t n, const void *x, int32_t x_type, int64_t x_stride, int32_t x_pairs, void *out,

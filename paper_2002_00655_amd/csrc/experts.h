@@ -71,7 +71,8 @@ struct LayArgs {
     int32_t K, N, turned;
     void *to; int64_t size;
 };
-int64_t dpaps_laid_size(int32_t K, int32_t N);
+int64_t dpaps_laid_size(int32_t K, int32_t N);                               // elements of a laid matrix: N as a multiple of 256, K of 32
+constexpr int64_t LAID_MOST = (int64_t)1 << 29;                              // elements that a call lays, at most: a GiB; beyond that its products go by tiles
 bool dpaps_laid_fits(const void *x, int64_t x_stride, int32_t K);
 // `each`: of the matrices of all groups that have rows (each.each: how many keys one has), and, if `one` is there, of a single one, in the same launch
 int dpaps_lay(dpaps_ps *ps, const RowGroups &g, int32_t type, const LayArgs &each, const LayArgs *one, hipStream_t st);

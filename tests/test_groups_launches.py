@@ -1,5 +1,5 @@
 """CPU: what the calls of models of many matrices launch, with a stand-in for the HIP runtime (tests/_hip_launches.hip): the numbers of the server that
-low-rank products read."""
+low-rank products read, and how much scratch laid matrices take."""
 import os
 import subprocess
 import sys
@@ -81,4 +81,33 @@ for rank in range(1, 65):
                     assert 0 <= first < end <= keys * L, (rank, rows, dim, n, kind, name, end, keys * L)
                 lib.ps_destroy(h)
 assert laid > 0
+""")
+
+
+def test_laid_adapters_are_bounded(run):
+    """Matrices are laid up to a GiB: a call of many adapters goes by tiles where its laid matrices would be more, and a gradient that is not asked for dx lays none."""
+    run("""
+room = 1.25                                          # what a server's scratch is larger than it has to be
+def up(x, by): return -(-x // by) * by
+for rows, rank, adapters, n in ((1024, 4, 32767, 64 * 32767), (1024, 64, 8000, 64 * 8000), (1024, 16, 200, 20000), (64, 4, 32767, 64 * 32767), (256, 33, 2000, 400000)):
+    dim = 1024
+    h = server(rows + 2 * adapters * rank, 1024)
+    for grad in (False, True):
+        K, N = (rows, dim) if grad else (dim, rows)
+        laid = 2 * up(K, 32) * up(N, 256) + 2 * adapters * up(rank, 32) * up(N, 256)
+        numbers = (10 if grad else 4) * up(rank, 8) * n + 4 * n
+        most = room * (numbers + min(laid, 1 << 30) + (1 << 29 if grad else 0) + 4096) + 4096
+        before = stub.allocated()
+        stub.refuse_allocations_from(i64(int(most) + 1))
+        args = (h, n, rows, dim, rows, rows + adapters * rank, adapters, rank, BF16)
+        if grad:
+            assert adapter_grad(*args, dx=False) == 0
+            got = launches()
+            assert not any("k_lay" in l[0] or "k_laid" in l[0] for l in got)
+            assert adapter_grad(*args) == 0, (rows, rank, adapters, lib.ps_last_error(h))
+        else:
+            assert adapter_matmul(*args) == 0, (rows, rank, adapters, lib.ps_last_error(h))
+        assert any("k_laid" in l[0] for l in launches()) == (laid <= 1 << 30), (rows, rank, adapters, grad)
+        stub.refuse_allocations_from(i64(1 << 62))
+    lib.ps_destroy(h)
 """)
