@@ -128,11 +128,13 @@ __global__ __launch_bounds__(256) void k_pair_sums(const float *in, int64_t n, i
 }  // namespace
 
 namespace {
+constexpr int64_t MOST_GRID = (int64_t)1 << 24;                      // workgroups of a launch, fewer
+
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
     const ExpertArgs &a = c.a[0];
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
     const int64_t tiles = row_tiles(a.g.n, a.g.groups, T::ROWS), grid = tiles * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
+    if (grid >= MOST_GRID) return dpaps_too_large(ps, "product");
     static LdsAllowed allowed;
     const int rc = dpaps_allow_lds(ps, allowed, reinterpret_cast<const void *>(&k_expert<CT, XT, TURNED, T>), T::LDS);
     if (rc) return rc;
@@ -140,12 +142,15 @@ template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, c
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
 }
+template <class CT, class XT, bool TURNED, int MT> int64_t few_grid(const ExpertArgs &a) {
+    return row_tiles(a.g.n, a.g.groups, 16 * MT) * ceil_div64(a.N, FewRows<CT, XT, TURNED, MT>::COLS);
+}
 template <class CT, class XT, bool TURNED, int MT> int few_of(dpaps_ps *ps, const ExpertCall &c, int count, hipStream_t st) {
     const ExpertArgs &a = c.a[0];
     typedef FewRows<CT, XT, TURNED, MT> F;
     const int32_t col_tiles = (a.N + F::COLS - 1) / F::COLS;
-    const int64_t grid = row_tiles(a.g.n, a.g.groups, 16 * MT) * col_tiles;
-    if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "product");
+    const int64_t grid = few_grid<CT, XT, TURNED, MT>(a);
+    if (grid >= MOST_GRID) return dpaps_too_large(ps, "product");
     k_expert_few<CT, XT, TURNED, MT><<<dim3((unsigned)grid, (unsigned)count), F::THREADS, 0, st>>>(c, col_tiles, ps->err);
     PS_HIP(ps, hipGetLastError());
     return PS_OK;
@@ -160,7 +165,8 @@ template <class CT, class XT, bool TURNED> int product_of(dpaps_ps *ps, const Ex
     // Turned in 32 bits, the longer the sum the more of them, as it is a tile's chain and shared by wavefronts here: 400 x 127, K 400, 3,998 rows of 64 experts 31.3 us and
     // 16.5 by tiles of 64, 1,000 rows 12.8 and 15.5;   1024 x 512, K 1024, 1,000 rows of 64 41 and 64
     const int64_t limit = sizeof(CT) == 4 ? (TURNED ? std::min(std::max(a.K / 64, 4), 16) : 16) : TURNED ? 8 : 5;
-    if (4 * few <= limit * cus) return few_of<CT, XT, TURNED, 1>(ps, c, count, st);
+    // (which launches workgroups for all groups: where those are too many, a quarter as many by tiles of 64)
+    if (4 * few <= limit * cus && few_grid<CT, XT, TURNED, 1>(a) < MOST_GRID) return few_of<CT, XT, TURNED, 1>(ps, c, count, st);
     // 32 columns: tiles of 128 rows (16,384 rows of 8 groups, 16 bits, 13.0 us, and 21.2 by the kernel for few rows; 100,000 of 16 groups, 32 bits, 131 and 213), but where the
     // rows' numbers are made longer on their way (two of 16,384 rows of 16 groups, K 512, 26 and 16.5)
     if (a.N <= 32) return sizeof(CT) != sizeof(XT) ? few_of<CT, XT, TURNED, 2>(ps, c, count, st) : tiles_of<CT, XT, TURNED, Narrow>(ps, c, count, st);

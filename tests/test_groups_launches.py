@@ -111,3 +111,31 @@ for rows, rank, adapters, n in ((1024, 4, 32767, 64 * 32767), (1024, 64, 8000, 6
         stub.refuse_allocations_from(i64(1 << 62))
     lib.ps_destroy(h)
 """)
+
+
+def test_few_rows_of_many_groups(run):
+    """Calls within the limit that the header states, workgroups of 64 x 64 numbers (32 x 16 of 32 columns and fewer) and one more row of them for each group, are taken."""
+    run("""
+import random
+rng = random.Random(3)
+def log_int(lo, hi): return int(round(lo * (hi / lo) ** rng.random()))
+cases = [(1, 65536, 4096, 1), (1, 65536, 1024, 8), (3, 5000, 65536, 1), (64, 65536, 16384, 2), (40, 65536, 40, 1024), (1, 65536, 16383, 1)]
+cases += [(log_int(1, 3000), log_int(1, 65536), log_int(1, 65536), log_int(1, 32)) for _ in range(300)]
+taken = 0
+for n, experts, rows, dim in cases:
+    if experts * rows > 1 << 31: continue
+    h = server(experts * rows, dim)
+    for turned in (0, 1):
+        N = dim if turned else rows
+        groups = (n // 64 + experts + 1) * -(-N // 64) if N > 32 else (n // 32 + experts + 1) * -(-N // 16)
+        for kind in (F32, BF16, F16):
+            rc = expert_matmul(h, n, experts, rows, dim, kind, turned)
+            got = [l for l in launches() if "k_expert" in l[0] or "k_laid" in l[0]]
+            if groups < 1 << 24:
+                assert rc == 0, (n, experts, rows, dim, turned, kind, lib.ps_last_error(h))
+                taken += 1
+            if rc == 0: assert len(got) == 1 and got[0][1] < (1 << 24) + 256, (got, n, experts, rows, dim)
+            else: assert rc == -9 and not got
+    lib.ps_destroy(h)
+assert taken > 500, taken
+""")
