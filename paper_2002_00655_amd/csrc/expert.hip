@@ -116,14 +116,17 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expe
 __global__ __launch_bounds__(256) void k_pair_sums(const float *in, int64_t n, int32_t b, int32_t N, void *out, int32_t out_type, int64_t out_stride, uint32_t P, double inv_P,
                                                    const int32_t *err) {
     if (*(volatile const int32_t *)err) return;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, t = quotient(i, P, inv_P);
-    if (t >= n) return;
-    const int c = (int)(i - t * P) * 4, left = N - c;
-    const float *p = in + t * b * N + c;
-    Vec<float, 4> v = load_some<float, 4>(p, left);
-    for (int j = 1; j < b; ++j) v = v + load_some<float, 4>(p + (int64_t)j * N, left);
-    put_typed<4>(out, out_type, t * out_stride + c, v, left);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = quotient(i, P, inv_P);
+        if (t >= n) return;
+        const int c = (int)(i - t * P) * 4, left = N - c;
+        const float *p = in + t * b * N + c;
+        Vec<float, 4> v = load_some<float, 4>(p, left);
+        for (int j = 1; j < b; ++j) v = v + load_some<float, 4>(p + (int64_t)j * N, left);
+        put_typed<4>(out, out_type, t * out_stride + c, v, left);
+    }
 }
+constexpr int64_t PAIR_SUMS_GRID = (int64_t)1 << 20;
 
 }  // namespace
 
@@ -233,8 +236,7 @@ extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, in
     if (out_pairs > 1) {
         const uint32_t P = (uint32_t)((N + 3) / 4);
         const int64_t blocks = ceil_div64(n / out_pairs * P, 256);
-        if (blocks >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "expert_matmul");
-        k_pair_sums<<<(unsigned)blocks, 256, 0, st>>>((const float *)ps->ws, n / out_pairs, out_pairs, N, out, out_type, out_stride, P, 1.0 / P, ps->err);
+        k_pair_sums<<<(unsigned)std::min(blocks, PAIR_SUMS_GRID), 256, 0, st>>>((const float *)ps->ws, n / out_pairs, out_pairs, N, out, out_type, out_stride, P, 1.0 / P, ps->err);
         PS_HIP(ps, hipGetLastError());
     }
     GroupKeys k;

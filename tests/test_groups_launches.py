@@ -139,3 +139,15 @@ for n, experts, rows, dim in cases:
     lib.ps_destroy(h)
 assert taken > 500, taken
 """)
+
+
+def test_sums_over_pairs_of_any_size(run):
+    """Products summed over pairs have the limit of the products, which come first."""
+    run("""
+for n, K, N, pairs in ((1 << 25, 8, 1024, 2), (1 << 26, 8, 1024, 4), ((1 << 21) + 6, 8, 1024, 2), (6, 8, 5, 3)):
+    h = server(K, 1024)
+    assert expert_matmul(h, n, 1, K, N, BF16, turned=1, out_pairs=pairs) == 0, (n, lib.ps_last_error(h))
+    got = [l for l in launches() if "k_pair_sums" in l[0]]
+    assert len(got) == 1 and got[0][1] < 1 << 24
+    lib.ps_destroy(h)
+""")
