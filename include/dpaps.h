@@ -389,8 +389,8 @@ int muon_step(ps_handle ps, int32_t worker, int64_t first_key, int32_t batch, in
  * fewer than 2^24 workgroups, each of which takes 64 x 64 numbers of a result at least (32 rows x 16 columns where there are 32 columns at most) and every
  * group one more row of them.
  * Precision.  Where rows and result both have 16 bits, products are of numbers of the rows' type, to which the server's 32-bit numbers, and an adapter's low-rank
- * numbers between its two matrices, are rounded on the way (beyond 65504 they become infinite in PS_F16); else of numbers of 32 bits.  Sums are in 32 bits; a
- * result is rounded to its type once.  The order of additions depends on the arguments only.
+ * numbers between its two matrices, are rounded on the way (beyond 65504 they become infinite in PS_F16), however many rows a call has; else of numbers of 32
+ * bits, as the low-rank numbers of adapter_grad always are.  Sums are in 32 bits; a result is rounded to its type once.  The order of additions depends on the arguments only.
  * Scratch, grown as needed (see above; a call that grows it cannot be captured): group_rows 512 bytes a group (of up to 2,046 groups and 2^21 rows), else 12 a row
  * and the sort's; the others as they say. */
 #define PS_MAX_GROUPS 65536

@@ -4,8 +4,8 @@
 //   dx_p = W' dy_p + s A_a' (B_a' dy_p)
 //   dA_a = s sum over a's rows of (B_a' dy_p) x_p',     dB_a' = s sum of (A_a x_p) dy_p'
 // W, the rows of A_a and the rows of B_a' (both `rank` keys of an adapter) lie in the server.  The low-rank numbers s A_a x_p and s B_a' dy_p are worked out first, in the
-// order of the groups, and kept in 32 bits; the second launch goes on, after the sum over W's side, with those of the adapters of its rows.  (Where products are of 16 bits,
-// tiles of one adapter round them for the product with B_a, as x is rounded: 2^-9 or 2^-12 of each term at most.)
+// order of the groups, and kept in 32 bits; the second launch goes on, after the sum over W's side, with those of the adapters of its rows.  Where products are of 16 bits, they
+// are rounded for the product with B_a, as B_a is, in every kernel: 2^-9 or 2^-12 of each term at most.
 //
 // The floor is W's product; what the adapters add are the low-rank numbers' launch, which reads x once more (16,001 rows x 1024 of 24 adapters, rank 32: 12.9 of 84 us), and `rank` further
 // terms.  64 rows of 200 adapters, rank 16, 1024 x 1024: 7.7 and 8.0 us, two launches of few workgroups that wait for memory.
@@ -15,12 +15,17 @@
 
 namespace {
 
-// v += the low-rank numbers of the row at a place times W columns of its adapter's second matrix
-template <int W> __device__ __forceinline__ void add_low(const AdapterArgs &a, int place, int group, int c, int left, Vec<float, W> &v) {
+// v += the low-rank numbers of the row at a place times W columns of its adapter's second matrix; both as numbers of CT, as where they meet on the matrix cores
+// (so that what a row's result is made of depends on its types, not on how many rows a call has and of which adapters), their products and sums in 32 bits
+template <class CT, int W> __device__ __forceinline__ void add_low(const AdapterArgs &a, int place, int group, int c, int left, Vec<float, W> &v) {
     const float *low = a.low + (int64_t)place * a.low_stride, *b = a.b + (int64_t)group * a.rank * a.L + c;
     Vec<float, W> w = {};
 #pragma unroll 4
-    for (int i = 0; i < a.rank; ++i) w = w + low[i] * load_some<float, W>(b + (int64_t)i * a.L, left);
+    for (int i = 0; i < a.rank; ++i) {
+        const Vec<float, W> of_b = as_type<float, CT, W>(as_type<CT, float, W>(load_some<float, W>(b + (int64_t)i * a.L, left)));
+        if constexpr (sizeof(CT) == 4) w = w + low[i] * of_b;
+        else w = __builtin_elementwise_fma(Vec<float, W>((float)(CT)low[i]), of_b, w);      // (a product of two numbers of 16 bits is exact in 32)
+    }
     v = v + w;
 }
 
@@ -92,7 +97,7 @@ __global__ __launch_bounds__(T::THREADS, T::BLOCKS) void k_adapter(AdapterArgs a
                       [&](int r, int c, int left, Vec<float, 8> &v) {
                           if (alone) return;
                           const uint32_t e = (uint32_t)a.group_of[first + r];
-                          if (e < (uint32_t)a.g.groups) add_low<8>(a, first + r, (int)e, c0 + c, left, v);
+                          if (e < (uint32_t)a.g.groups) add_low<CT, 8>(a, first + r, (int)e, c0 + c, left, v);
                       });
 }
 
@@ -120,7 +125,7 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_adap
         const int r = F::row_of(p), c = F::col_of(p), left = a.N - c0 - c;
         if (at[r] < 0 || left <= 0) continue;
         Vec<float, 4> v = F::sum(sums, p);
-        if ((uint32_t)group[r] < (uint32_t)a.g.groups) add_low<4>(a, first + r, group[r], c0 + c, left, v);       // (whatever the offsets are)
+        if ((uint32_t)group[r] < (uint32_t)a.g.groups) add_low<CT, 4>(a, first + r, group[r], c0 + c, left, v);       // (whatever the offsets are)
         put_typed<4>(a.out, a.out_type, (int64_t)at[r] * a.out_stride + c0 + c, v, left);
     }
 }
