@@ -132,10 +132,11 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_adap
 
 template <class CT, class XT, bool TURNED, class T> int tiles_of(dpaps_ps *ps, const AdapterArgs &a, hipStream_t st) {
     const int32_t col_tiles = (a.N + T::COLS - 1) / T::COLS;
-    // Tiles of one adapter leave the last tile of each half empty; mixed ones add up to `rank` terms number by number.  1024 x 1024, rank 32, rows of all adapters,
-    // 16 bits: 5,000 rows of 64 45 us by adapter and 66 mixed, 10,000 of 200 85 and 111, 2,000 of 64 34 and 27;   32 bits, where products take longer: 5,000 of 20
-    // 128 and 133, of 64 162 and 139
-    const bool by_group = sizeof(CT) == 4 ? a.g.n >= 4 * (int64_t)T::ROWS * a.g.groups : 3 * (int64_t)a.g.n >= (int64_t)T::ROWS * a.g.groups;
+    // Tiles of one adapter leave the last tile of each half empty; mixed ones add up to `rank` terms number by number, in 16 bits after rounding them.  K 1024, rows of a
+    // few requests an adapter, 16 bits, by adapter and mixed: x 1024 columns, rank 32, 2,000 rows of 100 45 us and 63, 2,400 of 100 52 and 62, 4,000 of 200 76 and 64, 1,500 of 64 31 and
+    // 27;   rank 64, 2,000 of 200 71 and 102;   rank 16, 2,000 of 64 42 and 42, 4,000 of 100 53 and 44;   rank 8, 4,100 of 64 46 and 34, 3,800 of 40 30 and 34.   32 bits, where
+    // products take longer: 5,000 of 20 132 and 135, of 64 161 and 143, 16,000 of 64 383 and 353; rank 8 139 and 124, 159 and 128, 370 and 341
+    const bool by_group = sizeof(CT) == 4 ? a.g.n >= 4 * (int64_t)T::ROWS * a.g.groups : (int64_t)a.g.n * a.rank >= 640 * (int64_t)a.g.groups;
     const int64_t tiles = by_group ? row_tiles(a.g.n, a.g.groups, T::ROWS) : ceil_div64(a.g.n, T::ROWS), grid = tiles * col_tiles;
     if (grid >= ((int64_t)1 << 24)) return dpaps_too_large(ps, "adapters");
     static LdsAllowed allowed;
