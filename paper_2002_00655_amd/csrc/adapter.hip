@@ -5,7 +5,8 @@
 //   dA_a = s sum over a's rows of (B_a' dy_p) x_p',     dB_a' = s sum of (A_a x_p) dy_p'
 // W, the rows of A_a and the rows of B_a' (both `rank` keys of an adapter) lie in the server.  The low-rank numbers s A_a x_p and s B_a' dy_p are worked out first, in the
 // order of the groups, and kept in 32 bits; the second launch goes on, after the sum over W's side, with those of the adapters of its rows.  Where products are of 16 bits, they
-// are rounded for the product with B_a, as B_a is, in every kernel: 2^-9 or 2^-12 of each term at most.
+// are rounded for the product with B_a, as B_a is, in every kernel: either costs a term 2^-8 (bf16) or 2^-11 (fp16) of it at most, or 2^-25 of the other factor
+// where it is below fp16's normal numbers.
 //
 // The floor is W's product; what the adapters add are the low-rank numbers' launch, which reads x once more (16,001 rows x 1024 of 24 adapters, rank 32: 12.9 of 84 us), and `rank` further
 // terms.  64 rows of 200 adapters, rank 16, 1024 x 1024: 7.7 and 8.0 us, two launches of few workgroups that wait for memory.

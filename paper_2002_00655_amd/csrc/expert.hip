@@ -4,7 +4,8 @@
 //   gradient   dW_e = sum over e's rows of dy_q x_q'
 // Rows are taken in the groups' order, in tiles of rows of one group; where they lie stays as it is: they are read, and results are written, through that order.
 // Products are of numbers of the rows' 16-bit type, with sums in 32 bits, where rows and results both have 16 bits: the server's numbers of 32 bits are rounded to it, which
-// puts as much error on a result as its own rounding does (2^-9 or 2^-12 of each term at most, on average over the terms).  Else of numbers of 32 bits.
+// puts as much error on a result as its own rounding does (bf16 2^-8, fp16 2^-11 of each term at most, or 2^-25 of the row's number where the server's is below fp16's normal ones; on
+// average over the terms less).  Else of numbers of 32 bits.
 #include "experts.h"
 
 #include <algorithm>
@@ -191,8 +192,9 @@ int dpaps_expert_product(dpaps_ps *ps, const ExpertArgs *a, int count, hipStream
     return a->precise ? product_either<float, f16_t>(ps, c, count, st) : product_either<f16_t, f16_t>(ps, c, count, st);
 }
 
-// From so many rows a group on, and tiles of 128 x 128 for two workgroups a compute unit, matrices are laid before the product (laid.hip): 16,384 rows of 8 groups,
-// bf16, 2048 x 1024, 108 us with the laying and 113 by tiles, 1024 x 1024 60 and 68; of 16 groups, 1,024 rows each, 69 and 74, 2048 x 1024 124 and 114; 8,192 rows of 16, 52 and 62.
+// From so many rows a group on, and tiles of 128 x 128 for two workgroups a compute unit, matrices are laid before the product (laid.hip).  K 1024, bf16, with the laying and by tiles:
+// 16,384 rows of 8 groups x 2048 120 us and 136, x 1024 64 and 73;  of 16 groups, 1,024 rows each, x 2048 139 and 149, x 1024 72 and 77, groups as uneven as rank^-0.7 145 and 139, turned,
+// K 2048, 163 and 145;  32,768 rows of 32 309 and 311.  With 512 rows a group it goes either way: 8,192 of 16 x 1024 52 and 60, x 2048 94 and 79;  16,384 of 32 x 2048 196 and 172.
 constexpr int64_t LAID_ROWS = 1024;
 
 extern "C" int expert_matmul(ps_handle ps, int32_t worker, int64_t first_key, int32_t num_experts, int32_t rows, int32_t dim, int32_t transposed,

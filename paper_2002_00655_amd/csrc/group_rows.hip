@@ -124,8 +124,9 @@ __global__ __launch_bounds__(THREADS) void k_group_one(GroupArgs a, int32_t *err
     put_rows(a, 0, count, held);
 }
 
-// More of them: what every workgroup counts, and then the places - each workgroup counts its own rows again and adds up the counts of those before it, which are at
-// most 128.  131,072 rows of 64 groups: 4.2 and 7.8 us; in one launch, workgroups would have to wait for each other.
+// More of them: what every workgroup counts, and then the places - each workgroup reads its own ids and votes on them once more, for its wavefronts' counts, which
+// the first launch leaves as one sum a group, and adds up the counts of those before it, which are at most 128.  131,072 rows of 64 groups: 4.2 and 7.8 us.  (In one launch, which would
+// save the second reading, workgroups would have to wait for each other.)
 __global__ __launch_bounds__(THREADS) void k_group_count(GroupArgs a, int32_t *err) {
     extern __shared__ uint32_t count[];
     Held held;
