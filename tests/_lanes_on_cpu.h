@@ -7,6 +7,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <setjmp.h>
 #include <sys/mman.h>
 #include <vector>
 
@@ -28,14 +29,14 @@ static inline int __popcll(unsigned long long x) { return __builtin_popcountll(x
 
 // A wavefront's 64 lanes run one after the other, again and again: a lane that comes to a vote whose outcome is not known yet says what it votes and ends; when
 // all have, the outcome is known to the next run.
-struct NotYet {};
 static std::vector<std::vector<uint64_t>> told;       // per vote, what each lane has said
 static size_t known, asked;                           // votes whose outcome is known; votes of this lane so far
+static jmp_buf lane_ends;
 static std::vector<uint64_t> said(64);
 static inline const std::vector<uint64_t> &of_all(uint64_t mine) {
     if (asked < known) return told[asked++];
     said[threadIdx.x & 63] = mine;
-    throw NotYet{};
+    longjmp(lane_ends, 1);
 }
 static inline unsigned long long __ballot(bool p) {
     const std::vector<uint64_t> &v = of_all(p);
@@ -53,11 +54,12 @@ static inline int read_lane(int x, int lane) {
 static inline void wave(const std::function<void(int)> &lane) {
     told.clear();
     for (known = 0;;) {
-        int through = 0;
+        static int through;
+        through = 0;
         for (int l = 0; l < 64; ++l) {
             threadIdx.x = (unsigned)l;
             asked = 0;
-            try { lane(l); ++through; } catch (NotYet) {}
+            if (!setjmp(lane_ends)) { lane(l); ++through; }
         }
         if (through == 64) return;
         if (through != 0) { fprintf(stderr, "lanes part\n"); abort(); }
