@@ -9,7 +9,7 @@
 // where it is below fp16's normal numbers.
 //
 // The floor is W's product; what the adapters add are the low-rank numbers' launch, which reads x once more (16,001 rows x 1024 of 24 adapters, rank 32: 12.9 of 84 us), and `rank` further
-// terms.  64 rows of 200 adapters, rank 16, 1024 x 1024: 7.7 and 8.0 us, two launches of few workgroups that wait for memory.
+// terms.  64 rows of 200 adapters, rank 16, 1024 x 1024: 7.5 and 8.3 us, two launches of few workgroups that wait for memory.
 #include "experts.h"
 
 #include <algorithm>
@@ -186,8 +186,8 @@ ExpertArgs low_numbers(const dpaps_ps *ps, const RowGroups &g, const void *x, in
 }
 
 // Scratch of a call, and the product with it.  Many rows of 16 bits, tiles of 128 x 128 for one and a half workgroups a compute unit: the shared matrix and the adapters'
-// second ones are laid (laid.hip).  1024 x 1024, rank 32, with the laying: 5,000 rows of 20 adapters 31 us and 31 without, 8,000 of 100 55 and 71, 16,384 of 200 99 and
-// 131, 16,001 of 64 (24 of them asked for) 71 and 92.
+// second ones are laid (laid.hip).  1024 x 1024, rank 32, with the laying: 5,000 rows of 20 adapters 32 us and 31 without, 8,000 of 100 54 and 59, 16,384 of 200 99 and
+// 123, 16,001 of 64 (24 of them asked for) 71 and 84;   rank 8, 5,000 of 20 32 and 31, 16,384 of 200 100 and 110;   512 x 512, rank 16, 8,000 of 16 20 and 19, 16,384 24 and 29.
 struct Scratch {
     bool laid = false;
     int64_t stride = 0, rounded_stride = 0, w_size = 0, b_size = 0;
