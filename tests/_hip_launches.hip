@@ -1,5 +1,5 @@
 // A stand-in for the HIP runtime, for tests of what the library's host code launches, on a machine without a GPU: nothing runs, device memory is
-// numbers of addresses, and launches are kept with their names, grids and, of products of grouped rows, the numbers of the server that they may read.
+// addresses only, and launches are kept with their names, grids and, of products of grouped rows, the numbers of the server that they may read.
 // Loaded with global symbols before the library.
 #include "experts.h"
 
@@ -7,7 +7,7 @@
 #include <map>
 
 namespace {
-struct Launch { std::string name; dim3 grid, block; size_t lds; int64_t first, end, scratch; };
+struct Launch { std::string name; dim3 grid; int64_t first, end; };
 std::vector<Launch> launches;
 std::map<const void *, std::string> kernels;
 struct Block { char *at; size_t bytes; };
@@ -32,12 +32,9 @@ extern "C" {
 int launch_count() { return (int)launches.size(); }
 const char *launch_name(int i) { return launches[i].name.c_str(); }
 int64_t launch_groups(int i) { const dim3 &g = launches[i].grid; return (int64_t)g.x * g.y * g.z; }
-int64_t launch_threads(int i) { return launches[i].block.x; }
 int64_t launch_reads_from(int i) { return launches[i].first; }
 int64_t launch_reads_to(int i) { return launches[i].end; }
 void launch_clear() { launches.clear(); }
-int64_t allocated() { size_t s = 0; for (const Block &b : blocks) s += b.bytes; return (int64_t)s; }
-int64_t largest_allocation() { size_t s = 0; for (const Block &b : blocks) if (b.bytes > s) s = b.bytes; return (int64_t)s; }
 void refuse_allocations_from(int64_t bytes) { refuse_from = (size_t)bytes; }
 
 void **__hipRegisterFatBinary(const void *) { static void *h; return &h; }
@@ -46,8 +43,8 @@ void __hipRegisterFunction(void **, const void *host, char *, const char *name, 
 void __hipRegisterVar(void **, void *, char *, char *, int, size_t, int, int) {}
 hipError_t __hipPushCallConfiguration(dim3 g, dim3 b, size_t s, hipStream_t st) { cfg_grid = g; cfg_block = b; cfg_lds = s; cfg_stream = st; return hipSuccess; }
 hipError_t __hipPopCallConfiguration(dim3 *g, dim3 *b, size_t *s, hipStream_t *st) { *g = cfg_grid; *b = cfg_block; *s = cfg_lds; *st = cfg_stream; return hipSuccess; }
-hipError_t hipLaunchKernel(const void *f, dim3 g, dim3 b, void **args, size_t s, hipStream_t) {
-    Launch l{kernels[f], g, b, s, 0, 0, 0};
+hipError_t hipLaunchKernel(const void *f, dim3 g, dim3, void **args, size_t, hipStream_t) {
+    Launch l{kernels[f], g, 0, 0};
     const bool few = l.name.find("12k_expert_few") != std::string::npos, tiles = l.name.find("8k_expertI") != std::string::npos;
     if (few || tiles) {
         const ExpertCall &c = *(const ExpertCall *)args[0];

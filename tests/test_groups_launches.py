@@ -1,5 +1,5 @@
 """CPU: what the calls of models of many matrices launch, with a stand-in for the HIP runtime (tests/_hip_launches.hip): the numbers of the server that
-low-rank products read, and how much scratch laid matrices take."""
+low-rank products read, how much scratch laid matrices take, how many workgroups a call has."""
 import os
 import subprocess
 import sys
@@ -13,7 +13,7 @@ PROGRAM = r"""
 import ctypes as C, sys
 stub, lib = C.CDLL(sys.argv[1], C.RTLD_GLOBAL), C.CDLL(sys.argv[2])
 i32, i64, f, vp = C.c_int32, C.c_int64, C.c_float, C.c_void_p
-for name in ("launch_groups", "launch_reads_from", "launch_reads_to", "allocated", "largest_allocation"):
+for name in ("launch_groups", "launch_reads_from", "launch_reads_to"):
     getattr(stub, name).restype = i64
 stub.launch_name.restype = C.c_char_p
 lib.ps_last_error.restype = C.c_char_p
@@ -97,7 +97,6 @@ for rows, rank, adapters, n in ((1024, 4, 32767, 64 * 32767), (1024, 64, 8000, 6
         laid = 2 * up(K, 32) * up(N, 256) + 2 * adapters * up(rank, 32) * up(N, 256)
         numbers = (10 if grad else 4) * up(rank, 8) * n + 4 * n
         most = room * (numbers + min(laid, 1 << 30) + (1 << 29 if grad else 0) + 4096) + 4096
-        before = stub.allocated()
         stub.refuse_allocations_from(i64(int(most) + 1))
         args = (h, n, rows, dim, rows, rows + adapters * rank, adapters, rank, BF16)
         if grad:
