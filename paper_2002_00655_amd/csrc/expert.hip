@@ -117,9 +117,8 @@ __global__ __launch_bounds__((FewRows<CT, XT, TURNED, MT>::THREADS)) void k_expe
 __global__ __launch_bounds__(256) void k_pair_sums(const float *in, int64_t n, int32_t b, int32_t N, void *out, int32_t out_type, int64_t out_stride, uint32_t P, double inv_P,
                                                    const int32_t *err) {
     if (*(volatile const int32_t *)err) return;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n * P; i += (int64_t)gridDim.x * 256) {
         const int64_t t = quotient(i, P, inv_P);
-        if (t >= n) return;
         const int c = (int)(i - t * P) * 4, left = N - c;
         const float *p = in + t * b * N + c;
         Vec<float, 4> v = load_some<float, 4>(p, left);

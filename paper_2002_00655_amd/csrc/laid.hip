@@ -7,7 +7,7 @@
 //
 // k_lay is bound by memory (16 matrices of 2048 x 1024, 131 MB, of which the counter sees 67 read, and 67 written, in 38 us: 5.2 TB/s), k_laid by how well its loads and reads of LDS
 // hide under the products, the matrix units busy for 0.4 to 0.5 of it: 32,768 rows of those 16, with the laying, 202 us (830 TFLOP/s without it) where some hundred calls have followed one
-// another, and 209 to 270 in the first thirty after a pause.  That is the card's clock under load: four draws of the groups, of 950 to 6,170 rows, agree within 2 us, and rows of
+// another, and 209 to 270 in the first thirty after a pause.  That is taken to be the clock, as the card lets it under load: four draws of the groups, of 950 to 6,170 rows, agree within 2 us, and rows of
 // zeros take 182.  16,001 rows x 1024 of 24 adapters of 32 ranks, 63 us, 550 TFLOP/s.
 #include "experts.h"
 
